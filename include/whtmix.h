@@ -368,6 +368,145 @@ WHTMIX_API int whtmix_module_backward_separable(const void *x, const void *w_in,
                                      void *stream,
                                      const whtmix_options *options);
 
+/*
+ * ---- The feed-forward sublayer ----
+ *
+ * The mixer is linear; what follows it in a layer is the residual's addition
+ * with a norm, and two matrix products with an activation between them (the
+ * feed-forward part of the transformer stack, section III-A).  Rules that these
+ * entry points share:
+ *   - rows are contiguous, channels fastest; rows of x are ldx elements apart
+ *     (ldx >= its width, so that x may be columns of a wider array);
+ *   - any width >= 1 and any count of rows >= 0, at most 2^30 rows and
+ *     2^22 columns (WHTMIX_ERROR_TOO_LARGE); with no rows the gradients of
+ *     weights are zeros and the rest is a no-op;
+ *   - pointers need the alignment of their elements (8-bit values: 16 bytes);
+ *   - matrices have the dtype of x, vectors (bias, norm weight) and their
+ *     gradients are float32;
+ *   - arithmetic is float32 and each output is rounded once, to nearest even;
+ *   - no output overlaps an input or another output, but for those named;
+ *   - the checks, the workspace, streams and errors are those of the mixer.
+ *
+ * Block-scaled 8 bits ("MX"): a row of C values is stored as C rounded up to a
+ * multiple of 32 float8 e4m3 values (those past C are zero) and one byte s per
+ * 32 of them; a value is q * 2^(s - 127).  The scale is the least power of two
+ * in 2^-126 .. 2^120 with which the block's largest finite magnitude stays
+ * within e4m3's 448; Inf and NaN are stored as NaN.
+ */
+typedef enum whtmix_activation {
+    WHTMIX_ACT_NONE = 0,
+    WHTMIX_ACT_RELU = 1,      /* max(z, 0); its derivative at 0 is 0 */
+    WHTMIX_ACT_GELU = 2,      /* z (1 + erf(z / sqrt 2)) / 2 */
+    WHTMIX_ACT_GELU_TANH = 3, /* z (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))) / 2 */
+    WHTMIX_ACT_SILU = 4       /* z / (1 + exp(-z)) */
+} whtmix_activation;
+
+/*
+ * whtmix_norm_forward -- root-mean-square norm with the residual's addition:
+ *     t = x + residual,   h = t,   y = t / sqrt(mean(t^2) + eps) * weight.
+ *   x         [rows] rows of C elements of `dtype`, ldx apart.
+ *   residual  [rows][C] or NULL (t = x).      weight  [C] float32.
+ *   y         [rows][C] of `dtype`; may be x (with ldx = C).
+ *   h         [rows][C] of `dtype`, t rounded, or NULL; may be x (with ldx =
+ *             C) or the residual, but not y.
+ * y is formed from t before its rounding.  eps >= 0 and finite.
+ */
+WHTMIX_API int whtmix_norm_forward(const void *x, const void *residual,
+                        const float *weight, void *y, void *h, int64_t rows,
+                        int64_t C, int64_t ldx, double eps, int dtype,
+                        void *stream);
+
+/*
+ * whtmix_norm_mx_forward -- whtmix_norm_forward with y in block-scaled 8 bits:
+ *   q [rows][C up to 32] e4m3, scales [rows][C up to 32 / 32].
+ */
+WHTMIX_API int whtmix_norm_mx_forward(const void *x, const void *residual,
+                           const float *weight, void *q, uint8_t *scales,
+                           void *h, int64_t rows, int64_t C, int64_t ldx,
+                           double eps, int dtype, void *stream);
+
+/*
+ * whtmix_norm_backward -- gradients of whtmix_norm_forward from the kept
+ * stream h: with r = 1 / sqrt(mean(h^2) + eps), n = h r, g = dy weight,
+ *     dx = dh + r (g - n mean(g n)),   dweight = sum over rows of dy n.
+ *   h, dy     [rows][C] of `dtype`.
+ *   dh        [rows][C] of `dtype`, the gradient of h, or NULL (zeros).
+ *   dx        [rows][C] of `dtype`: the gradient of x and of the residual;
+ *             may be dy or dh.
+ *   dweight   [C] float32, or NULL to skip.
+ * dweight is summed in a fixed order.  Workspace: up to 1024 rows of C floats.
+ */
+WHTMIX_API int whtmix_norm_backward(const void *h, const float *weight,
+                         const void *dy, const void *dh, void *dx,
+                         float *dweight, int64_t rows, int64_t C, double eps,
+                         int dtype, void *stream);
+
+/* whtmix_quantize_mx -- rows in block-scaled 8 bits: x [rows] rows of C
+ * elements of `dtype`, ldx apart; q and scales as whtmix_norm_mx_forward. */
+WHTMIX_API int whtmix_quantize_mx(const void *x, void *q, uint8_t *scales,
+                       int64_t rows, int64_t C, int64_t ldx, int dtype,
+                       void *stream);
+
+/* whtmix_dequantize_mx -- the values that q and scales stand for, rounded to
+ * `dtype`: y [rows][C]. */
+WHTMIX_API int whtmix_dequantize_mx(const void *q, const uint8_t *scales, void *y,
+                         int64_t rows, int64_t C, int dtype, void *stream);
+
+/*
+ * whtmix_linear_forward -- matrix product with bias, activation and residual:
+ *     z = x w + bias,   y = act(z) + residual.
+ *   x         [M] rows of K elements of `dtype`, ldx apart.
+ *   w         [K][N] of `dtype` (z[m][n] = sum_k x[m][k] w[k][n]).
+ *   bias      [N] float32, or NULL.
+ *   residual  [M][N] of `dtype`, or NULL.
+ *   y         [M][N] of `dtype`; may be the residual.
+ *   z         [M][N] of `dtype`, what the backward pass keeps, or NULL.
+ * Sums are float32; with float32 elements the products are six bf16 products
+ * of three-term splits (what they leave out is below 2^-24 |x| |w|), or float32
+ * ones where a tile's operands do not split (from 2^128 - 2^119, Inf, NaN, or
+ * below 2^-95 throughout).  Workspace: partial sums where k is split over
+ * workgroups.
+ */
+WHTMIX_API int whtmix_linear_forward(const void *x, const void *w,
+                          const float *bias, const void *residual, void *y,
+                          void *z, int64_t M, int64_t K, int64_t N,
+                          int64_t ldx, int activation, int dtype,
+                          void *stream);
+
+/*
+ * whtmix_linear_backward -- gradients of whtmix_linear_forward:
+ *     dz = dy act'(z),   dx = dz w^T,   dw = x^T dz,   dbias = sum_m dz.
+ *   x, w      as passed forward;  dy [M][N] of `dtype`.
+ *   z         [M][N] as kept (may be NULL with WHTMIX_ACT_NONE).
+ *   dx        [M][K] of `dtype`, or NULL to skip.
+ *   dw        [K][N] of `dtype`, or NULL to skip.
+ *   dbias     [N] float32, or NULL to skip.
+ * The residual's gradient is dy itself.  dz enters the products rounded to
+ * `dtype` (bf16: what the matrix cores read) and dbias unrounded.  Sums over
+ * rows are made in a fixed order.  Workspace: dz, and partial sums.
+ */
+WHTMIX_API int whtmix_linear_backward(const void *x, const void *w,
+                           const void *dy, const void *z, void *dx, void *dw,
+                           float *dbias, int64_t M, int64_t K, int64_t N,
+                           int64_t ldx, int activation, int dtype,
+                           void *stream);
+
+/*
+ * whtmix_linear_mx_forward -- whtmix_linear_forward on block-scaled 8 bits:
+ *   xq, xs    the activations, [M] rows of K values.
+ *   wq, ws    the weights' columns as rows: [N] rows of K values.
+ *   bias, residual  as whtmix_linear_forward, the residual of `dtype`.
+ *   y         [M][N] of `dtype` (may be the residual), or NULL with
+ *   yq, ys    the output in block-scaled 8 bits, [M] rows of N values.
+ * Either y or both yq and ys.
+ */
+WHTMIX_API int whtmix_linear_mx_forward(const void *xq, const uint8_t *xs,
+                             const void *wq, const uint8_t *ws,
+                             const float *bias, const void *residual, void *y,
+                             void *yq, uint8_t *ys, int64_t M, int64_t K,
+                             int64_t N, int activation, int dtype,
+                             void *stream);
+
 /* Fills *info with the plan whtmix_forward_ex would use.  Validates the
  * shape, dtype and options exactly as the forward call does (pointers are
  * not needed).  Returns a whtmix_status. */

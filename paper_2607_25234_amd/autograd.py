@@ -4,9 +4,11 @@
     y = whtmix_mix_separable(x, log_gain_tokens, log_gain_channels)
     y = whtmix_block(x, w_in, gain, w_out)                   # eqs. (1)-(4)
     y = whtmix_block_separable(x, w_in, log_gain_tokens, log_gain_channels, w_out)
+    y, h = whtmix_norm(x, weight, residual)                  # residual's addition and norm
+    y = whtmix_linear(x, w, bias, activation, residual)      # feed-forward product
 
 The forward and backward passes both run in the HIP kernels of libwhtmix.so
-(whtmix_forward*/whtmix_backward*); gradients flow to x and to the gains, as
+(whtmix_*forward*/whtmix_*backward*); gradients flow to x and to the gains, as
 when the paper trains the mixer (section IV-A).
 """
 from __future__ import annotations
@@ -82,6 +84,67 @@ class WHTMixBlockSeparableFunction(torch.autograd.Function):
         dx, dwi, dwo, dgt, dgc = whtmix.module_backward_separable(
             x, w_in, gt, gc, w_out, dy.contiguous(), want_dgains=want_g)
         return dx, dwi.to(w_in.dtype), dgt, dgc, dwo.to(w_out.dtype)
+
+
+class WHTMixNormFunction(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, residual, eps):
+        weight = weight.contiguous()
+        y, h = whtmix.norm(x, weight, None if residual is None else residual.contiguous(), eps)
+        if residual is None:      # the stream is x itself
+            h = x.contiguous()
+        ctx.save_for_backward(h, weight)
+        ctx.eps, ctx.residual = eps, residual is not None
+        return (y, h) if residual is not None else y
+
+    @staticmethod
+    def backward(ctx, dy, dh=None):
+        h, weight = ctx.saved_tensors
+        dx, dw = whtmix.norm_backward(h, weight, dy.contiguous(),
+                                      None if dh is None else dh.contiguous(), ctx.eps,
+                                      want_dweight=ctx.needs_input_grad[1])
+        return dx, dw, dx if ctx.residual else None, None
+
+
+class WHTMixLinearFunction(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, w, bias, activation, residual):
+        w = w.contiguous()
+        z = None
+        # z is kept only where the activation's derivative needs it
+        keep = activation != "none" and any(ctx.needs_input_grad[:3])
+        y = whtmix.linear(x, w, bias, activation,
+                          None if residual is None else residual.contiguous(), want_z=keep)
+        if keep:
+            y, z = y
+        ctx.save_for_backward(x, w, z)
+        ctx.activation = activation
+        return y
+
+    @staticmethod
+    def backward(ctx, dy):
+        x, w, z = ctx.saved_tensors
+        want = ctx.needs_input_grad
+        dx = dw = db = None
+        if any(want[:3]):
+            dx, dw, db = whtmix.linear_backward(x, w, dy.contiguous(), z, ctx.activation,
+                                                want_dx=want[0], want_dw=want[1],
+                                                want_dbias=want[2])
+        return dx, dw, db, None, dy if want[4] else None
+
+
+def whtmix_norm(x, weight, residual=None, eps: float = 1e-6):
+    """Differentiable norm with the residual's addition: (y, h), h = x + residual (x itself
+    without one).  weight float32, and its gradient."""
+    if residual is None:
+        return WHTMixNormFunction.apply(x, weight, None, eps), x
+    return WHTMixNormFunction.apply(x, weight, residual, eps)
+
+
+def whtmix_linear(x, w, bias=None, activation: str = "none", residual=None):
+    """Differentiable activation(x w + bias) + residual; dw in w's type, the
+    bias and its gradient float32."""
+    return WHTMixLinearFunction.apply(x, w, bias, activation, residual)
 
 
 def whtmix_block(x, w_in, gain, w_out):

@@ -12,6 +12,7 @@
 
 #include "whtmix.h"
 #include "whtmix_launch.h"
+#include "whtmix_layer.h"
 #include "whtmix_module.h"
 #include "whtmix_plan.h"
 
@@ -246,6 +247,20 @@ int get_counters(void *stream, uint32_t **out)
 }
 
 }  // namespace
+
+namespace whtmix {
+
+WorkspaceLock::WorkspaceLock() { g_ws_mutex.lock(); }
+WorkspaceLock::~WorkspaceLock() { g_ws_mutex.unlock(); }
+
+int stream_workspace(void *stream, int64_t bytes, float **out)
+{
+    return get_workspace(stream, bytes, out);
+}
+
+int report_hip(hipError_t e, const char *what) { return hip_fail(e, what); }
+
+}  // namespace whtmix
 
 extern "C" {
 

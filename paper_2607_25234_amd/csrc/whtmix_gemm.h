@@ -1,0 +1,172 @@
+// Matrix products on the matrix cores: what the kernels of the three element
+// types share, the epilogue first.
+#pragma once
+
+#include "whtmix_vec.h"
+
+namespace whtmix {
+
+// How an operand lies in memory: k contiguous, or its rows (the output's
+// dimension) contiguous.
+enum Layout { K_CONTIGUOUS = 0, K_STRIDED = 1 };
+
+// out [M][N] = act(A B + bias) + residual with A [M][K] and B [K][N].
+struct GemmArgs {
+    const void *a, *b;
+    const uint8_t *as, *bs;     // block scales (8-bit operands)
+    int64_t lda, ldb;           // elements between k rows or between output rows
+    int64_t M, N, K;
+    const float *bias;          // [N] or null
+    const void *residual;       // [M][N] of the output's type, or null
+    void *y;                    // [M][N], or null with yq
+    void *z;                    // [M][N] before the activation, or null
+    uint8_t *yq, *ys;           // 8-bit output and its scales
+    int act;
+    float *part;                // split: [splits][M][N] partial sums, or null
+    int64_t k_per;              // k of one split
+};
+
+template <typename T>
+__device__ __forceinline__ void load8(const T *p, int n, float (&v)[8])
+{
+    if constexpr (Chunk<T>::N == 8) {
+        Chunk<T>::load(p, n, v);
+    } else {
+        Chunk<T>::load(p, n, *(float(*)[4])v);
+        Chunk<T>::load(p + 4, n - 4, *(float(*)[4])(v + 4));
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ void store8(T *p, int n, const float (&v)[8])
+{
+    if constexpr (Chunk<T>::N == 8) {
+        Chunk<T>::store(p, n, v);
+    } else {
+        Chunk<T>::store(p, n, *(const float(*)[4])v);
+        Chunk<T>::store(p + 4, n - 4, *(const float(*)[4])(v + 4));
+    }
+}
+
+// Eight sums of row m from column n on, to the outputs.  With 8-bit output
+// four neighbouring lanes hold a block of 32 columns and call this together.
+template <typename T>
+__device__ __forceinline__ void finish8(const GemmArgs &g, int64_t m, int64_t n, float (&v)[8])
+{
+    const int cnt = m < g.M ? (int)min((int64_t)8, max((int64_t)0, g.N - n)) : 0;
+    const int64_t at = m * g.N + n;
+    if (g.bias) {
+        float b[8];
+        load8(g.bias + n, (int)min((int64_t)8, g.N - n), b);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] += b[i];
+    }
+    if (g.z && cnt > 0) store8((T *)g.z + at, cnt, v);
+    with_act(g.act, [&](auto act) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = act_of<decltype(act)::value>(v[i]);
+    });
+    if (g.residual) {
+        float r[8];
+        load8((const T *)g.residual + at, cnt, r);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] += r[i];
+    }
+    if (!g.yq) {
+        if (cnt > 0) store8((T *)g.y + at, cnt, v);
+        return;
+    }
+    const int64_t width = (g.N + kMxBlock - 1) / kMxBlock * kMxBlock;
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        if (i >= cnt) v[i] = 0.f;
+        top = max(top, mx_magnitude(v[i]));
+    }
+    top = max(top, (uint32_t)__shfl_xor((int)top, 1));
+    top = max(top, (uint32_t)__shfl_xor((int)top, 2));
+    const uint32_t byte = mx_scale_byte(top);
+    const float inv = mx_inverse(byte);
+    if (m < g.M && n < width) {
+        *(u32x2 *)(g.yq + m * width + n) =
+            (u32x2){mx_pack(v[0], v[1], v[2], v[3], inv), mx_pack(v[4], v[5], v[6], v[7], inv)};
+        if (n % kMxBlock == 0) g.ys[m * (width / kMxBlock) + n / kMxBlock] = (uint8_t)byte;
+    }
+}
+
+// Eight sums of a split to its partial sums.
+__device__ __forceinline__ void finish8_part(const GemmArgs &g, int64_t split, int64_t m,
+                                             int64_t n, const float (&v)[8])
+{
+    const int cnt = m < g.M ? (int)min((int64_t)8, g.N - n) : 0;
+    if (cnt > 0) store8(g.part + (split * g.M + m) * g.N + n, cnt, v);
+}
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+// Orders a wave's own LDS accesses (no other wave touches them).
+__device__ __forceinline__ void wave_lds_fence()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+// 32 rows x 64 columns of a wave's sums, from the matrix instructions' layout
+// (lane: row l % 32, columns 8 (r / 4) + 4 (l / 32) + r % 4 of each 32) through
+// the wave's LDS (kEpilogueFloats) to rows of 64, eight lanes a row, so that
+// stores and the residual's loads are 16 bytes a lane and whole cache lines a row.
+constexpr int kEpilogueStride = 68;      // floats: rows 4 banks apart
+constexpr int kEpilogueFloats = 32 * kEpilogueStride;
+
+template <typename T>
+__device__ __forceinline__ void store_tile32x64(const GemmArgs &g, float *lds, int64_t m0,
+                                                int64_t n0, int64_t split, const f32x16 &left,
+                                                const f32x16 &right)
+{
+    const int lane = threadIdx.x & 63;
+    float *w = lds + (lane & 31) * kEpilogueStride + (lane >> 5) * 4;
+    wave_lds_fence();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        *(f32x4 *)(w + 8 * i) = (f32x4){left[4 * i], left[4 * i + 1], left[4 * i + 2],
+                                        left[4 * i + 3]};
+        *(f32x4 *)(w + 32 + 8 * i) = (f32x4){right[4 * i], right[4 * i + 1], right[4 * i + 2],
+                                             right[4 * i + 3]};
+    }
+    wave_lds_fence();
+    const int64_t n = n0 + (lane & 7) * 8;
+    const bool in = n < (g.yq ? (g.N + kMxBlock - 1) / kMxBlock * kMxBlock : g.N);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int row = i * 8 + (lane >> 3);
+        const float *p = lds + row * kEpilogueStride + (lane & 7) * 8;
+        float v[8];
+        *(f32x4 *)v = *(const f32x4 *)p;
+        *(f32x4 *)(v + 4) = *(const f32x4 *)(p + 4);
+        if (!in) continue;      // whole blocks of 32 columns with 8-bit output
+        if (g.part) finish8_part(g, split, m0 + row, n, v);
+        else finish8<T>(g, m0 + row, n, v);
+    }
+}
+
+// Sums a split's partial sums in order and finishes them.
+template <typename T> __global__ void __launch_bounds__(256) split_sum_kernel(GemmArgs g, int splits)
+{
+    const int64_t width = g.yq ? (g.N + kMxBlock - 1) / kMxBlock * kMxBlock : (g.N + 7) / 8 * 8;
+    const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
+    const int64_t m = i / width, n = i - m * width;
+    if (m >= g.M) return;       // 8-bit output: the four lanes of a block leave together
+    float v[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = 0.f;
+    for (int s = 0; s < splits; ++s) {
+        float p[8];
+        load8(g.part + ((int64_t)s * g.M + m) * g.N + n, (int)min((int64_t)8, g.N - n), p);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] += p[k];
+    }
+    finish8<T>(g, m, n, v);
+}
+
+}  // namespace whtmix

@@ -1,0 +1,409 @@
+// Matrix products with bias, activation and residual in the epilogue, and
+// their gradients.
+//
+//   z = x w + bias,  y = act(z) + residual
+//   dz = dy act'(z),  dx = dz w^T,  dw = x^T dz,  dbias = column sums of dz
+//
+// One tile kernel for every type: a 128 x 128 tile of four waves, operands
+// converted to bf16 terms on their way to LDS (one for bf16 and for block-scaled
+// 8 bits, three for float32), products on v_mfma_f32_32x32x16_bf16, sums in
+// float32.
+#include "whtmix_gemm.h"
+
+#include <algorithm>
+
+namespace whtmix {
+namespace {
+
+constexpr int kTile = 128, kStep = 32;
+constexpr int kRowBytes = 80;      // K_CONTIGUOUS: 32 bf16 and 16 bytes of padding
+constexpr int kKBytes = 320;       // K_STRIDED: 128 bf16 and 64 bytes of padding
+constexpr int kPlane = 10240;      // either way
+constexpr int kF32Row = kTile + 4; // float32 staging: floats of one k
+// Three bf16 terms hold a float32 below 2^128 - 2^119 (above, the first rounds to Inf) and from
+// 2^-100 up (below, the last is subnormal); rows mixed with smaller values lose less than 2^-128.
+constexpr uint32_t kSplitMax = 0x7f7f8000u, kSplitMin = 0x10000000u;   // 2^-95
+static_assert(kTile * kRowBytes == kPlane && kStep * kKBytes == kPlane, "planes");
+
+struct Mx {};      // element type of 8-bit operands
+
+template <typename E> constexpr int terms() { return std::is_same_v<E, float> ? 3 : 1; }
+
+// Sixteen elements of an operand in a thread's registers: of one row (16 k) or
+// one k (16 rows).
+template <typename E, Layout L> struct Stage {
+    float v[16];
+    __device__ __forceinline__ void load(const void *p, const uint8_t *sc, int64_t ld, int64_t R,
+                                         int64_t K, int64_t r0, int64_t k0)
+    {
+        const int t = threadIdx.x;
+        int64_t outer, inner, n_outer, n_inner;
+        if (L == K_CONTIGUOUS) {
+            outer = r0 + (t >> 1), inner = k0 + (t & 1) * 16, n_outer = R, n_inner = K;
+        } else {
+            outer = k0 + (t >> 3), inner = r0 + (t & 7) * 16, n_outer = K, n_inner = R;
+        }
+        const int64_t left = outer < n_outer ? n_inner - inner : 0;
+        const int n = (int)min((int64_t)16, max((int64_t)0, left));
+        if constexpr (std::is_same_v<E, Mx>) {
+            const uint8_t *q = (const uint8_t *)p + (n ? outer * ld + inner : 0);
+            const float s = n ? bits_f32((uint32_t)sc[outer * (ld / kMxBlock) + inner / kMxBlock] << 23)
+                              : 0.f;
+            u32x4 w = {0, 0, 0, 0};
+            if (n) w = *(const u32x4 *)q;       // rows are whole blocks
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                v[4 * i] = __builtin_amdgcn_cvt_f32_fp8((int)w[i], 0) * s;
+                v[4 * i + 1] = __builtin_amdgcn_cvt_f32_fp8((int)w[i], 1) * s;
+                v[4 * i + 2] = __builtin_amdgcn_cvt_f32_fp8((int)w[i], 2) * s;
+                v[4 * i + 3] = __builtin_amdgcn_cvt_f32_fp8((int)w[i], 3) * s;
+            }
+        } else {
+            const E *q = (const E *)p + (n ? outer * ld + inner : 0);
+            load8(q, n, *(float(*)[8])v);
+            load8(q + 8, n - 8, *(float(*)[8])(v + 8));
+        }
+    }
+    // As float32, [k][row], for operands that do not split.
+    __device__ __forceinline__ void store_f32(float *lds) const
+    {
+        const int t = threadIdx.x;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            if (L == K_CONTIGUOUS) lds[((t & 1) * 16 + i) * kF32Row + (t >> 1)] = v[i];
+            else lds[(t >> 3) * kF32Row + (t & 7) * 16 + i] = v[i];
+        }
+    }
+    // The largest magnitude staged so far, as ordered bits (NaN above Inf).
+    __device__ __forceinline__ uint32_t largest(uint32_t top) const
+    {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) top = max(top, f32_bits(v[i]) & 0x7fffffffu);
+        return top;
+    }
+    __device__ __forceinline__ void store(char *lds)
+    {
+        const int t = threadIdx.x;
+        char *p = lds + (L == K_CONTIGUOUS ? (t >> 1) * kRowBytes + (t & 1) * 32
+                                           : (t >> 3) * kKBytes + (t & 7) * 32);
+#pragma unroll
+        for (int s = 0; s < terms<E>(); ++s) {
+            uint32_t w[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                w[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
+                if (s + 1 < terms<E>()) {
+                    v[2 * i] -= bits_f32(w[i] << 16);
+                    v[2 * i + 1] -= bits_f32(w[i] & 0xffff0000u);
+                }
+            }
+            *(u32x4 *)(p + s * kPlane) = (u32x4){w[0], w[1], w[2], w[3]};
+            *(u32x4 *)(p + s * kPlane + 16) = (u32x4){w[4], w[5], w[6], w[7]};
+        }
+    }
+};
+
+// The operand of a 32x32x16 product: lane l holds row l % 32, k 8 (l / 32) + 0..7.
+// K_STRIDED planes are read through the transposing LDS load: a group of 16
+// lanes reads 4 k of 16 rows and each lane gets one row's 4 k.
+template <Layout L> __device__ __forceinline__ bf16x8 fragment(const char *plane, int row0, int k0)
+{
+    const int lane = threadIdx.x & 63;
+    if constexpr (L == K_CONTIGUOUS) {
+        return *(const bf16x8 *)(plane + (row0 + (lane & 31)) * kRowBytes +
+                                 (k0 + (lane >> 5) * 8) * 2);
+    } else {
+        typedef short s4 __attribute__((ext_vector_type(4)));
+        typedef __attribute__((address_space(3))) s4 lds_s4;
+        const int k = k0 + (lane >> 5) * 8 + ((lane >> 2) & 3);
+        const int r = row0 + ((lane >> 4) & 1) * 16 + (lane & 3) * 4;
+        const char *p = plane + k * kKBytes + r * 2;
+        union {
+            s4 h[2];
+            bf16x8 f;
+        } u;
+        u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4 *)p);
+        u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4 *)(p + 4 * kKBytes));
+        return u.f;
+    }
+}
+
+// The tile again with float32 products (v_mfma_f32_32x32x2_f32).
+template <Layout LA, Layout LB>
+__device__ __noinline__ void float32_tile(const GemmArgs &g, Stage<float, LA> &sa,
+                                          Stage<float, LB> &sb, float *lds, int64_t m0, int64_t n0,
+                                          int64_t kbeg, int64_t kend, int wm, int wn,
+                                          f32x16 (&acc)[2][2])
+{
+    const int lane = threadIdx.x & 63;
+    float *la = lds, *lb = lds + kStep * kF32Row;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
+    for (int64_t k = kbeg; k < kend; k += kStep) {
+        sa.load(g.a, g.as, g.lda, g.M, kend, m0, k);
+        sb.load(g.b, g.bs, g.ldb, g.N, kend, n0, k);
+        __syncthreads();
+        sa.store_f32(la);
+        sb.store_f32(lb);
+        __syncthreads();
+        for (int kk = 0; kk < kStep; kk += 2) {
+            const float *pa = la + (kk + (lane >> 5)) * kF32Row + wm + (lane & 31);
+            const float *pb = lb + (kk + (lane >> 5)) * kF32Row + wn + (lane & 31);
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(pb[32 * j], pa[32 * i],
+                                                                     acc[i][j], 0, 0, 0);
+        }
+    }
+}
+
+template <typename E, typename T, Layout LA, Layout LB>
+__global__ void __launch_bounds__(256) gemm_kernel(GemmArgs g)
+{
+    constexpr int P = terms<E>();
+    __shared__ __attribute__((aligned(16))) char lds[2 * P * kPlane > 4 * kEpilogueFloats * 4
+                                                         ? 2 * P * kPlane
+                                                         : 4 * kEpilogueFloats * 4];
+    const int wave = threadIdx.x >> 6;
+    const int64_t m0 = (int64_t)blockIdx.x * kTile, n0 = (int64_t)blockIdx.y * kTile;
+    const int64_t kbeg = (int64_t)blockIdx.z * g.k_per, kend = min(g.K, kbeg + g.k_per);
+    const int wm = (wave & 1) * 64, wn = (wave >> 1) * 64;
+    char *la = lds, *lb = lds + P * kPlane;
+    f32x16 acc[2][2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
+
+    Stage<E, LA> sa;
+    Stage<E, LB> sb;
+    uint32_t top_a = 0, top_b = 0;     // float32: what the splits have to hold
+    sa.load(g.a, g.as, g.lda, g.M, kend, m0, kbeg);
+    sb.load(g.b, g.bs, g.ldb, g.N, kend, n0, kbeg);
+    for (int64_t k = kbeg; k < kend; k += kStep) {
+        __syncthreads();
+        if constexpr (P > 1) {
+            top_a = sa.largest(top_a);
+            top_b = sb.largest(top_b);
+        }
+        sa.store(la);
+        sb.store(lb);
+        if (k + kStep < kend) {
+            sa.load(g.a, g.as, g.lda, g.M, kend, m0, k + kStep);
+            sb.load(g.b, g.bs, g.ldb, g.N, kend, n0, k + kStep);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int kk = 0; kk < kStep; kk += 16) {
+            bf16x8 fa[P][2], fb[P][2];
+#pragma unroll
+            for (int p = 0; p < P; ++p)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    fa[p][i] = fragment<LA>(la + p * kPlane, wm + 32 * i, kk);
+                    fb[p][i] = fragment<LB>(lb + p * kPlane, wn + 32 * i, kk);
+                }
+            // Of the nine products of three terms the six largest: what is left
+            // out is below 2^-24 of |x| |w|.
+#pragma unroll
+            for (int s = P - 1; s >= 0; --s)
+#pragma unroll
+                for (int p = 0; p <= s; ++p)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+#pragma unroll
+                        for (int j = 0; j < 2; ++j)
+                            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                                fb[s - p][j], fa[p][i], acc[i][j], 0, 0, 0);
+        }
+    }
+    if constexpr (P > 1) {
+        auto bad = [](uint32_t top) { return top >= kSplitMax || (top != 0 && top < kSplitMin); };
+        // A thread's share is its row's (or its rows') k; one that does not split sends the
+        // whole tile through float32 products.
+        if (__syncthreads_or(bad(top_a) || bad(top_b)))
+            float32_tile(g, sa, sb, (float *)lds, m0, n0, kbeg, kend, wm, wn, acc);
+    }
+    __syncthreads();
+    float *out = (float *)lds + wave * kEpilogueFloats;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+        store_tile32x64<T>(g, out, m0 + wm + 32 * i, n0 + wn, blockIdx.z, acc[i][0], acc[i][1]);
+}
+
+// How many parts k is split into: enough workgroups for the device where the
+// output has few tiles, each with at least 8 steps of k.
+int64_t splits_of(int64_t M, int64_t N, int64_t K)
+{
+    const int64_t tiles = ((M + kTile - 1) / kTile) * ((N + kTile - 1) / kTile);
+    const int64_t steps = (K + kStep - 1) / kStep;
+    return std::max<int64_t>(1, std::min<int64_t>(512 / std::max<int64_t>(1, tiles), steps / 8));
+}
+
+uint64_t gemm_bytes(int64_t M, int64_t N, int64_t K)
+{
+    const int64_t s = splits_of(M, N, K);
+    return s > 1 ? (uint64_t)s * M * N * 4 : 0;
+}
+
+template <typename E, typename T, Layout LA, Layout LB>
+hipError_t run_gemm(GemmArgs g, float *ws, hipStream_t stream)
+{
+    const int64_t s = splits_of(g.M, g.N, g.K);
+    const int64_t steps = (g.K + kStep - 1) / kStep;
+    g.k_per = (steps + s - 1) / s * kStep;
+    const int64_t splits = (g.K + g.k_per - 1) / g.k_per;
+    g.part = splits > 1 ? ws : nullptr;
+    const dim3 grid((uint32_t)((g.M + kTile - 1) / kTile), (uint32_t)((g.N + kTile - 1) / kTile),
+                    (uint32_t)splits);
+    gemm_kernel<E, T, LA, LB><<<grid, dim3(256), 0, stream>>>(g);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || splits == 1) return e;
+    const int64_t width = g.yq ? mx_width(g.N) : (g.N + 7) / 8 * 8;
+    split_sum_kernel<T><<<dim3((uint32_t)((g.M * width / 8 + 255) / 256)), dim3(256), 0, stream>>>(
+        g, (int)splits);
+    return hipGetLastError();
+}
+
+// dz = dy act'(z), 8 columns a thread down `per` rows, with the columns' sums
+// of the unrounded values.
+template <typename T>
+__global__ void __launch_bounds__(256) dz_kernel(const T *dy, const T *z, T *dz, float *part,
+                                                 int64_t M, int64_t N, int64_t per, int act)
+{
+    const int64_t n = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
+    const int cnt = (int)min((int64_t)8, N - n);
+    if (cnt <= 0) return;
+    float s[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s[i] = 0.f;
+    const int64_t end = min(M, ((int64_t)blockIdx.y + 1) * per);
+    with_act(act, [&](auto tag) {
+        constexpr int ACT = decltype(tag)::value;
+        for (int64_t m = (int64_t)blockIdx.y * per; m < end; ++m) {
+            float d[8];
+            load8(dy + m * N + n, cnt, d);
+            if (ACT != ACT_NONE) {
+                float v[8];
+                load8(z + m * N + n, cnt, v);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) d[i] *= act_grad<ACT>(v[i]);
+                if (dz) store8(dz + m * N + n, cnt, d);
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s[i] += d[i];
+        }
+    });
+    if (part) store8(part + (int64_t)blockIdx.y * N + n, cnt, s);
+}
+
+int64_t dz_parts(int64_t M, int64_t N)
+{
+    const int64_t cols = (N + 2047) / 2048;
+    return std::min<int64_t>(M, std::max<int64_t>(1, 1024 / cols));
+}
+
+uint64_t align256(uint64_t v) { return (v + 255) / 256 * 256; }
+
+struct BackwardLayoutBytes {
+    uint64_t dz = 0, part = 0, gemm = 0;     // sizes
+};
+BackwardLayoutBytes backward_bytes(const LinearBackwardArgs &a)
+{
+    BackwardLayoutBytes l;
+    const int e = a.dtype == DTYPE_BF16 ? 2 : 4;
+    if (a.act != ACT_NONE) l.dz = align256((uint64_t)a.M * a.N * e);
+    if (a.dbias) l.part = align256((uint64_t)dz_parts(a.M, a.N) * a.N * 4);
+    if (a.dx) l.gemm = gemm_bytes(a.M, a.K, a.N);
+    if (a.dw) l.gemm = std::max(l.gemm, gemm_bytes(a.K, a.N, a.M));
+    return l;
+}
+
+template <typename T> hipError_t linear_backward(const LinearBackwardArgs &a)
+{
+    const BackwardLayoutBytes l = backward_bytes(a);
+    char *ws = (char *)a.ws;
+    T *dz = (T *)ws;
+    float *part = (float *)(ws + l.dz), *gemm = (float *)(ws + l.dz + l.part);
+    hipError_t e;
+    if (a.act != ACT_NONE || a.dbias) {
+        const int64_t parts = dz_parts(a.M, a.N);
+        const int64_t per = (a.M + parts - 1) / parts;
+        const dim3 grid((uint32_t)((a.N + 2047) / 2048), (uint32_t)((a.M + per - 1) / per));
+        dz_kernel<T><<<grid, dim3(256), 0, a.stream>>>(
+            (const T *)a.dy, (const T *)a.z, a.dx || a.dw ? dz : nullptr,
+            a.dbias ? part : nullptr, a.M, a.N, per, a.act);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+        if (a.dbias && (e = launch_column_sum(part, grid.y, a.N, a.dbias, a.stream)) != hipSuccess)
+            return e;
+    }
+    const void *d = a.act != ACT_NONE ? (const void *)dz : a.dy;
+    if (a.dx) {
+        GemmArgs g{};
+        g.a = d, g.lda = a.N, g.b = a.w, g.ldb = a.N;
+        g.M = a.M, g.N = a.K, g.K = a.N, g.y = a.dx;
+        if ((e = run_gemm<T, T, K_CONTIGUOUS, K_CONTIGUOUS>(g, gemm, a.stream)) != hipSuccess)
+            return e;
+    }
+    if (a.dw) {
+        GemmArgs g{};
+        g.a = a.x, g.lda = a.ldx, g.b = d, g.ldb = a.N;
+        g.M = a.K, g.N = a.N, g.K = a.M, g.y = a.dw;
+        if ((e = run_gemm<T, T, K_STRIDED, K_STRIDED>(g, gemm, a.stream)) != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
+template <typename T> hipError_t linear_forward(const LinearArgs &a)
+{
+    GemmArgs g{};
+    g.a = a.x, g.lda = a.ldx, g.b = a.w, g.ldb = a.N;
+    g.M = a.M, g.N = a.N, g.K = a.K;
+    g.bias = a.bias, g.residual = a.residual, g.y = a.y, g.z = a.z, g.act = a.act;
+    return run_gemm<T, T, K_CONTIGUOUS, K_STRIDED>(g, a.ws, a.stream);
+}
+
+}  // namespace
+
+uint64_t linear_bytes(const LinearArgs &a) { return gemm_bytes(a.M, a.N, a.K); }
+
+hipError_t launch_linear(const LinearArgs &a)
+{
+    return a.dtype == DTYPE_BF16 ? linear_forward<__bf16>(a) : linear_forward<float>(a);
+}
+
+uint64_t linear_backward_bytes(const LinearBackwardArgs &a)
+{
+    const BackwardLayoutBytes l = backward_bytes(a);
+    return l.dz + l.part + l.gemm;
+}
+
+hipError_t launch_linear_backward(const LinearBackwardArgs &a)
+{
+    return a.dtype == DTYPE_BF16 ? linear_backward<__bf16>(a) : linear_backward<float>(a);
+}
+
+uint64_t linear_mx_bytes(const LinearMxArgs &a) { return gemm_bytes(a.M, a.N, mx_width(a.K)); }
+
+hipError_t launch_linear_mx(const LinearMxArgs &a)
+{
+    GemmArgs g{};
+    g.a = a.xq, g.as = a.xs, g.b = a.wq, g.bs = a.ws8;
+    g.lda = g.ldb = g.K = mx_width(a.K);
+    g.M = a.M, g.N = a.N;
+    g.bias = a.bias, g.residual = a.residual, g.act = a.act;
+    g.y = a.y, g.yq = (uint8_t *)a.yq, g.ys = a.ys;
+    if (a.dtype == DTYPE_BF16)
+        return run_gemm<Mx, __bf16, K_CONTIGUOUS, K_CONTIGUOUS>(g, a.ws, a.stream);
+    return run_gemm<Mx, float, K_CONTIGUOUS, K_CONTIGUOUS>(g, a.ws, a.stream);
+}
+
+}  // namespace whtmix

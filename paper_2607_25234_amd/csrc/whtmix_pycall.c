@@ -1,5 +1,5 @@
 /* CPython-level calls of whtmix_forward_ex and whtmix_forward_separable, and of
- * the other entry points by address (call()).
+ * the other entry points by address (call(), call_rows()).
  *
  * Argument marshalling only: Python integers become the C ABI's pointers,
  * sizes and codes, and the library's status comes back as an int.  The
@@ -188,6 +188,98 @@ static PyObject *call(PyObject *self, PyObject *const *args, Py_ssize_t nargs)
     return PyLong_FromLong(status);
 }
 
+/* call_rows(function_address, pointers, sizes, codes, stream[, eps]) -> status
+ *
+ * The feed-forward sublayer's entry points: `pointers`, `sizes` and `codes` are
+ * tuples of the device pointers, the 64-bit sizes and the int codes (activation,
+ * dtype) in the entry point's order, eps the norms' last argument before dtype.
+ * Each signature is a case of its own. */
+static PyObject *call_rows(PyObject *self, PyObject *const *args, Py_ssize_t nargs)
+{
+    (void)self;
+    void *f, *p[9], *st;
+    int64_t z[4];
+    int c[2], status = 0;
+    double eps = 0.0;
+    if ((nargs != 5 && nargs != 6) || !PyTuple_Check(args[1]) || !PyTuple_Check(args[2]) ||
+        !PyTuple_Check(args[3])) {
+        PyErr_SetString(PyExc_TypeError,
+                        "call_rows() takes an address, three tuples, a stream and eps");
+        return NULL;
+    }
+    const Py_ssize_t np = PyTuple_GET_SIZE(args[1]), nz = PyTuple_GET_SIZE(args[2]),
+                     nc = PyTuple_GET_SIZE(args[3]);
+    /* pointers, sizes, codes and eps of each signature */
+    const int key = nargs == 6 ? (int)(1000 + np * 100 + nz * 10 + nc)
+                               : (int)(np * 100 + nz * 10 + nc);
+    if (np > 9 || nz > 4 || nc > 2 ||
+        (key != 1531 && key != 1631 && key != 1621 && key != 331 && key != 321 && key != 642 &&
+         key != 742 && key != 932)) {
+        PyErr_SetString(PyExc_TypeError, "call_rows(): no entry point takes these arguments");
+        return NULL;
+    }
+    if (as_ptr(args[0], &f))
+        return NULL;
+    if (!f) {
+        PyErr_SetString(PyExc_ValueError, "call_rows() needs a function address");
+        return NULL;
+    }
+    for (Py_ssize_t i = 0; i < np; ++i)
+        if (as_ptr(PyTuple_GET_ITEM(args[1], i), &p[i]))
+            return NULL;
+    for (Py_ssize_t i = 0; i < nz; ++i)
+        if (as_i64(PyTuple_GET_ITEM(args[2], i), &z[i]))
+            return NULL;
+    for (Py_ssize_t i = 0; i < nc; ++i)
+        if (as_int(PyTuple_GET_ITEM(args[3], i), &c[i]))
+            return NULL;
+    if (as_ptr(args[4], &st))
+        return NULL;
+    if (nargs == 6) {
+        eps = PyFloat_AsDouble(args[5]);
+        if (eps == -1.0 && PyErr_Occurred())
+            return NULL;
+    }
+    typedef void *P;
+    typedef int64_t I;
+    Py_BEGIN_ALLOW_THREADS
+    switch (key) {
+    case 1531: /* whtmix_norm_forward */
+        status = ((int (*)(P, P, P, P, P, I, I, I, double, int, P))f)(
+            p[0], p[1], p[2], p[3], p[4], z[0], z[1], z[2], eps, c[0], st);
+        break;
+    case 1631: /* whtmix_norm_mx_forward */
+        status = ((int (*)(P, P, P, P, P, P, I, I, I, double, int, P))f)(
+            p[0], p[1], p[2], p[3], p[4], p[5], z[0], z[1], z[2], eps, c[0], st);
+        break;
+    case 1621: /* whtmix_norm_backward */
+        status = ((int (*)(P, P, P, P, P, P, I, I, double, int, P))f)(
+            p[0], p[1], p[2], p[3], p[4], p[5], z[0], z[1], eps, c[0], st);
+        break;
+    case 331: /* whtmix_quantize_mx */
+        status = ((int (*)(P, P, P, I, I, I, int, P))f)(p[0], p[1], p[2], z[0], z[1], z[2], c[0],
+                                                        st);
+        break;
+    case 321: /* whtmix_dequantize_mx */
+        status = ((int (*)(P, P, P, I, I, int, P))f)(p[0], p[1], p[2], z[0], z[1], c[0], st);
+        break;
+    case 642: /* whtmix_linear_forward */
+        status = ((int (*)(P, P, P, P, P, P, I, I, I, I, int, int, P))f)(
+            p[0], p[1], p[2], p[3], p[4], p[5], z[0], z[1], z[2], z[3], c[0], c[1], st);
+        break;
+    case 742: /* whtmix_linear_backward */
+        status = ((int (*)(P, P, P, P, P, P, P, I, I, I, I, int, int, P))f)(
+            p[0], p[1], p[2], p[3], p[4], p[5], p[6], z[0], z[1], z[2], z[3], c[0], c[1], st);
+        break;
+    default: /* 932: whtmix_linear_mx_forward */
+        status = ((int (*)(P, P, P, P, P, P, P, P, P, I, I, I, int, int, P))f)(
+            p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7], p[8], z[0], z[1], z[2], c[0], c[1],
+            st);
+    }
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(status);
+}
+
 static PyMethodDef methods[] = {
     {"bind", (PyCFunction)(void (*)(void))bind, METH_FASTCALL,
      "bind(forward_ex_address, forward_separable_address)"},
@@ -197,6 +289,8 @@ static PyMethodDef methods[] = {
      "forward_separable(x, gain_t, gain_c, y, B, N, C, dtype, stream, options) -> status"},
     {"call", (PyCFunction)(void (*)(void))call, METH_FASTCALL,
      "call(function_address, pointer..., B, N, C, dtype, stream, options) -> status"},
+    {"call_rows", (PyCFunction)(void (*)(void))call_rows, METH_FASTCALL,
+     "call_rows(function_address, pointers, sizes, codes, stream[, eps]) -> status"},
     {NULL, NULL, 0, NULL}};
 
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_whtmix_call",

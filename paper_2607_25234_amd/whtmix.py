@@ -6,6 +6,9 @@ There is no fallback: if the library is missing, importing the functions
 that need it raises.
 
     y = forward(x, gain)          # x [B, N, C] (or [N, C]) f32/bf16, gain [N, C] f32
+    n, h = norm(y, weight, x)     # the residual's addition and a norm
+    u = linear(n, w1, b1, activation="gelu")      # the feed-forward products
+    o = linear(u, w2, b2, residual=h)
 """
 from __future__ import annotations
 
@@ -21,19 +24,30 @@ PLANS = {"auto": 0, "small": 1, "fused": 2, "three_pass": 3, "one_launch": 4,
          "wave_tiles": 5, "two_pass": 6}
 PLAN_NAMES = {v: k for k, v in PLANS.items()}
 
+ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
+MX_BLOCK = 32
+
 # Every symbol include/whtmix.h declares.
 EXPORTS = (
     "whtmix_backward",
     "whtmix_backward_separable",
+    "whtmix_dequantize_mx",
     "whtmix_forward",
     "whtmix_forward_ex",
     "whtmix_forward_noalloc",
     "whtmix_forward_separable",
+    "whtmix_linear_backward",
+    "whtmix_linear_forward",
+    "whtmix_linear_mx_forward",
     "whtmix_module_backward",
     "whtmix_module_backward_separable",
     "whtmix_module_forward",
     "whtmix_module_forward_separable",
+    "whtmix_norm_backward",
+    "whtmix_norm_forward",
+    "whtmix_norm_mx_forward",
     "whtmix_plan_describe",
+    "whtmix_quantize_mx",
     "whtmix_status_string",
     "whtmix_last_error",
     "whtmix_release_workspaces",
@@ -65,6 +79,19 @@ class PlanInfo(ctypes.Structure):
                 ("padded_tokens", ctypes.c_int64), ("module_path", ctypes.c_int),
                 ("module_outer_bits", ctypes.c_int), ("module_backward_fused", ctypes.c_int)]
 
+
+# The feed-forward entry points: counts of pointers, sizes and int codes, and whether
+# eps stands before the codes.
+_ROW_CALLS = {
+    "whtmix_norm_forward": (5, 3, 1, True),
+    "whtmix_norm_mx_forward": (6, 3, 1, True),
+    "whtmix_norm_backward": (6, 2, 1, True),
+    "whtmix_quantize_mx": (3, 3, 1, False),
+    "whtmix_dequantize_mx": (3, 2, 1, False),
+    "whtmix_linear_forward": (6, 4, 2, False),
+    "whtmix_linear_backward": (7, 4, 2, False),
+    "whtmix_linear_mx_forward": (9, 3, 2, False),
+}
 
 _lib = None
 
@@ -113,6 +140,11 @@ def lib():
         L.whtmix_backward_separable.argtypes = [vp, vp, vp, vp, vp, vp, vp, i64, i64, i64,
                                                 ctypes.c_int, vp, ctypes.POINTER(Options)]
         L.whtmix_backward_separable.restype = ctypes.c_int
+        for name, (np, nz, nc, eps) in _ROW_CALLS.items():
+            f = getattr(L, name)
+            f.argtypes = ([vp] * np + [i64] * nz + ([ctypes.c_double] if eps else [])
+                          + [ctypes.c_int] * nc + [vp])
+            f.restype = ctypes.c_int
         L.whtmix_plan_describe.argtypes = [i64, i64, i64, ctypes.c_int,
                                            ctypes.POINTER(Options), ctypes.POINTER(PlanInfo)]
         L.whtmix_plan_describe.restype = ctypes.c_int
@@ -575,6 +607,311 @@ def module_backward_separable(x, w_in, log_gain_tokens, log_gain_channels, w_out
     if status != SUCCESS:
         raise WhtmixError(status, "whtmix_module_backward_separable")
     return dx, dw_in, dw_out, dgt, dgc
+
+
+# ---- the feed-forward sublayer ----
+
+def call_rows(name, pointers, sizes, codes, stream, *eps) -> int:
+    """Direct call of a feed-forward entry point with integer pointers (0 for
+    none), its sizes and its int codes in the header's order; returns the status."""
+    addr = _entry.get(name)
+    if addr is None:
+        addr = _entry[name] = ctypes.cast(getattr(lib(), name), ctypes.c_void_p).value
+    return _call().call_rows(addr, pointers, sizes, codes, stream, *eps)
+
+
+def _run_rows(name, x, stream, pointers, sizes, codes, *eps):
+    """call_rows with x's device current; raises WhtmixError on a refusal."""
+    status = _on_device(
+        x, stream, lambda st: call_rows(name, pointers, sizes, codes, st, *eps), (), ())
+    if status != SUCCESS:
+        raise WhtmixError(status, name)
+
+
+def _dtype_code(t, what):
+    import torch
+
+    if not t.is_cuda:
+        raise ValueError(f"{what} must be on a GPU device")
+    if t.dtype is torch.float32:
+        return DTYPE_F32
+    if t.dtype is torch.bfloat16:
+        return DTYPE_BF16
+    raise TypeError(f"{what} must be float32 or bfloat16, got {t.dtype}")
+
+
+def _rows(t, what):
+    """(rows, width, ld) of a tensor [..., C] whose rows are contiguous and a
+    constant distance apart (columns of a wider tensor, or contiguous)."""
+    if t.dim() < 2:
+        raise ValueError(f"{what} must be [..., rows, columns]")
+    C = t.shape[-1]
+    if t.is_contiguous():
+        return (t.numel() // C if C else 0), C, C
+    if t.stride(-1) != 1 and C != 1:
+        raise ValueError(f"{what}'s rows must be contiguous")
+    ld, rows = t.stride(-2), t.shape[-2]
+    if rows == 1 and t.dim() == 2:
+        ld = max(ld, C)
+    for size, stride in zip(reversed(t.shape[:-2]), reversed(t.stride()[:-2])):
+        if rows == 1:
+            ld = stride
+        elif size != 1 and stride != rows * ld:
+            raise ValueError(f"{what}'s rows must be a constant distance apart")
+        rows *= size
+    return rows, C, max(ld, C) if rows <= 1 else ld
+
+
+def _tensor(t, shape, dtype, x, what):
+    """A contiguous tensor of this shape and dtype on x's device."""
+    if t.dtype is not dtype or t.get_device() != x.get_device() or not t.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous {dtype} tensor on x's device")
+    if t.shape != shape:
+        raise ValueError(f"{what} shape {tuple(t.shape)} != {tuple(shape)}")
+    return t.data_ptr()
+
+
+def _ptr(t):
+    return 0 if t is None else t.data_ptr()
+
+
+def _activation(name):
+    code = ACTIVATIONS.get(name)
+    if code is None:
+        raise ValueError(f"activation {name!r}: one of {', '.join(ACTIVATIONS)}")
+    return code
+
+
+def mx_width(C: int) -> int:
+    """Values stored for a row of C in block-scaled 8 bits."""
+    return -(-C // MX_BLOCK) * MX_BLOCK
+
+
+def _new_mx(x, lead, C):
+    import torch
+
+    w = mx_width(C)
+    return (torch.empty((*lead, w), dtype=torch.float8_e4m3fn, device=x.device),
+            torch.empty((*lead, w // MX_BLOCK), dtype=torch.uint8, device=x.device))
+
+
+def _mx(q, scales, what):
+    """(rows, stored width, the two pointers) of block-scaled rows."""
+    import torch
+
+    if not q.is_cuda:
+        raise ValueError(f"{what} must be on a GPU device")
+    if q.dtype is not torch.float8_e4m3fn or q.dim() < 2 or not q.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous float8_e4m3fn tensor [..., rows, columns]")
+    w = q.shape[-1]
+    if w % MX_BLOCK or w == 0:
+        raise ValueError(f"{what}'s width {w} is not a multiple of {MX_BLOCK}")
+    return (q.numel() // w, w, q.data_ptr(),
+            _tensor(scales, (*q.shape[:-1], w // MX_BLOCK), torch.uint8, q, f"{what}'s scales"))
+
+
+def norm(x, weight, residual=None, eps: float = 1e-6, out=None, stream=None):
+    """Root-mean-square norm with the residual's addition: (y, h) with
+    h = x + residual (x itself without one) and
+    y = h / sqrt(mean(h^2) + eps) * weight, formed before h is rounded.
+
+    x: [..., C] float32 or bfloat16 (rows may be columns of a wider tensor);
+    weight: float32 [C]; residual: a contiguous tensor of x's shape and type;
+    out: optional contiguous tensor for y (may be x itself)."""
+    import torch
+
+    dt = _dtype_code(x, "x")
+    rows, C, ld = _rows(x, "x")
+    _tensor(weight, (C,), torch.float32, x, "weight")
+    h = x
+    if residual is not None:
+        _tensor(residual, x.shape, x.dtype, x, "residual")
+        h = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    if out is None:
+        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    _run_rows("whtmix_norm_forward", x, stream,
+              (x.data_ptr(), _ptr(residual), weight.data_ptr(),
+               _tensor(out, x.shape, x.dtype, x, "out"), 0 if h is x else h.data_ptr()),
+              (rows, C, ld), (dt,), eps)
+    return out, h
+
+
+def norm_mx(x, weight, residual=None, eps: float = 1e-6, stream=None):
+    """norm() with y in block-scaled 8 bits: (q, scales, h), q float8_e4m3fn
+    [..., mx_width(C)] and scales uint8 [..., mx_width(C) / 32]; a value is
+    q * 2^(scale - 127)."""
+    import torch
+
+    dt = _dtype_code(x, "x")
+    rows, C, ld = _rows(x, "x")
+    _tensor(weight, (C,), torch.float32, x, "weight")
+    h = x
+    if residual is not None:
+        _tensor(residual, x.shape, x.dtype, x, "residual")
+        h = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    q, scales = _new_mx(x, x.shape[:-1], C)
+    _run_rows("whtmix_norm_mx_forward", x, stream,
+              (x.data_ptr(), _ptr(residual), weight.data_ptr(), q.data_ptr(), scales.data_ptr(),
+               0 if h is x else h.data_ptr()), (rows, C, ld), (dt,), eps)
+    return q, scales, h
+
+
+def norm_backward(h, weight, dy, dh=None, eps: float = 1e-6, want_dweight: bool = True, dx=None,
+                  stream=None):
+    """Gradients through norm() from its kept h: (dx, dweight), dx the gradient
+    of x and of the residual (dh, the gradient of h, is added), dweight float32
+    (None when not wanted).  dx may be dy or dh."""
+    import torch
+
+    dt = _dtype_code(h, "h")
+    C = h.shape[-1]
+    _tensor(h, h.shape, h.dtype, h, "h")
+    rows, _, _ = _rows(h, "h")
+    _tensor(weight, (C,), torch.float32, h, "weight")
+    _tensor(dy, h.shape, h.dtype, h, "dy")
+    if dh is not None:
+        _tensor(dh, h.shape, h.dtype, h, "dh")
+    if dx is None:
+        dx = torch.empty_like(h)
+    _tensor(dx, h.shape, h.dtype, h, "dx")
+    dweight = torch.empty_like(weight) if want_dweight else None
+    _run_rows("whtmix_norm_backward", h, stream,
+              (h.data_ptr(), weight.data_ptr(), dy.data_ptr(), _ptr(dh), dx.data_ptr(),
+               _ptr(dweight)), (rows, C), (dt,), eps)
+    return dx, dweight
+
+
+def quantize_mx(x, stream=None):
+    """x [..., C] in block-scaled 8 bits along its rows: (q, scales) as norm_mx.
+    Weights [K, N] are laid out once by their columns: quantize_mx(w.t())
+    after .contiguous()."""
+    dt = _dtype_code(x, "x")
+    rows, C, ld = _rows(x, "x")
+    q, scales = _new_mx(x, x.shape[:-1], C)
+    _run_rows("whtmix_quantize_mx", x, stream, (x.data_ptr(), q.data_ptr(), scales.data_ptr()),
+              (rows, C, ld), (dt,))
+    return q, scales
+
+
+def dequantize_mx(q, scales, C: int | None = None, dtype=None, stream=None):
+    """The values q and scales stand for, [..., C] (default: the stored width)
+    in dtype (bfloat16, the default, or float32)."""
+    import torch
+
+    rows, w, pq, ps = _mx(q, scales, "q")
+    C = w if C is None else C
+    if mx_width(C) != w:
+        raise ValueError(f"{C} columns are not stored in {w}")
+    y = torch.empty((*q.shape[:-1], C), dtype=dtype or torch.bfloat16, device=q.device)
+    _run_rows("whtmix_dequantize_mx", q, stream, (pq, ps, y.data_ptr()), (rows, C),
+              (_dtype_code(y, "the output"),))
+    return y
+
+
+def linear(x, w, bias=None, activation: str = "none", residual=None, want_z: bool = False,
+           out=None, stream=None):
+    """activation(x w + bias) + residual; with want_z also z = x w + bias, which
+    linear_backward reads: (y, z).
+
+    x: [..., K] float32 or bfloat16 (rows may be columns of a wider tensor);
+    w: [K, N] of x's type; bias: float32 [N]; residual: a contiguous [..., N]
+    of x's type; activation: "none", "relu", "gelu", "gelu_tanh" or "silu"; out:
+    optional contiguous tensor for y (may be the residual)."""
+    import torch
+
+    dt, act = _dtype_code(x, "x"), _activation(activation)
+    M, K, ld = _rows(x, "x")
+    if w.dim() != 2:
+        raise ValueError("w must be [K, N]")
+    N = w.shape[1]
+    _tensor(w, (K, N), x.dtype, x, "w")
+    shape = (*x.shape[:-1], N)
+    if bias is not None:
+        _tensor(bias, (N,), torch.float32, x, "bias")
+    if residual is not None:
+        _tensor(residual, shape, x.dtype, x, "residual")
+    if out is None:
+        out = torch.empty(shape, dtype=x.dtype, device=x.device)
+    else:
+        _tensor(out, shape, x.dtype, x, "out")
+    z = torch.empty(shape, dtype=x.dtype, device=x.device) if want_z else None
+    _run_rows("whtmix_linear_forward", x, stream,
+              (x.data_ptr(), w.data_ptr(), _ptr(bias), _ptr(residual), out.data_ptr(), _ptr(z)),
+              (M, K, N, ld), (act, dt))
+    return (out, z) if want_z else out
+
+
+def linear_backward(x, w, dy, z=None, activation: str = "none", want_dx: bool = True,
+                    want_dw: bool = True, want_dbias: bool = True, stream=None):
+    """Gradients through linear() for the upstream gradient dy: (dx, dw, dbias),
+    dx and dw in x's type, dbias float32; what is not wanted is None.  z: what
+    linear kept (not needed for activation "none").  The residual's gradient is dy."""
+    import torch
+
+    dt, act = _dtype_code(x, "x"), _activation(activation)
+    M, K, ld = _rows(x, "x")
+    if w.dim() != 2:
+        raise ValueError("w must be [K, N]")
+    N = w.shape[1]
+    _tensor(w, (K, N), x.dtype, x, "w")
+    shape = (*x.shape[:-1], N)
+    _tensor(dy, shape, x.dtype, x, "dy")
+    if act:
+        if z is None:
+            raise ValueError(f"activation {activation!r} needs z")
+        _tensor(z, shape, x.dtype, x, "z")
+    else:
+        z = None
+    if not (want_dx or want_dw or want_dbias):
+        raise ValueError("nothing to compute")
+    dx = torch.empty(x.shape, dtype=x.dtype, device=x.device) if want_dx else None
+    dw = torch.empty_like(w) if want_dw else None
+    db = torch.empty(N, dtype=torch.float32, device=x.device) if want_dbias else None
+    _run_rows("whtmix_linear_backward", x, stream,
+              (x.data_ptr(), w.data_ptr(), dy.data_ptr(), _ptr(z), _ptr(dx), _ptr(dw), _ptr(db)),
+              (M, K, N, ld), (act, dt))
+    return dx, dw, db
+
+
+def linear_mx(xq, xs, wq, ws, bias=None, activation: str = "none", residual=None,
+              out_mx: bool = False, dtype=None, out=None, stream=None):
+    """linear() on block-scaled 8 bits: xq, xs as norm_mx or quantize_mx give
+    them, [..., K]; wq, ws the weights' columns as rows, [N, K].  Returns y
+    [..., N] in dtype (the residual's or out's, else bfloat16), or with out_mx
+    (q, scales) of the result."""
+    import torch
+
+    M, K, pxq, pxs = _mx(xq, xs, "xq")
+    act = _activation(activation)
+    if wq.dim() != 2:
+        raise ValueError("wq must be [N, K]")
+    N, Kw, pwq, pws = _mx(wq, ws, "wq")
+    if Kw != K or wq.get_device() != xq.get_device():
+        raise ValueError(f"wq must hold rows of {K} on xq's device")
+    lead = xq.shape[:-1]
+    if bias is not None:
+        _tensor(bias, (N,), torch.float32, xq, "bias")
+    if dtype is None:
+        like = residual if residual is not None else out
+        dtype = like.dtype if like is not None else torch.bfloat16
+    if residual is not None:
+        _tensor(residual, (*lead, N), dtype, xq, "residual")
+    q = s = None
+    if out_mx:
+        if out is not None:
+            raise ValueError("out is for outputs that are not in 8 bits")
+        q, s = _new_mx(xq, lead, N)
+    elif out is None:
+        out = torch.empty((*lead, N), dtype=dtype, device=xq.device)
+    else:
+        _tensor(out, (*lead, N), dtype, xq, "out")
+    code = {torch.float32: DTYPE_F32, torch.bfloat16: DTYPE_BF16}.get(dtype)
+    if code is None:
+        raise TypeError(f"the output must be float32 or bfloat16, not {dtype}")
+    _run_rows("whtmix_linear_mx_forward", xq, stream,
+              (pxq, pxs, pwq, pws, _ptr(bias), _ptr(residual), _ptr(out), _ptr(q), _ptr(s)),
+              (M, K, N), (act, code))
+    return (q, s) if out_mx else out
 
 
 def release_workspaces() -> None:
