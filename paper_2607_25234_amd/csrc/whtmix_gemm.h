@@ -15,6 +15,7 @@ struct GemmArgs {
     const void *a, *b;
     const uint8_t *as, *bs;     // block scales (8-bit operands)
     int64_t lda, ldb;           // elements between k rows or between output rows
+    int64_t a_rows, a_k, b_rows, b_k;   // what the operands' memory holds (packed ones: padded)
     int64_t M, N, K;
     const float *bias;          // [N] or null
     const void *residual;       // [M][N] of the output's type, or null
@@ -168,5 +169,12 @@ template <typename T> __global__ void __launch_bounds__(256) split_sum_kernel(Ge
     }
     finish8<T>(g, m, n, v);
 }
+
+// Products of bf16 operands (whtmix_linear_bf16.hip) and of block-scaled 8-bit ones
+// (whtmix_linear_mx.hip) with `*_bytes` of workspace.
+uint64_t gemm_bf16_bytes(const GemmArgs &g, Layout la, Layout lb);
+hipError_t gemm_bf16(GemmArgs g, Layout la, Layout lb, void *ws, hipStream_t stream);
+uint64_t gemm_mx_bytes(const GemmArgs &g);
+hipError_t gemm_mx(GemmArgs g, int dtype, void *ws, hipStream_t stream);
 
 }  // namespace whtmix

@@ -1,0 +1,438 @@
+// The tile kernel of bf16 and block-scaled 8-bit products.
+//
+// A workgroup forms BM x BN sums.  Each step of 128 bytes of k (64 bf16, 128
+// 8-bit values) is copied to LDS without passing registers (16 bytes a lane), two
+// buffers deep: the copies of the next step are in flight while the matrix
+// instructions run on this one.  LDS takes a wave's copies in lane order, so what
+// keeps the fragments' reads free of bank conflicts is which 16 bytes each lane
+// fetches: chunks of a row are permuted by the row (K_CONTIGUOUS) or the k
+// (K_STRIDED).
+//
+// Each wave holds 32 WM x 64 sums.  The matrix instructions take the second operand's
+// columns as their rows, so that a lane's sums run along the output's row.
+#pragma once
+
+#include "whtmix_gemm.h"
+
+namespace whtmix {
+
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+
+// What copies fetch past the end of k.
+static __device__ __attribute__((aligned(16))) const uint32_t kZero16[4] = {0, 0, 0, 0};
+
+constexpr int kStepBytes = 128;
+
+typedef __attribute__((address_space(3))) void lds_void;
+
+// A wave's LDS address, uniform.
+__device__ __forceinline__ uint32_t lds_address(char *p)
+{
+    return (uint32_t)__builtin_amdgcn_readfirstlane((int)(uintptr_t)(lds_void *)p);
+}
+
+// 16 bytes a lane from memory to LDS (lane order from the wave's address), counted by vmcnt.
+// In assembler, because the compiler would have every later LDS read wait for the copies in
+// flight; the kernel waits for them itself, a step later.  No registers but m0 are written, which
+// nothing else in these kernels uses.
+__device__ __forceinline__ void copy16(const char *base, uint32_t off, uint32_t lds)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds),
+                 "v"(off), "s"(base)
+                 : "memory");
+}
+__device__ __forceinline__ void copy16(const char *src, uint32_t lds)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds),
+                 "v"(src)
+                 : "memory");
+}
+__device__ __forceinline__ void wait_copies() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+// One operand's tile: R rows of output (or k-strided columns), NW waves copying.
+template <int EB, Layout L, int R, int NW> struct Operand {
+    static constexpr int kStepK = kStepBytes / EB;
+    static constexpr int kCopies = R / 8 / NW;          // a wave's copies of a step
+    static_assert(R % (8 * NW) == 0, "whole copies");
+    static constexpr int kRowChunks = L == K_CONTIGUOUS ? 8 : R * EB / 16;
+
+    const char *base;       // of the tile at the current step (uniform)
+    uint32_t off[kCopies];  // of this lane's chunks from there
+    int64_t ld;             // bytes
+    int64_t k_end;          // of the operand: chunks from there on are zeros
+
+    static __device__ __forceinline__ int swizzle(int outer, int chunk)
+    {
+        if constexpr (L == K_CONTIGUOUS) return chunk ^ (outer & 7);
+        else return chunk ^ ((4 * (outer & 3)) & (kRowChunks - 1));
+    }
+    // The (row or k, chunk) that copy i of this lane fetches.
+    static __device__ __forceinline__ void place(int i, int &outer, int &chunk)
+    {
+        const int c = (i * NW + (int)(threadIdx.x >> 6)) * 64 + (int)(threadIdx.x & 63);
+        outer = c / kRowChunks;
+        chunk = swizzle(outer, c % kRowChunks);
+    }
+    // rows: of the operand; every chunk that starts before k_end (K_CONTIGUOUS) or
+    // rows (K_STRIDED) is whole.
+    __device__ __forceinline__ void init(const void *p, int64_t ld_elements, int64_t rows,
+                                         int64_t r0, int64_t k0, int64_t kend)
+    {
+        ld = ld_elements * EB;
+        k_end = kend;
+        base = (const char *)p + (L == K_CONTIGUOUS ? r0 * ld + k0 * EB : k0 * ld + r0 * EB);
+#pragma unroll
+        for (int i = 0; i < kCopies; ++i) {
+            int outer, chunk;
+            place(i, outer, chunk);
+            if constexpr (L == K_CONTIGUOUS)     // rows past the end repeat the last one
+                off[i] = (uint32_t)(min((int64_t)outer, rows - 1 - r0) * ld) + chunk * 16;
+            else                                 // columns likewise
+                off[i] = (uint32_t)(outer * ld) +
+                         (uint32_t)min((int64_t)chunk * 16, (rows - r0) * EB - 16);
+        }
+    }
+    // The step at k, and on to the next.
+    __device__ __forceinline__ void copy(char *lds, int64_t k)
+    {
+        const uint32_t to = lds_address(lds + (threadIdx.x >> 6) * 1024);
+        if (k + kStepK <= k_end) {
+#pragma unroll
+            for (int i = 0; i < kCopies; ++i) copy16(base, off[i], to + i * NW * 1024);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kCopies; ++i) {
+                int outer, chunk;
+                place(i, outer, chunk);
+                const int64_t at = k + (L == K_CONTIGUOUS ? chunk * (16 / EB) : outer);
+                copy16(at < k_end ? base + off[i] : (const char *)kZero16, to + i * NW * 1024);
+            }
+        }
+        base += L == K_CONTIGUOUS ? kStepBytes : kStepK * ld;
+    }
+};
+
+// A 32-row fragment of 16 bf16 of k (step kk of 4).
+template <Layout L, int R>
+__device__ __forceinline__ bf16x8 fragment16(const char *lds, int row0, int kk)
+{
+    const int lane = threadIdx.x & 63;
+    if constexpr (L == K_CONTIGUOUS) {
+        const int row = row0 + (lane & 31), chunk = kk * 2 + (lane >> 5);
+        return *(const bf16x8 *)(lds + row * kStepBytes +
+                                 Operand<2, L, R, 1>::swizzle(row, chunk) * 16);
+    } else {
+        // The transposing read: 16 lanes read 4 k of 16 rows, each gets one row's 4 k.
+        typedef short s4 __attribute__((ext_vector_type(4)));
+        typedef __attribute__((address_space(3))) s4 lds_s4;
+        const int k = kk * 16 + (lane >> 5) * 8 + ((lane >> 2) & 3);
+        const int r = row0 + ((lane >> 4) & 1) * 16 + (lane & 3) * 4;
+        const char *p = lds + k * (R * 2) + Operand<2, L, R, 1>::swizzle(k, r >> 3) * 16 +
+                        (r & 7) * 2;
+        union {
+            s4 h[2];
+            bf16x8 f;
+        } u;
+        u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4 *)p);
+        u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4 *)(p + 4 * R * 2));
+        return u.f;
+    }
+}
+
+// A 32-row fragment of 64 8-bit values of k (step kk of 2): lane l holds k
+// 16 (l / 32) + 0..15 and 32 more.
+template <int R> __device__ __forceinline__ i32x8 fragment64(const char *lds, int row0, int kk)
+{
+    const int lane = threadIdx.x & 63;
+    const int row = row0 + (lane & 31), chunk = kk * 4 + (lane >> 5);
+    union {
+        u32x4 h[2];
+        i32x8 f;
+    } u;
+    u.h[0] = *(const u32x4 *)(lds + row * kStepBytes +
+                              Operand<1, K_CONTIGUOUS, R, 1>::swizzle(row, chunk) * 16);
+    u.h[1] = *(const u32x4 *)(lds + row * kStepBytes +
+                              Operand<1, K_CONTIGUOUS, R, 1>::swizzle(row, chunk + 2) * 16);
+    return u.f;
+}
+
+// A 32-row fragment of 16 k (step kk of 8) of block-scaled values as bf16, which holds each
+// value: 4 significant bits.  s: the row's scales of the step.
+template <int R>
+__device__ __forceinline__ bf16x8 fragment_exact(const char *lds, uint32_t s, int row0, int kk)
+{
+    const int lane = threadIdx.x & 63, row = row0 + (lane & 31);
+    const u32x2 q = *(const u32x2 *)(lds + row * kStepBytes +
+                                     Operand<1, K_CONTIGUOUS, R, 1>::swizzle(row, kk) * 16 +
+                                     (lane >> 5) * 8);
+    const uint32_t byte = (s >> (kk / 2 * 8)) & 255u;
+    const float scale = bits_f32(byte == 0 ? 0x00400000u : byte == 255u ? 0x7fc00000u : byte << 23);
+    typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+    union {
+        b2 h[4];
+        bf16x8 f;
+    } u;
+    u.h[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(q[0], scale, false);
+    u.h[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(q[0], scale, true);
+    u.h[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(q[1], scale, false);
+    u.h[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(q[1], scale, true);
+    return u.f;
+}
+
+// Block scales of a step, a dword a row: bytes of 32 k each.
+template <int BM, int BN, int NT> struct Scales {
+    static constexpr int kLoads = (BM + BN + NT - 1) / NT;
+    uint32_t v[kLoads];
+    const uint8_t *p[kLoads];
+    __device__ __forceinline__ void init(const GemmArgs &g, int64_t m0, int64_t n0, int64_t k0)
+    {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int r = i * NT + (int)threadIdx.x;
+            const bool b = r >= BM;
+            const int64_t row = b ? min(n0 + r - BM, g.N - 1) : min(m0 + r, g.M - 1);
+            p[i] = (b ? g.bs + row * (g.ldb / kMxBlock) : g.as + row * (g.lda / kMxBlock)) +
+                   k0 / kMxBlock;
+        }
+    }
+    __device__ __forceinline__ void load(int64_t left)     // bytes of the row from here on
+    {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            if (left >= 4) {
+                __builtin_memcpy(&v[i], p[i], 4);
+            } else {
+                v[i] = 0x7f7f7f7fu;
+                for (int j = 0; j < (int)left; ++j)
+                    v[i] = (v[i] & ~(255u << (8 * j))) | (uint32_t)p[i][j] << (8 * j);
+            }
+            p[i] += 4;
+        }
+    }
+    __device__ __forceinline__ void store(uint32_t *lds) const
+    {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int r = i * NT + (int)threadIdx.x;
+            if ((BM + BN) % NT == 0 || r < BM + BN) lds[r] = v[i];
+        }
+    }
+};
+
+// Workgroup -> tile.  Consecutive workgroups go round the 8 XCDs, each with its own L2:
+// the tiles of an XCD are neighbours, in groups of 4 rows of tiles, so that the
+// tiles it holds at a time share operands.
+__device__ __forceinline__ void place_tile(uint32_t id, uint32_t tiles_m, uint32_t tiles_n,
+                                           uint32_t &tm, uint32_t &tn)
+{
+    const uint32_t total = tiles_m * tiles_n, per = total / 8, rest = total % 8;
+    const uint32_t x = id % 8, i = id / 8;
+    const uint32_t s = x * per + min(x, rest) + i;
+    const uint32_t group = s / (4 * tiles_n), first = group * 4;
+    const uint32_t rows = min(4u, tiles_m - first), in = s - group * 4 * tiles_n;
+    tm = first + in % rows;
+    tn = in / rows;
+}
+
+// EXACT: block-scaled values multiplied as bf16 (see gemm_mx).
+template <int EB, bool EXACT, typename T, Layout LA, Layout LB, int BM, int BN, int WAVES_M,
+          int WAVES_N>
+__global__ void __launch_bounds__(64 * WAVES_M *WAVES_N)
+    gemm_tile_kernel(GemmArgs g, uint32_t tiles_m, uint32_t tiles_n)
+{
+    constexpr int NW = WAVES_M * WAVES_N, NT = 64 * NW;
+    constexpr int WM = BM / WAVES_M / 32;
+    static_assert(BN / WAVES_N == 64, "a wave holds 64 columns");
+    constexpr int kA = BM * kStepBytes, kB = BN * kStepBytes;
+    constexpr int kScales = EB == 1 ? (BM + BN) * 4 : 0;
+    constexpr int kBuffer = kA + kB + kScales;
+    constexpr int kEpilogue = NW * kEpilogueFloats * 4;
+    __shared__ __attribute__((aligned(1024))) char lds[2 * kBuffer > kEpilogue ? 2 * kBuffer
+                                                                               : kEpilogue];
+    constexpr int kStepK = kStepBytes / EB;
+
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    uint32_t tm, tn;
+    place_tile(blockIdx.x, tiles_m, tiles_n, tm, tn);
+    const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * BN;
+    const int64_t kbeg = (int64_t)blockIdx.y * g.k_per, kend = min(g.K, kbeg + g.k_per);
+    const int wm = (wave % WAVES_M) * (WM * 32), wn = (wave / WAVES_M) * 64;
+
+    f32x16 acc[WM][2];
+#pragma unroll
+    for (int i = 0; i < WM; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
+
+    Operand<EB, LA, BM, NW> oa;
+    Operand<EB, LB, BN, NW> ob;
+    oa.init(g.a, g.lda, g.a_rows, m0, kbeg, LA == K_CONTIGUOUS ? min(kend, g.a_k) : min(kend, g.K));
+    ob.init(g.b, g.ldb, g.b_rows, n0, kbeg, LB == K_CONTIGUOUS ? min(kend, g.b_k) : min(kend, g.K));
+    Scales<BM, BN, NT> sc;
+    if constexpr (EB == 1) {
+        sc.init(g, m0, n0, kbeg);
+        sc.load((kend - kbeg) / kMxBlock);
+    }
+    oa.copy(lds, kbeg);
+    ob.copy(lds + kA, kbeg);
+    if constexpr (EB == 1) sc.store((uint32_t *)(lds + kA + kB));
+
+    int at = 0;
+    for (int64_t k = kbeg; k < kend; k += kStepK) {
+        wait_copies();
+        __syncthreads();
+        char *here = lds + at * kBuffer, *next = lds + (at ^ 1) * kBuffer;
+        at ^= 1;
+        const bool more = k + kStepK < kend;
+        if (more) {
+            if constexpr (EB == 1) sc.load((kend - k - kStepK) / kMxBlock);
+            oa.copy(next, k + kStepK);
+            ob.copy(next + kA, k + kStepK);
+        }
+        if constexpr (EB == 2) {
+            // The fragments of the next 16 k are read while the products of these run.
+            bf16x8 fa[2][WM], fb[2][2];
+            auto read = [&](int kk) {
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+                    fb[kk & 1][j] = fragment16<LB, BN>(here + kA, wn + 32 * j, kk);
+#pragma unroll
+                for (int i = 0; i < WM; ++i)
+                    fa[kk & 1][i] = fragment16<LA, BM>(here, wm + 32 * i, kk);
+            };
+            read(0);
+#pragma unroll
+            for (int kk = 0; kk < 4; ++kk) {
+                if (kk < 3) read(kk + 1);
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int i = 0; i < WM; ++i)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j)
+                        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                            fb[kk & 1][j], fa[kk & 1][i], acc[i][j], 0, 0, 0);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        } else if constexpr (EXACT) {
+            const uint32_t *s = (const uint32_t *)(here + kA + kB);
+            uint32_t sa[WM], sb[2];
+#pragma unroll
+            for (int i = 0; i < WM; ++i) sa[i] = s[wm + 32 * i + (lane & 31)];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) sb[j] = s[BM + wn + 32 * j + (lane & 31)];
+#pragma unroll
+            for (int kk = 0; kk < 8; ++kk) {
+                bf16x8 fa[WM], fb[2];
+#pragma unroll
+                for (int i = 0; i < WM; ++i)
+                    fa[i] = fragment_exact<BM>(here, sa[i], wm + 32 * i, kk);
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+                    fb[j] = fragment_exact<BN>(here + kA, sb[j], wn + 32 * j, kk);
+#pragma unroll
+                for (int i = 0; i < WM; ++i)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j)
+                        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[j], fa[i],
+                                                                            acc[i][j], 0, 0, 0);
+            }
+            if (more) sc.store((uint32_t *)(next + kA + kB));
+        } else {
+            // A lane's scale is of the 32 k its half of the wave stands for: byte
+            // 2 kk + lane / 32 of its row's dword.
+            const uint32_t *s = (const uint32_t *)(here + kA + kB);
+            int sa[WM], sb[2];
+#pragma unroll
+            for (int i = 0; i < WM; ++i) sa[i] = (int)(s[wm + 32 * i + (lane & 31)] >> ((lane >> 5) * 8));
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+                sb[j] = (int)(s[BM + wn + 32 * j + (lane & 31)] >> ((lane >> 5) * 8));
+#pragma unroll
+            for (int kk = 0; kk < 2; ++kk) {
+                i32x8 fa[WM], fb[2];
+#pragma unroll
+                for (int i = 0; i < WM; ++i) fa[i] = fragment64<BM>(here, wm + 32 * i, kk);
+#pragma unroll
+                for (int j = 0; j < 2; ++j) fb[j] = fragment64<BN>(here + kA, wn + 32 * j, kk);
+#pragma unroll
+                for (int i = 0; i < WM; ++i)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        if (kk == 0)
+                            acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
+                                fb[j], fa[i], acc[i][j], 0, 0, 0, sb[j], 0, sa[i]);
+                        else
+                            acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
+                                fb[j], fa[i], acc[i][j], 0, 0, 2, sb[j], 2, sa[i]);
+                    }
+            }
+            if (more) sc.store((uint32_t *)(next + kA + kB));
+        }
+    }
+    __syncthreads();
+    float *out = (float *)lds + wave * kEpilogueFloats;
+#pragma unroll
+    for (int i = 0; i < WM; ++i)
+        store_tile32x64<T>(g, out, m0 + wm + 32 * i, n0 + wn, blockIdx.y, acc[i][0], acc[i][1]);
+}
+
+// ---- shapes of tiles and splits of k ----
+struct TilePlan {
+    int bm, bn;
+    uint32_t tiles_m, tiles_n;
+    int64_t k_per;
+    int splits;
+};
+
+inline TilePlan plan_tiles(int64_t M, int64_t N, int64_t K, int step_k)
+{
+    TilePlan p{};
+    auto tiles = [&](int bm, int bn) { return ((M + bm - 1) / bm) * ((N + bn - 1) / bn); };
+    if (M <= 32) p.bm = 32, p.bn = 256;
+    else if (M <= 64) p.bm = 64, p.bn = 256;
+    else if (tiles(256, 256) >= 192) p.bm = 256, p.bn = 256;
+    else p.bm = 128, p.bn = 128;
+    p.tiles_m = (uint32_t)((M + p.bm - 1) / p.bm);
+    p.tiles_n = (uint32_t)((N + p.bn - 1) / p.bn);
+    const int64_t t = (int64_t)p.tiles_m * p.tiles_n, steps = (K + step_k - 1) / step_k;
+    // Fewer tiles than two a compute unit: k is split, four steps or more a part.
+    int64_t s = t >= 256 ? 1 : 512 / t;
+    s = s < steps / 4 ? s : steps / 4;
+    if (s < 1) s = 1;
+    p.k_per = (steps + s - 1) / s * step_k;
+    p.splits = (int)((K + p.k_per - 1) / p.k_per);
+    return p;
+}
+
+inline uint64_t tile_part_bytes(int64_t M, int64_t N, int64_t K, int step_k)
+{
+    const TilePlan p = plan_tiles(M, N, K, step_k);
+    return p.splits > 1 ? (uint64_t)p.splits * M * N * 4 : 0;
+}
+
+template <int EB, bool EXACT, typename T, Layout LA, Layout LB>
+hipError_t run_tiles(GemmArgs g, float *part, hipStream_t stream)
+{
+    const TilePlan p = plan_tiles(g.M, g.N, g.K, kStepBytes / EB);
+    g.k_per = p.k_per;
+    g.part = p.splits > 1 ? part : nullptr;
+    const dim3 grid(p.tiles_m * p.tiles_n, (uint32_t)p.splits);
+    if (p.bm == 32)
+        gemm_tile_kernel<EB, EXACT, T, LA, LB, 32, 256, 1, 4><<<grid, 256, 0, stream>>>(g, p.tiles_m, p.tiles_n);
+    else if (p.bm == 64)
+        gemm_tile_kernel<EB, EXACT, T, LA, LB, 64, 256, 1, 4><<<grid, 256, 0, stream>>>(g, p.tiles_m, p.tiles_n);
+    else if (p.bm == 256)
+        gemm_tile_kernel<EB, EXACT, T, LA, LB, 256, 256, 2, 4><<<grid, 512, 0, stream>>>(g, p.tiles_m, p.tiles_n);
+    else
+        gemm_tile_kernel<EB, EXACT, T, LA, LB, 128, 128, 2, 2><<<grid, 256, 0, stream>>>(g, p.tiles_m, p.tiles_n);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || p.splits == 1) return e;
+    const int64_t width = g.yq ? mx_width(g.N) : (g.N + 7) / 8 * 8;
+    split_sum_kernel<T><<<dim3((uint32_t)((g.M * width / 8 + 255) / 256)), dim3(256), 0, stream>>>(
+        g, p.splits);
+    return hipGetLastError();
+}
+
+}  // namespace whtmix

@@ -4,10 +4,9 @@
 //   z = x w + bias,  y = act(z) + residual
 //   dz = dy act'(z),  dx = dz w^T,  dw = x^T dz,  dbias = column sums of dz
 //
-// One tile kernel for every type: a 128 x 128 tile of four waves, operands
-// converted to bf16 terms on their way to LDS (one for bf16 and for block-scaled
-// 8 bits, three for float32), products on v_mfma_f32_32x32x16_bf16, sums in
-// float32.
+// bf16 and block-scaled 8 bits go to the tile kernel of whtmix_gemm_tile.h; float32 has its
+// own here: a 128 x 128 tile of four waves, operands split into three bf16 terms on
+// their way to LDS, products on v_mfma_f32_32x32x16_bf16, sums in float32.
 #include "whtmix_gemm.h"
 
 #include <algorithm>
@@ -25,16 +24,14 @@ constexpr int kF32Row = kTile + 4; // float32 staging: floats of one k
 constexpr uint32_t kSplitMax = 0x7f7f8000u, kSplitMin = 0x10000000u;   // 2^-95
 static_assert(kTile * kRowBytes == kPlane && kStep * kKBytes == kPlane, "planes");
 
-struct Mx {};      // element type of 8-bit operands
-
-template <typename E> constexpr int terms() { return std::is_same_v<E, float> ? 3 : 1; }
+constexpr int P = 3;               // bf16 terms of a float32
 
 // Sixteen elements of an operand in a thread's registers: of one row (16 k) or
 // one k (16 rows).
-template <typename E, Layout L> struct Stage {
+template <Layout L> struct Stage {
     float v[16];
-    __device__ __forceinline__ void load(const void *p, const uint8_t *sc, int64_t ld, int64_t R,
-                                         int64_t K, int64_t r0, int64_t k0)
+    __device__ __forceinline__ void load(const void *p, int64_t ld, int64_t R, int64_t K,
+                                         int64_t r0, int64_t k0)
     {
         const int t = threadIdx.x;
         int64_t outer, inner, n_outer, n_inner;
@@ -45,24 +42,9 @@ template <typename E, Layout L> struct Stage {
         }
         const int64_t left = outer < n_outer ? n_inner - inner : 0;
         const int n = (int)min((int64_t)16, max((int64_t)0, left));
-        if constexpr (std::is_same_v<E, Mx>) {
-            const uint8_t *q = (const uint8_t *)p + (n ? outer * ld + inner : 0);
-            const float s = n ? bits_f32((uint32_t)sc[outer * (ld / kMxBlock) + inner / kMxBlock] << 23)
-                              : 0.f;
-            u32x4 w = {0, 0, 0, 0};
-            if (n) w = *(const u32x4 *)q;       // rows are whole blocks
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                v[4 * i] = __builtin_amdgcn_cvt_f32_fp8((int)w[i], 0) * s;
-                v[4 * i + 1] = __builtin_amdgcn_cvt_f32_fp8((int)w[i], 1) * s;
-                v[4 * i + 2] = __builtin_amdgcn_cvt_f32_fp8((int)w[i], 2) * s;
-                v[4 * i + 3] = __builtin_amdgcn_cvt_f32_fp8((int)w[i], 3) * s;
-            }
-        } else {
-            const E *q = (const E *)p + (n ? outer * ld + inner : 0);
-            load8(q, n, *(float(*)[8])v);
-            load8(q + 8, n - 8, *(float(*)[8])(v + 8));
-        }
+        const float *q = (const float *)p + (n ? outer * ld + inner : 0);
+        load8(q, n, *(float(*)[8])v);
+        load8(q + 8, n - 8, *(float(*)[8])(v + 8));
     }
     // As float32, [k][row], for operands that do not split.
     __device__ __forceinline__ void store_f32(float *lds) const
@@ -87,12 +69,12 @@ template <typename E, Layout L> struct Stage {
         char *p = lds + (L == K_CONTIGUOUS ? (t >> 1) * kRowBytes + (t & 1) * 32
                                            : (t >> 3) * kKBytes + (t & 7) * 32);
 #pragma unroll
-        for (int s = 0; s < terms<E>(); ++s) {
+        for (int s = 0; s < P; ++s) {
             uint32_t w[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 w[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
-                if (s + 1 < terms<E>()) {
+                if (s + 1 < P) {
                     v[2 * i] -= bits_f32(w[i] << 16);
                     v[2 * i + 1] -= bits_f32(w[i] & 0xffff0000u);
                 }
@@ -130,8 +112,8 @@ template <Layout L> __device__ __forceinline__ bf16x8 fragment(const char *plane
 
 // The tile again with float32 products (v_mfma_f32_32x32x2_f32).
 template <Layout LA, Layout LB>
-__device__ __noinline__ void float32_tile(const GemmArgs &g, Stage<float, LA> &sa,
-                                          Stage<float, LB> &sb, float *lds, int64_t m0, int64_t n0,
+__device__ __forceinline__ void float32_tile(const GemmArgs &g, Stage<LA> &sa,
+                                          Stage<LB> &sb, float *lds, int64_t m0, int64_t n0,
                                           int64_t kbeg, int64_t kend, int wm, int wn,
                                           f32x16 (&acc)[2][2])
 {
@@ -144,8 +126,8 @@ __device__ __noinline__ void float32_tile(const GemmArgs &g, Stage<float, LA> &s
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
     for (int64_t k = kbeg; k < kend; k += kStep) {
-        sa.load(g.a, g.as, g.lda, g.M, kend, m0, k);
-        sb.load(g.b, g.bs, g.ldb, g.N, kend, n0, k);
+        sa.load(g.a, g.lda, g.M, kend, m0, k);
+        sb.load(g.b, g.ldb, g.N, kend, n0, k);
         __syncthreads();
         sa.store_f32(la);
         sb.store_f32(lb);
@@ -163,10 +145,9 @@ __device__ __noinline__ void float32_tile(const GemmArgs &g, Stage<float, LA> &s
     }
 }
 
-template <typename E, typename T, Layout LA, Layout LB>
+template <Layout LA, Layout LB>
 __global__ void __launch_bounds__(256) gemm_kernel(GemmArgs g)
 {
-    constexpr int P = terms<E>();
     __shared__ __attribute__((aligned(16))) char lds[2 * P * kPlane > 4 * kEpilogueFloats * 4
                                                          ? 2 * P * kPlane
                                                          : 4 * kEpilogueFloats * 4];
@@ -183,22 +164,20 @@ __global__ void __launch_bounds__(256) gemm_kernel(GemmArgs g)
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
 
-    Stage<E, LA> sa;
-    Stage<E, LB> sb;
-    uint32_t top_a = 0, top_b = 0;     // float32: what the splits have to hold
-    sa.load(g.a, g.as, g.lda, g.M, kend, m0, kbeg);
-    sb.load(g.b, g.bs, g.ldb, g.N, kend, n0, kbeg);
+    Stage<LA> sa;
+    Stage<LB> sb;
+    uint32_t top_a = 0, top_b = 0;     // what the splits have to hold
+    sa.load(g.a, g.lda, g.M, kend, m0, kbeg);
+    sb.load(g.b, g.ldb, g.N, kend, n0, kbeg);
     for (int64_t k = kbeg; k < kend; k += kStep) {
         __syncthreads();
-        if constexpr (P > 1) {
-            top_a = sa.largest(top_a);
-            top_b = sb.largest(top_b);
-        }
+        top_a = sa.largest(top_a);
+        top_b = sb.largest(top_b);
         sa.store(la);
         sb.store(lb);
         if (k + kStep < kend) {
-            sa.load(g.a, g.as, g.lda, g.M, kend, m0, k + kStep);
-            sb.load(g.b, g.bs, g.ldb, g.N, kend, n0, k + kStep);
+            sa.load(g.a, g.lda, g.M, kend, m0, k + kStep);
+            sb.load(g.b, g.ldb, g.N, kend, n0, k + kStep);
         }
         __syncthreads();
 #pragma unroll
@@ -225,18 +204,16 @@ __global__ void __launch_bounds__(256) gemm_kernel(GemmArgs g)
                                 fb[s - p][j], fa[p][i], acc[i][j], 0, 0, 0);
         }
     }
-    if constexpr (P > 1) {
-        auto bad = [](uint32_t top) { return top >= kSplitMax || (top != 0 && top < kSplitMin); };
-        // A thread's share is its row's (or its rows') k; one that does not split sends the
-        // whole tile through float32 products.
-        if (__syncthreads_or(bad(top_a) || bad(top_b)))
-            float32_tile(g, sa, sb, (float *)lds, m0, n0, kbeg, kend, wm, wn, acc);
-    }
+    auto bad = [](uint32_t top) { return top >= kSplitMax || (top != 0 && top < kSplitMin); };
+    // A thread's share is its row's (or its rows') k; one that does not split sends the
+    // whole tile through float32 products.
+    if (__syncthreads_or(bad(top_a) || bad(top_b)))
+        float32_tile(g, sa, sb, (float *)lds, m0, n0, kbeg, kend, wm, wn, acc);
     __syncthreads();
     float *out = (float *)lds + wave * kEpilogueFloats;
 #pragma unroll
     for (int i = 0; i < 2; ++i)
-        store_tile32x64<T>(g, out, m0 + wm + 32 * i, n0 + wn, blockIdx.z, acc[i][0], acc[i][1]);
+        store_tile32x64<float>(g, out, m0 + wm + 32 * i, n0 + wn, blockIdx.z, acc[i][0], acc[i][1]);
 }
 
 // How many parts k is split into: enough workgroups for the device where the
@@ -254,7 +231,7 @@ uint64_t gemm_bytes(int64_t M, int64_t N, int64_t K)
     return s > 1 ? (uint64_t)s * M * N * 4 : 0;
 }
 
-template <typename E, typename T, Layout LA, Layout LB>
+template <Layout LA, Layout LB>
 hipError_t run_gemm(GemmArgs g, float *ws, hipStream_t stream)
 {
     const int64_t s = splits_of(g.M, g.N, g.K);
@@ -264,11 +241,11 @@ hipError_t run_gemm(GemmArgs g, float *ws, hipStream_t stream)
     g.part = splits > 1 ? ws : nullptr;
     const dim3 grid((uint32_t)((g.M + kTile - 1) / kTile), (uint32_t)((g.N + kTile - 1) / kTile),
                     (uint32_t)splits);
-    gemm_kernel<E, T, LA, LB><<<grid, dim3(256), 0, stream>>>(g);
+    gemm_kernel<LA, LB><<<grid, dim3(256), 0, stream>>>(g);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || splits == 1) return e;
     const int64_t width = g.yq ? mx_width(g.N) : (g.N + 7) / 8 * 8;
-    split_sum_kernel<T><<<dim3((uint32_t)((g.M * width / 8 + 255) / 256)), dim3(256), 0, stream>>>(
+    split_sum_kernel<float><<<dim3((uint32_t)((g.M * width / 8 + 255) / 256)), dim3(256), 0, stream>>>(
         g, (int)splits);
     return hipGetLastError();
 }
@@ -311,10 +288,54 @@ int64_t dz_parts(int64_t M, int64_t N)
     return std::min<int64_t>(M, std::max<int64_t>(1, 1024 / cols));
 }
 
+template <typename T>
+hipError_t product(const GemmArgs &g, Layout la, Layout lb, void *ws, hipStream_t stream)
+{
+    if constexpr (std::is_same_v<T, __bf16>) {
+        return gemm_bf16(g, la, lb, ws, stream);
+    } else {
+        float *w = (float *)ws;
+        if (la == K_CONTIGUOUS && lb == K_STRIDED)
+            return run_gemm<K_CONTIGUOUS, K_STRIDED>(g, w, stream);
+        if (la == K_CONTIGUOUS) return run_gemm<K_CONTIGUOUS, K_CONTIGUOUS>(g, w, stream);
+        return run_gemm<K_STRIDED, K_STRIDED>(g, w, stream);
+    }
+}
+
+uint64_t product_bytes(const GemmArgs &g, Layout la, Layout lb, int dtype)
+{
+    return dtype == DTYPE_BF16 ? gemm_bf16_bytes(g, la, lb) : gemm_bytes(g.M, g.N, g.K);
+}
+
+GemmArgs forward_args(const LinearArgs &a)
+{
+    GemmArgs g{};
+    g.a = a.x, g.lda = a.ldx, g.b = a.w, g.ldb = a.N;
+    g.M = a.M, g.N = a.N, g.K = a.K;
+    g.bias = a.bias, g.residual = a.residual, g.y = a.y, g.z = a.z, g.act = a.act;
+    return g;
+}
+
+GemmArgs dx_args(const LinearBackwardArgs &a, const void *dz)
+{
+    GemmArgs g{};
+    g.a = dz, g.lda = a.N, g.b = a.w, g.ldb = a.N;
+    g.M = a.M, g.N = a.K, g.K = a.N, g.y = a.dx;
+    return g;
+}
+
+GemmArgs dw_args(const LinearBackwardArgs &a, const void *dz)
+{
+    GemmArgs g{};
+    g.a = a.x, g.lda = a.ldx, g.b = dz, g.ldb = a.N;
+    g.M = a.K, g.N = a.N, g.K = a.M, g.y = a.dw;
+    return g;
+}
+
 uint64_t align256(uint64_t v) { return (v + 255) / 256 * 256; }
 
 struct BackwardLayoutBytes {
-    uint64_t dz = 0, part = 0, gemm = 0;     // sizes
+    uint64_t dz = 0, part = 0, product = 0;
 };
 BackwardLayoutBytes backward_bytes(const LinearBackwardArgs &a)
 {
@@ -322,8 +343,10 @@ BackwardLayoutBytes backward_bytes(const LinearBackwardArgs &a)
     const int e = a.dtype == DTYPE_BF16 ? 2 : 4;
     if (a.act != ACT_NONE) l.dz = align256((uint64_t)a.M * a.N * e);
     if (a.dbias) l.part = align256((uint64_t)dz_parts(a.M, a.N) * a.N * 4);
-    if (a.dx) l.gemm = gemm_bytes(a.M, a.K, a.N);
-    if (a.dw) l.gemm = std::max(l.gemm, gemm_bytes(a.K, a.N, a.M));
+    const void *dz = a.act != ACT_NONE ? nullptr : a.dy;    // a workspace's address is aligned
+    if (a.dx) l.product = product_bytes(dx_args(a, dz), K_CONTIGUOUS, K_CONTIGUOUS, a.dtype);
+    if (a.dw)
+        l.product = std::max(l.product, product_bytes(dw_args(a, dz), K_STRIDED, K_STRIDED, a.dtype));
     return l;
 }
 
@@ -332,7 +355,8 @@ template <typename T> hipError_t linear_backward(const LinearBackwardArgs &a)
     const BackwardLayoutBytes l = backward_bytes(a);
     char *ws = (char *)a.ws;
     T *dz = (T *)ws;
-    float *part = (float *)(ws + l.dz), *gemm = (float *)(ws + l.dz + l.part);
+    float *part = (float *)(ws + l.dz);
+    void *rest = ws + l.dz + l.part;
     hipError_t e;
     if (a.act != ACT_NONE || a.dbias) {
         const int64_t parts = dz_parts(a.M, a.N);
@@ -346,54 +370,14 @@ template <typename T> hipError_t linear_backward(const LinearBackwardArgs &a)
             return e;
     }
     const void *d = a.act != ACT_NONE ? (const void *)dz : a.dy;
-    if (a.dx) {
-        GemmArgs g{};
-        g.a = d, g.lda = a.N, g.b = a.w, g.ldb = a.N;
-        g.M = a.M, g.N = a.K, g.K = a.N, g.y = a.dx;
-        if ((e = run_gemm<T, T, K_CONTIGUOUS, K_CONTIGUOUS>(g, gemm, a.stream)) != hipSuccess)
-            return e;
-    }
-    if (a.dw) {
-        GemmArgs g{};
-        g.a = a.x, g.lda = a.ldx, g.b = d, g.ldb = a.N;
-        g.M = a.K, g.N = a.N, g.K = a.M, g.y = a.dw;
-        if ((e = run_gemm<T, T, K_STRIDED, K_STRIDED>(g, gemm, a.stream)) != hipSuccess) return e;
-    }
+    if (a.dx && (e = product<T>(dx_args(a, d), K_CONTIGUOUS, K_CONTIGUOUS, rest, a.stream)) !=
+                    hipSuccess)
+        return e;
+    if (a.dw) return product<T>(dw_args(a, d), K_STRIDED, K_STRIDED, rest, a.stream);
     return hipSuccess;
 }
 
-template <typename T> hipError_t linear_forward(const LinearArgs &a)
-{
-    GemmArgs g{};
-    g.a = a.x, g.lda = a.ldx, g.b = a.w, g.ldb = a.N;
-    g.M = a.M, g.N = a.N, g.K = a.K;
-    g.bias = a.bias, g.residual = a.residual, g.y = a.y, g.z = a.z, g.act = a.act;
-    return run_gemm<T, T, K_CONTIGUOUS, K_STRIDED>(g, a.ws, a.stream);
-}
-
-}  // namespace
-
-uint64_t linear_bytes(const LinearArgs &a) { return gemm_bytes(a.M, a.N, a.K); }
-
-hipError_t launch_linear(const LinearArgs &a)
-{
-    return a.dtype == DTYPE_BF16 ? linear_forward<__bf16>(a) : linear_forward<float>(a);
-}
-
-uint64_t linear_backward_bytes(const LinearBackwardArgs &a)
-{
-    const BackwardLayoutBytes l = backward_bytes(a);
-    return l.dz + l.part + l.gemm;
-}
-
-hipError_t launch_linear_backward(const LinearBackwardArgs &a)
-{
-    return a.dtype == DTYPE_BF16 ? linear_backward<__bf16>(a) : linear_backward<float>(a);
-}
-
-uint64_t linear_mx_bytes(const LinearMxArgs &a) { return gemm_bytes(a.M, a.N, mx_width(a.K)); }
-
-hipError_t launch_linear_mx(const LinearMxArgs &a)
+GemmArgs mx_args(const LinearMxArgs &a)
 {
     GemmArgs g{};
     g.a = a.xq, g.as = a.xs, g.b = a.wq, g.bs = a.ws8;
@@ -401,9 +385,39 @@ hipError_t launch_linear_mx(const LinearMxArgs &a)
     g.M = a.M, g.N = a.N;
     g.bias = a.bias, g.residual = a.residual, g.act = a.act;
     g.y = a.y, g.yq = (uint8_t *)a.yq, g.ys = a.ys;
-    if (a.dtype == DTYPE_BF16)
-        return run_gemm<Mx, __bf16, K_CONTIGUOUS, K_CONTIGUOUS>(g, a.ws, a.stream);
-    return run_gemm<Mx, float, K_CONTIGUOUS, K_CONTIGUOUS>(g, a.ws, a.stream);
+    return g;
+}
+
+}  // namespace
+
+uint64_t linear_bytes(const LinearArgs &a)
+{
+    return product_bytes(forward_args(a), K_CONTIGUOUS, K_STRIDED, a.dtype);
+}
+
+hipError_t launch_linear(const LinearArgs &a)
+{
+    const GemmArgs g = forward_args(a);
+    return a.dtype == DTYPE_BF16 ? product<__bf16>(g, K_CONTIGUOUS, K_STRIDED, a.ws, a.stream)
+                                 : product<float>(g, K_CONTIGUOUS, K_STRIDED, a.ws, a.stream);
+}
+
+uint64_t linear_backward_bytes(const LinearBackwardArgs &a)
+{
+    const BackwardLayoutBytes l = backward_bytes(a);
+    return l.dz + l.part + l.product;
+}
+
+hipError_t launch_linear_backward(const LinearBackwardArgs &a)
+{
+    return a.dtype == DTYPE_BF16 ? linear_backward<__bf16>(a) : linear_backward<float>(a);
+}
+
+uint64_t linear_mx_bytes(const LinearMxArgs &a) { return gemm_mx_bytes(mx_args(a)); }
+
+hipError_t launch_linear_mx(const LinearMxArgs &a)
+{
+    return gemm_mx(mx_args(a), a.dtype, a.ws, a.stream);
 }
 
 }  // namespace whtmix
