@@ -161,11 +161,17 @@ template <typename T> __global__ void __launch_bounds__(256) split_sum_kernel(Ge
     float v[8];
 #pragma unroll
     for (int k = 0; k < 8; ++k) v[k] = 0.f;
-    for (int s = 0; s < splits; ++s) {
-        float p[8];
-        load8(g.part + ((int64_t)s * g.M + m) * g.N + n, (int)min((int64_t)8, g.N - n), p);
+    const int cnt = (int)min((int64_t)8, g.N - n);
+    for (int s = 0; s < splits; s += 4) {       // four parts' loads in flight
+        float p[4][8];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] += p[k];
+        for (int u = 0; u < 4; ++u)
+            load8(g.part + ((int64_t)min(s + u, splits - 1) * g.M + m) * g.N + n,
+                  s + u < splits ? cnt : 0, p[u]);
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] += p[u][k];
     }
     finish8<T>(g, m, n, v);
 }

@@ -63,7 +63,7 @@ template <int EB, Layout L, int R, int NW> struct Operand {
 
     static __device__ __forceinline__ int swizzle(int outer, int chunk)
     {
-        if constexpr (L == K_CONTIGUOUS) return chunk ^ (outer & 7);
+        if constexpr (L == K_CONTIGUOUS) return chunk ^ ((outer >> 1) & 7);
         else return chunk ^ ((4 * (outer & 3)) & (kRowChunks - 1));
     }
     // The (row or k, chunk) that copy i of this lane fetches.

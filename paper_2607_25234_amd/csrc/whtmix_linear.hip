@@ -250,43 +250,71 @@ hipError_t run_gemm(GemmArgs g, float *ws, hipStream_t stream)
     return hipGetLastError();
 }
 
-// dz = dy act'(z), 8 columns a thread down `per` rows, with the columns' sums
-// of the unrounded values.
+// dz = dy act'(z), with the columns' sums of the unrounded values: 32 threads across
+// 256 columns, 8 rows at a time, four of them in flight a thread; the workgroup's 8
+// sums of a column are added in order.
+constexpr int kDzRows = 8, kDzCols = 256;
+
 template <typename T>
 __global__ void __launch_bounds__(256) dz_kernel(const T *dy, const T *z, T *dz, float *part,
                                                  int64_t M, int64_t N, int64_t per, int act)
 {
-    const int64_t n = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
+    __shared__ float sums[kDzRows][kDzCols + 8];
+    const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
+    const int64_t n = (int64_t)blockIdx.x * kDzCols + tx * 8;
     const int cnt = (int)min((int64_t)8, N - n);
-    if (cnt <= 0) return;
     float s[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) s[i] = 0.f;
     const int64_t end = min(M, ((int64_t)blockIdx.y + 1) * per);
-    with_act(act, [&](auto tag) {
-        constexpr int ACT = decltype(tag)::value;
-        for (int64_t m = (int64_t)blockIdx.y * per; m < end; ++m) {
-            float d[8];
-            load8(dy + m * N + n, cnt, d);
-            if (ACT != ACT_NONE) {
-                float v[8];
-                load8(z + m * N + n, cnt, v);
+    if (cnt > 0)
+        with_act(act, [&](auto tag) {
+            constexpr int ACT = decltype(tag)::value;
+            constexpr int U = 4;
+            for (int64_t m = (int64_t)blockIdx.y * per + ty; m < end; m += U * kDzRows) {
+                float d[U][8], v[U][8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) d[i] *= act_grad<ACT>(v[i]);
-                if (dz) store8(dz + m * N + n, cnt, d);
+                for (int u = 0; u < U; ++u) {
+                    const int64_t r = m + u * kDzRows;
+                    const int c = r < end ? cnt : 0;
+                    const int64_t at = (r < end ? r : m) * N + n;
+                    load8(dy + at, c, d[u]);
+                    if (ACT != ACT_NONE) load8(z + at, c, v[u]);
+                }
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    const int64_t r = m + u * kDzRows;
+                    if (r >= end) break;
+                    if (ACT != ACT_NONE) {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) d[u][i] *= act_grad<ACT>(v[u][i]);
+                        if (dz) store8(dz + r * N + n, cnt, d[u]);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) s[i] += d[u][i];
+                }
             }
+        });
+    if (!part) return;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) s[i] += d[i];
-        }
-    });
-    if (part) store8(part + (int64_t)blockIdx.y * N + n, cnt, s);
+    for (int i = 0; i < 8; ++i) sums[ty][tx * 8 + i] = s[i];
+    __syncthreads();
+    const int64_t c = (int64_t)blockIdx.x * kDzCols + threadIdx.x;
+    if (c >= N) return;
+    float t = 0.f;
+#pragma unroll
+    for (int r = 0; r < kDzRows; ++r) t += sums[r][threadIdx.x];
+    part[(int64_t)blockIdx.y * N + c] = t;
 }
 
+// Workgroups down the rows: about 1024 in all, 32 rows or more each.
 int64_t dz_parts(int64_t M, int64_t N)
 {
-    const int64_t cols = (N + 2047) / 2048;
-    return std::min<int64_t>(M, std::max<int64_t>(1, 1024 / cols));
+    const int64_t cols = (N + kDzCols - 1) / kDzCols;
+    return std::max<int64_t>(1, std::min<int64_t>((M + 31) / 32, 1024 / cols));
 }
+
+uint64_t align256(uint64_t v) { return (v + 255) / 256 * 256; }
 
 template <typename T>
 hipError_t product(const GemmArgs &g, Layout la, Layout lb, void *ws, hipStream_t stream)
@@ -332,8 +360,6 @@ GemmArgs dw_args(const LinearBackwardArgs &a, const void *dz)
     return g;
 }
 
-uint64_t align256(uint64_t v) { return (v + 255) / 256 * 256; }
-
 struct BackwardLayoutBytes {
     uint64_t dz = 0, part = 0, product = 0;
 };
@@ -361,7 +387,8 @@ template <typename T> hipError_t linear_backward(const LinearBackwardArgs &a)
     if (a.act != ACT_NONE || a.dbias) {
         const int64_t parts = dz_parts(a.M, a.N);
         const int64_t per = (a.M + parts - 1) / parts;
-        const dim3 grid((uint32_t)((a.N + 2047) / 2048), (uint32_t)((a.M + per - 1) / per));
+        const dim3 grid((uint32_t)((a.N + kDzCols - 1) / kDzCols),
+                        (uint32_t)((a.M + per - 1) / per));
         dz_kernel<T><<<grid, dim3(256), 0, a.stream>>>(
             (const T *)a.dy, (const T *)a.z, a.dx || a.dw ? dz : nullptr,
             a.dbias ? part : nullptr, a.M, a.N, per, a.act);

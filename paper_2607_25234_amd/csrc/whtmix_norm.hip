@@ -392,7 +392,7 @@ __global__ void __launch_bounds__(256) norm_backward_columns(NormBackwardKernelA
 // Chunks of a row that stay in the backward kernel's registers, at most (a lane of 1024
 // threads has 128 of them).
 constexpr int64_t wide_chunks(int per) { return per == 8 ? 2048 : 4096; }
-constexpr int64_t kBackwardBlocks = 1024;  // workgroups, and so partial sums of dw, at most
+constexpr int64_t kBackwardBlocks = 768;   // workgroups, and so partial sums of dw, at most
 
 int64_t lanes_of(int64_t n)                // of the backward kernel for rows of n chunks
 {
@@ -459,8 +459,14 @@ __global__ void __launch_bounds__(1024) column_sum_kernel(const float *part, int
     const int cx = threadIdx.x & 31, ry = threadIdx.x >> 5;
     const int64_t c = (int64_t)blockIdx.x * 32 + cx;
     float t = 0.f;
-    if (c < C)
-        for (int64_t r = ry; r < n; r += 32) t += part[r * C + c];
+    for (int64_t r = ry; r < n; r += 8 * 32) {      // eight loads in flight
+        float v[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+            v[u] = c < C && r + u * 32 < n ? part[(r + u * 32) * C + c] : 0.f;
+#pragma unroll
+        for (int u = 0; u < 8; ++u) t += v[u];
+    }
     s[ry][cx] = t;
     __syncthreads();
     if (ry == 0 && c < C) {
