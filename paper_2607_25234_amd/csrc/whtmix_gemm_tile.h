@@ -23,18 +23,10 @@ static __device__ __attribute__((aligned(16))) const uint32_t kZero16[4] = {0, 0
 
 constexpr int kStepBytes = 128;
 
-typedef __attribute__((address_space(3))) void lds_void;
-
-// A wave's LDS address, uniform.
-__device__ __forceinline__ uint32_t lds_address(char *p)
-{
-    return (uint32_t)__builtin_amdgcn_readfirstlane((int)(uintptr_t)(lds_void *)p);
-}
-
-// 16 bytes a lane from memory to LDS (lane order from the wave's address), counted by vmcnt.
-// In assembler, because the compiler would have every later LDS read wait for the copies in
-// flight; the kernel waits for them itself, a step later.  No registers but m0 are written, which
-// nothing else in these kernels uses.
+// 16 bytes a lane from memory to LDS (lane order from the wave's address `lds`), counted by
+// vmcnt.  In assembler, because the compiler would have every later LDS read wait for the
+// copies in flight; the kernel waits for them itself, a step later.  No registers but m0 are
+// written, which nothing else in these kernels uses.
 __device__ __forceinline__ void copy16(const char *base, uint32_t off, uint32_t lds)
 {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds),
@@ -47,7 +39,11 @@ __device__ __forceinline__ void copy16(const char *src, uint32_t lds)
                  "v"(src)
                  : "memory");
 }
-__device__ __forceinline__ void wait_copies() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+// Until at most LEFT of the wave's copies (and loads) are in flight.
+template <int LEFT> __device__ __forceinline__ void wait_copies()
+{
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LEFT) : "memory");
+}
 
 // One operand's tile: R rows of output (or k-strided columns), NW waves copying.
 template <int EB, Layout L, int R, int NW> struct Operand {
@@ -56,13 +52,15 @@ template <int EB, Layout L, int R, int NW> struct Operand {
     static_assert(R % (8 * NW) == 0, "whole copies");
     static constexpr int kRowChunks = L == K_CONTIGUOUS ? 8 : R * EB / 16;
 
-    const char *base;       // of the tile at the current step (uniform)
+    const char *base;       // of the tile at the next step to copy (uniform)
     uint32_t off[kCopies];  // of this lane's chunks from there
-    int64_t ld;             // bytes
+    int64_t ahead;          // bytes from a step to the next
     int64_t k_end;          // of the operand: chunks from there on are zeros
 
     static __device__ __forceinline__ int swizzle(int outer, int chunk)
     {
+        // A cycle of an LDS read serves 16 lanes: 16 rows of 128 bytes fall on all 64 banks
+        // when every second row's chunks are permuted alike.
         if constexpr (L == K_CONTIGUOUS) return chunk ^ ((outer >> 1) & 7);
         else return chunk ^ ((4 * (outer & 3)) & (kRowChunks - 1));
     }
@@ -78,37 +76,39 @@ template <int EB, Layout L, int R, int NW> struct Operand {
     __device__ __forceinline__ void init(const void *p, int64_t ld_elements, int64_t rows,
                                          int64_t r0, int64_t k0, int64_t kend)
     {
-        ld = ld_elements * EB;
+        const int64_t ld = ld_elements * EB;
         k_end = kend;
+        ahead = L == K_CONTIGUOUS ? kStepBytes : kStepK * ld;
         base = (const char *)p + (L == K_CONTIGUOUS ? r0 * ld + k0 * EB : k0 * ld + r0 * EB);
+        const uint32_t ld32 = (uint32_t)ld, last = (uint32_t)min((int64_t)R, rows - r0);
 #pragma unroll
         for (int i = 0; i < kCopies; ++i) {
             int outer, chunk;
             place(i, outer, chunk);
             if constexpr (L == K_CONTIGUOUS)     // rows past the end repeat the last one
-                off[i] = (uint32_t)(min((int64_t)outer, rows - 1 - r0) * ld) + chunk * 16;
+                off[i] = min((uint32_t)outer, last - 1) * ld32 + (uint32_t)chunk * 16;
             else                                 // columns likewise
-                off[i] = (uint32_t)(outer * ld) +
-                         (uint32_t)min((int64_t)chunk * 16, (rows - r0) * EB - 16);
+                off[i] = (uint32_t)outer * ld32 + min((uint32_t)chunk * 16, last * EB - 16);
         }
     }
-    // The step at k, and on to the next.
-    __device__ __forceinline__ void copy(char *lds, int64_t k)
+    // The next step, to the LDS address of this wave's part.
+    __device__ __forceinline__ void copy(uint32_t lds)
     {
-        const uint32_t to = lds_address(lds + (threadIdx.x >> 6) * 1024);
-        if (k + kStepK <= k_end) {
 #pragma unroll
-            for (int i = 0; i < kCopies; ++i) copy16(base, off[i], to + i * NW * 1024);
-        } else {
+        for (int i = 0; i < kCopies; ++i) copy16(base, off[i], lds + i * NW * 1024);
+        base += ahead;
+    }
+    // The last step, at k, with zeros from k_end on.
+    __device__ __forceinline__ void copy_last(uint32_t lds, int64_t k)
+    {
+        const int left = (int)min(k_end - k, (int64_t)kStepK);
 #pragma unroll
-            for (int i = 0; i < kCopies; ++i) {
-                int outer, chunk;
-                place(i, outer, chunk);
-                const int64_t at = k + (L == K_CONTIGUOUS ? chunk * (16 / EB) : outer);
-                copy16(at < k_end ? base + off[i] : (const char *)kZero16, to + i * NW * 1024);
-            }
+        for (int i = 0; i < kCopies; ++i) {
+            int outer, chunk;
+            place(i, outer, chunk);
+            const int at = L == K_CONTIGUOUS ? chunk * (16 / EB) : outer;
+            copy16(at < left ? base + off[i] : (const char *)kZero16, lds + i * NW * 1024);
         }
-        base += L == K_CONTIGUOUS ? kStepBytes : kStepK * ld;
     }
 };
 
@@ -195,19 +195,21 @@ template <int BM, int BN, int NT> struct Scales {
                    k0 / kMxBlock;
         }
     }
-    __device__ __forceinline__ void load(int64_t left)     // bytes of the row from here on
+    __device__ __forceinline__ void load()
     {
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
-            if (left >= 4) {
-                __builtin_memcpy(&v[i], p[i], 4);
-            } else {
-                v[i] = 0x7f7f7f7fu;
-                for (int j = 0; j < (int)left; ++j)
-                    v[i] = (v[i] & ~(255u << (8 * j))) | (uint32_t)p[i][j] << (8 * j);
-            }
+            __builtin_memcpy(&v[i], p[i], 4);
             p[i] += 4;
         }
+    }
+    // The last step's `left` (1 to 4) bytes; the others' values are zeros whatever their scale.
+    __device__ __forceinline__ void load_last(int left)
+    {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i)
+            v[i] = (uint32_t)p[i][0] | (uint32_t)p[i][min(1, left - 1)] << 8 |
+                   (uint32_t)p[i][min(2, left - 1)] << 16 | (uint32_t)p[i][left - 1] << 24;
     }
     __device__ __forceinline__ void store(uint32_t *lds) const
     {
@@ -232,6 +234,14 @@ __device__ __forceinline__ void place_tile(uint32_t id, uint32_t tiles_m, uint32
     const uint32_t rows = min(4u, tiles_m - first), in = s - group * 4 * tiles_n;
     tm = first + in % rows;
     tn = in / rows;
+}
+
+template <int N, typename F, int I = 0> __device__ __forceinline__ void static_for(F f)
+{
+    if constexpr (I < N) {
+        f(std::integral_constant<int, I>{});
+        static_for<N, F, I + 1>(f);
+    }
 }
 
 // EXACT: block-scaled values multiplied as bf16 (see gemm_mx).
@@ -271,106 +281,121 @@ __global__ void __launch_bounds__(64 * WAVES_M *WAVES_N)
     oa.init(g.a, g.lda, g.a_rows, m0, kbeg, LA == K_CONTIGUOUS ? min(kend, g.a_k) : min(kend, g.K));
     ob.init(g.b, g.ldb, g.b_rows, n0, kbeg, LB == K_CONTIGUOUS ? min(kend, g.b_k) : min(kend, g.K));
     Scales<BM, BN, NT> sc;
-    if constexpr (EB == 1) {
-        sc.init(g, m0, n0, kbeg);
-        sc.load((kend - kbeg) / kMxBlock);
-    }
-    oa.copy(lds, kbeg);
-    ob.copy(lds + kA, kbeg);
-    if constexpr (EB == 1) sc.store((uint32_t *)(lds + kA + kB));
+    const int steps = (int)((kend - kbeg + kStepK - 1) / kStepK);
+    const uint32_t lds_wave = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds +
+                              (uint32_t)__builtin_amdgcn_readfirstlane(wave) * 1024;
+    auto copy = [&](int t) {
+        const uint32_t to = lds_wave + (t & 1) * kBuffer;
+        if constexpr (EB == 1) sc.load();
+        oa.copy(to);
+        ob.copy(to + kA);
+    };
+    auto copy_last = [&](int t) {
+        const uint32_t to = lds_wave + (t & 1) * kBuffer;
+        const int64_t k = kbeg + (int64_t)t * kStepK;
+        if constexpr (EB == 1) sc.load_last((int)min((kend - k) / kMxBlock, (int64_t)4));
+        oa.copy_last(to, k);
+        ob.copy_last(to + kA, k);
+    };
+    // A step's scales pass registers: they go to LDS once the copies have landed.
+    auto landed = [&](int t) {
+        if constexpr (EB == 1) sc.store((uint32_t *)(lds + (t & 1) * kBuffer + kA + kB));
+    };
+    constexpr int kParts = EB == 2 ? 4 : EXACT ? 8 : 2;
+    using Fragment = std::conditional_t<EB == 1 && !EXACT, i32x8, bf16x8>;
+    Fragment fa[WM], fb[2];
+    uint32_t sa[WM], sb[2], ua[WM], ub[2];      // scales of the fragments read, and in use
+    auto read_scales = [&](int t) {
+        if constexpr (EB == 1) {
+            // EXACT: the row's four scales.  Else a lane's scale is of the 32 k its half of
+            // the wave stands for: byte 2 kk + lane / 32.
+            const uint32_t *s = (const uint32_t *)(lds + (t & 1) * kBuffer + kA + kB);
+            const int shift = EXACT ? 0 : (lane >> 5) * 8;
+#pragma unroll
+            for (int j = 0; j < 2; ++j) sb[j] = s[BM + wn + 32 * j + (lane & 31)] >> shift;
+#pragma unroll
+            for (int i = 0; i < WM; ++i) sa[i] = s[wm + 32 * i + (lane & 31)] >> shift;
+        }
+    };
+    // Fragments of part kk of step t.
+    auto read_b = [&](int t, int kk, int j) {
+        const char *here = lds + (t & 1) * kBuffer + kA;
+        if constexpr (EB == 2) fb[j] = fragment16<LB, BN>(here, wn + 32 * j, kk);
+        else if constexpr (EXACT) fb[j] = fragment_exact<BN>(here, sb[j], wn + 32 * j, kk);
+        else fb[j] = fragment64<BN>(here, wn + 32 * j, kk);
+    };
+    auto read_a = [&](int t, int kk, int i) {
+        const char *here = lds + (t & 1) * kBuffer;
+        if constexpr (EB == 2) fa[i] = fragment16<LA, BM>(here, wm + 32 * i, kk);
+        else if constexpr (EXACT) fa[i] = fragment_exact<BM>(here, sa[i], wm + 32 * i, kk);
+        else fa[i] = fragment64<BM>(here, wm + 32 * i, kk);
+    };
+    // The products of part kk of step t.  Behind the last product that needs a fragment,
+    // the next part's is read into its registers, which the products between cover.
+    auto multiply = [&](auto part, int t) {
+        constexpr int kk = decltype(part)::value, next = (kk + 1) % kParts;
+        const int tn = kk + 1 == kParts ? t + 1 : t;
+        if constexpr (EB == 1 && kk == 0) {
+#pragma unroll
+            for (int i = 0; i < WM; ++i) ua[i] = sa[i];
+            ub[0] = sb[0], ub[1] = sb[1];
+        }
+        if constexpr (next == 0) read_scales(tn);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+#pragma unroll
+            for (int i = 0; i < WM; ++i) {
+                if constexpr (EB == 1 && !EXACT)
+                    acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
+                        fb[j], fa[i], acc[i][j], 0, 0, 2 * kk, (int)ub[j], 2 * kk, (int)ua[i]);
+                else
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[j], fa[i], acc[i][j],
+                                                                        0, 0, 0);
+                if (j == 1) {
+                    __builtin_amdgcn_sched_barrier(0);
+                    read_a(tn, next, i);
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            read_b(tn, next, j);
+        }
+    };
 
-    int at = 0;
-    for (int64_t k = kbeg; k < kend; k += kStepK) {
-        wait_copies();
-        __syncthreads();
-        char *here = lds + at * kBuffer, *next = lds + (at ^ 1) * kBuffer;
-        at ^= 1;
-        const bool more = k + kStepK < kend;
-        if (more) {
-            if constexpr (EB == 1) sc.load((kend - k - kStepK) / kMxBlock);
-            oa.copy(next, k + kStepK);
-            ob.copy(next + kA, k + kStepK);
-        }
-        if constexpr (EB == 2) {
-            // The fragments of the next 16 k are read while the products of these run.
-            bf16x8 fa[2][WM], fb[2][2];
-            auto read = [&](int kk) {
-#pragma unroll
-                for (int j = 0; j < 2; ++j)
-                    fb[kk & 1][j] = fragment16<LB, BN>(here + kA, wn + 32 * j, kk);
-#pragma unroll
-                for (int i = 0; i < WM; ++i)
-                    fa[kk & 1][i] = fragment16<LA, BM>(here, wm + 32 * i, kk);
-            };
-            read(0);
-#pragma unroll
-            for (int kk = 0; kk < 4; ++kk) {
-                if (kk < 3) read(kk + 1);
-                __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-                for (int i = 0; i < WM; ++i)
-#pragma unroll
-                    for (int j = 0; j < 2; ++j)
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                            fb[kk & 1][j], fa[kk & 1][i], acc[i][j], 0, 0, 0);
-                __builtin_amdgcn_sched_barrier(0);
-            }
-        } else if constexpr (EXACT) {
-            const uint32_t *s = (const uint32_t *)(here + kA + kB);
-            uint32_t sa[WM], sb[2];
-#pragma unroll
-            for (int i = 0; i < WM; ++i) sa[i] = s[wm + 32 * i + (lane & 31)];
-#pragma unroll
-            for (int j = 0; j < 2; ++j) sb[j] = s[BM + wn + 32 * j + (lane & 31)];
-#pragma unroll
-            for (int kk = 0; kk < 8; ++kk) {
-                bf16x8 fa[WM], fb[2];
-#pragma unroll
-                for (int i = 0; i < WM; ++i)
-                    fa[i] = fragment_exact<BM>(here, sa[i], wm + 32 * i, kk);
-#pragma unroll
-                for (int j = 0; j < 2; ++j)
-                    fb[j] = fragment_exact<BN>(here + kA, sb[j], wn + 32 * j, kk);
-#pragma unroll
-                for (int i = 0; i < WM; ++i)
-#pragma unroll
-                    for (int j = 0; j < 2; ++j)
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[j], fa[i],
-                                                                            acc[i][j], 0, 0, 0);
-            }
-            if (more) sc.store((uint32_t *)(next + kA + kB));
-        } else {
-            // A lane's scale is of the 32 k its half of the wave stands for: byte
-            // 2 kk + lane / 32 of its row's dword.
-            const uint32_t *s = (const uint32_t *)(here + kA + kB);
-            int sa[WM], sb[2];
-#pragma unroll
-            for (int i = 0; i < WM; ++i) sa[i] = (int)(s[wm + 32 * i + (lane & 31)] >> ((lane >> 5) * 8));
-#pragma unroll
-            for (int j = 0; j < 2; ++j)
-                sb[j] = (int)(s[BM + wn + 32 * j + (lane & 31)] >> ((lane >> 5) * 8));
-#pragma unroll
-            for (int kk = 0; kk < 2; ++kk) {
-                i32x8 fa[WM], fb[2];
-#pragma unroll
-                for (int i = 0; i < WM; ++i) fa[i] = fragment64<BM>(here, wm + 32 * i, kk);
-#pragma unroll
-                for (int j = 0; j < 2; ++j) fb[j] = fragment64<BN>(here + kA, wn + 32 * j, kk);
-#pragma unroll
-                for (int i = 0; i < WM; ++i)
-#pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        if (kk == 0)
-                            acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
-                                fb[j], fa[i], acc[i][j], 0, 0, 0, sb[j], 0, sa[i]);
-                        else
-                            acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
-                                fb[j], fa[i], acc[i][j], 0, 0, 2, sb[j], 2, sa[i]);
-                    }
-            }
-            if (more) sc.store((uint32_t *)(next + kA + kB));
-        }
+    if constexpr (EB == 1) sc.init(g, m0, n0, kbeg);
+    if (steps > 1) copy(0);
+    else copy_last(0);
+    landed(0);
+    if (steps > 1) {
+        if (steps > 2) copy(1);
+        else copy_last(1);
+        wait_copies<Operand<EB, LA, BM, NW>::kCopies + Operand<EB, LB, BN, NW>::kCopies>();
+    } else {
+        wait_copies<0>();
     }
+    __syncthreads();
+    read_scales(0);
+    read_b(0, 0, 0);
+    read_b(0, 0, 1);
+#pragma unroll
+    for (int i = 0; i < WM; ++i) read_a(0, 0, i);
+    // A step.  Before its last part, which reads the next step's first fragments: the next
+    // step's copies, in flight since the step before, have landed, and this step's buffer,
+    // which all waves have read, takes the copies after those (`more`).  The steps
+    // are straight code: a branch would let the compiler move products behind it.
+    auto step = [&](int t, auto more) {
+        static_for<kParts - 1>([&](auto part) { multiply(part, t); });
+        wait_copies<0>();
+        landed(t + 1);
+        __syncthreads();
+        more(t + 2);
+        multiply(std::integral_constant<int, kParts - 1>{}, t);
+    };
+    int t = 0;
+    for (; t + 3 < steps; ++t) step(t, copy);
+    if (t + 2 < steps) step(t++, copy_last);
+    if (t + 1 < steps) step(t++, [](int) {});
+    // (the reads behind the last products are of what an earlier step left in LDS, unused)
+    static_for<kParts>([&](auto part) { multiply(part, t); });
     __syncthreads();
     float *out = (float *)lds + wave * kEpilogueFloats;
 #pragma unroll
