@@ -14,6 +14,7 @@ enum Layout { K_CONTIGUOUS = 0, K_STRIDED = 1 };
 struct GemmArgs {
     const void *a, *b;
     const uint8_t *as, *bs;     // block scales (8-bit operands)
+    int64_t as_ld, bs_ld;       // bytes between their rows, whole dwords
     int64_t lda, ldb;           // elements between k rows or between output rows
     int64_t a_rows, a_k, b_rows, b_k;   // what the operands' memory holds (packed ones: padded)
     int64_t M, N, K;

@@ -23,14 +23,29 @@ static __device__ __attribute__((aligned(16))) const uint32_t kZero16[4] = {0, 0
 
 constexpr int kStepBytes = 128;
 
+// A pointer that is the same in all lanes, in scalar registers.
+__device__ __forceinline__ const char *uniform(const char *p)
+{
+    const uint64_t v = (uint64_t)p;
+    return (const char *)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)v) |
+                          (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32);
+}
+
 // 16 bytes a lane from memory to LDS (lane order from the wave's address `lds`), counted by
 // vmcnt.  In assembler, because the compiler would have every later LDS read wait for the
 // copies in flight; the kernel waits for them itself, a step later.  No registers but m0 are
 // written, which nothing else in these kernels uses.
 __device__ __forceinline__ void copy16(const char *base, uint32_t off, uint32_t lds)
 {
+    base = uniform(base);
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds),
                  "v"(off), "s"(base)
+                 : "memory");
+}
+__device__ __forceinline__ void copy4(const char *src, uint32_t lds)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds),
+                 "v"(src)
                  : "memory");
 }
 __device__ __forceinline__ void copy16(const char *src, uint32_t lds)
@@ -91,13 +106,12 @@ template <int EB, Layout L, int R, int NW> struct Operand {
                 off[i] = (uint32_t)outer * ld32 + min((uint32_t)chunk * 16, last * EB - 16);
         }
     }
-    // The next step, to the LDS address of this wave's part.
-    __device__ __forceinline__ void copy(uint32_t lds)
+    // The next step, to the LDS address of this wave's part: copy by copy, then on.
+    __device__ __forceinline__ void copy_one(uint32_t lds, int i)
     {
-#pragma unroll
-        for (int i = 0; i < kCopies; ++i) copy16(base, off[i], lds + i * NW * 1024);
-        base += ahead;
+        copy16(base, off[i], lds + i * NW * 1024);
     }
+    __device__ __forceinline__ void copied() { base += ahead; }
     // The last step, at k, with zeros from k_end on.
     __device__ __forceinline__ void copy_last(uint32_t lds, int64_t k)
     {
@@ -179,44 +193,30 @@ __device__ __forceinline__ bf16x8 fragment_exact(const char *lds, uint32_t s, in
     return u.f;
 }
 
-// Block scales of a step, a dword a row: bytes of 32 k each.
+// Block scales of a step, a dword a row (bytes of 32 k each), copied to LDS like the rest:
+// the tile's rows of both operands in order, 64 a wave's copy.  Rows of scales are whole
+// dwords, and those past the operands' ends repeat the last.
 template <int BM, int BN, int NT> struct Scales {
-    static constexpr int kLoads = (BM + BN + NT - 1) / NT;
-    uint32_t v[kLoads];
-    const uint8_t *p[kLoads];
+    static constexpr int kCopies = (BM + BN + NT - 1) / NT;
+    static constexpr int kBytes = kCopies * NT * 4;
+    const char *p[kCopies];
     __device__ __forceinline__ void init(const GemmArgs &g, int64_t m0, int64_t n0, int64_t k0)
     {
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
+        for (int i = 0; i < kCopies; ++i) {
             const int r = i * NT + (int)threadIdx.x;
             const bool b = r >= BM;
             const int64_t row = b ? min(n0 + r - BM, g.N - 1) : min(m0 + r, g.M - 1);
-            p[i] = (b ? g.bs + row * (g.ldb / kMxBlock) : g.as + row * (g.lda / kMxBlock)) +
-                   k0 / kMxBlock;
+            p[i] = (const char *)(b ? g.bs + row * g.bs_ld : g.as + row * g.as_ld) + k0 / kMxBlock;
         }
     }
-    __device__ __forceinline__ void load()
+    __device__ __forceinline__ void copy(uint32_t lds)
     {
+        const uint32_t to = lds + (uint32_t)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * 256;
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            __builtin_memcpy(&v[i], p[i], 4);
+        for (int i = 0; i < kCopies; ++i) {
+            copy4(p[i], to + i * NT * 4);
             p[i] += 4;
-        }
-    }
-    // The last step's `left` (1 to 4) bytes; the others' values are zeros whatever their scale.
-    __device__ __forceinline__ void load_last(int left)
-    {
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i)
-            v[i] = (uint32_t)p[i][0] | (uint32_t)p[i][min(1, left - 1)] << 8 |
-                   (uint32_t)p[i][min(2, left - 1)] << 16 | (uint32_t)p[i][left - 1] << 24;
-    }
-    __device__ __forceinline__ void store(uint32_t *lds) const
-    {
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            const int r = i * NT + (int)threadIdx.x;
-            if ((BM + BN) % NT == 0 || r < BM + BN) lds[r] = v[i];
         }
     }
 };
@@ -251,10 +251,10 @@ __global__ void __launch_bounds__(64 * WAVES_M *WAVES_N)
     gemm_tile_kernel(GemmArgs g, uint32_t tiles_m, uint32_t tiles_n)
 {
     constexpr int NW = WAVES_M * WAVES_N, NT = 64 * NW;
-    constexpr int WM = BM / WAVES_M / 32;
-    static_assert(BN / WAVES_N == 64, "a wave holds 64 columns");
+    constexpr int WM = BM / WAVES_M / 32, WN = BN / WAVES_N / 32;
+    static_assert(WN % 2 == 0, "a wave's epilogue takes 64 columns at a time");
     constexpr int kA = BM * kStepBytes, kB = BN * kStepBytes;
-    constexpr int kScales = EB == 1 ? (BM + BN) * 4 : 0;
+    constexpr int kScales = EB == 1 ? Scales<BM, BN, NT>::kBytes : 0;
     constexpr int kBuffer = kA + kB + kScales;
     constexpr int kEpilogue = NW * kEpilogueFloats * 4;
     __shared__ __attribute__((aligned(1024))) char lds[2 * kBuffer > kEpilogue ? 2 * kBuffer
@@ -266,13 +266,13 @@ __global__ void __launch_bounds__(64 * WAVES_M *WAVES_N)
     place_tile(blockIdx.x, tiles_m, tiles_n, tm, tn);
     const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * BN;
     const int64_t kbeg = (int64_t)blockIdx.y * g.k_per, kend = min(g.K, kbeg + g.k_per);
-    const int wm = (wave % WAVES_M) * (WM * 32), wn = (wave / WAVES_M) * 64;
+    const int wm = (wave % WAVES_M) * (WM * 32), wn = (wave / WAVES_M) * (WN * 32);
 
-    f32x16 acc[WM][2];
+    f32x16 acc[WM][WN];
 #pragma unroll
     for (int i = 0; i < WM; ++i)
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
+        for (int j = 0; j < WN; ++j)
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
 
@@ -282,125 +282,151 @@ __global__ void __launch_bounds__(64 * WAVES_M *WAVES_N)
     ob.init(g.b, g.ldb, g.b_rows, n0, kbeg, LB == K_CONTIGUOUS ? min(kend, g.b_k) : min(kend, g.K));
     Scales<BM, BN, NT> sc;
     const int steps = (int)((kend - kbeg + kStepK - 1) / kStepK);
-    const uint32_t lds_wave = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds +
-                              (uint32_t)__builtin_amdgcn_readfirstlane(wave) * 1024;
-    auto copy = [&](int t) {
+    const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
+    const uint32_t lds_wave = lds_base + (uint32_t)__builtin_amdgcn_readfirstlane(wave) * 1024;
+    // Step t's copies in kCopies pieces (the scales' loads with the first).
+    constexpr int kCopiesA = Operand<EB, LA, BM, NW>::kCopies;
+    constexpr int kCopies = kCopiesA + Operand<EB, LB, BN, NW>::kCopies;
+    auto copy_piece = [&](int t, int i) __attribute__((always_inline)) {
         const uint32_t to = lds_wave + (t & 1) * kBuffer;
-        if constexpr (EB == 1) sc.load();
-        oa.copy(to);
-        ob.copy(to + kA);
+        if (EB == 1 && i == 0) sc.copy(lds_base + (t & 1) * kBuffer + kA + kB);
+        if (i < kCopiesA) oa.copy_one(to, i);
+        else ob.copy_one(to + kA, i - kCopiesA);
+        if (i == kCopies - 1) oa.copied(), ob.copied();
     };
-    auto copy_last = [&](int t) {
+    auto copy = [&](int t) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < kCopies; ++i) copy_piece(t, i);
+    };
+    auto copy_last = [&](int t) __attribute__((always_inline)) {
         const uint32_t to = lds_wave + (t & 1) * kBuffer;
         const int64_t k = kbeg + (int64_t)t * kStepK;
-        if constexpr (EB == 1) sc.load_last((int)min((kend - k) / kMxBlock, (int64_t)4));
+        if constexpr (EB == 1) sc.copy(lds_base + (t & 1) * kBuffer + kA + kB);
         oa.copy_last(to, k);
         ob.copy_last(to + kA, k);
     };
-    // A step's scales pass registers: they go to LDS once the copies have landed.
-    auto landed = [&](int t) {
-        if constexpr (EB == 1) sc.store((uint32_t *)(lds + (t & 1) * kBuffer + kA + kB));
-    };
     constexpr int kParts = EB == 2 ? 4 : EXACT ? 8 : 2;
     using Fragment = std::conditional_t<EB == 1 && !EXACT, i32x8, bf16x8>;
-    Fragment fa[WM], fb[2];
-    uint32_t sa[WM], sb[2], ua[WM], ub[2];      // scales of the fragments read, and in use
-    auto read_scales = [&](int t) {
+    // Two sets of fragments where the registers hold them: a part's products run on one while
+    // the other is read.
+    constexpr int kSets = WN == 4 || EB == 2 ? 2 : 1;
+    Fragment fa[kSets][WM], fb[kSets][WN];
+    uint32_t sa[WM], sb[WN], ua[WM], ub[WN];    // scales of the fragments read, and in use
+    auto read_scales = [&](int t) __attribute__((always_inline)) {
         if constexpr (EB == 1) {
             // EXACT: the row's four scales.  Else a lane's scale is of the 32 k its half of
             // the wave stands for: byte 2 kk + lane / 32.
             const uint32_t *s = (const uint32_t *)(lds + (t & 1) * kBuffer + kA + kB);
             const int shift = EXACT ? 0 : (lane >> 5) * 8;
 #pragma unroll
-            for (int j = 0; j < 2; ++j) sb[j] = s[BM + wn + 32 * j + (lane & 31)] >> shift;
+            for (int j = 0; j < WN; ++j) sb[j] = s[BM + wn + 32 * j + (lane & 31)] >> shift;
 #pragma unroll
             for (int i = 0; i < WM; ++i) sa[i] = s[wm + 32 * i + (lane & 31)] >> shift;
         }
     };
     // Fragments of part kk of step t.
-    auto read_b = [&](int t, int kk, int j) {
+    auto read_b = [&](int t, int kk, int j) __attribute__((always_inline)) {
         const char *here = lds + (t & 1) * kBuffer + kA;
-        if constexpr (EB == 2) fb[j] = fragment16<LB, BN>(here, wn + 32 * j, kk);
-        else if constexpr (EXACT) fb[j] = fragment_exact<BN>(here, sb[j], wn + 32 * j, kk);
-        else fb[j] = fragment64<BN>(here, wn + 32 * j, kk);
+        Fragment &f = fb[kk % kSets][j];
+        if constexpr (EB == 2) f = fragment16<LB, BN>(here, wn + 32 * j, kk);
+        else if constexpr (EXACT) f = fragment_exact<BN>(here, sb[j], wn + 32 * j, kk);
+        else f = fragment64<BN>(here, wn + 32 * j, kk);
     };
-    auto read_a = [&](int t, int kk, int i) {
+    auto read_a = [&](int t, int kk, int i) __attribute__((always_inline)) {
         const char *here = lds + (t & 1) * kBuffer;
-        if constexpr (EB == 2) fa[i] = fragment16<LA, BM>(here, wm + 32 * i, kk);
-        else if constexpr (EXACT) fa[i] = fragment_exact<BM>(here, sa[i], wm + 32 * i, kk);
-        else fa[i] = fragment64<BM>(here, wm + 32 * i, kk);
+        Fragment &f = fa[kk % kSets][i];
+        if constexpr (EB == 2) f = fragment16<LA, BM>(here, wm + 32 * i, kk);
+        else if constexpr (EXACT) f = fragment_exact<BM>(here, sa[i], wm + 32 * i, kk);
+        else f = fragment64<BM>(here, wm + 32 * i, kk);
     };
-    // The products of part kk of step t.  Behind the last product that needs a fragment,
-    // the next part's is read into its registers, which the products between cover.
-    auto multiply = [&](auto part, int t) {
+    // The products of part kk of step t, columns by columns.  Between them the next part's
+    // fragments are read: into the other set, evenly, in the order of their use, or with one
+    // set behind the last product that needs the fragment before.  piece(i), i <
+    // kCopies, goes out between them too.
+    auto multiply = [&](auto part, int t, auto piece) __attribute__((always_inline)) {
         constexpr int kk = decltype(part)::value, next = (kk + 1) % kParts;
+        constexpr int kProducts = WM * WN, kReads = WM + WN;
         const int tn = kk + 1 == kParts ? t + 1 : t;
         if constexpr (EB == 1 && kk == 0) {
 #pragma unroll
             for (int i = 0; i < WM; ++i) ua[i] = sa[i];
-            ub[0] = sb[0], ub[1] = sb[1];
+#pragma unroll
+            for (int j = 0; j < WN; ++j) ub[j] = sb[j];
         }
         if constexpr (next == 0) read_scales(tn);
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
+        for (int j = 0; j < WN; ++j) {
 #pragma unroll
             for (int i = 0; i < WM; ++i) {
+                const int m = j * WM + i;
+                const Fragment &a = fa[kk % kSets][i], &b = fb[kk % kSets][j];
                 if constexpr (EB == 1 && !EXACT)
                     acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
-                        fb[j], fa[i], acc[i][j], 0, 0, 2 * kk, (int)ub[j], 2 * kk, (int)ua[i]);
+                        b, a, acc[i][j], 0, 0, 2 * kk, (int)ub[j], 2 * kk, (int)ua[i]);
                 else
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[j], fa[i], acc[i][j],
-                                                                        0, 0, 0);
-                if (j == 1) {
-                    __builtin_amdgcn_sched_barrier(0);
-                    read_a(tn, next, i);
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b, a, acc[i][j], 0, 0, 0);
+                __builtin_amdgcn_sched_barrier(0);
+                if constexpr (kSets == 2) {
+#pragma unroll
+                    for (int r = m * kReads / kProducts; r < (m + 1) * kReads / kProducts; ++r) {
+                        if (r == 0) read_b(tn, next, 0);
+                        else if (r <= WM) read_a(tn, next, r - 1);
+                        else read_b(tn, next, r - WM);
+                    }
+                } else {
+                    if (j == WN - 1) read_a(tn, next, i);
+                    if (i == WM - 1) read_b(tn, next, j);
                 }
+#pragma unroll
+                for (int c = m * kCopies / kProducts; c < (m + 1) * kCopies / kProducts; ++c)
+                    piece(c);
+                __builtin_amdgcn_sched_barrier(0);
             }
-            __builtin_amdgcn_sched_barrier(0);
-            read_b(tn, next, j);
         }
     };
+    auto nothing = [](int) __attribute__((always_inline)) {};
 
     if constexpr (EB == 1) sc.init(g, m0, n0, kbeg);
     if (steps > 1) copy(0);
     else copy_last(0);
-    landed(0);
     if (steps > 1) {
         if (steps > 2) copy(1);
         else copy_last(1);
-        wait_copies<Operand<EB, LA, BM, NW>::kCopies + Operand<EB, LB, BN, NW>::kCopies>();
+        wait_copies<kCopies + (EB == 1 ? Scales<BM, BN, NT>::kCopies : 0)>();
     } else {
         wait_copies<0>();
     }
     __syncthreads();
     read_scales(0);
-    read_b(0, 0, 0);
-    read_b(0, 0, 1);
+#pragma unroll
+    for (int j = 0; j < WN; ++j) read_b(0, 0, j);
 #pragma unroll
     for (int i = 0; i < WM; ++i) read_a(0, 0, i);
     // A step.  Before its last part, which reads the next step's first fragments: the next
     // step's copies, in flight since the step before, have landed, and this step's buffer,
     // which all waves have read, takes the copies after those (`more`).  The steps
     // are straight code: a branch would let the compiler move products behind it.
-    auto step = [&](int t, auto more) {
-        static_for<kParts - 1>([&](auto part) { multiply(part, t); });
+    auto step = [&](int t, auto before, auto piece) __attribute__((always_inline)) {
+        static_for<kParts - 1>([&](auto part) __attribute__((always_inline)) { multiply(part, t, nothing); });
         wait_copies<0>();
-        landed(t + 1);
         __syncthreads();
-        more(t + 2);
-        multiply(std::integral_constant<int, kParts - 1>{}, t);
+        before(t + 2);
+        multiply(std::integral_constant<int, kParts - 1>{}, t, piece);
     };
     int t = 0;
-    for (; t + 3 < steps; ++t) step(t, copy);
-    if (t + 2 < steps) step(t++, copy_last);
-    if (t + 1 < steps) step(t++, [](int) {});
+    for (; t + 3 < steps; ++t)
+        step(t, nothing, [&](int i) __attribute__((always_inline)) { copy_piece(t + 2, i); });
+    if (t + 2 < steps) step(t++, copy_last, nothing);
+    if (t + 1 < steps) step(t++, nothing, nothing);
     // (the reads behind the last products are of what an earlier step left in LDS, unused)
-    static_for<kParts>([&](auto part) { multiply(part, t); });
+    static_for<kParts>([&](auto part) __attribute__((always_inline)) { multiply(part, t, nothing); });
     __syncthreads();
     float *out = (float *)lds + wave * kEpilogueFloats;
-#pragma unroll
-    for (int i = 0; i < WM; ++i)
-        store_tile32x64<T>(g, out, m0 + wm + 32 * i, n0 + wn, blockIdx.y, acc[i][0], acc[i][1]);
+    static_for<WM * WN / 2>([&](auto at) __attribute__((always_inline)) {
+        constexpr int i = decltype(at)::value / (WN / 2), j = decltype(at)::value % (WN / 2) * 2;
+        store_tile32x64<T>(g, out, m0 + wm + 32 * i, n0 + wn + 32 * j, blockIdx.y, acc[i][j],
+                           acc[i][j + 1]);
+    });
 }
 
 // ---- shapes of tiles and splits of k ----
@@ -414,7 +440,7 @@ struct TilePlan {
 inline TilePlan plan_tiles(int64_t M, int64_t N, int64_t K, int step_k)
 {
     TilePlan p{};
-    auto tiles = [&](int bm, int bn) { return ((M + bm - 1) / bm) * ((N + bn - 1) / bn); };
+    auto tiles = [&](int bm, int bn) __attribute__((always_inline)) { return ((M + bm - 1) / bm) * ((N + bn - 1) / bn); };
     if (M <= 32) p.bm = 32, p.bn = 256;
     else if (M <= 64) p.bm = 64, p.bn = 256;
     else if (tiles(256, 256) >= 192) p.bm = 256, p.bn = 256;

@@ -12,7 +12,53 @@ namespace whtmix {
 
 constexpr int64_t kExactK = 512;
 
-uint64_t gemm_mx_bytes(const GemmArgs &g) { return tile_part_bytes(g.M, g.N, g.K, kStepBytes); }
+// Rows of scales to whole dwords, 1 past the end: the tile kernel copies dwords.
+__global__ void __launch_bounds__(256) pack_scales_kernel(const uint8_t *src, uint32_t *dst,
+                                                          int64_t rows, int width)
+{
+    const int dwords = (width + 3) / 4;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * dwords;
+         i += (int64_t)gridDim.x * 256) {
+        const int64_t row = i / dwords;
+        const int at = (int)(i - row * dwords) * 4;
+        uint32_t v = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            v |= (at + j < width ? (uint32_t)src[row * width + at + j] : 127u) << (8 * j);
+        dst[i] = v;
+    }
+}
+
+static bool whole_dwords(const uint8_t *p, int64_t width)
+{
+    return width % 4 == 0 && reinterpret_cast<uintptr_t>(p) % 4 == 0;
+}
+
+static uint64_t packed_bytes(const uint8_t *p, int64_t rows, int64_t width)
+{
+    return whole_dwords(p, width) ? 0 : (uint64_t)(rows * ((width + 3) / 4 * 4) + 255) / 256 * 256;
+}
+
+static hipError_t place_scales(const uint8_t *&p, int64_t &ld, int64_t rows, int64_t width,
+                               char *&ws, hipStream_t s)
+{
+    ld = width;
+    const uint64_t bytes = packed_bytes(p, rows, width);
+    if (!bytes) return hipSuccess;
+    const int64_t n = rows * ((width + 3) / 4), blocks = (n + 255) / 256;
+    pack_scales_kernel<<<dim3((uint32_t)(blocks < 65536 ? blocks : 65536)), dim3(256), 0, s>>>(
+        p, (uint32_t *)ws, rows, (int)width);
+    p = (const uint8_t *)ws;
+    ws += bytes;
+    ld = (width + 3) / 4 * 4;
+    return hipGetLastError();
+}
+
+uint64_t gemm_mx_bytes(const GemmArgs &g)
+{
+    return packed_bytes(g.as, g.M, g.K / kMxBlock) + packed_bytes(g.bs, g.N, g.K / kMxBlock) +
+           tile_part_bytes(g.M, g.N, g.K, kStepBytes);
+}
 
 template <bool EXACT, typename T> static hipError_t run(const GemmArgs &g, void *ws, hipStream_t s)
 {
@@ -22,6 +68,11 @@ template <bool EXACT, typename T> static hipError_t run(const GemmArgs &g, void 
 hipError_t gemm_mx(GemmArgs g, int dtype, void *ws, hipStream_t stream)
 {
     g.a_rows = g.M, g.b_rows = g.N, g.a_k = g.b_k = g.K;
+    char *w = (char *)ws;
+    hipError_t e = place_scales(g.as, g.as_ld, g.M, g.K / kMxBlock, w, stream);
+    if (e == hipSuccess) e = place_scales(g.bs, g.bs_ld, g.N, g.K / kMxBlock, w, stream);
+    if (e != hipSuccess) return e;
+    ws = w;
     const bool exact = g.K <= kExactK || (g.y && dtype == DTYPE_F32);
     if (dtype == DTYPE_BF16)
         return exact ? run<true, __bf16>(g, ws, stream) : run<false, __bf16>(g, ws, stream);
