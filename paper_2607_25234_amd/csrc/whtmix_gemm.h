@@ -50,6 +50,28 @@ __device__ __forceinline__ void store8(T *p, int n, const float (&v)[8])
     }
 }
 
+// Eight values of row m from column n on, the first cnt of them real, in block-scaled 8 bits;
+// four neighbouring lanes hold a block of 32 columns and call this together.
+__device__ __forceinline__ void store_mx8(float (&v)[8], int cnt, bool live, int64_t m, int64_t n,
+                                          int64_t width, uint8_t *q, uint8_t *scales)
+{
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        if (i >= cnt) v[i] = 0.f;
+        top = max(top, mx_magnitude(v[i]));
+    }
+    top = max(top, (uint32_t)__shfl_xor((int)top, 1));
+    top = max(top, (uint32_t)__shfl_xor((int)top, 2));
+    const uint32_t byte = mx_scale_byte(top);
+    const float inv = mx_inverse(byte);
+    if (live && n < width) {
+        *(u32x2 *)(q + m * width + n) =
+            (u32x2){mx_pack(v[0], v[1], v[2], v[3], inv), mx_pack(v[4], v[5], v[6], v[7], inv)};
+        if (n % kMxBlock == 0) scales[m * (width / kMxBlock) + n / kMxBlock] = (uint8_t)byte;
+    }
+}
+
 // Eight sums of row m from column n on, to the outputs.  With 8-bit output
 // four neighbouring lanes hold a block of 32 columns and call this together.
 template <typename T>
@@ -78,30 +100,7 @@ __device__ __forceinline__ void finish8(const GemmArgs &g, int64_t m, int64_t n,
         if (cnt > 0) store8((T *)g.y + at, cnt, v);
         return;
     }
-    const int64_t width = (g.N + kMxBlock - 1) / kMxBlock * kMxBlock;
-    uint32_t top = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        if (i >= cnt) v[i] = 0.f;
-        top = max(top, mx_magnitude(v[i]));
-    }
-    top = max(top, (uint32_t)__shfl_xor((int)top, 1));
-    top = max(top, (uint32_t)__shfl_xor((int)top, 2));
-    const uint32_t byte = mx_scale_byte(top);
-    const float inv = mx_inverse(byte);
-    if (m < g.M && n < width) {
-        *(u32x2 *)(g.yq + m * width + n) =
-            (u32x2){mx_pack(v[0], v[1], v[2], v[3], inv), mx_pack(v[4], v[5], v[6], v[7], inv)};
-        if (n % kMxBlock == 0) g.ys[m * (width / kMxBlock) + n / kMxBlock] = (uint8_t)byte;
-    }
-}
-
-// Eight sums of a split to its partial sums.
-__device__ __forceinline__ void finish8_part(const GemmArgs &g, int64_t split, int64_t m,
-                                             int64_t n, const float (&v)[8])
-{
-    const int cnt = m < g.M ? (int)min((int64_t)8, g.N - n) : 0;
-    if (cnt > 0) store8(g.part + (split * g.M + m) * g.N + n, cnt, v);
+    store_mx8(v, cnt, m < g.M, m, n, (g.N + kMxBlock - 1) / kMxBlock * kMxBlock, g.yq, g.ys);
 }
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
@@ -114,42 +113,97 @@ __device__ __forceinline__ void wave_lds_fence()
     __builtin_amdgcn_wave_barrier();
 }
 
-// 32 rows x 64 columns of a wave's sums, from the matrix instructions' layout
-// (lane: row l % 32, columns 8 (r / 4) + 4 (l / 32) + r % 4 of each 32) through
-// the wave's LDS (kEpilogueFloats) to rows of 64, eight lanes a row, so that
-// stores and the residual's loads are 16 bytes a lane and whole cache lines a row.
+template <int N, typename F, int I = 0> __device__ __forceinline__ void static_for(F f)
+{
+    if constexpr (I < N) {
+        f(std::integral_constant<int, I>{});
+        static_for<N, F, I + 1>(f);
+    }
+}
+
+// A wave's 32 WM x 64 sums to the outputs, 32 rows at a time: from the matrix instructions'
+// layout (lane: row l % 32, columns 8 (r / 4) + 4 (l / 32) + r % 4 of each 32)
+// through the wave's LDS (kEpilogueFloats) to rows of 64, eight lanes a row, so that
+// stores and the residual's loads are 16 bytes a lane and whole cache lines a row.  A lane's
+// columns stay the same: their bias is read once.
 constexpr int kEpilogueStride = 68;      // floats: rows 4 banks apart
 constexpr int kEpilogueFloats = 32 * kEpilogueStride;
 
-template <typename T>
-__device__ __forceinline__ void store_tile32x64(const GemmArgs &g, float *lds, int64_t m0,
-                                                int64_t n0, int64_t split, const f32x16 &left,
-                                                const f32x16 &right)
+template <typename T, int WM>
+__device__ __forceinline__ void finish_wave(const GemmArgs &g, float *lds, int64_t m0, int64_t n0,
+                                            int64_t split, const f32x16 (&acc)[WM][2])
 {
     const int lane = threadIdx.x & 63;
     float *w = lds + (lane & 31) * kEpilogueStride + (lane >> 5) * 4;
-    wave_lds_fence();
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        *(f32x4 *)(w + 8 * i) = (f32x4){left[4 * i], left[4 * i + 1], left[4 * i + 2],
-                                        left[4 * i + 3]};
-        *(f32x4 *)(w + 32 + 8 * i) = (f32x4){right[4 * i], right[4 * i + 1], right[4 * i + 2],
-                                             right[4 * i + 3]};
-    }
-    wave_lds_fence();
+    const float *p = lds + (lane >> 3) * kEpilogueStride + (lane & 7) * 8;
     const int64_t n = n0 + (lane & 7) * 8;
-    const bool in = n < (g.yq ? (g.N + kMxBlock - 1) / kMxBlock * kMxBlock : g.N);
+    const int cnt = (int)max((int64_t)0, min((int64_t)8, g.N - n));
+    const int rows = (int)min((int64_t)(32 * WM), g.M - m0) - (lane >> 3);   // left for this lane
+    // Rows 32 i .. 32 i + 31, of which the lane takes every eighth: f(row of the tile, sums).
+    auto each = [&](auto f) __attribute__((always_inline)) {
+        static_for<WM>([&](auto part) __attribute__((always_inline)) {
+            constexpr int I = decltype(part)::value;
+            wave_lds_fence();
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int row = i * 8 + (lane >> 3);
-        const float *p = lds + row * kEpilogueStride + (lane & 7) * 8;
-        float v[8];
-        *(f32x4 *)v = *(const f32x4 *)p;
-        *(f32x4 *)(v + 4) = *(const f32x4 *)(p + 4);
-        if (!in) continue;      // whole blocks of 32 columns with 8-bit output
-        if (g.part) finish8_part(g, split, m0 + row, n, v);
-        else finish8<T>(g, m0 + row, n, v);
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+                    *(f32x4 *)(w + 32 * j + 8 * r) =
+                        (f32x4){acc[I][j][4 * r], acc[I][j][4 * r + 1], acc[I][j][4 * r + 2],
+                                acc[I][j][4 * r + 3]};
+            wave_lds_fence();
+            float v[4][8];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                *(f32x4 *)v[r] = *(const f32x4 *)(p + 8 * r * kEpilogueStride);
+                *(f32x4 *)(v[r] + 4) = *(const f32x4 *)(p + 8 * r * kEpilogueStride + 4);
+            }
+            f(32 * I, v);
+        });
+    };
+    if (g.part) {
+        float *to = g.part + (split * g.M + m0 + (lane >> 3)) * g.N + n;
+        each([&](int i, float (&v)[4][8]) __attribute__((always_inline)) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                if (i + 8 * r < rows) store8(to + (int64_t)(i + 8 * r) * g.N, cnt, v[r]);
+        });
+        return;
     }
+    float b[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if (g.bias) load8(g.bias + n, cnt, b);
+    const int64_t at = (m0 + (lane >> 3)) * g.N + n;
+    const T *res = (const T *)g.residual + at;
+    T *y = (T *)g.y + at, *z = (T *)g.z + at;
+    const int64_t width = (g.N + kMxBlock - 1) / kMxBlock * kMxBlock;
+    with_act(g.act, [&](auto act) __attribute__((always_inline)) {
+        constexpr int ACT = decltype(act)::value;
+        each([&](int i, float (&v)[4][8]) __attribute__((always_inline)) {
+            float e[4][8];
+            if (g.residual) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    load8(res + (int64_t)(i + 8 * r) * g.N, i + 8 * r < rows ? cnt : 0, e[r]);
+            }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) v[r][k] += b[k];
+                if (g.z && i + 8 * r < rows) store8(z + (int64_t)(i + 8 * r) * g.N, cnt, v[r]);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    v[r][k] = act_of<ACT>(v[r][k]);
+                    if (g.residual) v[r][k] += e[r][k];
+                }
+                if (g.y) {
+                    if (i + 8 * r < rows) store8(y + (int64_t)(i + 8 * r) * g.N, cnt, v[r]);
+                } else if (n < width) {     // the four lanes of a block of 32 columns together
+                    store_mx8(v[r], cnt, i + 8 * r < rows, m0 + (lane >> 3) + i + 8 * r, n, width,
+                              g.yq, g.ys);
+                }
+            }
+        });
+    });
 }
 
 // Sums a split's partial sums in order and finishes them.

@@ -221,27 +221,21 @@ template <int BM, int BN, int NT> struct Scales {
     }
 };
 
-// Workgroup -> tile.  Consecutive workgroups go round the 8 XCDs, each with its own L2:
-// the tiles of an XCD are neighbours, in groups of 4 rows of tiles, so that the
-// tiles it holds at a time share operands.
-__device__ __forceinline__ void place_tile(uint32_t id, uint32_t tiles_m, uint32_t tiles_n,
-                                           uint32_t &tm, uint32_t &tn)
+// Workgroup -> tile and part of k.  Consecutive workgroups go round the 8 XCDs, each with its
+// own L2: an XCD's are neighbours in the order below (a part's tiles together, in groups
+// of 4 rows of tiles), so that those it holds at a time share operands.
+__device__ __forceinline__ void place_tile(uint32_t id, uint32_t total, uint32_t tiles_m,
+                                           uint32_t tiles_n, uint32_t &tm, uint32_t &tn,
+                                           uint32_t &split)
 {
-    const uint32_t total = tiles_m * tiles_n, per = total / 8, rest = total % 8;
-    const uint32_t x = id % 8, i = id / 8;
-    const uint32_t s = x * per + min(x, rest) + i;
-    const uint32_t group = s / (4 * tiles_n), first = group * 4;
-    const uint32_t rows = min(4u, tiles_m - first), in = s - group * 4 * tiles_n;
+    const uint32_t x = id % 8, tiles = tiles_m * tiles_n;
+    const uint32_t s = x * (total / 8) + min(x, total % 8) + id / 8;
+    split = s / tiles;
+    const uint32_t t = s - split * tiles;
+    const uint32_t group = t / (4 * tiles_n), first = group * 4;
+    const uint32_t rows = min(4u, tiles_m - first), in = t - group * 4 * tiles_n;
     tm = first + in % rows;
     tn = in / rows;
-}
-
-template <int N, typename F, int I = 0> __device__ __forceinline__ void static_for(F f)
-{
-    if constexpr (I < N) {
-        f(std::integral_constant<int, I>{});
-        static_for<N, F, I + 1>(f);
-    }
 }
 
 // EXACT: block-scaled values multiplied as bf16 (see gemm_mx).
@@ -252,7 +246,7 @@ __global__ void __launch_bounds__(64 * WAVES_M *WAVES_N)
 {
     constexpr int NW = WAVES_M * WAVES_N, NT = 64 * NW;
     constexpr int WM = BM / WAVES_M / 32, WN = BN / WAVES_N / 32;
-    static_assert(WN % 2 == 0, "a wave's epilogue takes 64 columns at a time");
+    static_assert(WN == 2, "a wave's epilogue takes 64 columns");
     constexpr int kA = BM * kStepBytes, kB = BN * kStepBytes;
     constexpr int kScales = EB == 1 ? Scales<BM, BN, NT>::kBytes : 0;
     constexpr int kBuffer = kA + kB + kScales;
@@ -262,10 +256,10 @@ __global__ void __launch_bounds__(64 * WAVES_M *WAVES_N)
     constexpr int kStepK = kStepBytes / EB;
 
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    uint32_t tm, tn;
-    place_tile(blockIdx.x, tiles_m, tiles_n, tm, tn);
+    uint32_t tm, tn, split;
+    place_tile(blockIdx.x, gridDim.x, tiles_m, tiles_n, tm, tn, split);
     const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * BN;
-    const int64_t kbeg = (int64_t)blockIdx.y * g.k_per, kend = min(g.K, kbeg + g.k_per);
+    const int64_t kbeg = (int64_t)split * g.k_per, kend = min(g.K, kbeg + g.k_per);
     const int wm = (wave % WAVES_M) * (WM * 32), wn = (wave / WAVES_M) * (WN * 32);
 
     f32x16 acc[WM][WN];
@@ -422,11 +416,7 @@ __global__ void __launch_bounds__(64 * WAVES_M *WAVES_N)
     static_for<kParts>([&](auto part) __attribute__((always_inline)) { multiply(part, t, nothing); });
     __syncthreads();
     float *out = (float *)lds + wave * kEpilogueFloats;
-    static_for<WM * WN / 2>([&](auto at) __attribute__((always_inline)) {
-        constexpr int i = decltype(at)::value / (WN / 2), j = decltype(at)::value % (WN / 2) * 2;
-        store_tile32x64<T>(g, out, m0 + wm + 32 * i, n0 + wn + 32 * j, blockIdx.y, acc[i][j],
-                           acc[i][j + 1]);
-    });
+    finish_wave<T>(g, out, m0 + wm, n0 + wn, split, acc);
 }
 
 // ---- shapes of tiles and splits of k ----
@@ -443,7 +433,11 @@ inline TilePlan plan_tiles(int64_t M, int64_t N, int64_t K, int step_k)
     auto tiles = [&](int bm, int bn) __attribute__((always_inline)) { return ((M + bm - 1) / bm) * ((N + bn - 1) / bn); };
     if (M <= 32) p.bm = 32, p.bn = 256;
     else if (M <= 64) p.bm = 64, p.bn = 256;
-    else if (tiles(256, 256) >= 192) p.bm = 256, p.bn = 256;
+    // 256 x 256 where most of the device has a tile and padding costs less than a quarter
+    // (262144 x 128 x 512 and its dx of 128 columns: 115 and 114 us in these tiles,
+    // 139 and 77 us in tiles of 128 x 128; 8192 x 2048 x 8192: 229 and 280 us).
+    else if (tiles(256, 256) >= 192 && 16 * tiles(256, 256) <= 5 * tiles(128, 128))
+        p.bm = 256, p.bn = 256;
     else p.bm = 128, p.bn = 128;
     p.tiles_m = (uint32_t)((M + p.bm - 1) / p.bm);
     p.tiles_n = (uint32_t)((N + p.bn - 1) / p.bn);
@@ -469,7 +463,7 @@ hipError_t run_tiles(GemmArgs g, float *part, hipStream_t stream)
     const TilePlan p = plan_tiles(g.M, g.N, g.K, kStepBytes / EB);
     g.k_per = p.k_per;
     g.part = p.splits > 1 ? part : nullptr;
-    const dim3 grid(p.tiles_m * p.tiles_n, (uint32_t)p.splits);
+    const dim3 grid(p.tiles_m * p.tiles_n * (uint32_t)p.splits);
     if (p.bm == 32)
         gemm_tile_kernel<EB, EXACT, T, LA, LB, 32, 256, 1, 4><<<grid, 256, 0, stream>>>(g, p.tiles_m, p.tiles_n);
     else if (p.bm == 64)

@@ -26,61 +26,71 @@ static_assert(kTile * kRowBytes == kPlane && kStep * kKBytes == kPlane, "planes"
 
 constexpr int P = 3;               // bf16 terms of a float32
 
-// Sixteen elements of an operand in a thread's registers: of one row (16 k) or
-// one k (16 rows).
+// Sixteen elements of an operand in a thread's registers, four times four along memory: a
+// row's chunks are neighbouring lanes'.
 template <Layout L> struct Stage {
-    float v[16];
+    float v[4][4];
+    // Chunk i of the thread: (row, k) of its first element.
+    static __device__ __forceinline__ void place(int i, int &row, int &k)
+    {
+        const int c = i * 256 + threadIdx.x;
+        if (L == K_CONTIGUOUS) row = c >> 3, k = (c & 7) * 4;
+        else k = c >> 5, row = (c & 31) * 4;
+    }
     __device__ __forceinline__ void load(const void *p, int64_t ld, int64_t R, int64_t K,
                                          int64_t r0, int64_t k0)
     {
-        const int t = threadIdx.x;
-        int64_t outer, inner, n_outer, n_inner;
-        if (L == K_CONTIGUOUS) {
-            outer = r0 + (t >> 1), inner = k0 + (t & 1) * 16, n_outer = R, n_inner = K;
-        } else {
-            outer = k0 + (t >> 3), inner = r0 + (t & 7) * 16, n_outer = K, n_inner = R;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            int row, k;
+            place(i, row, k);
+            const int64_t outer = L == K_CONTIGUOUS ? r0 + row : k0 + k,
+                          inner = L == K_CONTIGUOUS ? k0 + k : r0 + row;
+            const int64_t left = outer < (L == K_CONTIGUOUS ? R : K)
+                                     ? (L == K_CONTIGUOUS ? K : R) - inner : 0;
+            const int n = (int)min((int64_t)4, max((int64_t)0, left));
+            Chunk<float>::load((const float *)p + (n ? outer * ld + inner : 0), n, v[i]);
         }
-        const int64_t left = outer < n_outer ? n_inner - inner : 0;
-        const int n = (int)min((int64_t)16, max((int64_t)0, left));
-        const float *q = (const float *)p + (n ? outer * ld + inner : 0);
-        load8(q, n, *(float(*)[8])v);
-        load8(q + 8, n - 8, *(float(*)[8])(v + 8));
     }
     // As float32, [k][row], for operands that do not split.
     __device__ __forceinline__ void store_f32(float *lds) const
     {
-        const int t = threadIdx.x;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            if (L == K_CONTIGUOUS) lds[((t & 1) * 16 + i) * kF32Row + (t >> 1)] = v[i];
-            else lds[(t >> 3) * kF32Row + (t & 7) * 16 + i] = v[i];
+        for (int i = 0; i < 4; ++i) {
+            int row, k;
+            place(i, row, k);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                lds[(k + (L == K_CONTIGUOUS ? j : 0)) * kF32Row + row +
+                    (L == K_CONTIGUOUS ? 0 : j)] = v[i][j];
         }
     }
-    // The largest magnitude staged so far, as ordered bits (NaN above Inf).
-    __device__ __forceinline__ uint32_t largest(uint32_t top) const
+    // The largest magnitudes staged so far by chunk, as ordered bits (NaN above Inf).
+    __device__ __forceinline__ void largest(uint32_t (&top)[4]) const
     {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) top = max(top, f32_bits(v[i]) & 0x7fffffffu);
-        return top;
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) top[i] = max(top[i], f32_bits(v[i][j]) & 0x7fffffffu);
     }
     __device__ __forceinline__ void store(char *lds)
     {
-        const int t = threadIdx.x;
-        char *p = lds + (L == K_CONTIGUOUS ? (t >> 1) * kRowBytes + (t & 1) * 32
-                                           : (t >> 3) * kKBytes + (t & 7) * 32);
 #pragma unroll
-        for (int s = 0; s < P; ++s) {
-            uint32_t w[8];
+        for (int i = 0; i < 4; ++i) {
+            int row, k;
+            place(i, row, k);
+            char *p = lds + (L == K_CONTIGUOUS ? row * kRowBytes + k * 2 : k * kKBytes + row * 2);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                w[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
+            for (int s = 0; s < P; ++s) {
+                const uint32_t w0 = pack_bf16(v[i][0], v[i][1]), w1 = pack_bf16(v[i][2], v[i][3]);
+                *(u32x2 *)(p + s * kPlane) = (u32x2){w0, w1};
                 if (s + 1 < P) {
-                    v[2 * i] -= bits_f32(w[i] << 16);
-                    v[2 * i + 1] -= bits_f32(w[i] & 0xffff0000u);
+                    v[i][0] -= bits_f32(w0 << 16);
+                    v[i][1] -= bits_f32(w0 & 0xffff0000u);
+                    v[i][2] -= bits_f32(w1 << 16);
+                    v[i][3] -= bits_f32(w1 & 0xffff0000u);
                 }
             }
-            *(u32x4 *)(p + s * kPlane) = (u32x4){w[0], w[1], w[2], w[3]};
-            *(u32x4 *)(p + s * kPlane + 16) = (u32x4){w[4], w[5], w[6], w[7]};
         }
     }
 };
@@ -166,13 +176,13 @@ __global__ void __launch_bounds__(256) gemm_kernel(GemmArgs g)
 
     Stage<LA> sa;
     Stage<LB> sb;
-    uint32_t top_a = 0, top_b = 0;     // what the splits have to hold
+    uint32_t top_a[4] = {0, 0, 0, 0}, top_b[4] = {0, 0, 0, 0};   // what the splits have to hold
     sa.load(g.a, g.lda, g.M, kend, m0, kbeg);
     sb.load(g.b, g.ldb, g.N, kend, n0, kbeg);
     for (int64_t k = kbeg; k < kend; k += kStep) {
         __syncthreads();
-        top_a = sa.largest(top_a);
-        top_b = sb.largest(top_b);
+        sa.largest(top_a);
+        sb.largest(top_b);
         sa.store(la);
         sb.store(lb);
         if (k + kStep < kend) {
@@ -205,15 +215,16 @@ __global__ void __launch_bounds__(256) gemm_kernel(GemmArgs g)
         }
     }
     auto bad = [](uint32_t top) { return top >= kSplitMax || (top != 0 && top < kSplitMin); };
-    // A thread's share is its row's (or its rows') k; one that does not split sends the
+    // A chunk's elements along k are of one row (or four); one that does not split sends the
     // whole tile through float32 products.
-    if (__syncthreads_or(bad(top_a) || bad(top_b)))
+    bool any = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) any = any || bad(top_a[i]) || bad(top_b[i]);
+    if (__syncthreads_or(any))
         float32_tile(g, sa, sb, (float *)lds, m0, n0, kbeg, kend, wm, wn, acc);
     __syncthreads();
     float *out = (float *)lds + wave * kEpilogueFloats;
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-        store_tile32x64<float>(g, out, m0 + wm + 32 * i, n0 + wn, blockIdx.z, acc[i][0], acc[i][1]);
+    finish_wave<float>(g, out, m0 + wm, n0 + wn, blockIdx.z, acc);
 }
 
 // How many parts k is split into: enough workgroups for the device where the
