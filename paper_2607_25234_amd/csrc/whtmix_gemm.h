@@ -61,8 +61,8 @@ __device__ __forceinline__ void store_mx8(float (&v)[8], int cnt, bool live, int
         if (i >= cnt) v[i] = 0.f;
         top = max(top, mx_magnitude(v[i]));
     }
-    top = max(top, (uint32_t)__shfl_xor((int)top, 1));
-    top = max(top, (uint32_t)__shfl_xor((int)top, 2));
+    top = max(top, quad_xor<0>(top));
+    top = max(top, quad_xor<1>(top));
     const uint32_t byte = mx_scale_byte(top);
     const float inv = mx_inverse(byte);
     if (live && n < width) {
@@ -206,29 +206,57 @@ __device__ __forceinline__ void finish_wave(const GemmArgs &g, float *lds, int64
     });
 }
 
-// Sums a split's partial sums in order and finishes them.
-template <typename T> __global__ void __launch_bounds__(256) split_sum_kernel(GemmArgs g, int splits)
+// Adds the parts' partial sums and finishes them: eight columns a thread, and where the parts
+// are many, the workgroup's threads in GROUPS that take every GROUPS-th part, whose sums are
+// then added in order.
+template <typename T, int GROUPS>
+__global__ void __launch_bounds__(256) split_sum_kernel(GemmArgs g, int splits)
 {
+    constexpr int kChunks = 256 / GROUPS;
+    __shared__ float sums[GROUPS > 1 ? GROUPS : 1][GROUPS > 1 ? kChunks : 1][9];
     const int64_t width = g.yq ? (g.N + kMxBlock - 1) / kMxBlock * kMxBlock : (g.N + 7) / 8 * 8;
-    const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
+    const int c = threadIdx.x % kChunks, first = threadIdx.x / kChunks;
+    const int64_t i = ((int64_t)blockIdx.x * kChunks + c) * 8;
     const int64_t m = i / width, n = i - m * width;
-    if (m >= g.M) return;       // 8-bit output: the four lanes of a block leave together
+    const int cnt = m < g.M ? (int)max((int64_t)0, min((int64_t)8, g.N - n)) : 0;
+    const float *from = g.part + (m < g.M ? m * g.N + n : 0);
     float v[8];
 #pragma unroll
     for (int k = 0; k < 8; ++k) v[k] = 0.f;
-    const int cnt = (int)min((int64_t)8, g.N - n);
-    for (int s = 0; s < splits; s += 4) {       // four parts' loads in flight
+    for (int s = first; s < splits; s += 4 * GROUPS) {       // four parts' loads in flight
         float p[4][8];
 #pragma unroll
         for (int u = 0; u < 4; ++u)
-            load8(g.part + ((int64_t)min(s + u, splits - 1) * g.M + m) * g.N + n,
-                  s + u < splits ? cnt : 0, p[u]);
+            load8(from + (int64_t)min(s + u * GROUPS, splits - 1) * g.M * g.N,
+                  s + u * GROUPS < splits ? cnt : 0, p[u]);
 #pragma unroll
         for (int u = 0; u < 4; ++u)
 #pragma unroll
             for (int k = 0; k < 8; ++k) v[k] += p[u][k];
     }
-    finish8<T>(g, m, n, v);
+    if constexpr (GROUPS > 1) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) sums[first][c][k] = v[k];
+        __syncthreads();
+        if (first > 0) return;
+#pragma unroll
+        for (int f = 1; f < GROUPS; ++f)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] += sums[f][c][k];
+    }
+    if (m < g.M) finish8<T>(g, m, n, v);    // 8-bit output: the four lanes of a block together
+}
+
+template <typename T> hipError_t launch_split_sum(const GemmArgs &g, int splits, hipStream_t stream)
+{
+    const int64_t width = g.yq ? mx_width(g.N) : (g.N + 7) / 8 * 8, chunks = g.M * width / 8;
+    // 16 parts and more of an output that does not fill the device: 8 threads a chunk
+    // (65536 sums of 128 parts: 33 us with one)
+    if (splits >= 16 && chunks <= 1 << 16)
+        split_sum_kernel<T, 8><<<dim3((uint32_t)((chunks + 31) / 32)), dim3(256), 0, stream>>>(g, splits);
+    else
+        split_sum_kernel<T, 1><<<dim3((uint32_t)((chunks + 255) / 256)), dim3(256), 0, stream>>>(g, splits);
+    return hipGetLastError();
 }
 
 // Products of bf16 operands (whtmix_linear_bf16.hip) and of block-scaled 8-bit ones

@@ -474,10 +474,7 @@ hipError_t run_tiles(GemmArgs g, float *part, hipStream_t stream)
         gemm_tile_kernel<EB, EXACT, T, LA, LB, 128, 128, 2, 2><<<grid, 256, 0, stream>>>(g, p.tiles_m, p.tiles_n);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.splits == 1) return e;
-    const int64_t width = g.yq ? mx_width(g.N) : (g.N + 7) / 8 * 8;
-    split_sum_kernel<T><<<dim3((uint32_t)((g.M * width / 8 + 255) / 256)), dim3(256), 0, stream>>>(
-        g, p.splits);
-    return hipGetLastError();
+    return launch_split_sum<T>(g, p.splits, stream);
 }
 
 }  // namespace whtmix

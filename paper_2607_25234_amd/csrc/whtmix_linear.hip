@@ -21,7 +21,7 @@ constexpr int kPlane = 10240;      // either way
 constexpr int kF32Row = kTile + 4; // float32 staging: floats of one k
 // Three bf16 terms hold a float32 below 2^128 - 2^119 (above, the first rounds to Inf) and from
 // 2^-100 up (below, the last is subnormal); rows mixed with smaller values lose less than 2^-128.
-constexpr uint32_t kSplitMax = 0x7f7f8000u, kSplitMin = 0x10000000u;   // 2^-95
+constexpr float kSplitMax = 0x1.ffp127f, kSplitMin = 0x1p-95f;
 static_assert(kTile * kRowBytes == kPlane && kStep * kKBytes == kPlane, "planes");
 
 constexpr int P = 3;               // bf16 terms of a float32
@@ -65,13 +65,15 @@ template <Layout L> struct Stage {
                     (L == K_CONTIGUOUS ? 0 : j)] = v[i][j];
         }
     }
-    // The largest magnitudes staged so far by chunk, as ordered bits (NaN above Inf).
-    __device__ __forceinline__ void largest(uint32_t (&top)[4]) const
+    // The largest magnitudes staged so far by chunk.  (A NaN is passed over: it makes its
+    // row's sums NaN either way.)
+    __device__ __forceinline__ void largest(float (&top)[4]) const
     {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) top[i] = max(top[i], f32_bits(v[i][j]) & 0x7fffffffu);
+        for (int i = 0; i < 4; ++i) {
+            top[i] = fmaxf(fmaxf(top[i], fabsf(v[i][0])), fabsf(v[i][1]));
+            top[i] = fmaxf(fmaxf(top[i], fabsf(v[i][2])), fabsf(v[i][3]));
+        }
     }
     __device__ __forceinline__ void store(char *lds)
     {
@@ -176,7 +178,7 @@ __global__ void __launch_bounds__(256) gemm_kernel(GemmArgs g)
 
     Stage<LA> sa;
     Stage<LB> sb;
-    uint32_t top_a[4] = {0, 0, 0, 0}, top_b[4] = {0, 0, 0, 0};   // what the splits have to hold
+    float top_a[4] = {0.f, 0.f, 0.f, 0.f}, top_b[4] = {0.f, 0.f, 0.f, 0.f};  // of the splits
     sa.load(g.a, g.lda, g.M, kend, m0, kbeg);
     sb.load(g.b, g.ldb, g.N, kend, n0, kbeg);
     for (int64_t k = kbeg; k < kend; k += kStep) {
@@ -214,7 +216,7 @@ __global__ void __launch_bounds__(256) gemm_kernel(GemmArgs g)
                                 fb[s - p][j], fa[p][i], acc[i][j], 0, 0, 0);
         }
     }
-    auto bad = [](uint32_t top) { return top >= kSplitMax || (top != 0 && top < kSplitMin); };
+    auto bad = [](float top) { return top >= kSplitMax || (top != 0.f && top < kSplitMin); };
     // A chunk's elements along k are of one row (or four); one that does not split sends the
     // whole tile through float32 products.
     bool any = false;
@@ -255,10 +257,7 @@ hipError_t run_gemm(GemmArgs g, float *ws, hipStream_t stream)
     gemm_kernel<LA, LB><<<grid, dim3(256), 0, stream>>>(g);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || splits == 1) return e;
-    const int64_t width = g.yq ? mx_width(g.N) : (g.N + 7) / 8 * 8;
-    split_sum_kernel<float><<<dim3((uint32_t)((g.M * width / 8 + 255) / 256)), dim3(256), 0, stream>>>(
-        g, (int)splits);
-    return hipGetLastError();
+    return launch_split_sum<float>(g, (int)splits, stream);
 }
 
 // dz = dy act'(z), with the columns' sums of the unrounded values: 32 threads across

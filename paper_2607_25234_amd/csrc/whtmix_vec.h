@@ -85,6 +85,12 @@ template <> struct Chunk<__bf16> {
     }
 };
 
+// The value of the lane whose number differs in bit 0 or 1 (within a quad, no LDS).
+template <int BIT> __device__ __forceinline__ uint32_t quad_xor(uint32_t v)
+{
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, BIT == 0 ? 0xB1 : 0x4E, 0xf, 0xf, true);
+}
+
 // ---- block-scaled 8 bits ----
 // Magnitude of a finite value as ordered bits; 0 for Inf and NaN, which do not
 // count for a block's scale (they are stored as e4m3's NaN).
@@ -117,21 +123,25 @@ __device__ __forceinline__ uint32_t mx_pack(float a, float b, float c, float d, 
 }
 
 // ---- activations ----
-// erf by Abramowitz & Stegun 7.1.26: |error| <= 1.5e-7, below float32's own
-// rounding of 1 + erf.  e = exp(-x^2) is shared with the gaussian density.
-__device__ __forceinline__ float erf_with(float x, float e)
-{
-    const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, fabsf(x), 1.f));
-    float p = fmaf(1.061405429f, t, -1.453152027f);
-    p = fmaf(p, t, 1.421413741f);
-    p = fmaf(p, t, -0.284496736f);
-    p = fmaf(p, t, 0.254829592f);
-    return copysignf(fmaf(-p * t, e, 1.f), x);
-}
-
 __device__ __forceinline__ float fast_exp(float x)   // 2^(x log2 e), about 2 ulp + |x| 2^-24
 {
     return __builtin_amdgcn_exp2f(x * 1.44269504088896341f);
+}
+
+// (1 - erf(|z| / sqrt 2)) / 2, the gaussian's tail beyond |z|, by Abramowitz & Stegun
+// 7.1.26 (erf off by 1.5e-7 at most), with e = exp(-z^2 / 2), which the density shares.
+__device__ __forceinline__ float gauss_tail(float z, float e)
+{
+    const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f * 0.70710678118654752f, fabsf(z), 1.f));
+    float p = fmaf(0.5f * 1.061405429f, t, -0.5f * 1.453152027f);
+    p = fmaf(p, t, 0.5f * 1.421413741f);
+    p = fmaf(p, t, -0.5f * 0.284496736f);
+    p = fmaf(p, t, 0.5f * 0.254829592f);
+    return p * t * e;
+}
+__device__ __forceinline__ float gauss(float z)      // exp(-z^2 / 2)
+{
+    return __builtin_amdgcn_exp2f(z * z * (-0.5f * 1.44269504088896341f));
 }
 
 // z * sigmoid(u): 0 for u = -Inf with z finite, NaN for z = -Inf as the formula.
@@ -145,10 +155,9 @@ constexpr float kGeluC = 1.5957691216057308f;     // 2 sqrt(2 / pi): tanh(a) = 2
 template <int ACT> __device__ __forceinline__ float act_of(float z)
 {
     if constexpr (ACT == ACT_RELU) return z > 0.f || z != z ? z : 0.f;
-    if constexpr (ACT == ACT_GELU) {
-        const float x = z * 0.70710678118654752f;
-        return 0.5f * z * (1.f + erf_with(x, fast_exp(-x * x)));
-    }
+    // z for z > 0, less |z| times the tail (which is 0 long before 64: no Inf * 0)
+    if constexpr (ACT == ACT_GELU)
+        return fmaf(-fminf(fabsf(z), 64.f), gauss_tail(z, gauss(z)), fmaxf(z, 0.f));
     if constexpr (ACT == ACT_GELU_TANH)
         return gated(z, kGeluC * z * fmaf(0.044715f * z, z, 1.f));
     if constexpr (ACT == ACT_SILU) return gated(z, z);
@@ -159,9 +168,8 @@ template <int ACT> __device__ __forceinline__ float act_grad(float z)
 {
     if constexpr (ACT == ACT_RELU) return z > 0.f ? 1.f : z != z ? z : 0.f;
     if constexpr (ACT == ACT_GELU) {
-        const float x = z * 0.70710678118654752f;
-        const float e = fast_exp(-x * x);
-        return fmaf(z * 0.39894228040143268f, e, 0.5f + 0.5f * erf_with(x, e));
+        const float e = gauss(z), q = gauss_tail(z, e);
+        return fmaf(fminf(fmaxf(z, -64.f), 64.f) * 0.39894228040143268f, e, z < 0.f ? q : 1.f - q);
     }
     if constexpr (ACT == ACT_GELU_TANH) {
         const float s = __builtin_amdgcn_rcpf(
