@@ -103,6 +103,60 @@ __device__ __forceinline__ void finish8(const GemmArgs &g, int64_t m, int64_t n,
     store_mx8(v, cnt, m < g.M, m, n, (g.N + kMxBlock - 1) / kMxBlock * kMxBlock, g.yq, g.ys);
 }
 
+// A pointer that is the same in all lanes, in scalar registers.
+__device__ __forceinline__ const char *uniform(const char *p)
+{
+    const uint64_t v = (uint64_t)p;
+    return (const char *)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)v) |
+                          (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32);
+}
+
+// 16 bytes a lane from memory to LDS (lane order from the wave's address `lds`), counted by
+// vmcnt.  In assembler, because the compiler would have every later LDS read wait for the
+// copies in flight; the kernel waits for them itself, a step later.  No registers but m0 are
+// written, which nothing else in these kernels uses.
+__device__ __forceinline__ void copy16(const char *base, uint32_t off, uint32_t lds)
+{
+    base = uniform(base);
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds),
+                 "v"(off), "s"(base)
+                 : "memory");
+}
+__device__ __forceinline__ void copy4(const char *src, uint32_t lds)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds),
+                 "v"(src)
+                 : "memory");
+}
+__device__ __forceinline__ void copy16(const char *src, uint32_t lds)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds),
+                 "v"(src)
+                 : "memory");
+}
+// Until at most LEFT of the wave's copies (and loads) are in flight.
+template <int LEFT> __device__ __forceinline__ void wait_copies()
+{
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LEFT) : "memory");
+}
+
+// Workgroup -> tile and part of k.  Consecutive workgroups go round the 8 XCDs, each with its
+// own L2: an XCD's are neighbours in the order below (a part's tiles together, in groups
+// of 4 rows of tiles), so that those it holds at a time share operands.
+__device__ __forceinline__ void place_tile(uint32_t id, uint32_t total, uint32_t tiles_m,
+                                           uint32_t tiles_n, uint32_t &tm, uint32_t &tn,
+                                           uint32_t &split)
+{
+    const uint32_t x = id % 8, tiles = tiles_m * tiles_n;
+    const uint32_t s = x * (total / 8) + min(x, total % 8) + id / 8;
+    split = s / tiles;
+    const uint32_t t = s - split * tiles;
+    const uint32_t group = t / (4 * tiles_n), first = group * 4;
+    const uint32_t rows = min(4u, tiles_m - first), in = t - group * 4 * tiles_n;
+    tm = first + in % rows;
+    tn = in / rows;
+}
+
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
@@ -259,10 +313,12 @@ template <typename T> hipError_t launch_split_sum(const GemmArgs &g, int splits,
     return hipGetLastError();
 }
 
-// Products of bf16 operands (whtmix_linear_bf16.hip) and of block-scaled 8-bit ones
-// (whtmix_linear_mx.hip) with `*_bytes` of workspace.
+// Products of bf16 operands (whtmix_linear_bf16.hip), float32 ones (whtmix_linear_f32.hip)
+// and block-scaled 8-bit ones (whtmix_linear_mx.hip), with `*_bytes` of workspace.
 uint64_t gemm_bf16_bytes(const GemmArgs &g, Layout la, Layout lb);
 hipError_t gemm_bf16(GemmArgs g, Layout la, Layout lb, void *ws, hipStream_t stream);
+uint64_t gemm_f32_bytes(const GemmArgs &g);
+hipError_t gemm_f32(const GemmArgs &g, Layout la, Layout lb, void *ws, hipStream_t stream);
 uint64_t gemm_mx_bytes(const GemmArgs &g);
 hipError_t gemm_mx(GemmArgs g, int dtype, void *ws, hipStream_t stream);
 

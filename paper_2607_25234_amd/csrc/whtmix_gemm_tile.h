@@ -23,43 +23,6 @@ static __device__ __attribute__((aligned(16))) const uint32_t kZero16[4] = {0, 0
 
 constexpr int kStepBytes = 128;
 
-// A pointer that is the same in all lanes, in scalar registers.
-__device__ __forceinline__ const char *uniform(const char *p)
-{
-    const uint64_t v = (uint64_t)p;
-    return (const char *)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)v) |
-                          (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32);
-}
-
-// 16 bytes a lane from memory to LDS (lane order from the wave's address `lds`), counted by
-// vmcnt.  In assembler, because the compiler would have every later LDS read wait for the
-// copies in flight; the kernel waits for them itself, a step later.  No registers but m0 are
-// written, which nothing else in these kernels uses.
-__device__ __forceinline__ void copy16(const char *base, uint32_t off, uint32_t lds)
-{
-    base = uniform(base);
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds),
-                 "v"(off), "s"(base)
-                 : "memory");
-}
-__device__ __forceinline__ void copy4(const char *src, uint32_t lds)
-{
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds),
-                 "v"(src)
-                 : "memory");
-}
-__device__ __forceinline__ void copy16(const char *src, uint32_t lds)
-{
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds),
-                 "v"(src)
-                 : "memory");
-}
-// Until at most LEFT of the wave's copies (and loads) are in flight.
-template <int LEFT> __device__ __forceinline__ void wait_copies()
-{
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LEFT) : "memory");
-}
-
 // One operand's tile: R rows of output (or k-strided columns), NW waves copying.
 template <int EB, Layout L, int R, int NW> struct Operand {
     static constexpr int kStepK = kStepBytes / EB;
@@ -220,23 +183,6 @@ template <int BM, int BN, int NT> struct Scales {
         }
     }
 };
-
-// Workgroup -> tile and part of k.  Consecutive workgroups go round the 8 XCDs, each with its
-// own L2: an XCD's are neighbours in the order below (a part's tiles together, in groups
-// of 4 rows of tiles), so that those it holds at a time share operands.
-__device__ __forceinline__ void place_tile(uint32_t id, uint32_t total, uint32_t tiles_m,
-                                           uint32_t tiles_n, uint32_t &tm, uint32_t &tn,
-                                           uint32_t &split)
-{
-    const uint32_t x = id % 8, tiles = tiles_m * tiles_n;
-    const uint32_t s = x * (total / 8) + min(x, total % 8) + id / 8;
-    split = s / tiles;
-    const uint32_t t = s - split * tiles;
-    const uint32_t group = t / (4 * tiles_n), first = group * 4;
-    const uint32_t rows = min(4u, tiles_m - first), in = t - group * 4 * tiles_n;
-    tm = first + in % rows;
-    tn = in / rows;
-}
 
 // EXACT: block-scaled values multiplied as bf16 (see gemm_mx).
 template <int EB, bool EXACT, typename T, Layout LA, Layout LB, int BM, int BN, int WAVES_M,
