@@ -620,29 +620,51 @@ def call_rows(name, pointers, sizes, codes, stream, *eps) -> int:
     return _call().call_rows(addr, pointers, sizes, codes, stream, *eps)
 
 
-def _run_rows(name, x, stream, pointers, sizes, codes, *eps):
-    """call_rows with x's device current; raises WhtmixError on a refusal."""
-    status = _on_device(
-        x, stream, lambda st: call_rows(name, pointers, sizes, codes, st, *eps), (), ())
+def _run_rows(name, dev, stream, pointers, sizes, codes, *eps):
+    """The entry point on device number dev, on `stream` or its current stream; raises
+    WhtmixError on a refusal."""
+    device, current_stream = _current or _torch_current()
+    st = current_stream(dev) if stream is None else stream.cuda_stream
+    if device() == dev:
+        status = call_rows(name, pointers, sizes, codes, st, *eps)
+    else:
+        with _torch().cuda.device(dev):
+            status = call_rows(name, pointers, sizes, codes, st, *eps)
     if status != SUCCESS:
         raise WhtmixError(status, name)
 
 
-def _dtype_code(t, what):
-    import torch
+_torch_module = None
 
+
+def _torch():
+    """torch, imported on first use (an import statement in a call takes 0.3 us)."""
+    global _torch_module
+    if _torch_module is None:
+        import torch
+        _torch_module = torch
+        _CODES.update({torch.float32: DTYPE_F32, torch.bfloat16: DTYPE_BF16})
+    return _torch_module
+
+
+_CODES = {}
+
+
+def _operand(t, what):
+    """(dtype code, rows, width, ld, device number) of x: a float32 or bfloat16 tensor
+    [..., C] on a GPU whose rows are contiguous and a constant distance apart (columns of
+    a wider tensor, or contiguous)."""
+    _torch_module or _torch()
     if not t.is_cuda:
         raise ValueError(f"{what} must be on a GPU device")
-    if t.dtype is torch.float32:
-        return DTYPE_F32
-    if t.dtype is torch.bfloat16:
-        return DTYPE_BF16
-    raise TypeError(f"{what} must be float32 or bfloat16, got {t.dtype}")
+    code = _CODES.get(t.dtype)
+    if code is None:
+        raise TypeError(f"{what} must be float32 or bfloat16, got {t.dtype}")
+    return (code, *_rows(t, what), t.get_device())
 
 
 def _rows(t, what):
-    """(rows, width, ld) of a tensor [..., C] whose rows are contiguous and a
-    constant distance apart (columns of a wider tensor, or contiguous)."""
+    """(rows, width, ld) of a tensor [..., C] whose rows are a constant distance apart."""
     if t.dim() < 2:
         raise ValueError(f"{what} must be [..., rows, columns]")
     C = t.shape[-1]
@@ -662,13 +684,13 @@ def _rows(t, what):
     return rows, C, max(ld, C) if rows <= 1 else ld
 
 
-def _tensor(t, shape, dtype, x, what):
-    """A contiguous tensor of this shape and dtype on x's device."""
-    if t.dtype is not dtype or t.get_device() != x.get_device() or not t.is_contiguous():
-        raise ValueError(f"{what} must be a contiguous {dtype} tensor on x's device")
+def _tensor(t, shape, dtype, dev, what):
+    """The address of a contiguous tensor of this shape and dtype on device dev."""
+    if t.dtype is dtype and t.shape == shape and t.get_device() == dev and t.is_contiguous():
+        return t.data_ptr()
     if t.shape != shape:
         raise ValueError(f"{what} shape {tuple(t.shape)} != {tuple(shape)}")
-    return t.data_ptr()
+    raise ValueError(f"{what} must be a contiguous {dtype} tensor on x's device")
 
 
 def _ptr(t):
@@ -688,26 +710,23 @@ def mx_width(C: int) -> int:
 
 
 def _new_mx(x, lead, C):
-    import torch
-
-    w = mx_width(C)
-    return (torch.empty((*lead, w), dtype=torch.float8_e4m3fn, device=x.device),
-            torch.empty((*lead, w // MX_BLOCK), dtype=torch.uint8, device=x.device))
+    T, w = _torch(), mx_width(C)
+    return (x.new_empty((*lead, w), dtype=T.float8_e4m3fn),
+            x.new_empty((*lead, w // MX_BLOCK), dtype=T.uint8))
 
 
 def _mx(q, scales, what):
-    """(rows, stored width, the two pointers) of block-scaled rows."""
-    import torch
-
+    """(rows, stored width, the two addresses, device number) of block-scaled rows."""
+    T = _torch_module or _torch()
     if not q.is_cuda:
         raise ValueError(f"{what} must be on a GPU device")
-    if q.dtype is not torch.float8_e4m3fn or q.dim() < 2 or not q.is_contiguous():
+    if q.dtype is not T.float8_e4m3fn or q.dim() < 2 or not q.is_contiguous():
         raise ValueError(f"{what} must be a contiguous float8_e4m3fn tensor [..., rows, columns]")
-    w = q.shape[-1]
+    w, dev = q.shape[-1], q.get_device()
     if w % MX_BLOCK or w == 0:
         raise ValueError(f"{what}'s width {w} is not a multiple of {MX_BLOCK}")
     return (q.numel() // w, w, q.data_ptr(),
-            _tensor(scales, (*q.shape[:-1], w // MX_BLOCK), torch.uint8, q, f"{what}'s scales"))
+            _tensor(scales, (*q.shape[:-1], w // MX_BLOCK), T.uint8, dev, f"{what}'s scales"), dev)
 
 
 def norm(x, weight, residual=None, eps: float = 1e-6, out=None, stream=None):
@@ -718,21 +737,22 @@ def norm(x, weight, residual=None, eps: float = 1e-6, out=None, stream=None):
     x: [..., C] float32 or bfloat16 (rows may be columns of a wider tensor);
     weight: float32 [C]; residual: a contiguous tensor of x's shape and type;
     out: optional contiguous tensor for y (may be x itself)."""
-    import torch
-
-    dt = _dtype_code(x, "x")
-    rows, C, ld = _rows(x, "x")
-    _tensor(weight, (C,), torch.float32, x, "weight")
-    h = x
+    T = _torch_module or _torch()
+    dt, rows, C, ld, dev = _operand(x, "x")
+    shape, dtype = x.shape, x.dtype
+    pw = _tensor(weight, (C,), T.float32, dev, "weight")
+    h, pr, ph = x, 0, 0
     if residual is not None:
-        _tensor(residual, x.shape, x.dtype, x, "residual")
-        h = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        pr = _tensor(residual, shape, dtype, dev, "residual")
+        h = T.empty_like(residual)
+        ph = h.data_ptr()
     if out is None:
-        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    _run_rows("whtmix_norm_forward", x, stream,
-              (x.data_ptr(), _ptr(residual), weight.data_ptr(),
-               _tensor(out, x.shape, x.dtype, x, "out"), 0 if h is x else h.data_ptr()),
-              (rows, C, ld), (dt,), eps)
+        out = T.empty_like(x, memory_format=T.contiguous_format)
+        py = out.data_ptr()
+    else:
+        py = _tensor(out, shape, dtype, dev, "out")
+    _run_rows("whtmix_norm_forward", dev, stream, (x.data_ptr(), pr, pw, py, ph), (rows, C, ld),
+              (dt,), eps)
     return out, h
 
 
@@ -740,19 +760,19 @@ def norm_mx(x, weight, residual=None, eps: float = 1e-6, stream=None):
     """norm() with y in block-scaled 8 bits: (q, scales, h), q float8_e4m3fn
     [..., mx_width(C)] and scales uint8 [..., mx_width(C) / 32]; a value is
     q * 2^(scale - 127)."""
-    import torch
-
-    dt = _dtype_code(x, "x")
-    rows, C, ld = _rows(x, "x")
-    _tensor(weight, (C,), torch.float32, x, "weight")
-    h = x
+    T = _torch_module or _torch()
+    dt, rows, C, ld, dev = _operand(x, "x")
+    shape = x.shape
+    pw = _tensor(weight, (C,), T.float32, dev, "weight")
+    h, pr, ph = x, 0, 0
     if residual is not None:
-        _tensor(residual, x.shape, x.dtype, x, "residual")
-        h = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    q, scales = _new_mx(x, x.shape[:-1], C)
-    _run_rows("whtmix_norm_mx_forward", x, stream,
-              (x.data_ptr(), _ptr(residual), weight.data_ptr(), q.data_ptr(), scales.data_ptr(),
-               0 if h is x else h.data_ptr()), (rows, C, ld), (dt,), eps)
+        pr = _tensor(residual, shape, x.dtype, dev, "residual")
+        h = T.empty_like(residual)
+        ph = h.data_ptr()
+    q, scales = _new_mx(x, shape[:-1], C)
+    _run_rows("whtmix_norm_mx_forward", dev, stream,
+              (x.data_ptr(), pr, pw, q.data_ptr(), scales.data_ptr(), ph), (rows, C, ld), (dt,),
+              eps)
     return q, scales, h
 
 
@@ -761,23 +781,17 @@ def norm_backward(h, weight, dy, dh=None, eps: float = 1e-6, want_dweight: bool 
     """Gradients through norm() from its kept h: (dx, dweight), dx the gradient
     of x and of the residual (dh, the gradient of h, is added), dweight float32
     (None when not wanted).  dx may be dy or dh."""
-    import torch
-
-    dt = _dtype_code(h, "h")
-    C = h.shape[-1]
-    _tensor(h, h.shape, h.dtype, h, "h")
-    rows, _, _ = _rows(h, "h")
-    _tensor(weight, (C,), torch.float32, h, "weight")
-    _tensor(dy, h.shape, h.dtype, h, "dy")
-    if dh is not None:
-        _tensor(dh, h.shape, h.dtype, h, "dh")
+    T = _torch_module or _torch()
+    dt, rows, C, _, dev = _operand(h, "h")
+    shape, dtype = h.shape, h.dtype
+    ptr = (_tensor(h, shape, dtype, dev, "h"), _tensor(weight, (C,), T.float32, dev, "weight"),
+           _tensor(dy, shape, dtype, dev, "dy"),
+           0 if dh is None else _tensor(dh, shape, dtype, dev, "dh"))
     if dx is None:
-        dx = torch.empty_like(h)
-    _tensor(dx, h.shape, h.dtype, h, "dx")
-    dweight = torch.empty_like(weight) if want_dweight else None
-    _run_rows("whtmix_norm_backward", h, stream,
-              (h.data_ptr(), weight.data_ptr(), dy.data_ptr(), _ptr(dh), dx.data_ptr(),
-               _ptr(dweight)), (rows, C), (dt,), eps)
+        dx = T.empty_like(h)
+    dweight = T.empty_like(weight) if want_dweight else None
+    _run_rows("whtmix_norm_backward", dev, stream,
+              (*ptr, _tensor(dx, shape, dtype, dev, "dx"), _ptr(dweight)), (rows, C), (dt,), eps)
     return dx, dweight
 
 
@@ -785,10 +799,9 @@ def quantize_mx(x, stream=None):
     """x [..., C] in block-scaled 8 bits along its rows: (q, scales) as norm_mx.
     Weights [K, N] are laid out once by their columns: quantize_mx(w.t())
     after .contiguous()."""
-    dt = _dtype_code(x, "x")
-    rows, C, ld = _rows(x, "x")
+    dt, rows, C, ld, dev = _operand(x, "x")
     q, scales = _new_mx(x, x.shape[:-1], C)
-    _run_rows("whtmix_quantize_mx", x, stream, (x.data_ptr(), q.data_ptr(), scales.data_ptr()),
+    _run_rows("whtmix_quantize_mx", dev, stream, (x.data_ptr(), q.data_ptr(), scales.data_ptr()),
               (rows, C, ld), (dt,))
     return q, scales
 
@@ -796,15 +809,17 @@ def quantize_mx(x, stream=None):
 def dequantize_mx(q, scales, C: int | None = None, dtype=None, stream=None):
     """The values q and scales stand for, [..., C] (default: the stored width)
     in dtype (bfloat16, the default, or float32)."""
-    import torch
-
-    rows, w, pq, ps = _mx(q, scales, "q")
+    T = _torch_module or _torch()
+    rows, w, pq, ps, dev = _mx(q, scales, "q")
     C = w if C is None else C
     if mx_width(C) != w:
         raise ValueError(f"{C} columns are not stored in {w}")
-    y = torch.empty((*q.shape[:-1], C), dtype=dtype or torch.bfloat16, device=q.device)
-    _run_rows("whtmix_dequantize_mx", q, stream, (pq, ps, y.data_ptr()), (rows, C),
-              (_dtype_code(y, "the output"),))
+    dtype = dtype or T.bfloat16
+    code = _CODES.get(dtype)
+    if code is None:
+        raise TypeError(f"the output must be float32 or bfloat16, not {dtype}")
+    y = q.new_empty((*q.shape[:-1], C), dtype=dtype)
+    _run_rows("whtmix_dequantize_mx", dev, stream, (pq, ps, y.data_ptr()), (rows, C), (code,))
     return y
 
 
@@ -817,26 +832,23 @@ def linear(x, w, bias=None, activation: str = "none", residual=None, want_z: boo
     w: [K, N] of x's type; bias: float32 [N]; residual: a contiguous [..., N]
     of x's type; activation: "none", "relu", "gelu", "gelu_tanh" or "silu"; out:
     optional contiguous tensor for y (may be the residual)."""
-    import torch
-
-    dt, act = _dtype_code(x, "x"), _activation(activation)
-    M, K, ld = _rows(x, "x")
+    T = _torch_module or _torch()
+    dt, M, K, ld, dev = _operand(x, "x")
+    act, dtype = _activation(activation), x.dtype
     if w.dim() != 2:
         raise ValueError("w must be [K, N]")
     N = w.shape[1]
-    _tensor(w, (K, N), x.dtype, x, "w")
+    pw = _tensor(w, (K, N), dtype, dev, "w")
     shape = (*x.shape[:-1], N)
-    if bias is not None:
-        _tensor(bias, (N,), torch.float32, x, "bias")
-    if residual is not None:
-        _tensor(residual, shape, x.dtype, x, "residual")
+    pb = 0 if bias is None else _tensor(bias, (N,), T.float32, dev, "bias")
+    pr = 0 if residual is None else _tensor(residual, shape, dtype, dev, "residual")
     if out is None:
-        out = torch.empty(shape, dtype=x.dtype, device=x.device)
+        out = x.new_empty(shape)
+        py = out.data_ptr()
     else:
-        _tensor(out, shape, x.dtype, x, "out")
-    z = torch.empty(shape, dtype=x.dtype, device=x.device) if want_z else None
-    _run_rows("whtmix_linear_forward", x, stream,
-              (x.data_ptr(), w.data_ptr(), _ptr(bias), _ptr(residual), out.data_ptr(), _ptr(z)),
+        py = _tensor(out, shape, dtype, dev, "out")
+    z = T.empty_like(out) if want_z else None
+    _run_rows("whtmix_linear_forward", dev, stream, (x.data_ptr(), pw, pb, pr, py, _ptr(z)),
               (M, K, N, ld), (act, dt))
     return (out, z) if want_z else out
 
@@ -846,30 +858,27 @@ def linear_backward(x, w, dy, z=None, activation: str = "none", want_dx: bool = 
     """Gradients through linear() for the upstream gradient dy: (dx, dw, dbias),
     dx and dw in x's type, dbias float32; what is not wanted is None.  z: what
     linear kept (not needed for activation "none").  The residual's gradient is dy."""
-    import torch
-
-    dt, act = _dtype_code(x, "x"), _activation(activation)
-    M, K, ld = _rows(x, "x")
+    T = _torch_module or _torch()
+    dt, M, K, ld, dev = _operand(x, "x")
+    act, dtype = _activation(activation), x.dtype
     if w.dim() != 2:
         raise ValueError("w must be [K, N]")
     N = w.shape[1]
-    _tensor(w, (K, N), x.dtype, x, "w")
+    pw = _tensor(w, (K, N), dtype, dev, "w")
     shape = (*x.shape[:-1], N)
-    _tensor(dy, shape, x.dtype, x, "dy")
+    pdy = _tensor(dy, shape, dtype, dev, "dy")
+    pz = 0
     if act:
         if z is None:
             raise ValueError(f"activation {activation!r} needs z")
-        _tensor(z, shape, x.dtype, x, "z")
-    else:
-        z = None
+        pz = _tensor(z, shape, dtype, dev, "z")
     if not (want_dx or want_dw or want_dbias):
         raise ValueError("nothing to compute")
-    dx = torch.empty(x.shape, dtype=x.dtype, device=x.device) if want_dx else None
-    dw = torch.empty_like(w) if want_dw else None
-    db = torch.empty(N, dtype=torch.float32, device=x.device) if want_dbias else None
-    _run_rows("whtmix_linear_backward", x, stream,
-              (x.data_ptr(), w.data_ptr(), dy.data_ptr(), _ptr(z), _ptr(dx), _ptr(dw), _ptr(db)),
-              (M, K, N, ld), (act, dt))
+    dx = T.empty_like(x, memory_format=T.contiguous_format) if want_dx else None
+    dw = T.empty_like(w) if want_dw else None
+    db = x.new_empty(N, dtype=T.float32) if want_dbias else None
+    _run_rows("whtmix_linear_backward", dev, stream,
+              (x.data_ptr(), pw, pdy, pz, _ptr(dx), _ptr(dw), _ptr(db)), (M, K, N, ld), (act, dt))
     return dx, dw, db
 
 
@@ -879,38 +888,34 @@ def linear_mx(xq, xs, wq, ws, bias=None, activation: str = "none", residual=None
     them, [..., K]; wq, ws the weights' columns as rows, [N, K].  Returns y
     [..., N] in dtype (the residual's or out's, else bfloat16), or with out_mx
     (q, scales) of the result."""
-    import torch
-
-    M, K, pxq, pxs = _mx(xq, xs, "xq")
+    T = _torch_module or _torch()
+    M, K, pxq, pxs, dev = _mx(xq, xs, "xq")
     act = _activation(activation)
     if wq.dim() != 2:
         raise ValueError("wq must be [N, K]")
-    N, Kw, pwq, pws = _mx(wq, ws, "wq")
-    if Kw != K or wq.get_device() != xq.get_device():
+    N, Kw, pwq, pws, wdev = _mx(wq, ws, "wq")
+    if Kw != K or wdev != dev:
         raise ValueError(f"wq must hold rows of {K} on xq's device")
     lead = xq.shape[:-1]
-    if bias is not None:
-        _tensor(bias, (N,), torch.float32, xq, "bias")
+    pb = 0 if bias is None else _tensor(bias, (N,), T.float32, dev, "bias")
     if dtype is None:
         like = residual if residual is not None else out
-        dtype = like.dtype if like is not None else torch.bfloat16
-    if residual is not None:
-        _tensor(residual, (*lead, N), dtype, xq, "residual")
+        dtype = like.dtype if like is not None else T.bfloat16
+    code = _CODES.get(dtype)
+    if code is None:
+        raise TypeError(f"the output must be float32 or bfloat16, not {dtype}")
+    pr = 0 if residual is None else _tensor(residual, (*lead, N), dtype, dev, "residual")
     q = s = None
     if out_mx:
         if out is not None:
             raise ValueError("out is for outputs that are not in 8 bits")
         q, s = _new_mx(xq, lead, N)
     elif out is None:
-        out = torch.empty((*lead, N), dtype=dtype, device=xq.device)
+        out = xq.new_empty((*lead, N), dtype=dtype)
     else:
-        _tensor(out, (*lead, N), dtype, xq, "out")
-    code = {torch.float32: DTYPE_F32, torch.bfloat16: DTYPE_BF16}.get(dtype)
-    if code is None:
-        raise TypeError(f"the output must be float32 or bfloat16, not {dtype}")
-    _run_rows("whtmix_linear_mx_forward", xq, stream,
-              (pxq, pxs, pwq, pws, _ptr(bias), _ptr(residual), _ptr(out), _ptr(q), _ptr(s)),
-              (M, K, N), (act, code))
+        _tensor(out, (*lead, N), dtype, dev, "out")
+    _run_rows("whtmix_linear_mx_forward", dev, stream,
+              (pxq, pxs, pwq, pws, pb, pr, _ptr(out), _ptr(q), _ptr(s)), (M, K, N), (act, code))
     return (q, s) if out_mx else out
 
 
