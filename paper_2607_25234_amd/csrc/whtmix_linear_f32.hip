@@ -13,9 +13,20 @@ namespace whtmix {
 namespace {
 
 constexpr int kTile = 128, kStep = 32;
-constexpr int kRowBytes = 80;      // K_CONTIGUOUS: 32 bf16 and 16 bytes of padding
-constexpr int kKBytes = 320;       // K_STRIDED: 128 bf16 and 64 bytes of padding
-constexpr int kPlane = 10240;      // either way
+constexpr int kRowBytes = 64;      // K_CONTIGUOUS: 32 bf16 a row
+constexpr int kKBytes = 256;       // K_STRIDED: 128 bf16 a k
+constexpr int kPlane = 8192;       // either way
+static_assert(kTile * kRowBytes == kPlane && kStep * kKBytes == kPlane, "planes");
+
+// Where 16-byte chunk `chunk` of a row (or k) lies in a plane: permuted so that the 16 lanes
+// of an LDS cycle fall on all banks (rows of a fragment; 4 k x 2 groups of 16 rows of a
+// transposing read).
+template <Layout L> __device__ __forceinline__ int place_chunk(int outer, int chunk)
+{
+    if constexpr (L == K_CONTIGUOUS) return outer * kRowBytes + (chunk ^ ((outer >> 2) & 3)) * 16;
+    else return outer * kKBytes + (chunk ^ (4 * (outer & 3))) * 16;
+}
+
 constexpr int kF32Row = kTile + 4; // float32 staging: floats of one k
 // Three bf16 terms hold a float32 below 2^128 - 2^119 (above, the first rounds to Inf) and from
 // 2^-100 up (below, the last is subnormal); rows mixed with smaller values lose less than 2^-128.
@@ -35,20 +46,31 @@ template <Layout L> struct Stage {
         if (L == K_CONTIGUOUS) row = c >> 3, k = (c & 7) * 4;
         else k = c >> 5, row = (c & 31) * 4;
     }
-    __device__ __forceinline__ void load(const void *p, int64_t ld, int64_t R, int64_t K,
+    // The thread's first chunk at the current step; the others are a constant way apart.
+    const float *at;
+    int64_t apart, ahead;
+    int rows, ks;           // left of the operand from there on
+    __device__ __forceinline__ void init(const void *p, int64_t ld, int64_t R, int64_t K,
                                          int64_t r0, int64_t k0)
+    {
+        int row, k;
+        place(0, row, k);
+        at = (const float *)p + (L == K_CONTIGUOUS ? (r0 + row) * ld + k0 + k
+                                                   : (k0 + k) * ld + r0 + row);
+        apart = (L == K_CONTIGUOUS ? 32 : 8) * ld;
+        ahead = L == K_CONTIGUOUS ? kStep : kStep * ld;
+        rows = (int)max(min(R - r0 - row, (int64_t)1 << 20), (int64_t)-(1 << 20));
+        ks = (int)min(K - k0 - k, ((int64_t)1 << 31) - 1);
+    }
+    __device__ __forceinline__ void load()
     {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            int row, k;
-            place(i, row, k);
-            const int64_t outer = L == K_CONTIGUOUS ? r0 + row : k0 + k,
-                          inner = L == K_CONTIGUOUS ? k0 + k : r0 + row;
-            const int64_t left = outer < (L == K_CONTIGUOUS ? R : K)
-                                     ? (L == K_CONTIGUOUS ? K : R) - inner : 0;
-            const int n = (int)min((int64_t)4, max((int64_t)0, left));
-            Chunk<float>::load((const float *)p + (n ? outer * ld + inner : 0), n, v[i]);
+            const bool in = L == K_CONTIGUOUS ? rows > 32 * i : ks > 8 * i;
+            Chunk<float>::load(at + i * apart, in ? (L == K_CONTIGUOUS ? ks : rows) : 0, v[i]);
         }
+        at += ahead;
+        ks -= kStep;
     }
     // As float32, [k][row], for operands that do not split.
     __device__ __forceinline__ void store_f32(float *lds) const
@@ -79,7 +101,8 @@ template <Layout L> struct Stage {
         for (int i = 0; i < 4; ++i) {
             int row, k;
             place(i, row, k);
-            char *p = lds + (L == K_CONTIGUOUS ? row * kRowBytes + k * 2 : k * kKBytes + row * 2);
+            const int inner = L == K_CONTIGUOUS ? k : row;
+            char *p = lds + place_chunk<L>(L == K_CONTIGUOUS ? row : k, inner >> 3) + (inner & 7) * 2;
 #pragma unroll
             for (int s = 0; s < P; ++s) {
                 const uint32_t w0 = pack_bf16(v[i][0], v[i][1]), w1 = pack_bf16(v[i][2], v[i][3]);
@@ -102,14 +125,13 @@ template <Layout L> __device__ __forceinline__ bf16x8 fragment(const char *plane
 {
     const int lane = threadIdx.x & 63;
     if constexpr (L == K_CONTIGUOUS) {
-        return *(const bf16x8 *)(plane + (row0 + (lane & 31)) * kRowBytes +
-                                 (k0 + (lane >> 5) * 8) * 2);
+        return *(const bf16x8 *)(plane + place_chunk<L>(row0 + (lane & 31), (k0 >> 3) + (lane >> 5)));
     } else {
         typedef short s4 __attribute__((ext_vector_type(4)));
         typedef __attribute__((address_space(3))) s4 lds_s4;
         const int k = k0 + (lane >> 5) * 8 + ((lane >> 2) & 3);
         const int r = row0 + ((lane >> 4) & 1) * 16 + (lane & 3) * 4;
-        const char *p = plane + k * kKBytes + r * 2;
+        const char *p = plane + place_chunk<L>(k, r >> 3) + (r & 7) * 2;    // k + 4: alike
         union {
             s4 h[2];
             bf16x8 f;
@@ -135,9 +157,11 @@ __device__ __forceinline__ void float32_tile(const GemmArgs &g, Stage<LA> &sa,
         for (int j = 0; j < 2; ++j)
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
+    sa.init(g.a, g.lda, g.M, kend, m0, kbeg);
+    sb.init(g.b, g.ldb, g.N, kend, n0, kbeg);
     for (int64_t k = kbeg; k < kend; k += kStep) {
-        sa.load(g.a, g.lda, g.M, kend, m0, k);
-        sb.load(g.b, g.ldb, g.N, kend, n0, k);
+        sa.load();
+        sb.load();
         __syncthreads();
         sa.store_f32(la);
         sb.store_f32(lb);
@@ -177,8 +201,10 @@ __global__ void __launch_bounds__(256) gemm_kernel(GemmArgs g)
     Stage<LA> sa;
     Stage<LB> sb;
     float top_a[4] = {0.f, 0.f, 0.f, 0.f}, top_b[4] = {0.f, 0.f, 0.f, 0.f};  // of the splits
-    sa.load(g.a, g.lda, g.M, kend, m0, kbeg);
-    sb.load(g.b, g.ldb, g.N, kend, n0, kbeg);
+    sa.init(g.a, g.lda, g.M, kend, m0, kbeg);
+    sb.init(g.b, g.ldb, g.N, kend, n0, kbeg);
+    sa.load();
+    sb.load();
     for (int64_t k = kbeg; k < kend; k += kStep) {
         __syncthreads();
         sa.largest(top_a);
@@ -186,32 +212,34 @@ __global__ void __launch_bounds__(256) gemm_kernel(GemmArgs g)
         sa.store(la);
         sb.store(lb);
         if (k + kStep < kend) {
-            sa.load(g.a, g.lda, g.M, kend, m0, k + kStep);
-            sb.load(g.b, g.ldb, g.N, kend, n0, k + kStep);
+            sa.load();
+            sb.load();
         }
         __syncthreads();
 #pragma unroll
         for (int kk = 0; kk < kStep; kk += 16) {
-            bf16x8 fa[P][2], fb[P][2];
+            bf16x8 fa[P][2];
 #pragma unroll
             for (int p = 0; p < P; ++p)
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
+                for (int i = 0; i < 2; ++i)
                     fa[p][i] = fragment<LA>(la + p * kPlane, wm + 32 * i, kk);
-                    fb[p][i] = fragment<LB>(lb + p * kPlane, wn + 32 * i, kk);
-                }
-            // Of the nine products of three terms the six largest: what is left
-            // out is below 2^-24 of |x| |w|.
+            // Of the nine products of three terms the six largest, small ones first: what is
+            // left out is below 2^-24 of |x| |w|.
 #pragma unroll
-            for (int s = P - 1; s >= 0; --s)
+            for (int j = 0; j < 2; ++j) {
+                bf16x8 fb[P];
 #pragma unroll
-                for (int p = 0; p <= s; ++p)
+                for (int p = 0; p < P; ++p) fb[p] = fragment<LB>(lb + p * kPlane, wn + 32 * j, kk);
 #pragma unroll
-                    for (int i = 0; i < 2; ++i)
+                for (int s = P - 1; s >= 0; --s)
 #pragma unroll
-                        for (int j = 0; j < 2; ++j)
-                            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                                fb[s - p][j], fa[p][i], acc[i][j], 0, 0, 0);
+                    for (int p = 0; p <= s; ++p)
+#pragma unroll
+                        for (int i = 0; i < 2; ++i)
+                            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[s - p], fa[p][i],
+                                                                                acc[i][j], 0, 0, 0);
+            }
         }
     }
     auto bad = [](float top) { return top >= kSplitMax || (top != 0.f && top < kSplitMin); };
