@@ -12,39 +12,35 @@
 namespace whtmix {
 namespace {
 
-constexpr int kTile = 128, kStep = 32;
-constexpr int kRowBytes = 64;      // K_CONTIGUOUS: 32 bf16 a row
-constexpr int kKBytes = 256;       // K_STRIDED: 128 bf16 a k
-constexpr int kPlane = 8192;       // either way
-static_assert(kTile * kRowBytes == kPlane && kStep * kKBytes == kPlane, "planes");
+constexpr int kStep = 32;
+constexpr int kRowBytes = 64;      // of a plane: 32 bf16, of one row or of 32 rows of one k
 
-// Where 16-byte chunk `chunk` of a row (or k) lies in a plane: permuted so that the 16 lanes
-// of an LDS cycle fall on all banks (rows of a fragment; 4 k x 2 groups of 16 rows of a
-// transposing read).
-template <Layout L> __device__ __forceinline__ int place_chunk(int outer, int chunk)
+// Where 16-byte chunk `chunk` of a row (or k) lies in a plane of ROWS rows: permuted so that
+// the 16 lanes of an LDS cycle fall on all banks (rows of a fragment; 4 k x 2 groups of 16
+// rows of a transposing read).
+template <Layout L, int ROWS> __device__ __forceinline__ int place_chunk(int outer, int chunk)
 {
     if constexpr (L == K_CONTIGUOUS) return outer * kRowBytes + (chunk ^ ((outer >> 2) & 3)) * 16;
-    else return outer * kKBytes + (chunk ^ (4 * (outer & 3))) * 16;
+    else return outer * (2 * ROWS) + (chunk ^ ((4 * (outer & 3)) & (ROWS / 8 - 1))) * 16;
 }
 
-constexpr int kF32Row = kTile + 4; // float32 staging: floats of one k
 // Three bf16 terms hold a float32 below 2^128 - 2^119 (above, the first rounds to Inf) and from
 // 2^-100 up (below, the last is subnormal); rows mixed with smaller values lose less than 2^-128.
 constexpr float kSplitMax = 0x1.ffp127f, kSplitMin = 0x1p-95f;
-static_assert(kTile * kRowBytes == kPlane && kStep * kKBytes == kPlane, "planes");
-
 constexpr int P = 3;               // bf16 terms of a float32
 
-// Sixteen elements of an operand in a thread's registers, four times four along memory: a
-// row's chunks are neighbouring lanes'.
-template <Layout L> struct Stage {
-    float v[4][4];
+// A step of ROWS rows of an operand in the workgroup's registers, four elements along memory
+// at a time: a row's chunks are neighbouring lanes'.
+template <Layout L, int ROWS> struct Stage {
+    static constexpr int kChunks = ROWS / 32, kPlane = ROWS * kRowBytes;
+    static constexpr int kF32Row = ROWS + 4;        // float32 staging: floats of one k
+    float v[kChunks][4];
     // Chunk i of the thread: (row, k) of its first element.
     static __device__ __forceinline__ void place(int i, int &row, int &k)
     {
         const int c = i * 256 + threadIdx.x;
         if (L == K_CONTIGUOUS) row = c >> 3, k = (c & 7) * 4;
-        else k = c >> 5, row = (c & 31) * 4;
+        else k = c / (ROWS / 4), row = c % (ROWS / 4) * 4;
     }
     // The thread's first chunk at the current step; the others are a constant way apart.
     const float *at;
@@ -57,7 +53,7 @@ template <Layout L> struct Stage {
         place(0, row, k);
         at = (const float *)p + (L == K_CONTIGUOUS ? (r0 + row) * ld + k0 + k
                                                    : (k0 + k) * ld + r0 + row);
-        apart = (L == K_CONTIGUOUS ? 32 : 8) * ld;
+        apart = (L == K_CONTIGUOUS ? 32 : 1024 / ROWS) * ld;
         ahead = L == K_CONTIGUOUS ? kStep : kStep * ld;
         rows = (int)max(min(R - r0 - row, (int64_t)1 << 20), (int64_t)-(1 << 20));
         ks = (int)min(K - k0 - k, ((int64_t)1 << 31) - 1);
@@ -65,8 +61,8 @@ template <Layout L> struct Stage {
     __device__ __forceinline__ void load()
     {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const bool in = L == K_CONTIGUOUS ? rows > 32 * i : ks > 8 * i;
+        for (int i = 0; i < kChunks; ++i) {
+            const bool in = L == K_CONTIGUOUS ? rows > 32 * i : ks > 1024 / ROWS * i;
             Chunk<float>::load(at + i * apart, in ? (L == K_CONTIGUOUS ? ks : rows) : 0, v[i]);
         }
         at += ahead;
@@ -76,7 +72,7 @@ template <Layout L> struct Stage {
     __device__ __forceinline__ void store_f32(float *lds) const
     {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < kChunks; ++i) {
             int row, k;
             place(i, row, k);
 #pragma unroll
@@ -87,10 +83,10 @@ template <Layout L> struct Stage {
     }
     // The largest magnitudes staged so far by chunk.  (A NaN is passed over: it makes its
     // row's sums NaN either way.)
-    __device__ __forceinline__ void largest(float (&top)[4]) const
+    __device__ __forceinline__ void largest(float (&top)[kChunks]) const
     {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < kChunks; ++i) {
             top[i] = fmaxf(fmaxf(top[i], fabsf(v[i][0])), fabsf(v[i][1]));
             top[i] = fmaxf(fmaxf(top[i], fabsf(v[i][2])), fabsf(v[i][3]));
         }
@@ -98,11 +94,11 @@ template <Layout L> struct Stage {
     __device__ __forceinline__ void store(char *lds)
     {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < kChunks; ++i) {
             int row, k;
             place(i, row, k);
             const int inner = L == K_CONTIGUOUS ? k : row;
-            char *p = lds + place_chunk<L>(L == K_CONTIGUOUS ? row : k, inner >> 3) + (inner & 7) * 2;
+            char *p = lds + place_chunk<L, ROWS>(L == K_CONTIGUOUS ? row : k, inner >> 3) + (inner & 7) * 2;
 #pragma unroll
             for (int s = 0; s < P; ++s) {
                 const uint32_t w0 = pack_bf16(v[i][0], v[i][1]), w1 = pack_bf16(v[i][2], v[i][3]);
@@ -121,38 +117,41 @@ template <Layout L> struct Stage {
 // The operand of a 32x32x16 product: lane l holds row l % 32, k 8 (l / 32) + 0..7.
 // K_STRIDED planes are read through the transposing LDS load: a group of 16
 // lanes reads 4 k of 16 rows and each lane gets one row's 4 k.
-template <Layout L> __device__ __forceinline__ bf16x8 fragment(const char *plane, int row0, int k0)
+template <Layout L, int ROWS>
+__device__ __forceinline__ bf16x8 fragment(const char *plane, int row0, int k0)
 {
     const int lane = threadIdx.x & 63;
     if constexpr (L == K_CONTIGUOUS) {
-        return *(const bf16x8 *)(plane + place_chunk<L>(row0 + (lane & 31), (k0 >> 3) + (lane >> 5)));
+        return *(const bf16x8 *)(plane + place_chunk<L, ROWS>(row0 + (lane & 31),
+                                                              (k0 >> 3) + (lane >> 5)));
     } else {
         typedef short s4 __attribute__((ext_vector_type(4)));
         typedef __attribute__((address_space(3))) s4 lds_s4;
         const int k = k0 + (lane >> 5) * 8 + ((lane >> 2) & 3);
         const int r = row0 + ((lane >> 4) & 1) * 16 + (lane & 3) * 4;
-        const char *p = plane + place_chunk<L>(k, r >> 3) + (r & 7) * 2;    // k + 4: alike
+        const char *p = plane + place_chunk<L, ROWS>(k, r >> 3) + (r & 7) * 2;    // k + 4: alike
         union {
             s4 h[2];
             bf16x8 f;
         } u;
         u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4 *)p);
-        u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4 *)(p + 4 * kKBytes));
+        u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4 *)(p + 4 * 2 * ROWS));
         return u.f;
     }
 }
 
 // The tile again with float32 products (v_mfma_f32_32x32x2_f32).
-template <Layout LA, Layout LB>
-__device__ __forceinline__ void float32_tile(const GemmArgs &g, Stage<LA> &sa,
-                                          Stage<LB> &sb, float *lds, int64_t m0, int64_t n0,
-                                          int64_t kbeg, int64_t kend, int wm, int wn,
-                                          f32x16 (&acc)[2][2])
+template <Layout LA, Layout LB, int BM, int BN, int WM>
+__device__ __forceinline__ void float32_tile(const GemmArgs &g, Stage<LA, BM> &sa,
+                                             Stage<LB, BN> &sb, float *lds, int64_t m0, int64_t n0,
+                                             int64_t kbeg, int64_t kend, int wm, int wn,
+                                             f32x16 (&acc)[WM][2])
 {
+    constexpr int kA = Stage<LA, BM>::kF32Row, kB = Stage<LB, BN>::kF32Row;
     const int lane = threadIdx.x & 63;
-    float *la = lds, *lb = lds + kStep * kF32Row;
+    float *la = lds, *lb = lds + kStep * kA;
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < WM; ++i)
 #pragma unroll
         for (int j = 0; j < 2; ++j)
 #pragma unroll
@@ -167,10 +166,10 @@ __device__ __forceinline__ void float32_tile(const GemmArgs &g, Stage<LA> &sa,
         sb.store_f32(lb);
         __syncthreads();
         for (int kk = 0; kk < kStep; kk += 2) {
-            const float *pa = la + (kk + (lane >> 5)) * kF32Row + wm + (lane & 31);
-            const float *pb = lb + (kk + (lane >> 5)) * kF32Row + wn + (lane & 31);
+            const float *pa = la + (kk + (lane >> 5)) * kA + wm + (lane & 31);
+            const float *pb = lb + (kk + (lane >> 5)) * kB + wn + (lane & 31);
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
+            for (int i = 0; i < WM; ++i)
 #pragma unroll
                 for (int j = 0; j < 2; ++j)
                     acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(pb[32 * j], pa[32 * i],
@@ -179,28 +178,33 @@ __device__ __forceinline__ void float32_tile(const GemmArgs &g, Stage<LA> &sa,
     }
 }
 
-template <Layout LA, Layout LB>
+// BM x BN sums by four waves of 64 columns.  The next step's loads are in flight during the
+// products of this one; two or three workgroups fill in for each other at the barriers.
+template <Layout LA, Layout LB, int BM, int BN>
 __global__ void __launch_bounds__(256) gemm_kernel(GemmArgs g)
 {
-    __shared__ __attribute__((aligned(16))) char lds[2 * P * kPlane > 4 * kEpilogueFloats * 4
-                                                         ? 2 * P * kPlane
-                                                         : 4 * kEpilogueFloats * 4];
+    constexpr int WAVES_N = BN / 64, WAVES_M = 4 / WAVES_N, WM = BM / WAVES_M / 32;
+    constexpr int kPlaneA = Stage<LA, BM>::kPlane, kPlaneB = Stage<LB, BN>::kPlane;
+    constexpr int kPlanes = P * (kPlaneA + kPlaneB), kEpilogue = 4 * kEpilogueFloats * 4;
+    static_assert(kStep * (Stage<LA, BM>::kF32Row + Stage<LB, BN>::kF32Row) * 4 <= kPlanes,
+                  "float32 staging in the planes' place");
+    __shared__ __attribute__((aligned(16))) char lds[kPlanes > kEpilogue ? kPlanes : kEpilogue];
     const int wave = threadIdx.x >> 6;
-    const int64_t m0 = (int64_t)blockIdx.x * kTile, n0 = (int64_t)blockIdx.y * kTile;
+    const int64_t m0 = (int64_t)blockIdx.x * BM, n0 = (int64_t)blockIdx.y * BN;
     const int64_t kbeg = (int64_t)blockIdx.z * g.k_per, kend = min(g.K, kbeg + g.k_per);
-    const int wm = (wave & 1) * 64, wn = (wave >> 1) * 64;
-    char *la = lds, *lb = lds + P * kPlane;
-    f32x16 acc[2][2];
+    const int wm = wave % WAVES_M * (WM * 32), wn = wave / WAVES_M * 64;
+    char *la = lds, *lb = lds + P * kPlaneA;
+    f32x16 acc[WM][2];
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < WM; ++i)
 #pragma unroll
         for (int j = 0; j < 2; ++j)
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
 
-    Stage<LA> sa;
-    Stage<LB> sb;
-    float top_a[4] = {0.f, 0.f, 0.f, 0.f}, top_b[4] = {0.f, 0.f, 0.f, 0.f};  // of the splits
+    Stage<LA, BM> sa;
+    Stage<LB, BN> sb;
+    float top_a[BM / 32] = {}, top_b[BN / 32] = {};     // what the splits have to hold
     sa.init(g.a, g.lda, g.M, kend, m0, kbeg);
     sb.init(g.b, g.ldb, g.N, kend, n0, kbeg);
     sa.load();
@@ -218,25 +222,26 @@ __global__ void __launch_bounds__(256) gemm_kernel(GemmArgs g)
         __syncthreads();
 #pragma unroll
         for (int kk = 0; kk < kStep; kk += 16) {
-            bf16x8 fa[P][2];
+            bf16x8 fa[P][WM];
 #pragma unroll
             for (int p = 0; p < P; ++p)
 #pragma unroll
-                for (int i = 0; i < 2; ++i)
-                    fa[p][i] = fragment<LA>(la + p * kPlane, wm + 32 * i, kk);
+                for (int i = 0; i < WM; ++i)
+                    fa[p][i] = fragment<LA, BM>(la + p * kPlaneA, wm + 32 * i, kk);
             // Of the nine products of three terms the six largest, small ones first: what is
             // left out is below 2^-24 of |x| |w|.
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
                 bf16x8 fb[P];
 #pragma unroll
-                for (int p = 0; p < P; ++p) fb[p] = fragment<LB>(lb + p * kPlane, wn + 32 * j, kk);
+                for (int p = 0; p < P; ++p)
+                    fb[p] = fragment<LB, BN>(lb + p * kPlaneB, wn + 32 * j, kk);
 #pragma unroll
                 for (int s = P - 1; s >= 0; --s)
 #pragma unroll
                     for (int p = 0; p <= s; ++p)
 #pragma unroll
-                        for (int i = 0; i < 2; ++i)
+                        for (int i = 0; i < WM; ++i)
                             acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[s - p], fa[p][i],
                                                                                 acc[i][j], 0, 0, 0);
             }
@@ -247,21 +252,29 @@ __global__ void __launch_bounds__(256) gemm_kernel(GemmArgs g)
     // whole tile through float32 products.
     bool any = false;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) any = any || bad(top_a[i]) || bad(top_b[i]);
+    for (int i = 0; i < BM / 32; ++i) any = any || bad(top_a[i]);
+#pragma unroll
+    for (int i = 0; i < BN / 32; ++i) any = any || bad(top_b[i]);
     if (__syncthreads_or(any))
-        float32_tile(g, sa, sb, (float *)lds, m0, n0, kbeg, kend, wm, wn, acc);
+        float32_tile<LA, LB, BM, BN, WM>(g, sa, sb, (float *)lds, m0, n0, kbeg, kend, wm, wn, acc);
     __syncthreads();
     float *out = (float *)lds + wave * kEpilogueFloats;
     finish_wave<float>(g, out, m0 + wm, n0 + wn, blockIdx.z, acc);
 }
 
-// How many parts k is split into: enough workgroups for the device where the
-// output has few tiles, each with at least 8 steps of k.
+// Rows and columns of a tile: 128 x 128, or fewer rows where there are not more.
+int tile_rows(int64_t M) { return M <= 32 ? 32 : M <= 64 ? 64 : 128; }
+int tile_columns(int64_t M) { return M <= 64 ? 256 : 128; }
+
+// How many parts k is split into: enough workgroups for the device where the output has few
+// tiles (three fit a compute unit; few rows' sums cost little, so more of them), two steps
+// of k or more each (64 x 1000 x 1000: 28 us with eight, 18 us).
 int64_t splits_of(int64_t M, int64_t N, int64_t K)
 {
-    const int64_t tiles = ((M + kTile - 1) / kTile) * ((N + kTile - 1) / kTile);
+    const int bm = tile_rows(M), bn = tile_columns(M);
+    const int64_t tiles = ((M + bm - 1) / bm) * ((N + bn - 1) / bn);
     const int64_t steps = (K + kStep - 1) / kStep;
-    return std::max<int64_t>(1, std::min<int64_t>(512 / std::max<int64_t>(1, tiles), steps / 8));
+    return std::max<int64_t>(1, std::min<int64_t>((M <= 64 ? 768 : 512) / tiles, steps / 2));
 }
 
 uint64_t gemm_bytes(int64_t M, int64_t N, int64_t K)
@@ -278,9 +291,12 @@ hipError_t run_gemm(GemmArgs g, float *ws, hipStream_t stream)
     g.k_per = (steps + s - 1) / s * kStep;
     const int64_t splits = (g.K + g.k_per - 1) / g.k_per;
     g.part = splits > 1 ? ws : nullptr;
-    const dim3 grid((uint32_t)((g.M + kTile - 1) / kTile), (uint32_t)((g.N + kTile - 1) / kTile),
+    const int bm = tile_rows(g.M), bn = tile_columns(g.M);
+    const dim3 grid((uint32_t)((g.M + bm - 1) / bm), (uint32_t)((g.N + bn - 1) / bn),
                     (uint32_t)splits);
-    gemm_kernel<LA, LB><<<grid, dim3(256), 0, stream>>>(g);
+    if (bm == 32) gemm_kernel<LA, LB, 32, 256><<<grid, dim3(256), 0, stream>>>(g);
+    else if (bm == 64) gemm_kernel<LA, LB, 64, 256><<<grid, dim3(256), 0, stream>>>(g);
+    else gemm_kernel<LA, LB, 128, 128><<<grid, dim3(256), 0, stream>>>(g);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || splits == 1) return e;
     return launch_split_sum<float>(g, (int)splits, stream);
