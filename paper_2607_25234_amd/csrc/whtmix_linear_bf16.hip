@@ -7,16 +7,25 @@ namespace {
 
 // Rows of `inner` elements, ld apart, to rows of `width` (a multiple of 8) with zeros
 // past `inner`; eight elements a thread.
-__global__ void __launch_bounds__(256) pack_kernel(const __bf16 *src, __bf16 *dst, int64_t outer,
-                                                   int64_t inner, int64_t ld, int64_t width)
+struct PackJob {
+    const __bf16 *src;
+    __bf16 *dst;
+    int64_t outer, inner, ld, width;
+    uint32_t blocks;
+};
+
+// Both operands in one launch: the first `a.blocks` workgroups take a, the others b.
+__global__ void __launch_bounds__(256) pack_kernel(PackJob a, PackJob b)
 {
-    const int64_t per = width / 8, total = outer * per;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total;
-         i += (int64_t)gridDim.x * 256) {
+    const bool first = blockIdx.x < a.blocks;
+    const PackJob &j = first ? a : b;
+    const int64_t per = j.width / 8, total = j.outer * per;
+    for (int64_t i = (int64_t)(first ? blockIdx.x : blockIdx.x - a.blocks) * 256 + threadIdx.x;
+         i < total; i += (int64_t)j.blocks * 256) {
         const int64_t r = i / per, c = (i - r * per) * 8;
         float v[8];
-        Chunk<__bf16>::load(src + r * ld + c, (int)min((int64_t)8, inner - c), v);
-        Chunk<__bf16>::store(dst + r * width + c, 8, v);
+        Chunk<__bf16>::load(j.src + r * j.ld + c, (int)min((int64_t)8, j.inner - c), v);
+        Chunk<__bf16>::store(j.dst + r * j.width + c, 8, v);
     }
 }
 
@@ -41,23 +50,23 @@ Side side(const void *p, Layout l, int64_t rows, int64_t k, int64_t ld)
     return s;
 }
 
-hipError_t place(const void *&p, int64_t &ld, int64_t &rows, int64_t &k, Layout l, const Side &s,
-                 char *&ws, hipStream_t stream)
+// Where the tile kernel finds an operand, and the packing that puts it there.
+PackJob place(const void *&p, int64_t &ld, int64_t &rows, int64_t &k, Layout l, const Side &s,
+              char *&ws)
 {
-    hipError_t e = hipSuccess;
+    PackJob j{};
     int64_t width = s.inner;
     if (s.pack) {
         const int64_t blocks = (s.outer * (s.width / 8) + 255) / 256;
-        pack_kernel<<<dim3((uint32_t)(blocks < 65536 ? blocks : 65536)), dim3(256), 0, stream>>>(
-            (const __bf16 *)p, (__bf16 *)ws, s.outer, s.inner, ld, s.width);
-        e = hipGetLastError();
+        j = {(const __bf16 *)p, (__bf16 *)ws, s.outer, s.inner, ld, s.width,
+             (uint32_t)(blocks < 65536 ? blocks : 65536)};
         p = ws;
         ws += s.bytes();
         ld = width = s.width;
     }
     rows = l == K_CONTIGUOUS ? s.outer : width;
     k = l == K_CONTIGUOUS ? width : s.outer;
-    return e;
+    return j;
 }
 
 }  // namespace
@@ -71,10 +80,13 @@ uint64_t gemm_bf16_bytes(const GemmArgs &g, Layout la, Layout lb)
 hipError_t gemm_bf16(GemmArgs g, Layout la, Layout lb, void *ws, hipStream_t stream)
 {
     char *w = (char *)ws;
-    hipError_t e = place(g.a, g.lda, g.a_rows, g.a_k, la, side(g.a, la, g.M, g.K, g.lda), w, stream);
-    if (e != hipSuccess) return e;
-    e = place(g.b, g.ldb, g.b_rows, g.b_k, lb, side(g.b, lb, g.N, g.K, g.ldb), w, stream);
-    if (e != hipSuccess) return e;
+    const PackJob a = place(g.a, g.lda, g.a_rows, g.a_k, la, side(g.a, la, g.M, g.K, g.lda), w);
+    const PackJob b = place(g.b, g.ldb, g.b_rows, g.b_k, lb, side(g.b, lb, g.N, g.K, g.ldb), w);
+    if (a.blocks + b.blocks) {
+        pack_kernel<<<dim3(a.blocks + b.blocks), dim3(256), 0, stream>>>(a, b);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
     if (la == K_CONTIGUOUS && lb == K_STRIDED)
         return run_tiles<2, false, __bf16, K_CONTIGUOUS, K_STRIDED>(g, (float *)w, stream);
     if (la == K_CONTIGUOUS)

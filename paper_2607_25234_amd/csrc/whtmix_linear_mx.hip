@@ -12,20 +12,30 @@ namespace whtmix {
 
 constexpr int64_t kExactK = 512;
 
-// Rows of scales to whole dwords, 1 past the end: the tile kernel copies dwords.
-__global__ void __launch_bounds__(256) pack_scales_kernel(const uint8_t *src, uint32_t *dst,
-                                                          int64_t rows, int width)
+// Rows of scales to whole dwords, 1 past the end: the tile kernel copies dwords.  Both
+// operands' in one launch.
+struct ScalesJob {
+    const uint8_t *src;
+    uint32_t *dst;
+    int64_t rows;
+    int width;
+    uint32_t blocks;
+};
+
+__global__ void __launch_bounds__(256) pack_scales_kernel(ScalesJob a, ScalesJob b)
 {
-    const int dwords = (width + 3) / 4;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * dwords;
-         i += (int64_t)gridDim.x * 256) {
+    const bool first = blockIdx.x < a.blocks;
+    const ScalesJob &j = first ? a : b;
+    const int dwords = (j.width + 3) / 4;
+    for (int64_t i = (int64_t)(first ? blockIdx.x : blockIdx.x - a.blocks) * 256 + threadIdx.x;
+         i < j.rows * dwords; i += (int64_t)j.blocks * 256) {
         const int64_t row = i / dwords;
         const int at = (int)(i - row * dwords) * 4;
         uint32_t v = 0;
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-            v |= (at + j < width ? (uint32_t)src[row * width + at + j] : 127u) << (8 * j);
-        dst[i] = v;
+        for (int k = 0; k < 4; ++k)
+            v |= (at + k < j.width ? (uint32_t)j.src[row * j.width + at + k] : 127u) << (8 * k);
+        j.dst[i] = v;
     }
 }
 
@@ -39,19 +49,19 @@ static uint64_t packed_bytes(const uint8_t *p, int64_t rows, int64_t width)
     return whole_dwords(p, width) ? 0 : (uint64_t)(rows * ((width + 3) / 4 * 4) + 255) / 256 * 256;
 }
 
-static hipError_t place_scales(const uint8_t *&p, int64_t &ld, int64_t rows, int64_t width,
-                               char *&ws, hipStream_t s)
+static ScalesJob place_scales(const uint8_t *&p, int64_t &ld, int64_t rows, int64_t width,
+                              char *&ws)
 {
     ld = width;
     const uint64_t bytes = packed_bytes(p, rows, width);
-    if (!bytes) return hipSuccess;
+    if (!bytes) return ScalesJob{};
     const int64_t n = rows * ((width + 3) / 4), blocks = (n + 255) / 256;
-    pack_scales_kernel<<<dim3((uint32_t)(blocks < 65536 ? blocks : 65536)), dim3(256), 0, s>>>(
-        p, (uint32_t *)ws, rows, (int)width);
+    const ScalesJob j{p, (uint32_t *)ws, rows, (int)width,
+                      (uint32_t)(blocks < 65536 ? blocks : 65536)};
     p = (const uint8_t *)ws;
     ws += bytes;
     ld = (width + 3) / 4 * 4;
-    return hipGetLastError();
+    return j;
 }
 
 uint64_t gemm_mx_bytes(const GemmArgs &g)
@@ -69,9 +79,13 @@ hipError_t gemm_mx(GemmArgs g, int dtype, void *ws, hipStream_t stream)
 {
     g.a_rows = g.M, g.b_rows = g.N, g.a_k = g.b_k = g.K;
     char *w = (char *)ws;
-    hipError_t e = place_scales(g.as, g.as_ld, g.M, g.K / kMxBlock, w, stream);
-    if (e == hipSuccess) e = place_scales(g.bs, g.bs_ld, g.N, g.K / kMxBlock, w, stream);
-    if (e != hipSuccess) return e;
+    const ScalesJob a = place_scales(g.as, g.as_ld, g.M, g.K / kMxBlock, w);
+    const ScalesJob b = place_scales(g.bs, g.bs_ld, g.N, g.K / kMxBlock, w);
+    if (a.blocks + b.blocks) {
+        pack_scales_kernel<<<dim3(a.blocks + b.blocks), dim3(256), 0, stream>>>(a, b);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
     ws = w;
     const bool exact = g.K <= kExactK || (g.y && dtype == DTYPE_F32);
     if (dtype == DTYPE_BF16)
