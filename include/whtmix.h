@@ -434,7 +434,7 @@ WHTMIX_API int whtmix_norm_mx_forward(const void *x, const void *residual,
  *   dx        [rows][C] of `dtype`: the gradient of x and of the residual;
  *             may be dy or dh.
  *   dweight   [C] float32, or NULL to skip.
- * dweight is summed in a fixed order.  Workspace: up to 1024 rows of C floats.
+ * dweight is summed in a fixed order.  Workspace: up to 2048 rows of C floats.
  */
 WHTMIX_API int whtmix_norm_backward(const void *h, const float *weight,
                          const void *dy, const void *dh, void *dx,

@@ -392,7 +392,9 @@ __global__ void __launch_bounds__(256) norm_backward_columns(NormBackwardKernelA
 // Chunks of a row that stay in the backward kernel's registers, at most (a lane of 1024
 // threads has 128 of them).
 constexpr int64_t wide_chunks(int per) { return per == 8 ? 2048 : 4096; }
-constexpr int64_t kBackwardBlocks = 768;   // workgroups, and so partial sums of dw, at most
+// Workgroups of the backward pass, and so rows of partial sums of dw: enough to hide the loads,
+// and for wide rows no more than 2^20 partial sums (a hundredth of what the pass moves).
+int64_t backward_blocks(int64_t C) { return std::max<int64_t>(768, std::min<int64_t>(2048, (1 << 20) / C)); }
 
 int64_t lanes_of(int64_t n)                // of the backward kernel for rows of n chunks
 {
@@ -406,7 +408,7 @@ int64_t backward_parts(int64_t rows, int64_t C, int dtype)
     if (n > wide_chunks(per)) return rows < 64 ? rows : 64;
     const int64_t g = lanes_of(n), in_block = g > 256 ? 1 : 256 / g;
     const int64_t blocks = (rows + in_block - 1) / in_block;
-    return blocks < kBackwardBlocks ? blocks : kBackwardBlocks;
+    return std::min(blocks, backward_blocks(C));
 }
 
 template <typename T, int G, int R>
