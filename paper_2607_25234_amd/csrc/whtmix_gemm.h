@@ -319,6 +319,11 @@ uint64_t gemm_bf16_bytes(const GemmArgs &g, Layout la, Layout lb);
 hipError_t gemm_bf16(GemmArgs g, Layout la, Layout lb, void *ws, hipStream_t stream);
 uint64_t gemm_f32_bytes(const GemmArgs &g);
 hipError_t gemm_f32(const GemmArgs &g, Layout la, Layout lb, void *ws, hipStream_t stream);
+// dz, its columns' partial sums (dzx_parts rows, or null) and dx in one kernel
+// (whtmix_linear_dzx.hip), for calls that it takes.
+bool dzx_takes(const LinearBackwardArgs &a);
+int64_t dzx_parts(int64_t M);
+hipError_t launch_dzx(const LinearBackwardArgs &a, void *dz, float *part);
 uint64_t gemm_mx_bytes(const GemmArgs &g);
 hipError_t gemm_mx(GemmArgs g, int dtype, void *ws, hipStream_t stream);
 

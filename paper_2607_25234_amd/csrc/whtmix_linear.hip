@@ -124,9 +124,11 @@ BackwardLayoutBytes backward_bytes(const LinearBackwardArgs &a)
     BackwardLayoutBytes l;
     const int e = a.dtype == DTYPE_BF16 ? 2 : 4;
     if (a.act != ACT_NONE) l.dz = align256((uint64_t)a.M * a.N * e);
-    if (a.dbias) l.part = align256((uint64_t)dz_parts(a.M, a.N) * a.N * 4);
+    if (a.dbias)
+        l.part = align256((uint64_t)(dzx_takes(a) ? dzx_parts(a.M) : dz_parts(a.M, a.N)) * a.N * 4);
     const void *dz = a.act != ACT_NONE ? nullptr : a.dy;    // a workspace's address is aligned
-    if (a.dx) l.product = product_bytes(dx_args(a, dz), K_CONTIGUOUS, K_CONTIGUOUS, a.dtype);
+    if (a.dx && !dzx_takes(a))
+        l.product = product_bytes(dx_args(a, dz), K_CONTIGUOUS, K_CONTIGUOUS, a.dtype);
     if (a.dw)
         l.product = std::max(l.product, product_bytes(dw_args(a, dz), K_STRIDED, K_STRIDED, a.dtype));
     return l;
@@ -140,7 +142,13 @@ template <typename T> hipError_t linear_backward(const LinearBackwardArgs &a)
     float *part = (float *)(ws + l.dz);
     void *rest = ws + l.dz + l.part;
     hipError_t e;
-    if (a.act != ACT_NONE || a.dbias) {
+    const bool together = dzx_takes(a);
+    if (together) {
+        if ((e = launch_dzx(a, dz, a.dbias ? part : nullptr)) != hipSuccess) return e;
+        if (a.dbias && (e = launch_column_sum(part, dzx_parts(a.M), a.N, a.dbias, a.stream)) !=
+                           hipSuccess)
+            return e;
+    } else if (a.act != ACT_NONE || a.dbias) {
         const int64_t parts = dz_parts(a.M, a.N);
         const int64_t per = (a.M + parts - 1) / parts;
         const dim3 grid((uint32_t)((a.N + kDzCols - 1) / kDzCols),
@@ -153,8 +161,8 @@ template <typename T> hipError_t linear_backward(const LinearBackwardArgs &a)
             return e;
     }
     const void *d = a.act != ACT_NONE ? (const void *)dz : a.dy;
-    if (a.dx && (e = product<T>(dx_args(a, d), K_CONTIGUOUS, K_CONTIGUOUS, rest, a.stream)) !=
-                    hipSuccess)
+    if (a.dx && !together &&
+        (e = product<T>(dx_args(a, d), K_CONTIGUOUS, K_CONTIGUOUS, rest, a.stream)) != hipSuccess)
         return e;
     if (a.dw) return product<T>(dw_args(a, d), K_STRIDED, K_STRIDED, rest, a.stream);
     return hipSuccess;

@@ -120,3 +120,32 @@ def test_large_float32_operands_that_do_not_split():
     rows = [r for r in range(M) if not (0 <= r < 256 or 512 <= r < 768 or r >= 1792)]
     cols = [c for c in range(N) if not (1280 <= c < 1536 or 1792 <= c < 2048)]
     assert torch.equal(got[rows][:, cols], plain.cpu()[rows][:, cols])
+
+
+@pytest.mark.parametrize("M,K,N,act", [(32768, 128, 64, "gelu"), (33001, 100, 200, "silu"),
+                                       (32800, 1, 72, "relu"), (40000, 128, 520, "gelu_tanh"),
+                                       (36000, 127, 136, "gelu")])
+def test_narrow_backward(M, K, N, act):
+    """Many rows of narrow bf16 inputs: dz, its sums and dx in one pass."""
+    from paper_2607_25234_amd import whtmix
+    dev = device()
+    say("narrow_backward", M, K, N, act)
+    dt = torch.bfloat16
+    x, w = draw(1, M, K, dtype=dt), draw(2, K, N, std=K ** -0.5, dtype=dt)
+    dy, z = draw(3, M, N, dtype=dt), draw(4, M, N, std=2.0, dtype=dt)
+    args = x.to(dev), w.to(dev), dy.to(dev), z.to(dev), act
+    dx, dw, db = whtmix.linear_backward(*args)
+    X, W, D = x.double(), w.double(), dy.double()
+    d = D * ref.act_grad(act, z.double())
+    own = D.abs() * ref.grad_bound(act, z.double())
+    rnd = own + d.abs() * 2.0 ** -7.99
+    rx, rw = d @ W.t(), X.t() @ d
+    ref.check("dx", dx, rx, ref.sum_bound(N, d.abs() @ W.abs().t()) + rnd @ W.abs().t()
+              + ref.rounded(rx, True))
+    ref.check("dw", dw, rw, ref.sum_bound(M, X.abs().t() @ d.abs()) + X.abs().t() @ rnd
+              + ref.rounded(rw, True))
+    ref.check("db", db, d.sum(0), ref.sum_bound(M, d.abs().sum(0)) + own.sum(0) + 1e-30)
+    again = whtmix.linear_backward(*args)
+    assert all(torch.equal(a, b) for a, b in zip(again, (dx, dw, db)))
+    only, none, nodb = whtmix.linear_backward(*args, want_dw=False, want_dbias=False)
+    assert torch.equal(only, dx) and none is None and nodb is None
