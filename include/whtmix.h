@@ -465,7 +465,8 @@ WHTMIX_API int whtmix_dequantize_mx(const void *q, const uint8_t *scales, void *
  * of three-term splits (what they leave out is below 2^-24 |x| |w|), or float32
  * ones where a tile's operands do not split (from 2^128 - 2^119, Inf, NaN, or
  * below 2^-95 throughout).  Workspace: partial sums where k is split over
- * workgroups.
+ * workgroups; large float32 operands' terms (six bytes an element); bf16
+ * operands whose rows do not start at 16 bytes, packed.
  */
 WHTMIX_API int whtmix_linear_forward(const void *x, const void *w,
                           const float *bias, const void *residual, void *y,
@@ -483,7 +484,8 @@ WHTMIX_API int whtmix_linear_forward(const void *x, const void *w,
  *   dbias     [N] float32, or NULL to skip.
  * The residual's gradient is dy itself.  dz enters the products rounded to
  * `dtype` (bf16: what the matrix cores read) and dbias unrounded.  Sums over
- * rows are made in a fixed order.  Workspace: dz, and partial sums.
+ * rows are made in a fixed order.  Workspace: dz, partial sums, and what the
+ * forward product takes.
  */
 WHTMIX_API int whtmix_linear_backward(const void *x, const void *w,
                            const void *dy, const void *z, void *dx, void *dw,
@@ -498,7 +500,10 @@ WHTMIX_API int whtmix_linear_backward(const void *x, const void *w,
  *   bias, residual  as whtmix_linear_forward, the residual of `dtype`.
  *   y         [M][N] of `dtype` (may be the residual), or NULL with
  *   yq, ys    the output in block-scaled 8 bits, [M] rows of N values.
- * Either y or both yq and ys.
+ * Either y or both yq and ys.  Products of K > 512 with a bfloat16 or 8-bit
+ * output run on the scaled matrix instructions, which keep about 15 bits below
+ * the largest of 64 products before they add to a float32 sum (2e-6 of the sum
+ * of magnitudes, root mean square); the others' sums are float32 throughout.
  */
 WHTMIX_API int whtmix_linear_mx_forward(const void *xq, const uint8_t *xs,
                              const void *wq, const uint8_t *ws,

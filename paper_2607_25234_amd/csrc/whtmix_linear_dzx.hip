@@ -5,6 +5,7 @@
 // Here a workgroup takes 128 rows through all N in steps of 64: it forms dz in registers, writes
 // it to memory for dw's product and to LDS for its own, and multiplies with w's step, which copies
 // bring to LDS meanwhile.  The next step's dy and z are on their way during the products.
+// Together 197-232 us: 872 MB at 3.8-4.4 TB/s, about what dz alone took.
 #include "whtmix_gemm_tile.h"
 
 namespace whtmix {
@@ -148,12 +149,13 @@ __global__ void __launch_bounds__(256) dzx_kernel(DzxArgs d, GemmArgs g)
 
 int64_t dzx_parts(int64_t M) { return (M + kRows - 1) / kRows; }
 
-// Narrow inputs, whole 16-byte chunks, and rows enough for the device.
+// Narrow inputs, whole 16-byte chunks (32-bit offsets of w's), and rows enough for the device.
 bool dzx_takes(const LinearBackwardArgs &a)
 {
     auto aligned = [](const void *p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; };
     return a.dtype == DTYPE_BF16 && a.act != ACT_NONE && a.dx && a.K <= kCols && a.N % 8 == 0 &&
-           a.N >= kN && a.M >= 256 * kRows && aligned(a.dy) && aligned(a.z) && aligned(a.w);
+           a.N >= kN && a.N <= (int64_t(1) << 22) && a.M >= 256 * kRows && aligned(a.dy) &&
+           aligned(a.z) && aligned(a.w);
 }
 
 hipError_t launch_dzx(const LinearBackwardArgs &a, void *dz, float *part)

@@ -180,6 +180,8 @@ __device__ __forceinline__ void float32_tile(const GemmArgs &g, Stage<LA, BM> &s
 
 // BM x BN sums by four waves of 64 columns.  The next step's loads are in flight during the
 // products of this one; two or three workgroups fill in for each other at the barriers.
+// Bound by the splits' vector instructions: 131072 x 64 x 256 with gelu 57-66 us (168 MB at
+// 2.5-2.9 TB/s, two steps a tile), 3001 x 1000 x 2003's gradients 105 us each, 115 TFLOP/s.
 template <Layout LA, Layout LB, int BM, int BN>
 __global__ void __launch_bounds__(256) gemm_kernel(GemmArgs g)
 {
@@ -405,6 +407,9 @@ __device__ __forceinline__ void float32_wave(const GemmArgs &g, Layout la, Layou
 }
 
 // Three buffers: a step's copies (16 k of three terms of both operands) have two steps to land.
+// 16384 x 4096 x 4096 2500 us, 219 TFLOP/s of float32 or 1.3 PFLOP/s of bf16 products; 3001 x 1000
+// x 2003 85 us, 141: 384 tiles of 128 x 128 leave the second of two places on half of the units
+// empty.
 template <int BM, int BN, int WAVES_M, int WAVES_N>
 __global__ void __launch_bounds__(64 * WAVES_M *WAVES_N)
     gemm_split_kernel(GemmArgs g, SplitOperand a, SplitOperand b, uint32_t tiles_m, uint32_t tiles_n)
