@@ -36,6 +36,22 @@ template <int G> __device__ __forceinline__ float row_sum(float v, float *part)
     return v;
 }
 
+// Two sums over a row's lanes at once; `part` is another one (2 * G / 64 floats) than in
+// the call before, whose reads may still be under way.
+template <int G> __device__ __forceinline__ void row_sums(float &u, float &v, float *part)
+{
+#pragma unroll
+    for (int d = 1; d < (G < 64 ? G : 64); d <<= 1) u += __shfl_xor(u, d), v += __shfl_xor(v, d);
+    if constexpr (G > 64) {
+        if ((threadIdx.x & 63) == 0)
+            part[threadIdx.x >> 6] = u, part[G / 64 + (threadIdx.x >> 6)] = v;
+        __syncthreads();
+        u = v = 0.f;
+#pragma unroll
+        for (int i = 0; i < G / 64; ++i) u += part[i], v += part[G / 64 + i];
+    }
+}
+
 struct NormKernelArgs {
     const void *x, *residual;
     const float *weight;
@@ -243,16 +259,25 @@ struct NormBackwardKernelArgs {
     float eps;
 };
 
+// Waves a SIMD that the registers of `values` values a lane leave room for (h, dy, the sums
+// of dw, and what is computed from them).
+constexpr int backward_waves(int lanes, int values)
+{
+    return values <= 8 ? (lanes > 64 ? 5 : 6) : values <= 16 ? 4 : 2;
+}
+
 // Rows go round the grid; a lane keeps its columns' sums of dy n.  The groups
 // of a workgroup add theirs in order through LDS.  One pass: h and dy stay in registers
-// between a row's two sums and its dx.  Bound by memory: 262144 x 128 bf16 with dh and dw
-// 62-68 us (268 MB at 4.0-4.3 TB/s), float32 3001 x 2003 20 us out of the caches.
+// between a row's two sums (which go over the lanes together) and its dx.  Bound by memory:
+// 262144 x 128 bf16 48 us, 65536 x 2048 186 us (805 MB at 4.3 TB/s; 360 us with 64 lanes of four
+// chunks a row, two waves a SIMD), 16384 x 4096 107 us, float32 32768 x 1000 87 us.
 template <typename T, int G, int R>
-__global__ void __launch_bounds__(G > 256 ? G : 256) norm_backward_kernel(NormBackwardKernelArgs a)
+__global__ void __launch_bounds__(G > 256 ? G : 256, backward_waves(G, Chunk<T>::N *R))
+    norm_backward_kernel(NormBackwardKernelArgs a)
 {
     constexpr int N = Chunk<T>::N;
     constexpr int kRows = G > 256 ? 1 : 256 / G;
-    __shared__ float part[16];
+    __shared__ float parts[2][32];
     __shared__ float sums[kRows > 1 ? 256 * R * N : 1];
     const int lane = threadIdx.x % G, grp = threadIdx.x / G;
     float dw[R][N];
@@ -261,8 +286,9 @@ __global__ void __launch_bounds__(G > 256 ? G : 256) norm_backward_kernel(NormBa
 #pragma unroll
         for (int i = 0; i < N; ++i) dw[j][i] = 0.f;
 
+    int turn = 0;
     for (int64_t base = (int64_t)blockIdx.x * kRows; base < a.rows;
-         base += (int64_t)gridDim.x * kRows) {
+         base += (int64_t)gridDim.x * kRows, turn ^= 1) {
         const int64_t row = base + grp;
         const bool live = row < a.rows;
         const int64_t at = live ? row * a.C : 0;
@@ -289,8 +315,9 @@ __global__ void __launch_bounds__(G > 256 ? G : 256) norm_backward_kernel(NormBa
                 p = fmaf(h[j][i], dy[j][i] * w[i], p);
             }
         }
-        const float rstd = rsqrtf(row_sum<G>(s, part) / (float)a.C + a.eps);
-        const float k = row_sum<G>(p, part) * rstd * rstd / (float)a.C;   // mean(g n) * rstd
+        row_sums<G>(s, p, parts[turn]);
+        const float rstd = rsqrtf(s / (float)a.C + a.eps);
+        const float k = p * rstd * rstd / (float)a.C;   // mean(g n) * rstd
 #pragma unroll
         for (int j = 0; j < R; ++j) {
             const int64_t c = ((int64_t)j * G + lane) * N;
@@ -402,13 +429,18 @@ __global__ void __launch_bounds__(256) norm_backward_columns(NormBackwardKernelA
 // Chunks of a row that stay in the backward kernel's registers, at most (a lane of 1024
 // threads has 128 of them).
 constexpr int64_t wide_chunks(int per) { return per == 8 ? 2048 : 4096; }
-// Workgroups of the backward pass, and so rows of partial sums of dw: enough to hide the loads,
-// and for wide rows no more than 2^20 partial sums (a hundredth of what the pass moves).
-int64_t backward_blocks(int64_t C) { return std::max<int64_t>(768, std::min<int64_t>(2048, (1 << 20) / C)); }
-
-int64_t lanes_of(int64_t n)                // of the backward kernel for rows of n chunks
+// Lanes and chunks a lane of the backward kernel for rows of n chunks.
+struct BackwardShape {
+    int lanes, chunks;
+    int threads() const { return lanes > 256 ? lanes : 256; }
+};
+BackwardShape backward_shape(int64_t n)
 {
-    return n <= 8 ? 8 : n <= 16 ? 16 : n <= 32 ? 32 : n <= 256 ? 64 : n <= 1024 ? 256 : 1024;
+    if (n <= 64) return {n <= 8 ? 8 : n <= 16 ? 16 : n <= 32 ? 32 : 64, 1};
+    if (n <= 128) return {64, 2};
+    if (n <= 256) return {256, 1};
+    if (n <= 1024) return {256, n <= 512 ? 2 : 4};
+    return {1024, n <= 2048 ? 2 : 4};
 }
 
 int64_t backward_parts(int64_t rows, int64_t C, int dtype)
@@ -416,9 +448,13 @@ int64_t backward_parts(int64_t rows, int64_t C, int dtype)
     const int per = dtype == DTYPE_BF16 ? 8 : 4;
     const int64_t n = (C + per - 1) / per;
     if (n > wide_chunks(per)) return rows < 64 ? rows : 64;
-    const int64_t g = lanes_of(n), in_block = g > 256 ? 1 : 256 / g;
-    const int64_t blocks = (rows + in_block - 1) / in_block;
-    return std::min(blocks, backward_blocks(C));
+    // As many workgroups as the 256 compute units hold at a time, each of the same count of
+    // rows: with half as many again the last ones ran alone (262144 x 128 bf16: 61 us with 2048,
+    // 48 us with 1536).
+    const BackwardShape s = backward_shape(n);
+    const int64_t in_block = s.threads() / s.lanes, blocks = (rows + in_block - 1) / in_block;
+    return std::min<int64_t>(
+        blocks, 256 * (backward_waves(s.lanes, per * s.chunks) * 4 / (s.threads() / 64)));
 }
 
 template <typename T, int G, int R>
@@ -452,7 +488,7 @@ template <typename T> hipError_t pick_backward(const NormBackwardArgs &a)
     else if (n <= 32) e = run_backward<T, 32, 1>(a, b);
     else if (n <= 64) e = run_backward<T, 64, 1>(a, b);
     else if (n <= 128) e = run_backward<T, 64, 2>(a, b);
-    else if (n <= 256) e = run_backward<T, 64, 4>(a, b);
+    else if (n <= 256) e = run_backward<T, 256, 1>(a, b);
     else if (n <= 512) e = run_backward<T, 256, 2>(a, b);
     else if (n <= 1024) e = run_backward<T, 256, 4>(a, b);
     else if (n <= 2048) e = run_backward<T, 1024, 2>(a, b);
