@@ -387,8 +387,11 @@ inline TilePlan plan_tiles(int64_t M, int64_t N, int64_t K, int step_k)
 {
     TilePlan p{};
     auto tiles = [&](int bm, int bn) __attribute__((always_inline)) { return ((M + bm - 1) / bm) * ((N + bn - 1) / bn); };
+    // Few rows: the sums of rows that are not there would cost what the bytes of b leave (17 x
+    // 4096 x 16384 bf16 26 us, 32 us in tiles of 128 x 128).  Past 32 rows with few columns
+    // the parts' sums do (64 x 4096 x 16384 32 and 36 us, 64 x 4096 x 4096 18 and 16 us).
     if (M <= 32) p.bm = 32, p.bn = 256;
-    else if (M <= 64) p.bm = 64, p.bn = 256;
+    else if (M <= 64 && tiles(64, 256) >= 64) p.bm = 64, p.bn = 256;
     // 256 x 256 where most of the device has a tile and padding costs less than a quarter
     // (262144 x 128 x 512 and its dx of 128 columns: 115 and 114 us in these tiles,
     // 139 and 77 us in tiles of 128 x 128; 8192 x 2048 x 8192: 229 and 280 us).
@@ -398,8 +401,11 @@ inline TilePlan plan_tiles(int64_t M, int64_t N, int64_t K, int step_k)
     p.tiles_m = (uint32_t)((M + p.bm - 1) / p.bm);
     p.tiles_n = (uint32_t)((N + p.bn - 1) / p.bn);
     const int64_t t = (int64_t)p.tiles_m * p.tiles_n, steps = (K + step_k - 1) / step_k;
-    // Fewer tiles than two a compute unit: k is split, four steps or more a part.
-    int64_t s = t >= 256 ? 1 : 512 / t;
+    // Fewer tiles than compute units: k is split, four steps or more a part, over one workgroup
+    // a unit (512 x 4096 x 1024: 22 us, 28 us with two, whose partial sums cost more than they
+    // hide), or two where their parts stay long (128 x 262144 x 512: 76 us, 84 us with one).
+    int64_t s = t >= 256 ? 1 : 256 / t;
+    if (t < 256 && p.bm < 256 && steps / (2 * s) >= 32) s *= 2;
     s = s < steps / 4 ? s : steps / 4;
     if (s < 1) s = 1;
     p.k_per = (steps + s - 1) / s * step_k;
