@@ -434,7 +434,7 @@ WHTMIX_API int whtmix_norm_mx_forward(const void *x, const void *residual,
  *   dx        [rows][C] of `dtype`: the gradient of x and of the residual;
  *             may be dy or dh.
  *   dweight   [C] float32, or NULL to skip.
- * dweight is summed in a fixed order.  Workspace: up to 2048 rows of C floats.
+ * dweight is summed in a fixed order.  Workspace: up to 1536 rows of C floats.
  */
 WHTMIX_API int whtmix_norm_backward(const void *h, const float *weight,
                          const void *dy, const void *dh, void *dx,
@@ -500,7 +500,7 @@ WHTMIX_API int whtmix_linear_backward(const void *x, const void *w,
  *   bias, residual  as whtmix_linear_forward, the residual of `dtype`.
  *   y         [M][N] of `dtype` (may be the residual), or NULL with
  *   yq, ys    the output in block-scaled 8 bits, [M] rows of N values.
- * Either y or both yq and ys.  Products of K > 512 with a bfloat16 or 8-bit
+ * Either y or both yq and ys.  Products of K > 128 with a bfloat16 or 8-bit
  * output run on the scaled matrix instructions, which keep about 15 bits below
  * the largest of 64 products before they add to a float32 sum (2e-6 of the sum
  * of magnitudes, root mean square); the others' sums are float32 throughout.
