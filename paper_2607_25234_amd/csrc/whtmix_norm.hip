@@ -19,15 +19,16 @@ namespace {
 
 enum Mode { MODE_NORM = 0, MODE_NORM_MX = 1, MODE_QUANT = 2 };
 
-// Sum over the G lanes that hold a row; `part` is G / 64 floats of LDS for
-// rows wider than a wave.
+// Sum over the G lanes that hold a row; `part` is a float of LDS for each wave of the
+// workgroup, for rows wider than a wave.
 template <int G> __device__ __forceinline__ float row_sum(float v, float *part)
 {
 #pragma unroll
     for (int d = 1; d < (G < 64 ? G : 64); d <<= 1) v += __shfl_xor(v, d);
     if constexpr (G > 64) {
+        part += threadIdx.x / G * (G / 64);
         __syncthreads();   // the reads of the sum before
-        if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
+        if ((threadIdx.x & 63) == 0) part[threadIdx.x % G >> 6] = v;
         __syncthreads();
         v = 0.f;
 #pragma unroll
@@ -40,6 +41,7 @@ template <int G> __device__ __forceinline__ float row_sum(float v, float *part)
 // the call before, whose reads may still be under way.
 template <int G> __device__ __forceinline__ void row_sums(float &u, float &v, float *part)
 {
+    static_assert(G <= 64 || G >= 256, "a workgroup's waves hold one row");
 #pragma unroll
     for (int d = 1; d < (G < 64 ? G : 64); d <<= 1) u += __shfl_xor(u, d), v += __shfl_xor(v, d);
     if constexpr (G > 64) {
@@ -88,11 +90,10 @@ __device__ __forceinline__ void store_mx(const float (&v)[Chunk<T>::N], uint8_t 
 constexpr int64_t kMaxBlocks = int64_t(1) << 21;
 
 // One row on G lanes.  R chunks a lane stay in registers; with R = 0 (rows
-// wider than that) the row is read twice.  Bound by memory: G is the least that
-// holds the row with two chunks a lane or fewer, so that a wave's loads are whole cache
-// lines and narrow rows share a workgroup.  Measured (x, residual, y and h of bf16):
-// 262144 x 128 45 us, 268 MB at 6.0 TB/s; 8192 x 4096 with MX output 56 us, 237 MB at
-// 4.2 TB/s; float32 32768 x 128 13 us (67 MB, the caches' rate); one row of 4096 3.5 us,
+// wider than that) the row is read twice.  Bound by memory, and narrow rows share a workgroup.
+// Measured (x, residual, y and h): 262144 x 128 bf16 45 us, 268 MB at 6.0 TB/s; 16384 x 4096 99 us,
+// 537 MB at 5.4 TB/s; 8192 x 4096 with 8-bit output 52 us, 237 MB at 4.6 TB/s; float32 32768 x 128
+// 13 us (67 MB, the caches' rate); one row of 4096 3.5 us,
 // the latency of its loads and of one sum.
 template <typename T, int G, int R, int MODE>
 __global__ void __launch_bounds__(G > 256 ? G : 256) norm_kernel(NormKernelArgs a)
@@ -192,7 +193,10 @@ hipError_t run_norm(const NormArgs &a)
     return hipGetLastError();
 }
 
-// Chunks of a row -> lanes and chunks a lane.
+// Chunks of a row -> lanes and chunks a lane: one chunk a lane up to 512 lanes.  With two or
+// more on fewer lanes: 65536 x 512 float32 114 and 95 us (64 x 2, 128 x 1), 16384 x 4096 bf16 102
+// and 99, 3001 x 1111 float32 14 and 11 (256 x 2, 512 x 1), 8192 x 8192 bf16 110 and 103 us (256
+// x 4, 512 x 2); 8-bit output of 8192 x 8192 124 and 100 us (1024 x 1, 512 x 2).
 template <typename T, int MODE> hipError_t pick_norm(const NormArgs &a)
 {
     const int64_t width = MODE == MODE_NORM ? a.C : mx_width(a.C);
@@ -201,10 +205,10 @@ template <typename T, int MODE> hipError_t pick_norm(const NormArgs &a)
     if (n <= 16) return run_norm<T, 16, 1, MODE>(a);
     if (n <= 32) return run_norm<T, 32, 1, MODE>(a);
     if (n <= 64) return run_norm<T, 64, 1, MODE>(a);
-    if (n <= 128) return run_norm<T, 64, 2, MODE>(a);
+    if (n <= 128) return run_norm<T, 128, 1, MODE>(a);
     if (n <= 256) return run_norm<T, 256, 1, MODE>(a);
-    if (n <= 512) return run_norm<T, 256, 2, MODE>(a);
-    if (n <= 1024) return run_norm<T, 256, 4, MODE>(a);
+    if (n <= 512) return run_norm<T, 512, 1, MODE>(a);
+    if (n <= 1024) return run_norm<T, 512, 2, MODE>(a);
     if (n <= 2048) return run_norm<T, 1024, 2, MODE>(a);
     if (n <= 4096) return run_norm<T, 1024, 4, MODE>(a);
     return run_norm<T, 1024, 0, MODE>(a);
