@@ -150,6 +150,8 @@ __global__ void __launch_bounds__(256) dzx_kernel(DzxArgs d, GemmArgs g)
 int64_t dzx_parts(int64_t M) { return (M + kRows - 1) / kRows; }
 
 // Narrow inputs, whole 16-byte chunks (32-bit offsets of w's), and rows enough for the device.
+// Together and apart: 262144 x 128 x 512 199 and 238 us, 131072 x 64 x 64 27 and 50, 65536 x 64 x
+// 256 31 and 35, 32768 x 128 x 512 37 and 35, 4096 x 128 x 512 28 and 20.
 bool dzx_takes(const LinearBackwardArgs &a)
 {
     auto aligned = [](const void *p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; };

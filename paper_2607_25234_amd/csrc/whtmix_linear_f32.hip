@@ -264,19 +264,21 @@ __global__ void __launch_bounds__(256) gemm_kernel(GemmArgs g)
     finish_wave<float>(g, out, m0 + wm, n0 + wn, blockIdx.z, acc);
 }
 
-// Rows and columns of a tile: 128 x 128, or fewer rows where there are not more.
+// Rows and columns of a tile: 128 x 128, or fewer rows where there are not more (1 x 2048 x
+// 4096 14 us, 16 in tiles of 64 rows, 24 of 128; 64 x 2048 x 4096 26 us, 30 of 128).
 int tile_rows(int64_t M) { return M <= 32 ? 32 : M <= 64 ? 64 : 128; }
 int tile_columns(int64_t M) { return M <= 64 ? 256 : 128; }
 
-// How many parts k is split into: enough workgroups for the device where the output has few
-// tiles (three fit a compute unit; few rows' sums cost little, so more of them), two steps
-// of k or more each (64 x 1000 x 1000: 28 us with eight, 18 us).
+// How many parts k is split into: two workgroups a unit where the output has few tiles (three
+// fit), four steps of k or more each, or two where few rows make the sums cheap.  Fewer
+// parts: 154 x 1491 x 16384 77 and 99 us with one workgroup a unit.  Shorter ones: 512 x 2048 x 512
+// 22 and 25 us with two steps; 64 x 1000 x 1000 15 and 20 us with four.
 int64_t splits_of(int64_t M, int64_t N, int64_t K)
 {
     const int bm = tile_rows(M), bn = tile_columns(M);
     const int64_t tiles = ((M + bm - 1) / bm) * ((N + bn - 1) / bn);
     const int64_t steps = (K + kStep - 1) / kStep;
-    return std::max<int64_t>(1, std::min<int64_t>((M <= 64 ? 768 : 512) / tiles, steps / 2));
+    return std::max<int64_t>(1, std::min<int64_t>(512 / tiles, steps / (M <= 64 ? 2 : 4)));
 }
 
 uint64_t gemm_bytes(int64_t M, int64_t N, int64_t K)
