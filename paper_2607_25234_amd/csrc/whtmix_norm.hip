@@ -92,9 +92,9 @@ constexpr int64_t kMaxBlocks = int64_t(1) << 21;
 // One row on G lanes.  R chunks a lane stay in registers; with R = 0 (rows
 // wider than that) the row is read twice.  Bound by memory, and narrow rows share a workgroup.
 // Measured (x, residual, y and h): 262144 x 128 bf16 45 us, 268 MB at 6.0 TB/s; 16384 x 4096 99 us,
-// 537 MB at 5.4 TB/s; 8192 x 4096 with 8-bit output 52 us, 237 MB at 4.6 TB/s; float32 32768 x 128
-// 13 us (67 MB, the caches' rate); one row of 4096 3.5 us,
-// the latency of its loads and of one sum.
+// 537 MB at 5.4 TB/s; 8192 x 4096 with 8-bit output 50-54 us, 237 MB at 4.4-4.7 TB/s; float32 32768 x 128
+// 13 us (67 MB, the caches' rate); one row of 4096 2.6 us, the latency of its loads and of
+// one sum.
 template <typename T, int G, int R, int MODE>
 __global__ void __launch_bounds__(G > 256 ? G : 256) norm_kernel(NormKernelArgs a)
 {
