@@ -500,10 +500,13 @@ WHTMIX_API int whtmix_linear_backward(const void *x, const void *w,
  *   bias, residual  as whtmix_linear_forward, the residual of `dtype`.
  *   y         [M][N] of `dtype` (may be the residual), or NULL with
  *   yq, ys    the output in block-scaled 8 bits, [M] rows of N values.
- * Either y or both yq and ys.  Products of K > 128 with a bfloat16 or 8-bit
+ * Either y or both yq and ys.  Products of K > 512 with a bfloat16 or 8-bit
  * output run on the scaled matrix instructions, which keep about 15 bits below
- * the largest of 64 products before they add to a float32 sum (2e-6 of the sum
- * of magnitudes, root mean square); the others' sums are float32 throughout.
+ * the largest of 64 products before they add to a float32 sum: off by 1e-6 of
+ * the sum of magnitudes, root mean square, for normal values, by 1e-5 for
+ * values spread over 2^6.  The others' sums are float32 throughout; a caller
+ * that wants such sums of more k takes y in float32 and rounds it, or
+ * quantises it with whtmix_quantize_mx.
  */
 WHTMIX_API int whtmix_linear_mx_forward(const void *xq, const uint8_t *xs,
                              const void *wq, const uint8_t *ws,

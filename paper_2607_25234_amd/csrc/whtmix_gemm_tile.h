@@ -144,7 +144,8 @@ template <int R> __device__ __forceinline__ i32x8 fragment64(const char *lds, in
 }
 
 // A 32-row fragment of 16 k (step kk of 8) of block-scaled values as bf16, which holds each
-// value: 4 significant bits.  s: the row's scales of the step.
+// value: 4 significant bits, from scale byte 3 on (below, multiples of 2^-133).  s: the row's
+// scales of the step.
 template <int R>
 __device__ __forceinline__ bf16x8 fragment_exact(const char *lds, uint32_t s, int row0, int kk)
 {

@@ -1,17 +1,19 @@
 // Products of block-scaled 8-bit rows.
 //
 // The scaled matrix instructions (twice the rate of bf16) line the products of 64 k up
-// with the largest and drop what lies some 2^-15 below it: 2e-6 of the sum of magnitudes,
-// root mean square, measured on normal values.  A rounding to bf16 or 8 bits hides that but
-// where a sum cancels.  A float32 output, and sums of few k (whose float32 rounding
-// is smaller than that), are formed of bf16 products instead (bf16 holds each value), whose
-// sums keep float32's accuracy.  32768 x K x 2048, bf16 products first: K = 128 41 and 34
-// us, 256 54 and 39, 512 84 and 51; 8192 x 2048 x 2048 65 and 33 us.
+// with the largest and drop what lies some 2^-15 below it.  Measured error over the sum of
+// magnitudes, root mean square: 1e-6 at K = 256 and 7e-7 at 512 for normal values, 1e-5 for values
+// spread over 2^6, where float32 sums are off by 5e-9.  Of few k that is more than the float32
+// sum's own bound (up to 14 times it at K = 192 and 256), and no rounding to bf16 or 8 bits
+// hides it where a sum cancels.  So sums of up to 512 k, and float32 outputs of any K, are formed of
+// bf16 products instead (bf16 holds each value, to multiples of 2^-133), whose sums keep
+// float32's accuracy.  32768 x K x 2048, bf16 products first: K = 160 56 and 41 us, 256 54 and
+// 38, 512 84 and 53; 17 x 512 x 4096 8.9 and 8.5, 17 x 8192 x 4096 14.3 and 13.3 us.
 #include "whtmix_gemm_tile.h"
 
 namespace whtmix {
 
-constexpr int64_t kExactK = 128;
+constexpr int64_t kExactK = 512;
 
 // Rows of scales to whole dwords, 1 past the end: the tile kernel copies dwords.  Both
 // operands' in one launch.

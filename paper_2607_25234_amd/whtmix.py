@@ -887,7 +887,8 @@ def linear_mx(xq, xs, wq, ws, bias=None, activation: str = "none", residual=None
     """linear() on block-scaled 8 bits: xq, xs as norm_mx or quantize_mx give
     them, [..., K]; wq, ws the weights' columns as rows, [N, K].  Returns y
     [..., N] in dtype (the residual's or out's, else bfloat16), or with out_mx
-    (q, scales) of the result."""
+    (q, scales) of the result.  Sums of more than 512 k are float32 throughout
+    only for a float32 y (the others: up to 1e-5 of the sum of magnitudes off)."""
     T = _torch_module or _torch()
     M, K, pxq, pxs, dev = _mx(xq, xs, "xq")
     act = _activation(activation)
