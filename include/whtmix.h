@@ -463,10 +463,12 @@ WHTMIX_API int whtmix_dequantize_mx(const void *q, const uint8_t *scales, void *
  *   z         [M][N] of `dtype`, what the backward pass keeps, or NULL.
  * Sums are float32; with float32 elements the products are six bf16 products
  * of three-term splits (what they leave out is below 2^-24 |x| |w|), or float32
- * ones where a tile's operands do not split (from 2^128 - 2^119, Inf, NaN, or
- * below 2^-95 throughout).  Workspace: partial sums where k is split over
- * workgroups; large float32 operands' terms (six bytes an element); bf16
- * operands whose rows do not start at 16 bytes, packed.
+ * ones in tiles where a value is 2^128 - 2^119 or more, or where a row of x or a
+ * column of w is nonzero and below 2^-95 throughout.  (A value below 2^-109
+ * beside larger ones of its row or column is off by 2^-134 at most.)
+ * Workspace: partial sums where k is split over workgroups; large float32
+ * operands' terms (six bytes an element); bf16 operands whose rows do not start
+ * at 16 bytes, packed.
  */
 WHTMIX_API int whtmix_linear_forward(const void *x, const void *w,
                           const float *bias, const void *residual, void *y,

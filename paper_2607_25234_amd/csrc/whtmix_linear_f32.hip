@@ -25,7 +25,8 @@ template <Layout L, int ROWS> __device__ __forceinline__ int place_chunk(int out
 }
 
 // Three bf16 terms hold a float32 below 2^128 - 2^119 (above, the first rounds to Inf) and from
-// 2^-100 up (below, the last is subnormal); rows mixed with smaller values lose less than 2^-128.
+// 2^-100 up (below, the last is subnormal).  Smaller values beside larger ones of their row of x
+// or column of w are off by half of 2^-133 at most, bf16's least value.
 constexpr float kSplitMax = 0x1.ffp127f, kSplitMin = 0x1p-95f;
 constexpr int P = 3;               // bf16 terms of a float32
 
@@ -81,14 +82,23 @@ template <Layout L, int ROWS> struct Stage {
                     (L == K_CONTIGUOUS ? 0 : j)] = v[i][j];
         }
     }
-    // The largest magnitudes staged so far by chunk.  (A NaN is passed over: it makes its
-    // row's sums NaN either way.)
-    __device__ __forceinline__ void largest(float (&top)[kChunks]) const
+    // The largest magnitudes staged so far of each row that the thread's chunks are of: one a
+    // chunk (K_CONTIGUOUS), or the same four in all of them.  (A NaN is passed over: it
+    // makes its row's sums NaN either way.)
+    static constexpr int kTops = L == K_CONTIGUOUS ? kChunks : 4;
+    __device__ __forceinline__ void largest(float (&top)[kTops]) const
     {
+        if constexpr (L == K_CONTIGUOUS) {
 #pragma unroll
-        for (int i = 0; i < kChunks; ++i) {
-            top[i] = fmaxf(fmaxf(top[i], fabsf(v[i][0])), fabsf(v[i][1]));
-            top[i] = fmaxf(fmaxf(top[i], fabsf(v[i][2])), fabsf(v[i][3]));
+            for (int i = 0; i < kChunks; ++i) {
+                top[i] = fmaxf(fmaxf(top[i], fabsf(v[i][0])), fabsf(v[i][1]));
+                top[i] = fmaxf(fmaxf(top[i], fabsf(v[i][2])), fabsf(v[i][3]));
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < kChunks; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) top[j] = fmaxf(top[j], fabsf(v[i][j]));
         }
     }
     __device__ __forceinline__ void store(char *lds)
@@ -206,7 +216,7 @@ __global__ void __launch_bounds__(256) gemm_kernel(GemmArgs g)
 
     Stage<LA, BM> sa;
     Stage<LB, BN> sb;
-    float top_a[BM / 32] = {}, top_b[BN / 32] = {};     // what the splits have to hold
+    float top_a[Stage<LA, BM>::kTops] = {}, top_b[Stage<LB, BN>::kTops] = {};   // what the splits hold
     sa.init(g.a, g.lda, g.M, kend, m0, kbeg);
     sb.init(g.b, g.ldb, g.N, kend, n0, kbeg);
     sa.load();
@@ -250,13 +260,13 @@ __global__ void __launch_bounds__(256) gemm_kernel(GemmArgs g)
         }
     }
     auto bad = [](float top) { return top >= kSplitMax || (top != 0.f && top < kSplitMin); };
-    // A chunk's elements along k are of one row (or four); one that does not split sends the
-    // whole tile through float32 products.
+    // A row's values (of this thread's k) that do not split send the whole tile through
+    // float32 products.
     bool any = false;
 #pragma unroll
-    for (int i = 0; i < BM / 32; ++i) any = any || bad(top_a[i]);
+    for (int i = 0; i < Stage<LA, BM>::kTops; ++i) any = any || bad(top_a[i]);
 #pragma unroll
-    for (int i = 0; i < BN / 32; ++i) any = any || bad(top_b[i]);
+    for (int i = 0; i < Stage<LB, BN>::kTops; ++i) any = any || bad(top_b[i]);
     if (__syncthreads_or(any))
         float32_tile<LA, LB, BM, BN, WM>(g, sa, sb, (float *)lds, m0, n0, kbeg, kend, wm, wn, acc);
     __syncthreads();

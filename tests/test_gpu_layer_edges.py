@@ -48,3 +48,35 @@ def test_mx_sums_of_few_k_are_float32(M, N, K, out):
         y = whtmix.linear_mx(*rows(x), *rows(w), dtype=DTYPES[out])
         bound = bound * 1.01
     ref.check("sum", y, torch.zeros_like(mag), bound)
+
+
+# gemm_kernel's tiles of 32, 64 and 128 rows: float32 operands split on their way
+@pytest.mark.parametrize("M,K,N", [(9, 72, 40), (50, 96, 136), (140, 96, 136), (300, 200, 133)])
+def test_float32_tiny_columns_among_others(M, K, N):
+    """A column of w (and of x and dy, for dw; a row of w, for dx) far below what three bf16 terms
+    hold, among normal ones: its sums, which a large other operand brings back to the normal
+    range, keep float32's accuracy."""
+    from paper_2607_25234_amd import whtmix
+    dev = device()
+    say("tiny_columns", M, K, N)
+    for e in (-112, -120, -124):
+        x, w, dy = draw(1, M, K), draw(2, K, N), draw(3, M, N)
+        tiny = w.clone()
+        tiny[:, 5] *= 2.0 ** e
+        tiny[7] *= 2.0 ** e
+        big = x * 2.0 ** 60
+        z = big.double() @ tiny.double()
+        y = whtmix.linear(big.to(dev), tiny.to(dev))
+        ref.check("z", y, z, ref.sum_bound(K, big.double().abs() @ tiny.double().abs()))
+        dx = whtmix.linear_backward(x.to(dev), tiny.to(dev), (dy * 2.0 ** 60).to(dev),
+                                    want_dw=False, want_dbias=False)[0]
+        d = dy.double() * 2.0 ** 60
+        ref.check("dx", dx, d @ tiny.double().t(),
+                  ref.sum_bound(N, d.abs() @ tiny.double().abs().t()))
+        for of_x in (True, False):
+            a, b = (x.clone(), dy * 2.0 ** 60) if of_x else (big, dy.clone())
+            (a if of_x else b)[:, 6] *= 2.0 ** e
+            dw = whtmix.linear_backward(a.to(dev), w.to(dev), b.to(dev), want_dx=False,
+                                        want_dbias=False)[1]
+            a, b = a.double(), b.double()
+            ref.check(f"dw {of_x}", dw, a.t() @ b, ref.sum_bound(M, a.abs().t() @ b.abs()))
