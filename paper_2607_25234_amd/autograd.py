@@ -9,13 +9,41 @@
 
 The forward and backward passes both run in the HIP kernels of libwhtmix.so
 (whtmix_*forward*/whtmix_*backward*); gradients flow to x and to the gains, as
-when the paper trains the mixer (section IV-A).
+when the paper trains the mixer (section IV-A).  The gradients have no gradients
+of their own: a second backward pass through the norm and the product raises.
 """
 from __future__ import annotations
+
+import functools
 
 import torch
 
 from . import whtmix
+
+
+class _Gradients(torch.autograd.Function):
+    """backward(ctx, *dys) as a node of the graph that a pass with create_graph=True records, with
+    edges to all it depends on (dys and what ctx saved).  torch's once_differentiable has
+    none to the saved tensors: a second pass that reaches them another way skips its error."""
+
+    @staticmethod
+    def forward(_, backward, ctx, count, *tensors):
+        return backward(ctx, *tensors[:count])
+
+    @staticmethod
+    def backward(_, *grads):
+        raise RuntimeError("libwhtmix forms first derivatives only: no second derivative goes "
+                           "through its gradients")
+
+
+def _first_order(backward):
+    """A Function's backward whose results the kernels form."""
+    @functools.wraps(backward)
+    def run(ctx, *dys):
+        if not torch.is_grad_enabled():
+            return backward(ctx, *dys)
+        return _Gradients.apply(backward, ctx, len(dys), *dys, *ctx.saved_tensors)
+    return run
 
 
 class WHTMixFunction(torch.autograd.Function):
@@ -98,6 +126,7 @@ class WHTMixNormFunction(torch.autograd.Function):
         return (y, h) if residual is not None else y
 
     @staticmethod
+    @_first_order
     def backward(ctx, dy, dh=None):
         h, weight = ctx.saved_tensors
         dx, dw = whtmix.norm_backward(h, weight, dy.contiguous(),
@@ -122,6 +151,7 @@ class WHTMixLinearFunction(torch.autograd.Function):
         return y
 
     @staticmethod
+    @_first_order
     def backward(ctx, dy):
         x, w, z = ctx.saved_tensors
         want = ctx.needs_input_grad

@@ -1,0 +1,87 @@
+"""The feed-forward sublayer's Python side without a GPU: autograd wrappers and the layer with
+plain torch functions in the entry points' place."""
+from __future__ import annotations
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from paper_2607_25234_amd import autograd, whtmix  # noqa: E402
+from tests import layer_ref as ref  # noqa: E402
+
+
+def plain_norm(x, weight, residual=None, eps=1e-6):
+    h = x if residual is None else x + residual
+    return h * torch.rsqrt(h.square().mean(-1, keepdim=True) + eps) * weight, h
+
+
+def plain_linear(x, w, bias=None, activation="none", residual=None, want_z=False):
+    z = x @ w if bias is None else x @ w + bias
+    y = ref.act(activation, z)
+    y = y if residual is None else y + residual
+    return (y, z) if want_z else y
+
+
+def plain_norm_backward(h, weight, dy, dh=None, eps=1e-6, want_dweight=True):
+    r = torch.rsqrt(h.square().mean(-1, keepdim=True) + eps)
+    n, g = h * r, dy * weight
+    dx = r * (g - n * (g * n).mean(-1, keepdim=True))
+    dw = (dy * n).reshape(-1, h.shape[-1]).sum(0)
+    return dx if dh is None else dx + dh, dw if want_dweight else None
+
+
+def plain_linear_backward(x, w, dy, z=None, activation="none", want_dx=True, want_dw=True,
+                          want_dbias=True):
+    dz = dy if z is None else dy * ref.act_grad(activation, z)
+    K, N = w.shape
+    return (dz @ w.t() if want_dx else None,
+            x.reshape(-1, K).t() @ dz.reshape(-1, N) if want_dw else None,
+            dz.reshape(-1, N).sum(0) if want_dbias else None)
+
+
+@pytest.fixture
+def plain(monkeypatch):
+    for name in ("norm", "linear", "norm_backward", "linear_backward"):
+        monkeypatch.setattr(whtmix, name, globals()["plain_" + name])
+
+
+def test_second_derivatives_of_the_sublayer_are_refused(plain):
+    """The kernels' gradients have no graph: a second backward pass through them raises, where
+    it would return the share of what else it reaches (the residual's, here) alone."""
+    x = torch.randn(6, 8, dtype=torch.float64, requires_grad=True)
+    w = torch.randn(8, 8, dtype=torch.float64, requires_grad=True)
+    b = torch.randn(8, dtype=torch.float64, requires_grad=True)
+    for f, leaves in ((lambda: autograd.whtmix_linear(x, w, b, "silu", x), (x, w, b)),
+                      (lambda: autograd.whtmix_linear(x, w, b), (x, w, b)),
+                      (lambda: autograd.whtmix_norm(x, b, x)[0], (x, b)),
+                      (lambda: autograd.whtmix_norm(x, b)[0], (x, b))):
+        for leaf in leaves:
+            loss = f().square().sum() + x.pow(3).sum()
+            first, = torch.autograd.grad(loss, x, create_graph=True)
+            with pytest.raises(RuntimeError, match="second derivative"):
+                torch.autograd.grad(first.sum() + leaf.sum(), leaf)
+            with pytest.raises(RuntimeError, match="second derivative"):
+                first.sum().backward()
+
+
+def test_first_derivatives_are_as_before(plain):
+    """With and without a graph of the gradients, the plain functions' own."""
+    x, r = (torch.randn(2, 3, 8, dtype=torch.float64, requires_grad=True) for _ in range(2))
+    w = torch.randn(8, 5, dtype=torch.float64, requires_grad=True)
+    b = torch.randn(5, dtype=torch.float64, requires_grad=True)
+    g = torch.randn(8, dtype=torch.float64, requires_grad=True)
+    leaves = (x, r, w, b, g)
+
+    def loss(norm, linear):
+        y, h = norm(x, g, r)
+        return (linear(y, w, b, "gelu") * torch.arange(5)).sum() + h.pow(3).sum()
+
+    want = torch.autograd.grad(loss(plain_norm, plain_linear), leaves)
+    for graph in (False, True):
+        got = torch.autograd.grad(loss(autograd.whtmix_norm, autograd.whtmix_linear), leaves,
+                                  create_graph=graph)
+        for a, b_ in zip(got, want):
+            assert torch.allclose(a, b_, rtol=1e-10, atol=1e-12)
+    res = autograd.whtmix_linear(x, w, b, "none", r @ w)         # the residual's own gradient
+    a, = torch.autograd.grad((res * torch.arange(5)).sum(), r)
+    assert torch.allclose(a, (torch.arange(5).double() @ w.t()).expand_as(r))
