@@ -10,7 +10,7 @@
 The forward and backward passes both run in the HIP kernels of libwhtmix.so
 (whtmix_*forward*/whtmix_*backward*); gradients flow to x and to the gains, as
 when the paper trains the mixer (section IV-A).  The gradients have no gradients
-of their own: a second backward pass through the norm and the product raises.
+of their own: a second backward pass through them raises.
 """
 from __future__ import annotations
 
@@ -55,6 +55,7 @@ class WHTMixFunction(torch.autograd.Function):
         return whtmix.forward(x, gain)
 
     @staticmethod
+    @_first_order
     def backward(ctx, dy):
         x, gain = ctx.saved_tensors
         dx, dgain = whtmix.backward(x, dy.contiguous(), gain,
@@ -73,6 +74,7 @@ class WHTMixSeparableFunction(torch.autograd.Function):
         return whtmix.forward_separable(x, gt, gc)
 
     @staticmethod
+    @_first_order
     def backward(ctx, dy):
         x, gt, gc = ctx.saved_tensors
         want_g = ctx.needs_input_grad[1] or ctx.needs_input_grad[2]
@@ -90,6 +92,7 @@ class WHTMixBlockFunction(torch.autograd.Function):
         return whtmix.module_forward(x, w_in, gain, w_out)
 
     @staticmethod
+    @_first_order
     def backward(ctx, dy):
         x, w_in, gain, w_out = ctx.saved_tensors
         dx, dwi, dwo, dg = whtmix.module_backward(x, w_in, gain, w_out, dy.contiguous(),
@@ -106,6 +109,7 @@ class WHTMixBlockSeparableFunction(torch.autograd.Function):
         return whtmix.module_forward_separable(x, w_in, gt, gc, w_out)
 
     @staticmethod
+    @_first_order
     def backward(ctx, dy):
         x, w_in, gt, gc, w_out = ctx.saved_tensors
         want_g = ctx.needs_input_grad[2] or ctx.needs_input_grad[3]

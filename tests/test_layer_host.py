@@ -85,3 +85,34 @@ def test_first_derivatives_are_as_before(plain):
     res = autograd.whtmix_linear(x, w, b, "none", r @ w)         # the residual's own gradient
     a, = torch.autograd.grad((res * torch.arange(5)).sum(), r)
     assert torch.allclose(a, (torch.arange(5).double() @ w.t()).expand_as(r))
+
+
+def test_second_derivatives_of_the_mixer_are_refused(monkeypatch):
+    """The mixer's and the block's functions likewise (entry points of the right shapes)."""
+    def grads(*ts):
+        return tuple(torch.ones_like(t) for t in ts)
+
+    for name, f in {
+            "forward": lambda x, g: x * g,
+            "backward": lambda x, dy, g, **k: grads(x, g),
+            "forward_separable": lambda x, a, b: x * a[:, None] * b,
+            "backward_separable": lambda x, dy, a, b, **k: grads(x, a, b),
+            "module_forward": lambda x, i, g, o: x * g,
+            "module_backward": lambda x, i, g, o, dy, **k: grads(x, i, o, g),
+            "module_forward_separable": lambda x, i, a, b, o: x * a[:, None] * b,
+            "module_backward_separable":
+                lambda x, i, a, b, o, dy, **k: grads(x, i, o, a, b)}.items():
+        monkeypatch.setattr(whtmix, name, f)
+    x, g = (torch.randn(4, 8, requires_grad=True) for _ in range(2))
+    a, b = (torch.randn(n, requires_grad=True) for n in (4, 8))
+    i, o = (torch.randn(8, 8, requires_grad=True) for _ in range(2))
+    for y, leaves in ((autograd.whtmix_mix(x, g), (x, g)),
+                      (autograd.whtmix_mix_separable(x, a, b), (x, a, b)),
+                      (autograd.whtmix_block(x, i, g, o), (x, i, g, o)),
+                      (autograd.whtmix_block_separable(x, i, a, b, o), (x, i, a, b, o))):
+        for leaf in leaves:
+            first, = torch.autograd.grad(y.square().sum() + x.pow(3).sum(), x, create_graph=True)
+            with pytest.raises(RuntimeError, match="second derivative"):
+                torch.autograd.grad(first.sum() + leaf.sum(), leaf)
+        first = torch.autograd.grad(y.sum(), leaves)
+        assert all(torch.equal(f, torch.ones_like(t)) for f, t in zip(first, leaves))
