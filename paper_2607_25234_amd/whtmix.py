@@ -642,8 +642,9 @@ def _torch():
     global _torch_module
     if _torch_module is None:
         import torch
-        _torch_module = torch
+        # the codes first: another thread takes the module for the sign that they are there
         _CODES.update({torch.float32: DTYPE_F32, torch.bfloat16: DTYPE_BF16})
+        _torch_module = torch
     return _torch_module
 
 

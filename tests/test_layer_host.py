@@ -116,3 +116,18 @@ def test_second_derivatives_of_the_mixer_are_refused(monkeypatch):
                 torch.autograd.grad(first.sum() + leaf.sum(), leaf)
         first = torch.autograd.grad(y.sum(), leaves)
         assert all(torch.equal(f, torch.ones_like(t)) for f, t in zip(first, leaves))
+
+
+def test_dtype_codes_before_torch_is_published(monkeypatch):
+    """A thread that finds torch imported finds the element types' codes too."""
+    seen = []
+
+    class Codes(dict):
+        def update(self, *a, **k):
+            seen.append(whtmix._torch_module)
+            super().update(*a, **k)
+
+    monkeypatch.setattr(whtmix, "_torch_module", None)
+    monkeypatch.setattr(whtmix, "_CODES", Codes())
+    assert whtmix._torch() is torch and whtmix._torch_module is torch
+    assert seen == [None] and whtmix._CODES[torch.bfloat16] == whtmix.DTYPE_BF16
