@@ -5,7 +5,7 @@ residual's addition with a norm, and the feed-forward sublayer.
     y = h + act(norm(h) W1 + b1) W2 + b2
 
 MixerLayer trains it (every step in the library's kernels, forward and backward).
-MixerLayerMx serves a trained layer with its feed-forward weights in block-scaled
+MixerLayerMx serves the state of a trained layer with its feed-forward weights in block-scaled
 8 bits, laid out once: the norm writes 8-bit rows, the first product reads them
 and writes 8-bit rows again, the second adds its result to the stream.
 
@@ -50,19 +50,22 @@ class MixerLayer(torch.nn.Module):
 
 
 class MixerLayerMx:
-    """A trained MixerLayer at inference, its feed-forward weights in 8 bits."""
+    """A trained MixerLayer at inference, its feed-forward weights in 8 bits.  It holds copies
+    of all the layer's weights: what the layer learns afterwards does not reach it."""
 
     def __init__(self, layer: MixerLayer):
-        self.layer = layer
         with torch.no_grad():
+            for name in ("w_in", "w_out", "log_gain_tokens", "log_gain_channels", "norm_weight",
+                         "b1", "b2"):
+                setattr(self, name, getattr(layer, name).detach().clone())
             self.w1 = whtmix.quantize_mx(layer.w1.t().contiguous())
             self.w2 = whtmix.quantize_mx(layer.w2.t().contiguous())
+        self.activation, self.eps = layer.activation, layer.eps
 
     @torch.no_grad()
     def __call__(self, x):
-        p = self.layer
-        m = whtmix.module_forward_separable(x, p.w_in, p.log_gain_tokens, p.log_gain_channels,
-                                            p.w_out)
-        q, scales, h = whtmix.norm_mx(m, p.norm_weight, x, p.eps)
-        q, scales = whtmix.linear_mx(q, scales, *self.w1, p.b1, p.activation, out_mx=True)
-        return whtmix.linear_mx(q, scales, *self.w2, p.b2, residual=h)
+        m = whtmix.module_forward_separable(x, self.w_in, self.log_gain_tokens,
+                                            self.log_gain_channels, self.w_out)
+        q, scales, h = whtmix.norm_mx(m, self.norm_weight, x, self.eps)
+        q, scales = whtmix.linear_mx(q, scales, *self.w1, self.b1, self.activation, out_mx=True)
+        return whtmix.linear_mx(q, scales, *self.w2, self.b2, residual=h)

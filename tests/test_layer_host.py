@@ -131,3 +131,26 @@ def test_dtype_codes_before_torch_is_published(monkeypatch):
     monkeypatch.setattr(whtmix, "_CODES", Codes())
     assert whtmix._torch() is torch and whtmix._torch_module is torch
     assert seen == [None] and whtmix._CODES[torch.bfloat16] == whtmix.DTYPE_BF16
+
+
+def test_served_layer_keeps_the_weights_it_was_made_of(plain, monkeypatch):
+    """MixerLayerMx is of one state of the layer, whatever becomes of the layer afterwards."""
+    from paper_2607_25234_amd.layer import MixerLayer, MixerLayerMx
+    monkeypatch.setattr(whtmix, "quantize_mx", lambda x: (x.clone(), None))
+    monkeypatch.setattr(whtmix, "module_forward_separable",
+                        lambda x, i, a, b, o: (x @ i) * (a[:, None] + 1) * (b + 1) @ o)
+    monkeypatch.setattr(whtmix, "norm_mx", lambda x, w, r, eps: (
+        (n := plain_norm(x, w, r, eps))[0], None, n[1]))
+    monkeypatch.setattr(whtmix, "linear_mx", lambda q, s, w, ws, b, act="none", residual=None,
+                        out_mx=False: (y := plain_linear(q, w.t(), b, act, residual),
+                                       None) if out_mx else plain_linear(q, w.t(), b, act, residual))
+    torch.manual_seed(0)
+    layer = MixerLayer(4, 8, 16, dtype=torch.float32)
+    x = torch.randn(2, 4, 8)
+    served = MixerLayerMx(layer)
+    want = served(x)
+    for p in layer.parameters():
+        with torch.no_grad():
+            p.add_(torch.randn_like(p))
+    assert torch.equal(served(x), want)
+    assert not torch.equal(MixerLayerMx(layer)(x), want)
