@@ -118,10 +118,19 @@ class WHTMixBlockSeparableFunction(torch.autograd.Function):
         return dx, dwi.to(w_in.dtype), dgt, dgc, dwo.to(w_out.dtype)
 
 
+def _strided_rows(x):
+    """x, or a copy where its rows are not contiguous or not a constant distance apart."""
+    try:
+        rows, width, ld = whtmix._rows(x, "x")
+    except ValueError:
+        return x.contiguous()
+    return x if rows <= 1 or ld >= width else x.contiguous()
+
+
 class WHTMixNormFunction(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, residual, eps):
-        weight = weight.contiguous()
+        x, weight = _strided_rows(x), weight.contiguous()
         y, h = whtmix.norm(x, weight, None if residual is None else residual.contiguous(), eps)
         if residual is None:      # the stream is x itself
             h = x.contiguous()
@@ -142,11 +151,11 @@ class WHTMixNormFunction(torch.autograd.Function):
 class WHTMixLinearFunction(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, w, bias, activation, residual):
-        w = w.contiguous()
+        x, w = _strided_rows(x), w.contiguous()
         z = None
         # z is kept only where the activation's derivative needs it
         keep = activation != "none" and any(ctx.needs_input_grad[:3])
-        y = whtmix.linear(x, w, bias, activation,
+        y = whtmix.linear(x, w, None if bias is None else bias.contiguous(), activation,
                           None if residual is None else residual.contiguous(), want_z=keep)
         if keep:
             y, z = y

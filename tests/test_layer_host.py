@@ -154,3 +154,34 @@ def test_served_layer_keeps_the_weights_it_was_made_of(plain, monkeypatch):
             p.add_(torch.randn_like(p))
     assert torch.equal(served(x), want)
     assert not torch.equal(MixerLayerMx(layer)(x), want)
+
+
+def test_rows_of_any_strides_are_copied(plain, monkeypatch):
+    """x in strides that the entry points refuse (rows not contiguous, not a constant distance
+    apart, or overlapping) is copied, as the mixer's functions do; other strides are passed on."""
+    taken = []
+    for name in ("norm", "linear", "linear_backward"):
+        def entry(x, *a, f=getattr(whtmix, name), **k):
+            taken.append(x)
+            assert all(t.is_contiguous() for t in a if torch.is_tensor(t))
+            return f(x, *a, **k)
+        monkeypatch.setattr(whtmix, name, entry)
+    w = torch.randn(8, 5, dtype=torch.float64, requires_grad=True)
+    g = torch.randn(8, dtype=torch.float64)
+    t = torch.randn(4, 6, 16, dtype=torch.float64, requires_grad=True)
+    for view, copied in ((t[..., 3:11], False), (t[:, :3, :8], True),
+                         (t.transpose(0, 1)[..., 4:12], True), (t[:, :, ::2], True),
+                         (t[0, :1, :8].expand(5, 8), True), (t[0, :, 4:12], False)):
+        taken.clear()
+        bias = torch.randn(5, 2, dtype=torch.float64)[:, 0]
+        loss = autograd.whtmix_linear(view, w, bias, "silu").sum()
+        loss = loss + autograd.whtmix_norm(view, g, view.contiguous())[0].square().sum()
+        got = torch.autograd.grad(loss, (t, w))
+        for x in taken:
+            rows, width, ld = whtmix._rows(x, "x")
+            assert width == 8 and (rows <= 1 or ld >= 8)
+            assert (x.data_ptr() == view.data_ptr()) is not copied
+        loss = plain_linear(view, w, bias, "silu").sum()
+        loss = loss + plain_norm(view, g, view)[0].square().sum()
+        for a, b in zip(got, torch.autograd.grad(loss, (t, w))):
+            assert torch.allclose(a, b, rtol=1e-9, atol=1e-11)
