@@ -174,7 +174,9 @@ template <int ACT> __device__ __forceinline__ float act_grad(float z)
     if constexpr (ACT == ACT_GELU_TANH) {
         const float s = __builtin_amdgcn_rcpf(
             1.f + fast_exp(-kGeluC * z * fmaf(0.044715f * z, z, 1.f)));
-        return fmaf(z * s * (1.f - s), kGeluC * fmaf(0.134145f * z, z, 1.f), s);
+        // beyond 64, where s (1 - s) is 0, the square would overflow: no 0 * Inf
+        const float c = fminf(fmaxf(z, -64.f), 64.f);
+        return fmaf(c * s * (1.f - s), kGeluC * fmaf(0.134145f * c, c, 1.f), s);
     }
     if constexpr (ACT == ACT_SILU) {
         const float s = __builtin_amdgcn_rcpf(1.f + fast_exp(-z));

@@ -80,3 +80,26 @@ def test_float32_tiny_columns_among_others(M, K, N):
                                         want_dbias=False)[1]
             a, b = a.double(), b.double()
             ref.check(f"dw {of_x}", dw, a.t() @ b, ref.sum_bound(M, a.abs().t() @ b.abs()))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("act", ref.ACTS)
+@pytest.mark.parametrize("M", [2, 32768])
+def test_derivatives_at_large_values(M, dtype, act):
+    """Every derivative at finite values up to the type's largest: 1 above zero and 0 below, from
+    where float32 does not tell them apart.  (Many rows of narrow bf16 inputs take the pass
+    that forms dz and dx together.)"""
+    from paper_2607_25234_amd import whtmix
+    dev, dt = device(), DTYPES[dtype]
+    say("large_values", M, dtype, act)
+    at = [200.0, 512.0, 1e3, 1e10, 1.9e19, 4.5e19, 1e20, 3e38]
+    z = torch.tensor([s * v for v in at for s in (1, -1)] * 4).repeat(M, 1).to(dt)
+    K, N = 4, z.shape[1]
+    x, w, dy = (torch.ones(s, dtype=dt) for s in ((M, K), (K, N), (M, N)))
+    w[:, 1::2] = 2
+    dx, dw, db = whtmix.linear_backward(x.to(dev), w.to(dev), dy.to(dev),
+                                        None if act == "none" else z.to(dev), act)
+    d = (z > 0).double() if act != "none" else dy.double()
+    assert torch.equal(db.cpu().double(), d.sum(0))
+    assert torch.equal(dw.cpu().double(), (x.double().t() @ d).to(dt).double())
+    assert torch.equal(dx.cpu().double(), d @ w.double().t())
