@@ -434,7 +434,8 @@ WHTMIX_API int whtmix_norm_mx_forward(const void *x, const void *residual,
  *   dx        [rows][C] of `dtype`: the gradient of x and of the residual;
  *             may be dy or dh.
  *   dweight   [C] float32, or NULL to skip.
- * dweight is summed in a fixed order.  Workspace: up to 1536 rows of C floats.
+ * dweight is summed in a fixed order.  Workspace: for dweight, up to 1536 rows
+ * of C floats; for rows of more than 16384 elements, two floats a row besides.
  */
 WHTMIX_API int whtmix_norm_backward(const void *h, const float *weight,
                          const void *dy, const void *dh, void *dx,

@@ -185,7 +185,8 @@ int get_workspace(void *stream, int64_t bytes, float **out)
     // workspace request fails as an allocation failure would, before any HIP
     // call, so the status path can be tested without exhausting the device.
     if (std::getenv("WHTMIX_TEST_FAIL_WORKSPACE")) {
-        g_last_error = "workspace allocation refused (WHTMIX_TEST_FAIL_WORKSPACE)";
+        g_last_error = "workspace allocation of " + std::to_string(bytes) +
+                       " bytes refused (WHTMIX_TEST_FAIL_WORKSPACE)";
         return WHTMIX_ERROR_OUT_OF_MEMORY;
     }
     int dev = 0;

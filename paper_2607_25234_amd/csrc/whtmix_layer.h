@@ -47,7 +47,7 @@ struct NormBackwardArgs {
     int dtype;
     hipStream_t stream;
 };
-uint64_t norm_backward_floats(int64_t rows, int64_t C, int dtype);
+uint64_t norm_backward_floats(int64_t rows, int64_t C, int dtype, bool dweight);
 hipError_t launch_norm_backward(const NormBackwardArgs &a);
 
 hipError_t launch_dequantize(const void *q, const uint8_t *scales, void *y, int64_t rows,

@@ -204,7 +204,7 @@ int whtmix_norm_backward(const void *h, const float *weight, const void *dy, con
         if (!apart(rx, {rh, rg, rw}) || (dx != dy && overlap(rx, ry)) ||
             (dx != dh && overlap(rx, rd)) || !apart(rw, {rh, ry, rd, rg}))
             return WHTMIX_ERROR_INVALID_VALUE;
-        const uint64_t floats = whtmix::norm_backward_floats(rows, C, dtype);
+        const uint64_t floats = whtmix::norm_backward_floats(rows, C, dtype, dweight != nullptr);
         return with_workspace(stream, floats * 4, "norm backward", [&](float *ws) {
             const whtmix::NormBackwardArgs a{h, weight, dy, dh, dx, dweight, ws, rows, C,
                                              (float)eps, dtype, s};

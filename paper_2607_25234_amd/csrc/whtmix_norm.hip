@@ -477,7 +477,7 @@ template <typename T> hipError_t pick_backward(const NormBackwardArgs &a)
     const uint32_t b = (uint32_t)parts;
     hipError_t e;
     if (n > wide_chunks(Chunk<T>::N)) {
-        float *stat = a.ws + parts * a.C;
+        float *stat = a.ws + (a.dweight ? parts * a.C : 0);
         const NormBackwardKernelArgs k{a.h, a.dy, a.dh, a.weight, a.dx,
                                        a.dweight ? a.ws : nullptr, a.rows, a.C, a.eps};
         norm_backward_stats<T><<<dim3((uint32_t)std::min<int64_t>(a.rows, 1 << 16)), dim3(1024), 0,
@@ -550,10 +550,12 @@ hipError_t launch_norm(const NormArgs &a)
     return a.dtype == DTYPE_BF16 ? pick_mode<__bf16>(a) : pick_mode<float>(a);
 }
 
-uint64_t norm_backward_floats(int64_t rows, int64_t C, int dtype)
+uint64_t norm_backward_floats(int64_t rows, int64_t C, int dtype, bool dweight)
 {
+    const int per = dtype == DTYPE_BF16 ? 8 : 4;
     // the partial sums, and two numbers a row where rows are too wide for registers
-    return (uint64_t)backward_parts(rows, C, dtype) * C + 2 * (uint64_t)rows;
+    return (dweight ? (uint64_t)backward_parts(rows, C, dtype) * C : 0) +
+           ((C + per - 1) / per > wide_chunks(per) ? 2 * (uint64_t)rows : 0);
 }
 
 hipError_t launch_norm_backward(const NormBackwardArgs &a)

@@ -185,3 +185,29 @@ def test_rows_of_any_strides_are_copied(plain, monkeypatch):
         loss = loss + plain_norm(view, g, view)[0].square().sum()
         for a, b in zip(got, torch.autograd.grad(loss, (t, w))):
             assert torch.allclose(a, b, rtol=1e-9, atol=1e-11)
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+def test_workspace_of_the_norms_backward(monkeypatch, dtype):
+    """What the header says: partial rows for dweight alone, and two floats a row for rows of more
+    than 16384 elements alone."""
+    import re
+    if torch.cuda.device_count() > 0:
+        pytest.skip("fake device addresses are for hosts without a GPU")
+    monkeypatch.setenv("WHTMIX_TEST_FAIL_WORKSPACE", "1")
+
+    def floats(rows, C, dweight):
+        p = [(1 << 44) + (i << 40) for i in range(6)]
+        p[5] *= dweight
+        status = whtmix.call_rows("whtmix_norm_backward", tuple(p), (rows, C), (dtype,), 0, 1e-6)
+        if status != 5:          # out of memory: the test hook's
+            assert status         # (no GPU to launch on)
+            return 0
+        return int(re.search(r"of (\d+) bytes", whtmix.last_error()).group(1)) // 4
+
+    for rows, C in ((1, 64), (10 ** 8, 8), (10 ** 6, 128), (5000, 4096), (3000, 16384)):
+        assert C <= floats(rows, C, True) <= 1536 * C, (rows, C)
+        assert floats(rows, C, False) == 0, (rows, C)
+    for rows, C in ((1, 16392), (5000, 20000), (10 ** 6, 70001)):
+        assert floats(rows, C, False) == 2 * rows, (rows, C)
+        assert 2 * rows + C <= floats(rows, C, True) <= 2 * rows + 1536 * C, (rows, C)
