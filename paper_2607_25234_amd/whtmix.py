@@ -737,7 +737,8 @@ def norm(x, weight, residual=None, eps: float = 1e-6, out=None, stream=None):
 
     x: [..., C] float32 or bfloat16 (rows may be columns of a wider tensor);
     weight: float32 [C]; residual: a contiguous tensor of x's shape and type;
-    out: optional contiguous tensor for y (may be x itself)."""
+    out: optional contiguous tensor for y (may be x itself; without a residual
+    h is None then, since x holds y)."""
     T = _torch_module or _torch()
     dt, rows, C, ld, dev = _operand(x, "x")
     shape, dtype = x.shape, x.dtype
@@ -752,6 +753,8 @@ def norm(x, weight, residual=None, eps: float = 1e-6, out=None, stream=None):
         py = out.data_ptr()
     else:
         py = _tensor(out, shape, dtype, dev, "out")
+        if residual is None and py == x.data_ptr():
+            h = None
     _run_rows("whtmix_norm_forward", dev, stream, (x.data_ptr(), pr, pw, py, ph), (rows, C, ld),
               (dt,), eps)
     return out, h

@@ -103,3 +103,22 @@ def test_derivatives_at_large_values(M, dtype, act):
     assert torch.equal(db.cpu().double(), d.sum(0))
     assert torch.equal(dw.cpu().double(), (x.double().t() @ d).to(dt).double())
     assert torch.equal(dx.cpu().double(), d @ w.double().t())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_norm_in_place(dtype):
+    """y in x's place: with a residual h is a tensor of its own, without one x is gone."""
+    from paper_2607_25234_amd import whtmix
+    dev, dt = device(), DTYPES[dtype]
+    for rows, C in ((1, 7), (9, 520), (3, 20000)):
+        say("norm_in_place", rows, C, dtype)
+        x, r = draw(1, rows, C, dtype=dt).to(dev), draw(2, rows, C, dtype=dt).to(dev)
+        w = draw(3, C).to(dev)
+        for res in (None, r):
+            want, kept = whtmix.norm(x, w, res)
+            y = x.clone()
+            out, h = whtmix.norm(y, w, res, out=y)
+            assert out is y and torch.equal(y, want)
+            assert h is None if res is None else torch.equal(h, kept)
+        other = torch.empty_like(x)
+        assert torch.equal(whtmix.norm(x, w, out=other)[1], x)
