@@ -57,7 +57,7 @@ hipError_t launch_dequantize(const void *q, const uint8_t *scales, void *y, int6
 hipError_t launch_column_sum(const float *part, int64_t n, int64_t C, float *out,
                              hipStream_t stream);
 
-// Zeros, by a kernel (a fill that a captured graph replays).
+// Zeros, by a kernel (a fill that a captured graph replays); an even count of bytes.
 hipError_t launch_zero(void *p, uint64_t bytes, hipStream_t stream);
 
 // ---- matrix products ----

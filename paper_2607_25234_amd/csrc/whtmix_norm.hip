@@ -530,18 +530,27 @@ __global__ void __launch_bounds__(1024) column_sum_kernel(const float *part, int
     }
 }
 
-__global__ void __launch_bounds__(256) zero_kernel(uint16_t *p, uint64_t n)
+// 16 bytes a thread round the grid; the first workgroup takes what lies before and after them, in
+// 2-byte words.
+__global__ void __launch_bounds__(256) zero_kernel(char *p, uint64_t bytes)
 {
-    const uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i < n) p[i] = 0;
+    const uint64_t before = min(bytes, (16 - (uint64_t)(uintptr_t)p % 16) % 16);
+    const uint64_t wide = (bytes - before) / 16;
+    for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < wide;
+         i += (uint64_t)gridDim.x * 256)
+        *(u32x4 *)(p + before + 16 * i) = (u32x4){0, 0, 0, 0};
+    if (blockIdx.x > 0 || threadIdx.x >= 8) return;
+    const uint64_t at = 2 * threadIdx.x, end = before + 16 * wide;
+    if (at < before) *(uint16_t *)(p + at) = 0;
+    if (end + at < bytes) *(uint16_t *)(p + end + at) = 0;
 }
 
 }  // namespace
 
 hipError_t launch_zero(void *p, uint64_t bytes, hipStream_t stream)
 {
-    zero_kernel<<<dim3((uint32_t)((bytes / 2 + 255) / 256)), dim3(256), 0, stream>>>(
-        (uint16_t *)p, bytes / 2);
+    const uint64_t blocks = std::min<uint64_t>(bytes / 4096 + 1, kMaxBlocks);
+    zero_kernel<<<dim3((uint32_t)blocks), dim3(256), 0, stream>>>((char *)p, bytes);
     return hipGetLastError();
 }
 

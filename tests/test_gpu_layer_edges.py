@@ -122,3 +122,29 @@ def test_norm_in_place(dtype):
             assert h is None if res is None else torch.equal(h, kept)
         other = torch.empty_like(x)
         assert torch.equal(whtmix.norm(x, w, out=other)[1], x)
+
+
+def test_no_rows_zeros_gradients_of_any_size():
+    """M = 0: dw and dbias are zeros to the last element and nothing around them is written,
+    from any alignment and past the 2^32 threads that one launch holds (8.6 GB of dw)."""
+    from paper_2607_25234_amd import whtmix
+    dev = device()
+    for dt, code in ((torch.float32, 0), (torch.bfloat16, 1)):
+        for K, N in ((1, 1), (3, 5), (1, 8), (7, 33), (65, 4099)):
+            for at in (0, 1, 2, 5, 7):
+                say("no_rows", dt, K, N, at)
+                t = torch.ones(K * N + 32, dtype=dt, device=dev)
+                b = torch.ones(N + 8, device=dev)
+                status = whtmix.call_rows(
+                    "whtmix_linear_backward",
+                    (0, 0, 0, 0, 0, t[at:].data_ptr(), b[1:].data_ptr()), (0, K, N, K), (0, code),
+                    torch.cuda.current_stream().cuda_stream)
+                assert status == 0
+                assert t[:at].all() and not t[at:at + K * N].any() and t[at + K * N:].all()
+                assert b[0] == 1 and not b[1:N + 1].any() and b[N + 1:].all()
+    K, N = (1 << 16) + 3, 1 << 15
+    say("no_rows", K, N)
+    t = torch.ones(K * N + 8, device=dev)
+    assert whtmix.call_rows("whtmix_linear_backward", (0, 0, 0, 0, 0, t[1:].data_ptr(), 0),
+                            (0, K, N, K), (0, 0), torch.cuda.current_stream().cuda_stream) == 0
+    assert int(torch.count_nonzero(t)) == 8 and t[0] == 1 and t[-7:].all()
