@@ -149,15 +149,19 @@ __global__ void __launch_bounds__(256) dzx_kernel(DzxArgs d, GemmArgs g)
 
 int64_t dzx_parts(int64_t M) { return (M + kRows - 1) / kRows; }
 
-// Narrow inputs, whole 16-byte chunks (32-bit offsets of w's), and rows enough for the device.
-// Together and apart: 262144 x 128 x 512 199 and 238 us, 131072 x 64 x 64 27 and 50, 65536 x 64 x
-// 256 31 and 35, 32768 x 128 x 512 37 and 35, 4096 x 128 x 512 28 and 20.
+// Narrow inputs, whole 16-byte chunks (32-bit offsets of w's), and rows enough for the device, more
+// of them where a workgroup's rows take long.  dx and dbias, together and apart:
+//   32768 x 128 x 64 12 and 21 us, x 128 15 and 25, x 256 23 and 26, x 512 37 and 35;
+//   49152 x 128 x 512 49 and 51, x 1024 82 and 84; 40960 x 128 x 1024 78 and 74;
+//   65536 x 128 x 512 54 and 61, x 2048 240 and 229; 262144 x 128 x 512 195 and 240, and with dw
+//   131072 x 128 x 1024 262 and 295, x 2048 588 and 590, x 4096 1105 and 1068;
+//   4096 x 128 x 512 28 and 20.
 bool dzx_takes(const LinearBackwardArgs &a)
 {
     auto aligned = [](const void *p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; };
     return a.dtype == DTYPE_BF16 && a.act != ACT_NONE && a.dx && a.K <= kCols && a.N % 8 == 0 &&
-           a.N >= kN && a.N <= (int64_t(1) << 22) && a.M >= 256 * kRows && aligned(a.dy) &&
-           aligned(a.z) && aligned(a.w);
+           a.N >= kN && a.N <= 1024 && a.M >= (a.N <= 256 ? 256 : 384) * kRows &&
+           aligned(a.dy) && aligned(a.z) && aligned(a.w);
 }
 
 hipError_t launch_dzx(const LinearBackwardArgs &a, void *dz, float *part)

@@ -148,3 +148,27 @@ def test_no_rows_zeros_gradients_of_any_size():
     assert whtmix.call_rows("whtmix_linear_backward", (0, 0, 0, 0, 0, t[1:].data_ptr(), 0),
                             (0, K, N, K), (0, 0), torch.cuda.current_stream().cuda_stream) == 0
     assert int(torch.count_nonzero(t)) == 8 and t[0] == 1 and t[-7:].all()
+
+
+@pytest.mark.parametrize("M,K,N,act", [(49152, 128, 520, "gelu"), (49200, 60, 1024, "silu"),
+                                       (49155, 7, 272, "gelu_tanh"), (32769, 128, 256, "relu"),
+                                       (49151, 16, 264, "silu"), (50001, 9, 1032, "relu")])
+def test_narrow_backward_on_both_sides_of_its_rule(M, K, N, act):
+    """dz, its sums and dx of narrow bf16 inputs: rows and columns at which they are formed in
+    one pass, and the next ones, at which they are not."""
+    from paper_2607_25234_amd import whtmix
+    dev, dt = device(), torch.bfloat16
+    say("narrow_rule", M, K, N, act)
+    x, w = draw(1, M, K, dtype=dt), draw(2, K, N, std=K ** -0.5, dtype=dt)
+    dy, z = draw(3, M, N, dtype=dt), draw(4, M, N, std=2.0, dtype=dt)
+    dx, dw, db = whtmix.linear_backward(x.to(dev), w.to(dev), dy.to(dev), z.to(dev), act)
+    X, W, D = x.double(), w.double(), dy.double()
+    d = D * ref.act_grad(act, z.double())
+    own = D.abs() * ref.grad_bound(act, z.double())
+    rnd = own + d.abs() * 2.0 ** -7.99
+    rx, rw = d @ W.t(), X.t() @ d
+    ref.check("dx", dx, rx, ref.sum_bound(N, d.abs() @ W.abs().t()) + rnd @ W.abs().t()
+              + ref.rounded(rx, True))
+    ref.check("dw", dw, rw, ref.sum_bound(M, X.abs().t() @ d.abs()) + X.abs().t() @ rnd
+              + ref.rounded(rw, True))
+    ref.check("db", db, d.sum(0), ref.sum_bound(M, d.abs().sum(0)) + own.sum(0) + 1e-30)
