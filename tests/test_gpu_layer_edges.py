@@ -172,3 +172,166 @@ def test_narrow_backward_on_both_sides_of_its_rule(M, K, N, act):
     ref.check("dw", dw, rw, ref.sum_bound(M, X.abs().t() @ d.abs()) + X.abs().t() @ rnd
               + ref.rounded(rw, True))
     ref.check("db", db, d.sum(0), ref.sum_bound(M, d.abs().sum(0)) + own.sum(0) + 1e-30)
+
+
+def test_graph_replays():
+    """The sublayer forward and backward, and its 8-bit form, captured on a stream whose workspace
+    earlier calls sized, then replayed on new inputs with eager work between: every replay
+    gives the eager call's bits."""
+    from paper_2607_25234_amd import whtmix
+    dev, bf = device(), torch.bfloat16
+    say("graph_replays")
+    M, C, N = 300, 264, 520
+    x, r, dy = (draw(i, M, C, dtype=bf).to(dev) for i in (1, 2, 3))
+    w1, w2 = draw(4, C, N, std=C ** -0.5, dtype=bf).to(dev), draw(5, N, C, std=0.04, dtype=bf).to(dev)
+    f1 = w1.float()
+    g, b1, b2 = 1 + draw(6, C, std=0.1).to(dev), draw(7, N).to(dev), draw(8, C).to(dev)
+    q1, q2 = whtmix.quantize_mx(w1.t().contiguous()), whtmix.quantize_mx(w2.t().contiguous())
+
+    def step():
+        y, h = whtmix.norm(x, g, r)
+        u, z = whtmix.linear(y, w1, b1, "gelu", want_z=True)
+        o = whtmix.linear(u, w2, b2, residual=h)
+        du, dw2, db2 = whtmix.linear_backward(u, w2, dy)
+        dn, dw1, db1 = whtmix.linear_backward(y, w1, du, z, "gelu")
+        dx, dg = whtmix.norm_backward(h, g, dn, dy)
+        wide = whtmix.linear(y.float(), f1, b1, "silu")
+        q, s, k = whtmix.norm_mx(x, g, r)
+        q, s = whtmix.linear_mx(q, s, *q1, b1, "gelu_tanh", out_mx=True)
+        return [o, dx, dg, dw1, db1, dw2, db2, wide, whtmix.linear_mx(q, s, *q2, b2, residual=k)]
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        outs = step()
+    for k in range(4):
+        for t, seed in ((x, 20), (r, 30), (dy, 40)):
+            t.copy_(draw(seed + k, M, C, dtype=bf))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in outs]
+        for a, b in zip(got, step()):
+            assert torch.equal(a, b), k
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,C", [(4000, 2048), (1000, 16384), (1300, 9000), (3001, 1023)])
+def test_norm_backward_round_the_grid(rows, C, dtype):
+    """Rows on several waves that go round the grid three times and more."""
+    from paper_2607_25234_amd import whtmix
+    dev, dt = device(), DTYPES[dtype]
+    say("norm_backward_round", rows, C, dtype)
+    h, w = draw(1, rows, C, dtype=dt), 1 + draw(2, C, std=0.1)
+    dy, dh = draw(3, rows, C, dtype=dt), draw(4, rows, C, dtype=dt)
+    dx, dw = whtmix.norm_backward(h.to(dev), w.to(dev), dy.to(dev), dh.to(dev), eps=1e-5)
+    H, W, D = h.double(), w.double(), dy.double()
+    rstd = 1 / (H.square().mean(-1, keepdim=True) + 1e-5).sqrt()
+    n, g = H * rstd, D * W
+    rx = rstd * (g - n * (g * n).mean(-1, keepdim=True)) + dh.double()
+    mag = rstd * (g.abs() + n.abs() * (g * n).abs().mean(-1, keepdim=True)) + dh.double().abs()
+    ref.check("dx", dx, rx, ref.sum_bound(C, mag) + ref.rounded(rx, dtype == "bf16"))
+    mag = (D * n).abs().sum(0)
+    ref.check("dw", dw, (D * n).sum(0), ref.sum_bound(rows, mag) + ref.sum_bound(C, mag))
+
+
+def test_two_threads():
+    """Two host threads, each on a stream of its own, get what one gets alone."""
+    import threading
+    from paper_2607_25234_amd import whtmix
+    dev = device()
+    say("two_threads")
+    cases = []
+    for i, dt in enumerate((torch.bfloat16, torch.float32)):
+        M, K, N = 700 + 100 * i, 200 + 40 * i, 136
+        cases.append((draw(1 + i, M, K, dtype=dt).to(dev), draw(3 + i, K, N, dtype=dt).to(dev),
+                      draw(5 + i, M, N, dtype=dt).to(dev), draw(7 + i, K).to(dev)))
+
+    def calls(x, w, dy, g):
+        return (*whtmix.linear_backward(x, w, dy, dy, "silu"), whtmix.linear(x, w),
+                *whtmix.norm_backward(x, g, x))
+
+    alone = [calls(*c) for c in cases]
+    torch.cuda.synchronize()
+    wrong = []
+
+    def run(c, want):
+        try:
+            stream = torch.cuda.Stream()
+            with torch.cuda.stream(stream):
+                for _ in range(20):
+                    got = calls(*c)
+                    stream.synchronize()
+                    if not all(torch.equal(a, b) for a, b in zip(got, want)):
+                        wrong.append("other bits")
+        except Exception as e:      # told to the test's own thread
+            wrong.append(repr(e))
+
+    threads = [threading.Thread(target=run, args=a) for a in zip(cases, alone)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not wrong, wrong
+
+
+def hadamard(n):
+    h = torch.ones(1, 1, dtype=torch.float64)
+    while h.shape[0] < n:
+        h = torch.cat([torch.cat([h, h], 1), torch.cat([h, -h], 1)], 0)
+    return h / math.sqrt(n)
+
+
+# Each tensor a bf16 layer holds is rounded by up to 2^-8 of itself: in the forward pass the block's
+# result, h, the norm's, the hidden values and the output, each passed on with a slope of up to
+# 1.3 (ten of them allowed); backward du, z, dz, the norm's gradient, h, dx, the block's three and
+# the sum of x's two (fourteen).  float32: 1e-5, as the mixer's own tests have it.
+@pytest.mark.parametrize("dtype,forward,backward", [("f32", 1e-5, 1e-5),
+                                                    ("bf16", 10 * 2.0 ** -8, 14 * 2.0 ** -8)])
+def test_layer_and_its_gradients(dtype, forward, backward):
+    """MixerLayer's output and every gradient, and MixerLayerMx's output, against the layer
+    written out in 64 bits (dense Hadamard products)."""
+    from paper_2607_25234_amd.layer import MixerLayer, MixerLayerMx
+    dev, dt = device(), DTYPES[dtype]
+    torch.manual_seed(0)
+    B, N, C, H = 2, 100, 64, 256
+    say("layer", dtype)
+    layer = MixerLayer(N, C, H, dtype=dt, device=dev)
+    with torch.no_grad():
+        for p in (layer.log_gain_tokens, layer.log_gain_channels, layer.b1, layer.b2,
+                  layer.norm_weight):
+            p.add_(torch.randn_like(p) * 0.1)
+    x, dy = draw(1, B, N, C, dtype=dt), draw(2, B, N, C, dtype=dt)
+    xd = x.to(dev).requires_grad_()
+    y = layer(xd)
+    y.backward(dy.to(dev))
+
+    p = {k: v.detach().cpu().double().requires_grad_() for k, v in layer.named_parameters()}
+    X = x.double().requires_grad_()
+    ht, hc = hadamard(128), hadamard(C)
+    u = torch.nn.functional.pad(X @ p["w_in"], (0, 0, 0, 28))
+    gain = torch.exp(p["log_gain_tokens"])[:, None] * torch.exp(p["log_gain_channels"])
+    m = (ht @ (gain * (ht @ u @ hc)) @ hc)[:, :N] @ p["w_out"]
+    h = X + m
+    n = h / (h.square().mean(-1, keepdim=True) + 1e-6).sqrt() * p["norm_weight"]
+    f = ref.act("gelu", n @ p["w1"] + p["b1"]) @ p["w2"] + p["b2"]
+    r = h + f
+    r.backward(dy.double())
+
+    def off(name, got, want, tol):
+        err = float((got.detach().cpu().double() - want).norm() / want.norm())
+        say(f"  {name}: {err:.2e} of {tol:.2e}")
+        assert err <= tol, (name, err)
+
+    off("y", y, r.detach(), forward)
+    off("dx", xd.grad, X.grad, backward)
+    for name, q in layer.named_parameters():
+        assert q.grad.dtype == q.dtype
+        off("d " + name, q.grad, p[name].grad, backward)
+    served = MixerLayerMx(layer)(x.to(dev))
+    assert served.dtype is dt
+    off("served", served, r.detach(),
+        float(0.1 * f.detach().norm() / r.detach().norm()) + forward)
