@@ -35,7 +35,10 @@
  * B*N_pad*C*4 bytes per (device, stream) for shapes that need more than one
  * pass; it is allocated (or grown) on the first call that needs it, which
  * therefore synchronises that stream and is not safe inside HIP graph
- * capture.
+ * capture.  A captured graph keeps the address of the workspace that its calls
+ * took: size it by such calls on the capturing stream beforehand, and let no
+ * larger call on that stream grow it, and nothing release it, while the graph
+ * is in use.
  */
 #ifndef WHTMIX_H
 #define WHTMIX_H
