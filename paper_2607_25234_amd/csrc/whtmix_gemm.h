@@ -114,7 +114,8 @@ __device__ __forceinline__ const char *uniform(const char *p)
 // 16 bytes a lane from memory to LDS (lane order from the wave's address `lds`), counted by
 // vmcnt.  In assembler, because the compiler would have every later LDS read wait for the
 // copies in flight; the kernel waits for them itself, a step later.  No registers but m0 are
-// written, which nothing else in these kernels uses.
+// written, which the compiler reserves (it may not be named as clobbered) and uses nowhere else
+// in these kernels.
 __device__ __forceinline__ void copy16(const char *base, uint32_t off, uint32_t lds)
 {
     base = uniform(base);

@@ -15,7 +15,8 @@ namespace {
 
 // dz = dy act'(z), with the columns' sums of the unrounded values: 32 threads across
 // 256 columns, 8 rows at a time, four of them in flight a thread; the workgroup's 8
-// sums of a column are added in order.  Bound by memory and, with gelu in bf16, by its
+// sums of a column are added in order.  dz is rounded to the type of dy: bf16 is what the matrix
+// cores read, and half the bytes for both products.  Bound by memory and, with gelu in bf16, by its
 // vector instructions as much: 262144 x 512 bf16 192 us (805 MB at 4.2 TB/s; wide products of
 // it follow, narrow ones are formed in launch_dzx's pass), float32 3001 x 2003 21 us.
 constexpr int kDzRows = 8, kDzCols = 256;

