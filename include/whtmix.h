@@ -510,9 +510,10 @@ WHTMIX_API int whtmix_linear_backward(const void *x, const void *w,
  * output run on the scaled matrix instructions, which keep about 15 bits below
  * the largest of 64 products before they add to a float32 sum: off by 1e-6 of
  * the sum of magnitudes, root mean square, for normal values, by 1e-5 for
- * values spread over 2^6.  The others' sums are float32 throughout; a caller
- * that wants such sums of more k takes y in float32 and rounds it, or
- * quantises it with whtmix_quantize_mx.
+ * values spread over 2^6.  The others' sums are float32 throughout, of bf16
+ * values (what lies below 2^-125 is taken to the nearest 2^-133); a caller that
+ * wants such sums of more k takes y in float32 and rounds it, or quantises it
+ * with whtmix_quantize_mx.
  */
 WHTMIX_API int whtmix_linear_mx_forward(const void *xq, const uint8_t *xs,
                              const void *wq, const uint8_t *ws,
