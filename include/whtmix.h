@@ -522,6 +522,147 @@ WHTMIX_API int whtmix_linear_mx_forward(const void *xq, const uint8_t *xs,
                              int64_t N, int activation, int dtype,
                              void *stream);
 
+/*
+ * ---- What a text model has besides: layer norm, gated products, embedding ----
+ *
+ * The rules of the feed-forward sublayer hold for these too.
+ */
+
+/*
+ * whtmix_layer_norm_forward -- layer norm with the residual's addition:
+ *     t = x + residual,   h = t,
+ *     y = (t - mean(t)) / sqrt(mean((t - mean(t))^2) + eps) * weight + bias.
+ *   x         [rows] rows of C elements of `dtype`, ldx apart.
+ *   residual  [rows][C] or NULL (t = x).
+ *   weight    [C] float32.      bias  [C] float32, or NULL (zeros).
+ *   y         [rows][C] of `dtype`; may be x (with ldx = C).
+ *   h         [rows][C] of `dtype`, t rounded, or NULL; may be x (with ldx =
+ *             C) or the residual, but not y.
+ * y is formed from t before its rounding.  eps >= 0 and finite.  Squares are of
+ * distances from the mean, in float32 (below 2^64 in magnitude).
+ */
+WHTMIX_API int whtmix_layer_norm_forward(const void *x, const void *residual,
+                              const float *weight, const float *bias, void *y,
+                              void *h, int64_t rows, int64_t C, int64_t ldx,
+                              double eps, int dtype, void *stream);
+
+/*
+ * whtmix_layer_norm_mx_forward -- whtmix_layer_norm_forward with y in
+ * block-scaled 8 bits: q [rows][C up to 32] e4m3, scales [rows][C up to 32 / 32].
+ */
+WHTMIX_API int whtmix_layer_norm_mx_forward(const void *x, const void *residual,
+                                 const float *weight, const float *bias,
+                                 void *q, uint8_t *scales, void *h,
+                                 int64_t rows, int64_t C, int64_t ldx,
+                                 double eps, int dtype, void *stream);
+
+/*
+ * whtmix_layer_norm_backward -- gradients of whtmix_layer_norm_forward from the
+ * kept stream h: with r = 1 / sqrt(mean((h - mean(h))^2) + eps), n = (h -
+ * mean(h)) r, g = dy weight,
+ *     dx = dh + r (g - mean(g) - n mean(g n)),
+ *     dweight = sum over rows of dy n,   dbias = sum over rows of dy.
+ *   h, dy     [rows][C] of `dtype`.
+ *   dh        [rows][C] of `dtype`, the gradient of h, or NULL (zeros).
+ *   dx        [rows][C] of `dtype`: the gradient of x and of the residual;
+ *             may be dy or dh.
+ *   dweight, dbias  [C] float32, or NULL to skip.
+ * Both are summed in a fixed order.  Workspace: for them, up to 1536 rows of 2 C
+ * floats; for rows of more than 16384 elements, five floats a row besides.
+ */
+WHTMIX_API int whtmix_layer_norm_backward(const void *h, const float *weight,
+                               const void *dy, const void *dh, void *dx,
+                               float *dweight, float *dbias, int64_t rows,
+                               int64_t C, double eps, int dtype, void *stream);
+
+/*
+ * whtmix_gated_forward -- gated product, both projections in one kernel:
+ *     zg = x wg + bg,   zu = x wu + bu,   y = act(zg) zu  (element by element).
+ *   x         [M] rows of K elements of `dtype`, ldx apart.
+ *   wg, wu    [K][N] of `dtype`, N <= 2^21.
+ *   bg, bu    [N] float32, each or NULL.
+ *   y         [M][N] of `dtype`.
+ *   zg, zu    [M][N] of `dtype`, what the backward pass keeps, each or NULL.
+ * y is formed from zg and zu before their rounding.  Sums as
+ * whtmix_linear_forward's.  Workspace: as whtmix_linear_forward's, for both
+ * products.
+ */
+WHTMIX_API int whtmix_gated_forward(const void *x, const void *wg, const void *wu,
+                         const float *bg, const float *bu, void *y, void *zg,
+                         void *zu, int64_t M, int64_t K, int64_t N, int64_t ldx,
+                         int activation, int dtype, void *stream);
+
+/*
+ * whtmix_gated_backward -- gradients of whtmix_gated_forward:
+ *     dzg = dy zu act'(zg),   dzu = dy act(zg),
+ *     dx = dzg wg^T + dzu wu^T,   dwg = x^T dzg,   dwu = x^T dzu,
+ *     dbg = sum_m dzg,   dbu = sum_m dzu.
+ *   x, wg, wu  as passed forward;  dy [M][N] of `dtype`.
+ *   zg, zu    [M][N] as kept (needed with WHTMIX_ACT_NONE too).
+ *   dx        [M][K] of `dtype`, or NULL to skip.
+ *   dwg, dwu  [K][N] of `dtype`, or both NULL to skip.
+ *   dbg, dbu  [N] float32, or both NULL to skip.
+ * dzg and dzu enter the products rounded to `dtype` (as whtmix_linear_backward's
+ * dz) and the biases' sums unrounded.  Sums over rows are made in a fixed
+ * order.  Workspace: dzg and dzu, partial sums, the weights side by side where
+ * N is not a multiple of 64 (or `dtype` float32), and what the products take.
+ */
+WHTMIX_API int whtmix_gated_backward(const void *x, const void *wg, const void *wu,
+                          const void *dy, const void *zg, const void *zu,
+                          void *dx, void *dwg, void *dwu, float *dbg,
+                          float *dbu, int64_t M, int64_t K, int64_t N,
+                          int64_t ldx, int activation, int dtype, void *stream);
+
+/*
+ * whtmix_gated_mx_forward -- whtmix_gated_forward on block-scaled 8 bits:
+ *   xq, xs    the activations, [M] rows of K values.
+ *   wgq, wgs, wuq, wus  the weights' columns as rows: [N] rows of K values.
+ *   bg, bu    [N] float32, each or NULL.
+ *   y         [M][N] of `dtype`, or NULL with
+ *   yq, ys    the output in block-scaled 8 bits, [M] rows of N values.
+ * Either y or both yq and ys.  Sums as whtmix_linear_mx_forward's.
+ */
+WHTMIX_API int whtmix_gated_mx_forward(const void *xq, const uint8_t *xs,
+                            const void *wgq, const uint8_t *wgs,
+                            const void *wuq, const uint8_t *wus,
+                            const float *bg, const float *bu, void *y, void *yq,
+                            uint8_t *ys, int64_t M, int64_t K, int64_t N,
+                            int activation, int dtype, void *stream);
+
+/* Element type of token ids. */
+typedef enum whtmix_index {
+    WHTMIX_INDEX_I32 = 0,
+    WHTMIX_INDEX_I64 = 1
+} whtmix_index;
+
+/*
+ * whtmix_embedding_forward -- rows of a table by token ids:
+ *     y[n] = scale table[ids[n]].
+ *   ids       [rows] of the type `index`.
+ *   table     [vocab][C] of `dtype`, vocab <= 2^30.
+ *   y         [rows][C] of `dtype`.
+ * A negative id is padding: its row is zeros.  An id of vocab or more names no
+ * row: its row is NaN.  scale is finite.
+ */
+WHTMIX_API int whtmix_embedding_forward(const void *ids, const void *table, void *y,
+                             int64_t rows, int64_t vocab, int64_t C,
+                             double scale, int index, int dtype, void *stream);
+
+/*
+ * whtmix_embedding_backward -- the table's gradient:
+ *     dtable[v] = scale (sum of dy[n] over the n with ids[n] = v).
+ *   ids       [rows] of the type `index`, as passed forward.
+ *   dy        [rows][C] of `dtype`.
+ *   dtable    [vocab][C] of `dtype`: every row is written, zeros where no id
+ *             names it.  Padding and ids of vocab or more have no gradient.
+ * Sums are float32, in an order that ids, rows, vocab and C fix.  Workspace: 16
+ * bytes a token, 2048 bytes for 4096 tokens, and partial sums of C floats for
+ * every 4 to 128 tokens.
+ */
+WHTMIX_API int whtmix_embedding_backward(const void *ids, const void *dy, void *dtable,
+                              int64_t rows, int64_t vocab, int64_t C,
+                              double scale, int index, int dtype, void *stream);
+
 /* Fills *info with the plan whtmix_forward_ex would use.  Validates the
  * shape, dtype and options exactly as the forward call does (pointers are
  * not needed).  Returns a whtmix_status. */

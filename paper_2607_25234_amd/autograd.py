@@ -6,6 +6,9 @@
     y = whtmix_block_separable(x, w_in, log_gain_tokens, log_gain_channels, w_out)
     y, h = whtmix_norm(x, weight, residual)                  # residual's addition and norm
     y = whtmix_linear(x, w, bias, activation, residual)      # feed-forward product
+    y, h = whtmix_layer_norm(x, weight, bias, residual)      # residual's addition and layer norm
+    y = whtmix_gated(x, w_gate, w_up, b_gate, b_up, activation)        # gated product
+    y = whtmix_embedding(ids, table, scale)                  # rows of a table
 
 The forward and backward passes both run in the HIP kernels of libwhtmix.so
 (whtmix_*forward*/whtmix_*backward*); gradients flow to x and to the gains, as
@@ -176,6 +179,70 @@ class WHTMixLinearFunction(torch.autograd.Function):
         return dx, dw, db, None, dy if want[4] else None
 
 
+class WHTMixLayerNormFunction(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, bias, residual, eps):
+        x, weight = _strided_rows(x), weight.contiguous()
+        y, h = whtmix.layer_norm(x, weight, None if bias is None else bias.contiguous(),
+                                 None if residual is None else residual.contiguous(), eps)
+        if residual is None:      # the stream is x itself
+            h = x.contiguous()
+        ctx.save_for_backward(h, weight)
+        ctx.eps, ctx.residual = eps, residual is not None
+        return (y, h) if residual is not None else y
+
+    @staticmethod
+    @_first_order
+    def backward(ctx, dy, dh=None):
+        h, weight = ctx.saved_tensors
+        dx, dw, db = whtmix.layer_norm_backward(h, weight, dy.contiguous(),
+                                                None if dh is None else dh.contiguous(), ctx.eps,
+                                                want_dweight=ctx.needs_input_grad[1],
+                                                want_dbias=ctx.needs_input_grad[2])
+        return dx, dw, db, dx if ctx.residual else None, None
+
+
+class WHTMixGatedFunction(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, w_gate, w_up, b_gate, b_up, activation):
+        x, w_gate, w_up = _strided_rows(x), w_gate.contiguous(), w_up.contiguous()
+        zg = zu = None
+        keep = any(ctx.needs_input_grad)
+        y = whtmix.gated(x, w_gate, w_up, None if b_gate is None else b_gate.contiguous(),
+                         None if b_up is None else b_up.contiguous(), activation, want_z=keep)
+        if keep:
+            y, zg, zu = y
+        ctx.save_for_backward(x, w_gate, w_up, zg, zu)
+        ctx.activation = activation
+        return y
+
+    @staticmethod
+    @_first_order
+    def backward(ctx, dy):
+        x, w_gate, w_up, zg, zu = ctx.saved_tensors
+        want = ctx.needs_input_grad
+        dx, dwg, dwu, dbg, dbu = whtmix.gated_backward(
+            x, w_gate, w_up, dy.contiguous(), zg, zu, ctx.activation, want_dx=want[0],
+            want_dw=want[1] or want[2], want_dbias=want[3] or want[4])
+        return (dx, dwg if want[1] else None, dwu if want[2] else None,
+                dbg if want[3] else None, dbu if want[4] else None, None)
+
+
+class WHTMixEmbeddingFunction(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, ids, table, scale):
+        ids = ids.contiguous()
+        ctx.save_for_backward(ids)
+        ctx.vocab, ctx.scale = table.shape[0], scale
+        return whtmix.embedding(ids, table.contiguous(), scale)
+
+    @staticmethod
+    @_first_order
+    def backward(ctx, dy):
+        ids, = ctx.saved_tensors
+        return None, whtmix.embedding_backward(ids, dy.contiguous(), ctx.vocab, ctx.scale), None
+
+
 def whtmix_norm(x, weight, residual=None, eps: float = 1e-6):
     """Differentiable norm with the residual's addition: (y, h), h = x + residual (x itself
     without one).  weight float32, and its gradient."""
@@ -188,6 +255,26 @@ def whtmix_linear(x, w, bias=None, activation: str = "none", residual=None):
     """Differentiable activation(x w + bias) + residual; dw in w's type, the
     bias and its gradient float32."""
     return WHTMixLinearFunction.apply(x, w, bias, activation, residual)
+
+
+def whtmix_layer_norm(x, weight, bias=None, residual=None, eps: float = 1e-6):
+    """Differentiable layer norm with the residual's addition: (y, h), h = x + residual (x
+    itself without one).  weight and bias float32, and their gradients."""
+    if residual is None:
+        return WHTMixLayerNormFunction.apply(x, weight, bias, None, eps), x
+    return WHTMixLayerNormFunction.apply(x, weight, bias, residual, eps)
+
+
+def whtmix_gated(x, w_gate, w_up, b_gate=None, b_up=None, activation: str = "silu"):
+    """Differentiable activation(x w_gate + b_gate) * (x w_up + b_up); the weights' gradients
+    in their type, the biases and theirs float32."""
+    return WHTMixGatedFunction.apply(x, w_gate, w_up, b_gate, b_up, activation)
+
+
+def whtmix_embedding(ids, table, scale: float = 1.0):
+    """Differentiable scale * table[ids] (negative ids: padding); the table's gradient in its
+    type, every row of it."""
+    return WHTMixEmbeddingFunction.apply(ids, table, scale)
 
 
 def whtmix_block(x, w_in, gain, w_out):

@@ -10,6 +10,14 @@ namespace whtmix {
 // dimension) contiguous.
 enum Layout { K_CONTIGUOUS = 0, K_STRIDED = 1 };
 
+// What a product is beside the plain one:
+//   GATED   two products of the same A, act(A B + bias) o (A B2 + bias2): a tile's columns are the
+//           first's and the second's of the same n, 32 of each a wave, which has both sums of an
+//           output in its registers
+//   HALVES  the columns from `half` on are those of another output, y2; both have half_n
+//   TWO_K   the k from `half` on are those of another B, b2, whose k starts at 0 again
+enum Form { PLAIN = 0, GATED = 1, HALVES = 2, TWO_K = 3 };
+
 // out [M][N] = act(A B + bias) + residual with A [M][K] and B [K][N].
 struct GemmArgs {
     const void *a, *b;
@@ -26,6 +34,13 @@ struct GemmArgs {
     int act;
     float *part;                // split: [splits][M][N] partial sums, or null
     int64_t k_per;              // k of one split
+    const void *b2;             // GATED: like b, bs, ldb, bias and z; TWO_K
+    const uint8_t *bs2;
+    int64_t ldb2, bs2_ld;
+    const float *bias2;
+    void *z2;
+    void *y2;                   // HALVES
+    int64_t half, half_n;
 };
 
 template <typename T>
@@ -184,7 +199,7 @@ template <int N, typename F, int I = 0> __device__ __forceinline__ void static_f
 constexpr int kEpilogueStride = 68;      // floats: rows 4 banks apart
 constexpr int kEpilogueFloats = 32 * kEpilogueStride;
 
-template <typename T, int WM>
+template <typename T, int FORM, int WM>
 __device__ __forceinline__ void finish_wave(const GemmArgs &g, float *lds, int64_t m0, int64_t n0,
                                             int64_t split, const f32x16 (&acc)[WM][2])
 {
@@ -225,6 +240,18 @@ __device__ __forceinline__ void finish_wave(const GemmArgs &g, float *lds, int64
         });
         return;
     }
+    if constexpr (FORM == HALVES) {     // whole chunks of 8 columns on either side
+        const bool second = n >= g.half;
+        const int64_t in = second ? n - g.half : n;
+        const int own = (int)max((int64_t)0, min((int64_t)cnt, g.half_n - in));
+        T *to = (T *)(second ? g.y2 : g.y) + (m0 + (lane >> 3)) * g.half_n + in;
+        each([&](int i, float (&v)[4][8]) __attribute__((always_inline)) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                if (i + 8 * r < rows) store8(to + (int64_t)(i + 8 * r) * g.half_n, own, v[r]);
+        });
+        return;
+    }
     float b[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     if (g.bias) load8(g.bias + n, cnt, b);
     const int64_t at = (m0 + (lane >> 3)) * g.N + n;
@@ -261,57 +288,177 @@ __device__ __forceinline__ void finish_wave(const GemmArgs &g, float *lds, int64
     });
 }
 
+// Eight sums of both products of row m from column n on, to the outputs of a gated product.
+template <typename T, int ACT>
+__device__ __forceinline__ void finish_gated8(const GemmArgs &g, int64_t m, int64_t n, int cnt,
+                                              bool live, float (&v)[8], float (&u)[8])
+{
+    const int64_t at = m * g.N + n;
+    if (live && cnt > 0) {
+        if (g.z) store8((T *)g.z + at, cnt, v);
+        if (g.z2) store8((T *)g.z2 + at, cnt, u);
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = act_of<ACT>(v[k]) * u[k];
+    if (g.y) {
+        if (live && cnt > 0) store8((T *)g.y + at, cnt, v);
+    } else {
+        const int64_t width = (g.N + kMxBlock - 1) / kMxBlock * kMxBlock;
+        store_mx8(v, cnt, live, m, n, width, g.yq, g.ys);
+    }
+}
+
+// A wave's 32 WM x 32 pairs of sums to the outputs of a gated product: as finish_wave, but four
+// lanes a row, each with 8 columns of both.  n0: of the wave's columns.
+template <typename T, int WM>
+__device__ __forceinline__ void finish_gated_wave(const GemmArgs &g, float *lds, int64_t m0,
+                                                  int64_t n0, int64_t split,
+                                                  const f32x16 (&acc)[WM][2])
+{
+    const int lane = threadIdx.x & 63;
+    float *w = lds + (lane & 31) * kEpilogueStride + (lane >> 5) * 4;
+    // 16 lanes, a cycle of an LDS read, take rows 0, 1, 8 and 9 of 16 (and so on): 16 different
+    // groups of 4 banks.
+    const int row = (lane >> 2 & 1) | (lane >> 4) << 1 | (lane >> 3 & 1) << 3;
+    const float *p = lds + row * kEpilogueStride + (lane & 3) * 8;
+    const int64_t n = n0 + (lane & 3) * 8;
+    const int cnt = (int)max((int64_t)0, min((int64_t)8, g.N - n));
+    const int rows = (int)min((int64_t)(32 * WM), g.M - m0) - row;     // left for this lane
+    auto each = [&](auto f) __attribute__((always_inline)) {
+        static_for<WM>([&](auto part) __attribute__((always_inline)) {
+            constexpr int I = decltype(part)::value;
+            wave_lds_fence();
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+                    *(f32x4 *)(w + 32 * j + 8 * r) =
+                        (f32x4){acc[I][j][4 * r], acc[I][j][4 * r + 1], acc[I][j][4 * r + 2],
+                                acc[I][j][4 * r + 3]};
+            wave_lds_fence();
+            float v[2][8], u[2][8];
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                const float *q = p + 16 * r * kEpilogueStride;
+                *(f32x4 *)v[r] = *(const f32x4 *)q;
+                *(f32x4 *)(v[r] + 4) = *(const f32x4 *)(q + 4);
+                *(f32x4 *)u[r] = *(const f32x4 *)(q + 32);
+                *(f32x4 *)(u[r] + 4) = *(const f32x4 *)(q + 36);
+            }
+            f(32 * I, v, u);
+        });
+    };
+    if (g.part) {       // [splits][2][M][N]
+        float *to = g.part + (2 * split * g.M + m0 + row) * g.N + n;
+        each([&](int i, float (&v)[2][8], float (&u)[2][8]) __attribute__((always_inline)) {
+#pragma unroll
+            for (int r = 0; r < 2; ++r)
+                if (i + 16 * r < rows) {
+                    store8(to + (int64_t)(i + 16 * r) * g.N, cnt, v[r]);
+                    store8(to + (i + 16 * r + g.M) * g.N, cnt, u[r]);
+                }
+        });
+        return;
+    }
+    float b[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    float b2[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if (g.bias) load8(g.bias + n, cnt, b);
+    if (g.bias2) load8(g.bias2 + n, cnt, b2);
+    if (n0 >= (g.N + kMxBlock - 1) / kMxBlock * kMxBlock) return;
+    with_act(g.act, [&](auto act) __attribute__((always_inline)) {
+        constexpr int ACT = decltype(act)::value;
+        each([&](int i, float (&v)[2][8], float (&u)[2][8]) __attribute__((always_inline)) {
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) v[r][k] += b[k], u[r][k] += b2[k];
+                finish_gated8<T, ACT>(g, m0 + row + i + 16 * r, n, cnt, i + 16 * r < rows, v[r],
+                                      u[r]);
+            }
+        });
+    });
+}
+
 // Adds the parts' partial sums and finishes them: eight columns a thread, and where the parts
 // are many, the workgroup's threads in GROUPS that take every GROUPS-th part, whose sums are
 // then added in order.  A launch and the parts' loads: 4-5 us for one row of 16384 or 17 of 4096,
 // 10 us for 3001 x 1000 float32.
-template <typename T, int GROUPS>
+template <typename T, int FORM, int GROUPS>
 __global__ void __launch_bounds__(256) split_sum_kernel(GemmArgs g, int splits)
 {
-    constexpr int kChunks = 256 / GROUPS;
-    __shared__ float sums[GROUPS > 1 ? GROUPS : 1][GROUPS > 1 ? kChunks : 1][9];
+    constexpr int kChunks = 256 / GROUPS, P = FORM == GATED ? 2 : 1;
+    __shared__ float sums[GROUPS > 1 ? GROUPS : 1][GROUPS > 1 ? kChunks : 1][8 * P + 1];
     const int64_t width = g.yq ? (g.N + kMxBlock - 1) / kMxBlock * kMxBlock : (g.N + 7) / 8 * 8;
     const int c = threadIdx.x % kChunks, first = threadIdx.x / kChunks;
     const int64_t i = ((int64_t)blockIdx.x * kChunks + c) * 8;
     const int64_t m = i / width, n = i - m * width;
     const int cnt = m < g.M ? (int)max((int64_t)0, min((int64_t)8, g.N - n)) : 0;
     const float *from = g.part + (m < g.M ? m * g.N + n : 0);
-    float v[8];
+    float v[P][8];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = 0.f;
+    for (int q = 0; q < P; ++q)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[q][k] = 0.f;
     for (int s = first; s < splits; s += 4 * GROUPS) {       // four parts' loads in flight
-        float p[4][8];
-#pragma unroll
-        for (int u = 0; u < 4; ++u)
-            load8(from + (int64_t)min(s + u * GROUPS, splits - 1) * g.M * g.N,
-                  s + u * GROUPS < splits ? cnt : 0, p[u]);
+        float p[4][P][8];
 #pragma unroll
         for (int u = 0; u < 4; ++u)
 #pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] += p[u][k];
+            for (int q = 0; q < P; ++q)
+                load8(from + (int64_t)(min(s + u * GROUPS, splits - 1) * P + q) * g.M * g.N,
+                      s + u * GROUPS < splits ? cnt : 0, p[u][q]);
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int q = 0; q < P; ++q)
+#pragma unroll
+                for (int k = 0; k < 8; ++k) v[q][k] += p[u][q][k];
     }
     if constexpr (GROUPS > 1) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) sums[first][c][k] = v[k];
+        for (int q = 0; q < P; ++q)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) sums[first][c][8 * q + k] = v[q][k];
         __syncthreads();
         if (first > 0) return;
 #pragma unroll
         for (int f = 1; f < GROUPS; ++f)
 #pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] += sums[f][c][k];
+            for (int q = 0; q < P; ++q)
+#pragma unroll
+                for (int k = 0; k < 8; ++k) v[q][k] += sums[f][c][8 * q + k];
     }
-    if (m < g.M) finish8<T>(g, m, n, v);    // 8-bit output: the four lanes of a block together
+    if (m >= g.M) return;
+    // 8-bit output: the four lanes of a block together
+    if constexpr (FORM == GATED) {
+        float b[8], b2[8];
+        load8(g.bias ? g.bias + n : g.part, g.bias ? cnt : 0, b);
+        load8(g.bias2 ? g.bias2 + n : g.part, g.bias2 ? cnt : 0, b2);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[0][k] += b[k], v[1][k] += b2[k];
+        with_act(g.act, [&](auto act) {
+            finish_gated8<T, decltype(act)::value>(g, m, n, cnt, true, v[0], v[1]);
+        });
+    } else if constexpr (FORM == HALVES) {
+        const bool second = n >= g.half;
+        const int64_t in = second ? n - g.half : n;
+        store8((T *)(second ? g.y2 : g.y) + m * g.half_n + in,
+               (int)max((int64_t)0, min((int64_t)cnt, g.half_n - in)), v[0]);
+    } else {
+        finish8<T>(g, m, n, v[0]);
+    }
 }
 
-template <typename T> hipError_t launch_split_sum(const GemmArgs &g, int splits, hipStream_t stream)
+template <typename T, int FORM>
+hipError_t launch_split_sum(const GemmArgs &g, int splits, hipStream_t stream)
 {
     const int64_t width = g.yq ? mx_width(g.N) : (g.N + 7) / 8 * 8, chunks = g.M * width / 8;
     // 16 parts and more of an output that does not fill the device: 8 threads a chunk
     // (65536 sums of 128 parts: 33 us with one)
     if (splits >= 16 && chunks <= 1 << 16)
-        split_sum_kernel<T, 8><<<dim3((uint32_t)((chunks + 31) / 32)), dim3(256), 0, stream>>>(g, splits);
+        split_sum_kernel<T, FORM, 8><<<dim3((uint32_t)((chunks + 31) / 32)), dim3(256), 0, stream>>>(g, splits);
     else
-        split_sum_kernel<T, 1><<<dim3((uint32_t)((chunks + 255) / 256)), dim3(256), 0, stream>>>(g, splits);
+        split_sum_kernel<T, FORM, 1><<<dim3((uint32_t)((chunks + 255) / 256)), dim3(256), 0, stream>>>(g, splits);
     return hipGetLastError();
 }
 
@@ -321,6 +468,15 @@ uint64_t gemm_bf16_bytes(const GemmArgs &g, Layout la, Layout lb);
 hipError_t gemm_bf16(GemmArgs g, Layout la, Layout lb, void *ws, hipStream_t stream);
 uint64_t gemm_f32_bytes(const GemmArgs &g);
 hipError_t gemm_f32(const GemmArgs &g, Layout la, Layout lb, void *ws, hipStream_t stream);
+// The other forms (whtmix_gated_bf16.hip, whtmix_linear_f32.hip, whtmix_gated_mx.hip): GATED with
+// K_CONTIGUOUS a and K_STRIDED b, HALVES with both K_STRIDED, TWO_K (bf16, whole steps of k and
+// aligned operands) with both K_CONTIGUOUS.
+uint64_t gemm_bf16_bytes(const GemmArgs &g, Form form);
+hipError_t gemm_bf16(GemmArgs g, Form form, void *ws, hipStream_t stream);
+uint64_t gemm_f32_bytes(const GemmArgs &g, Form form);
+hipError_t gemm_f32(const GemmArgs &g, Form form, void *ws, hipStream_t stream);
+uint64_t gated_mx_gemm_bytes(const GemmArgs &g);
+hipError_t gated_mx_gemm(GemmArgs g, int dtype, void *ws, hipStream_t stream);
 // dz, its columns' partial sums (dzx_parts rows, or null) and dx in one kernel
 // (whtmix_linear_dzx.hip), for calls that it takes.
 bool dzx_takes(const LinearBackwardArgs &a);

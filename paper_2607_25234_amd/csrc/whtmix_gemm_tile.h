@@ -51,6 +51,7 @@ template <int EB, Layout L, int R, int NW> struct Operand {
         // A cycle of an LDS read serves 16 lanes: 16 rows of 128 bytes fall on all 64 banks
         // when every second row's chunks are permuted alike.
         if constexpr (L == K_CONTIGUOUS) return chunk ^ ((outer >> 1) & 7);
+        else if constexpr (kRowChunks == 8) return chunk ^ (2 * outer & 4);   // two k on all banks
         else return chunk ^ ((4 * (outer & 3)) & (kRowChunks - 1));
     }
     // The (row or k, chunk) that copy i of this lane fetches.
@@ -171,7 +172,7 @@ __device__ __forceinline__ bf16x8 fragment_exact(const char *lds, uint32_t s, in
 // Block scales of a step, a dword a row (bytes of 32 k each), copied to LDS like the rest:
 // the tile's rows of both operands in order, 64 a wave's copy.  Rows of scales are whole
 // dwords, and those past the operands' ends repeat the last.
-template <int BM, int BN, int NT> struct Scales {
+template <int BM, int BN, int NT, int FORM> struct Scales {
     static constexpr int kCopies = (BM + BN + NT - 1) / NT;
     static constexpr int kBytes = kCopies * NT * 4;
     const char *p[kCopies];
@@ -181,6 +182,14 @@ template <int BM, int BN, int NT> struct Scales {
         for (int i = 0; i < kCopies; ++i) {
             const int r = i * NT + (int)threadIdx.x;
             const bool b = r >= BM;
+            if constexpr (FORM == GATED) {      // the first's columns, then the second's
+                const bool second = r >= BM + BN / 2;
+                const int64_t row = b ? min(n0 + (r - BM) % (BN / 2), g.N - 1) : min(m0 + r, g.M - 1);
+                p[i] = (const char *)(second ? g.bs2 + row * g.bs2_ld
+                                             : b ? g.bs + row * g.bs_ld : g.as + row * g.as_ld) +
+                       k0 / kMxBlock;
+                continue;
+            }
             const int64_t row = b ? min(n0 + r - BM, g.N - 1) : min(m0 + r, g.M - 1);
             p[i] = (const char *)(b ? g.bs + row * g.bs_ld : g.as + row * g.as_ld) + k0 / kMxBlock;
         }
@@ -197,8 +206,8 @@ template <int BM, int BN, int NT> struct Scales {
 };
 
 // EXACT: block-scaled values multiplied as bf16 (see gemm_mx).
-template <int EB, bool EXACT, typename T, Layout LA, Layout LB, int BM, int BN, int WAVES_M,
-          int WAVES_N>
+template <int EB, bool EXACT, typename T, int FORM, Layout LA, Layout LB, int BM, int BN,
+          int WAVES_M, int WAVES_N>
 __global__ void __launch_bounds__(64 * WAVES_M *WAVES_N)
     gemm_tile_kernel(GemmArgs g, uint32_t tiles_m, uint32_t tiles_n)
 {
@@ -206,7 +215,7 @@ __global__ void __launch_bounds__(64 * WAVES_M *WAVES_N)
     constexpr int WM = BM / WAVES_M / 32, WN = BN / WAVES_N / 32;
     static_assert(WN == 2, "a wave's epilogue takes 64 columns");
     constexpr int kA = BM * kStepBytes, kB = BN * kStepBytes;
-    constexpr int kScales = EB == 1 ? Scales<BM, BN, NT>::kBytes : 0;
+    constexpr int kScales = EB == 1 ? Scales<BM, BN, NT, FORM>::kBytes : 0;
     constexpr int kBuffer = kA + kB + kScales;
     constexpr int kEpilogue = NW * kEpilogueFloats * 4;
     __shared__ __attribute__((aligned(1024))) char lds[2 * kBuffer > kEpilogue ? 2 * kBuffer
@@ -216,9 +225,11 @@ __global__ void __launch_bounds__(64 * WAVES_M *WAVES_N)
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     uint32_t tm, tn, split;
     place_tile(blockIdx.x, gridDim.x, tiles_m, tiles_n, tm, tn, split);
-    const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * BN;
+    // B's tile, or GATED both B's, one after the other, of as many columns each.
+    constexpr int NB = FORM == GATED ? 2 : 1, BC = BN / NB;
+    const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * BC;
     const int64_t kbeg = (int64_t)split * g.k_per, kend = min(g.K, kbeg + g.k_per);
-    const int wm = (wave % WAVES_M) * (WM * 32), wn = (wave / WAVES_M) * (WN * 32);
+    const int wm = (wave % WAVES_M) * (WM * 32), wn = (wave / WAVES_M) * (WN * 32 / NB);
 
     f32x16 acc[WM][WN];
 #pragma unroll
@@ -229,22 +240,37 @@ __global__ void __launch_bounds__(64 * WAVES_M *WAVES_N)
             for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
 
     Operand<EB, LA, BM, NW> oa;
-    Operand<EB, LB, BN, NW> ob;
+    Operand<EB, LB, BC, NW> ob[NB];
     oa.init(g.a, g.lda, g.a_rows, m0, kbeg, LA == K_CONTIGUOUS ? min(kend, g.a_k) : min(kend, g.K));
-    ob.init(g.b, g.ldb, g.b_rows, n0, kbeg, LB == K_CONTIGUOUS ? min(kend, g.b_k) : min(kend, g.K));
-    Scales<BM, BN, NT> sc;
+    const int64_t b_end = LB == K_CONTIGUOUS ? min(kend, g.b_k) : min(kend, g.K);
+    int to_second = 0;          // TWO_K: steps until the second B
+    if constexpr (FORM == TWO_K) {
+        const bool second = kbeg >= g.half;
+        ob[0].init(second ? g.b2 : g.b, g.ldb, g.b_rows, n0, second ? kbeg - g.half : kbeg, kend);
+        to_second = second ? 0 : (int)((g.half - kbeg) / kStepK);
+    } else {
+        ob[0].init(g.b, g.ldb, g.b_rows, n0, kbeg, b_end);
+        if constexpr (FORM == GATED) ob[1].init(g.b2, g.ldb2, g.b_rows, n0, kbeg, b_end);
+    }
+    Scales<BM, BN, NT, FORM> sc;
     const int steps = (int)((kend - kbeg + kStepK - 1) / kStepK);
     const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
     const uint32_t lds_wave = lds_base + (uint32_t)__builtin_amdgcn_readfirstlane(wave) * 1024;
     // Step t's copies in kCopies pieces (the scales' loads with the first).
     constexpr int kCopiesA = Operand<EB, LA, BM, NW>::kCopies;
-    constexpr int kCopies = kCopiesA + Operand<EB, LB, BN, NW>::kCopies;
+    constexpr int kCopiesB = Operand<EB, LB, BC, NW>::kCopies, kCopies = kCopiesA + NB * kCopiesB;
     auto copy_piece = [&](int t, int i) __attribute__((always_inline)) {
         const uint32_t to = lds_wave + (t & 1) * kBuffer;
         if (EB == 1 && i == 0) sc.copy(lds_base + (t & 1) * kBuffer + kA + kB);
         if (i < kCopiesA) oa.copy_one(to, i);
-        else ob.copy_one(to + kA, i - kCopiesA);
-        if (i == kCopies - 1) oa.copied(), ob.copied();
+        else if (i < kCopiesA + kCopiesB) ob[0].copy_one(to + kA, i - kCopiesA);
+        else ob[NB - 1].copy_one(to + kA + kB / NB, i - kCopiesA - kCopiesB);
+        if (i == kCopies - 1) {
+            oa.copied(), ob[0].copied();
+            if constexpr (FORM == GATED) ob[1].copied();
+            if constexpr (FORM == TWO_K)
+                if (--to_second == 0) ob[0].base = (const char *)g.b2 + n0 * g.ldb * EB;
+        }
     };
     auto copy = [&](int t) __attribute__((always_inline)) {
 #pragma unroll
@@ -255,8 +281,11 @@ __global__ void __launch_bounds__(64 * WAVES_M *WAVES_N)
         const int64_t k = kbeg + (int64_t)t * kStepK;
         if constexpr (EB == 1) sc.copy(lds_base + (t & 1) * kBuffer + kA + kB);
         oa.copy_last(to, k);
-        ob.copy_last(to + kA, k);
+        ob[0].copy_last(to + kA, k);
+        if constexpr (FORM == GATED) ob[1].copy_last(to + kA + kB / 2, k);
     };
+    // Where a wave's j-th 32 columns are in B's tile.
+    auto column = [&](int j) __attribute__((always_inline)) { return wn + (NB == 1 ? 32 * j : 0); };
     constexpr int kParts = EB == 2 ? 4 : EXACT ? 8 : 2;
     using Fragment = std::conditional_t<EB == 1 && !EXACT, i32x8, bf16x8>;
     // Two sets of fragments where the registers hold them: a part's products run on one while
@@ -271,18 +300,18 @@ __global__ void __launch_bounds__(64 * WAVES_M *WAVES_N)
             const uint32_t *s = (const uint32_t *)(lds + (t & 1) * kBuffer + kA + kB);
             const int shift = EXACT ? 0 : (lane >> 5) * 8;
 #pragma unroll
-            for (int j = 0; j < WN; ++j) sb[j] = s[BM + wn + 32 * j + (lane & 31)] >> shift;
+            for (int j = 0; j < WN; ++j) sb[j] = s[BM + (NB - 1) * j * BC + column(j) + (lane & 31)] >> shift;
 #pragma unroll
             for (int i = 0; i < WM; ++i) sa[i] = s[wm + 32 * i + (lane & 31)] >> shift;
         }
     };
     // Fragments of part kk of step t.
     auto read_b = [&](int t, int kk, int j) __attribute__((always_inline)) {
-        const char *here = lds + (t & 1) * kBuffer + kA;
+        const char *here = lds + (t & 1) * kBuffer + kA + (NB - 1) * j * (kB / 2);
         Fragment &f = fb[kk % kSets][j];
-        if constexpr (EB == 2) f = fragment16<LB, BN>(here, wn + 32 * j, kk);
-        else if constexpr (EXACT) f = fragment_exact<BN>(here, sb[j], wn + 32 * j, kk);
-        else f = fragment64<BN>(here, wn + 32 * j, kk);
+        if constexpr (EB == 2) f = fragment16<LB, BC>(here, column(j), kk);
+        else if constexpr (EXACT) f = fragment_exact<BC>(here, sb[j], column(j), kk);
+        else f = fragment64<BC>(here, column(j), kk);
     };
     auto read_a = [&](int t, int kk, int i) __attribute__((always_inline)) {
         const char *here = lds + (t & 1) * kBuffer;
@@ -344,7 +373,7 @@ __global__ void __launch_bounds__(64 * WAVES_M *WAVES_N)
     if (steps > 1) {
         if (steps > 2) copy(1);
         else copy_last(1);
-        wait_copies<kCopies + (EB == 1 ? Scales<BM, BN, NT>::kCopies : 0)>();
+        wait_copies<kCopies + (EB == 1 ? Scales<BM, BN, NT, FORM>::kCopies : 0)>();
     } else {
         wait_copies<0>();
     }
@@ -374,7 +403,8 @@ __global__ void __launch_bounds__(64 * WAVES_M *WAVES_N)
     static_for<kParts>([&](auto part) __attribute__((always_inline)) { multiply(part, t, nothing); });
     __syncthreads();
     float *out = (float *)lds + wave * kEpilogueFloats;
-    finish_wave<T>(g, out, m0 + wm, n0 + wn, split, acc);
+    if constexpr (FORM == GATED) finish_gated_wave<T>(g, out, m0 + wm, n0 + wn, split, acc);
+    else finish_wave<T, FORM>(g, out, m0 + wm, n0 + wn, split, acc);
 }
 
 // ---- shapes of tiles and splits of k ----
@@ -421,24 +451,24 @@ inline uint64_t tile_part_bytes(int64_t M, int64_t N, int64_t K, int step_k)
     return p.splits > 1 ? (uint64_t)p.splits * M * N * 4 : 0;
 }
 
-template <int EB, bool EXACT, typename T, Layout LA, Layout LB>
+template <int EB, bool EXACT, typename T, Layout LA, Layout LB, int FORM = PLAIN>
 hipError_t run_tiles(GemmArgs g, float *part, hipStream_t stream)
 {
-    const TilePlan p = plan_tiles(g.M, g.N, g.K, kStepBytes / EB);
+    const TilePlan p = plan_tiles(g.M, FORM == GATED ? 2 * g.N : g.N, g.K, kStepBytes / EB);
     g.k_per = p.k_per;
     g.part = p.splits > 1 ? part : nullptr;
     const dim3 grid(p.tiles_m * p.tiles_n * (uint32_t)p.splits);
     if (p.bm == 32)
-        gemm_tile_kernel<EB, EXACT, T, LA, LB, 32, 256, 1, 4><<<grid, 256, 0, stream>>>(g, p.tiles_m, p.tiles_n);
+        gemm_tile_kernel<EB, EXACT, T, FORM, LA, LB, 32, 256, 1, 4><<<grid, 256, 0, stream>>>(g, p.tiles_m, p.tiles_n);
     else if (p.bm == 64)
-        gemm_tile_kernel<EB, EXACT, T, LA, LB, 64, 256, 1, 4><<<grid, 256, 0, stream>>>(g, p.tiles_m, p.tiles_n);
+        gemm_tile_kernel<EB, EXACT, T, FORM, LA, LB, 64, 256, 1, 4><<<grid, 256, 0, stream>>>(g, p.tiles_m, p.tiles_n);
     else if (p.bm == 256)
-        gemm_tile_kernel<EB, EXACT, T, LA, LB, 256, 256, 2, 4><<<grid, 512, 0, stream>>>(g, p.tiles_m, p.tiles_n);
+        gemm_tile_kernel<EB, EXACT, T, FORM, LA, LB, 256, 256, 2, 4><<<grid, 512, 0, stream>>>(g, p.tiles_m, p.tiles_n);
     else
-        gemm_tile_kernel<EB, EXACT, T, LA, LB, 128, 128, 2, 2><<<grid, 256, 0, stream>>>(g, p.tiles_m, p.tiles_n);
+        gemm_tile_kernel<EB, EXACT, T, FORM, LA, LB, 128, 128, 2, 2><<<grid, 256, 0, stream>>>(g, p.tiles_m, p.tiles_n);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.splits == 1) return e;
-    return launch_split_sum<T>(g, p.splits, stream);
+    return launch_split_sum<T, FORM>(g, p.splits, stream);
 }
 
 }  // namespace whtmix

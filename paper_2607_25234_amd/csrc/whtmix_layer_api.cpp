@@ -14,6 +14,7 @@ using whtmix::mx_width;
 
 constexpr int64_t kMaxRows = int64_t(1) << 30;
 constexpr int64_t kMaxWidth = int64_t(1) << 22;
+constexpr int64_t kMaxGated = kMaxWidth / 2;    // both halves of a row of the gradients
 
 struct Range {
     const void *p;
@@ -121,6 +122,45 @@ int norm_impl(const void *x, const void *residual, const float *weight, bool mx,
     const whtmix::NormArgs a{x, residual, weight, y, h, q, scales, rows, C, ldx, (float)eps,
                              dtype, static_cast<hipStream_t>(stream)};
     return done(whtmix::launch_norm(a), mx ? "norm in 8 bits" : "norm");
+}
+
+int layer_norm_impl(const void *x, const void *residual, const float *weight, const float *bias,
+                    bool mx, void *y, void *q, uint8_t *scales, void *h, int64_t rows, int64_t C,
+                    int64_t ldx, double eps, int dtype, void *stream)
+{
+    int st = check_dtype(dtype);
+    if (st == WHTMIX_SUCCESS) st = check_sizes(rows, {C}, ldx, C);
+    if (st != WHTMIX_SUCCESS) return st;
+    if (bad_eps(eps)) return WHTMIX_ERROR_INVALID_VALUE;
+    if (rows == 0) return WHTMIX_SUCCESS;
+    if (!x || !weight || (mx ? !q || !scales : !y)) return WHTMIX_ERROR_INVALID_VALUE;
+    const uint64_t e = elt(dtype);
+    if (!aligned({x, residual, y, h}, e) || !aligned({weight, bias}, 4) || !aligned({q}, 16))
+        return WHTMIX_ERROR_MISALIGNED;
+    const Range rx{x, span(rows, C, ldx, e)}, rr{residual, span(rows, C, C, e)},
+        rw{weight, (uint64_t)C * 4}, rb{bias, (uint64_t)C * 4}, ry{y, span(rows, C, C, e)},
+        rh{h, span(rows, C, C, e)}, rq{q, (uint64_t)rows * mx_width(C)},
+        rs{scales, (uint64_t)rows * (mx_width(C) / whtmix::kMxBlock)};
+    const bool same_y = y == x && ldx == C, h_x = h == x && ldx == C, h_r = h == residual;
+    if (!apart(ry, {rr, rw, rb, rh}) || (!same_y && overlap(ry, rx)) ||
+        !apart(rh, {rw, rb, rq, rs}) || (!h_x && overlap(rh, rx)) || (!h_r && overlap(rh, rr)) ||
+        !apart(rq, {rx, rr, rw, rb, rs}) || !apart(rs, {rx, rr, rw, rb}))
+        return WHTMIX_ERROR_INVALID_VALUE;
+    const whtmix::LayerNormArgs a{x, residual, weight, bias, y, h, q, scales, rows, C, ldx,
+                                  (float)eps, dtype, static_cast<hipStream_t>(stream)};
+    return done(whtmix::launch_layer_norm(a), mx ? "layer norm in 8 bits" : "layer norm");
+}
+
+// The arguments that both directions of the embedding share.
+int check_embedding(int64_t rows, int64_t vocab, int64_t C, double scale, int index, int dtype)
+{
+    int st = check_dtype(dtype);
+    if (st == WHTMIX_SUCCESS && index != WHTMIX_INDEX_I32 && index != WHTMIX_INDEX_I64)
+        st = WHTMIX_ERROR_UNSUPPORTED_DTYPE;
+    if (st == WHTMIX_SUCCESS) st = check_sizes(rows, {C}, C, C);
+    if (st != WHTMIX_SUCCESS) return st;
+    if (vocab < 1 || !std::isfinite((float)scale)) return WHTMIX_ERROR_INVALID_VALUE;
+    return vocab > kMaxRows ? WHTMIX_ERROR_TOO_LARGE : WHTMIX_SUCCESS;
 }
 
 int check_act(int act)
@@ -308,6 +348,216 @@ int whtmix_linear_mx_forward(const void *xq, const uint8_t *xs, const void *wq, 
                               [&](float *p) {
                                   a.ws = p;
                                   return whtmix::launch_linear_mx(a);
+                              });
+    });
+}
+
+int whtmix_layer_norm_forward(const void *x, const void *residual, const float *weight,
+                              const float *bias, void *y, void *h, int64_t rows, int64_t C,
+                              int64_t ldx, double eps, int dtype, void *stream)
+{
+    return guarded([&] {
+        return layer_norm_impl(x, residual, weight, bias, false, y, nullptr, nullptr, h, rows, C,
+                               ldx, eps, dtype, stream);
+    });
+}
+
+int whtmix_layer_norm_mx_forward(const void *x, const void *residual, const float *weight,
+                                 const float *bias, void *q, uint8_t *scales, void *h, int64_t rows,
+                                 int64_t C, int64_t ldx, double eps, int dtype, void *stream)
+{
+    return guarded([&] {
+        return layer_norm_impl(x, residual, weight, bias, true, nullptr, q, scales, h, rows, C, ldx,
+                               eps, dtype, stream);
+    });
+}
+
+int whtmix_layer_norm_backward(const void *h, const float *weight, const void *dy, const void *dh,
+                               void *dx, float *dweight, float *dbias, int64_t rows, int64_t C,
+                               double eps, int dtype, void *stream)
+{
+    return guarded([&]() -> int {
+        int st = check_dtype(dtype);
+        if (st == WHTMIX_SUCCESS) st = check_sizes(rows, {C}, C, C);
+        if (st != WHTMIX_SUCCESS) return st;
+        if (bad_eps(eps)) return WHTMIX_ERROR_INVALID_VALUE;
+        const hipStream_t s = static_cast<hipStream_t>(stream);
+        const uint64_t e = elt(dtype);
+        if (!aligned({h, dy, dh, dx}, e) || !aligned({weight, dweight, dbias}, 4))
+            return WHTMIX_ERROR_MISALIGNED;
+        if (rows == 0) {
+            hipError_t er = hipSuccess;
+            if (dweight) er = whtmix::launch_zero(dweight, (uint64_t)C * 4, s);
+            if (dbias && er == hipSuccess) er = whtmix::launch_zero(dbias, (uint64_t)C * 4, s);
+            return done(er, "layer norm backward");
+        }
+        if (!h || !weight || !dy || !dx) return WHTMIX_ERROR_INVALID_VALUE;
+        const uint64_t n = span(rows, C, C, e);
+        const Range rx{dx, n}, rw{dweight, (uint64_t)C * 4}, rb{dbias, (uint64_t)C * 4}, rh{h, n},
+            ry{dy, n}, rd{dh, n}, rg{weight, (uint64_t)C * 4};
+        if (!apart(rx, {rh, rg, rw, rb}) || (dx != dy && overlap(rx, ry)) ||
+            (dx != dh && overlap(rx, rd)) || !apart(rw, {rh, ry, rd, rg, rb}) ||
+            !apart(rb, {rh, ry, rd, rg}))
+            return WHTMIX_ERROR_INVALID_VALUE;
+        const uint64_t floats =
+            whtmix::layer_norm_backward_floats(rows, C, dtype, dweight || dbias);
+        return with_workspace(stream, floats * 4, "layer norm backward", [&](float *ws) {
+            const whtmix::LayerNormBackwardArgs a{h, weight, dy, dh, dx, dweight, dbias, ws, rows, C,
+                                                  (float)eps, dtype, s};
+            return whtmix::launch_layer_norm_backward(a);
+        });
+    });
+}
+
+int whtmix_gated_forward(const void *x, const void *wg, const void *wu, const float *bg,
+                         const float *bu, void *y, void *zg, void *zu, int64_t M, int64_t K,
+                         int64_t N, int64_t ldx, int activation, int dtype, void *stream)
+{
+    return guarded([&]() -> int {
+        int st = check_dtype(dtype);
+        if (st == WHTMIX_SUCCESS) st = check_sizes(M, {K, N}, ldx, K);
+        if (st == WHTMIX_SUCCESS) st = check_act(activation);
+        if (st == WHTMIX_SUCCESS && N > kMaxGated) st = WHTMIX_ERROR_TOO_LARGE;
+        if (st != WHTMIX_SUCCESS || M == 0) return st;
+        if (!x || !wg || !wu || !y) return WHTMIX_ERROR_INVALID_VALUE;
+        const uint64_t e = elt(dtype);
+        if (!aligned({x, wg, wu, y, zg, zu}, e) || !aligned({bg, bu}, 4))
+            return WHTMIX_ERROR_MISALIGNED;
+        const uint64_t out = span(M, N, N, e), w = span(K, N, N, e), b = (uint64_t)N * 4;
+        const Range rx{x, span(M, K, ldx, e)}, rg{wg, w}, ru{wu, w}, rbg{bg, b}, rbu{bu, b},
+            ry{y, out}, rzg{zg, out}, rzu{zu, out};
+        if (!apart(ry, {rx, rg, ru, rbg, rbu, rzg, rzu}) ||
+            !apart(rzg, {rx, rg, ru, rbg, rbu, rzu}) || !apart(rzu, {rx, rg, ru, rbg, rbu}))
+            return WHTMIX_ERROR_INVALID_VALUE;
+        whtmix::GatedArgs a{x, wg, wu, bg, bu, y, zg, zu, M, K, N, ldx, activation, dtype, nullptr,
+                            static_cast<hipStream_t>(stream)};
+        return with_workspace(stream, whtmix::gated_bytes(a), "gated", [&](float *ws) {
+            a.ws = ws;
+            return whtmix::launch_gated(a);
+        });
+    });
+}
+
+int whtmix_gated_backward(const void *x, const void *wg, const void *wu, const void *dy,
+                          const void *zg, const void *zu, void *dx, void *dwg, void *dwu,
+                          float *dbg, float *dbu, int64_t M, int64_t K, int64_t N, int64_t ldx,
+                          int activation, int dtype, void *stream)
+{
+    return guarded([&]() -> int {
+        int st = check_dtype(dtype);
+        if (st == WHTMIX_SUCCESS) st = check_sizes(M, {K, N}, ldx, K);
+        if (st == WHTMIX_SUCCESS) st = check_act(activation);
+        if (st == WHTMIX_SUCCESS && N > kMaxGated) st = WHTMIX_ERROR_TOO_LARGE;
+        if (st != WHTMIX_SUCCESS) return st;
+        if ((!dx && !dwg && !dbg) || !dwg != !dwu || !dbg != !dbu)
+            return WHTMIX_ERROR_INVALID_VALUE;
+        const uint64_t e = elt(dtype);
+        if (!aligned({x, wg, wu, dy, zg, zu, dx, dwg, dwu}, e) || !aligned({dbg, dbu}, 4))
+            return WHTMIX_ERROR_MISALIGNED;
+        const hipStream_t s = static_cast<hipStream_t>(stream);
+        if (M == 0) {
+            hipError_t er = hipSuccess;
+            for (void *p : {dwg, dwu})
+                if (p && er == hipSuccess) er = whtmix::launch_zero(p, (uint64_t)K * N * e, s);
+            for (float *p : {dbg, dbu})
+                if (p && er == hipSuccess) er = whtmix::launch_zero(p, (uint64_t)N * 4, s);
+            return done(er, "gated backward");
+        }
+        if (!dy || !zg || !zu || (dx && (!wg || !wu)) || (dwg && !x))
+            return WHTMIX_ERROR_INVALID_VALUE;
+        const uint64_t out = span(M, N, N, e), w = span(K, N, N, e), b = (uint64_t)N * 4;
+        const Range rx{x, span(M, K, ldx, e)}, rg{wg, w}, ru{wu, w}, ry{dy, out}, rzg{zg, out},
+            rzu{zu, out}, ox{dx, span(M, K, K, e)}, og{dwg, w}, ou{dwu, w}, obg{dbg, b},
+            obu{dbu, b};
+        if (!apart(ox, {rx, rg, ru, ry, rzg, rzu, og, ou, obg, obu}) ||
+            !apart(og, {rx, rg, ru, ry, rzg, rzu, ou, obg, obu}) ||
+            !apart(ou, {rx, rg, ru, ry, rzg, rzu, obg, obu}) ||
+            !apart(obg, {rx, rg, ru, ry, rzg, rzu, obu}) || !apart(obu, {rx, rg, ru, ry, rzg, rzu}))
+            return WHTMIX_ERROR_INVALID_VALUE;
+        whtmix::GatedBackwardArgs a{x, wg, wu, dy, zg, zu, dx, dwg, dwu, dbg, dbu, M, K, N, ldx,
+                                    activation, dtype, nullptr, s};
+        return with_workspace(stream, whtmix::gated_backward_bytes(a), "gated backward",
+                              [&](float *ws) {
+                                  a.ws = ws;
+                                  return whtmix::launch_gated_backward(a);
+                              });
+    });
+}
+
+int whtmix_gated_mx_forward(const void *xq, const uint8_t *xs, const void *wgq, const uint8_t *wgs,
+                            const void *wuq, const uint8_t *wus, const float *bg, const float *bu,
+                            void *y, void *yq, uint8_t *ys, int64_t M, int64_t K, int64_t N,
+                            int activation, int dtype, void *stream)
+{
+    return guarded([&]() -> int {
+        int st = check_dtype(dtype);
+        if (st == WHTMIX_SUCCESS) st = check_sizes(M, {K, N}, K, K);
+        if (st == WHTMIX_SUCCESS) st = check_act(activation);
+        if (st == WHTMIX_SUCCESS && N > kMaxGated) st = WHTMIX_ERROR_TOO_LARGE;
+        if (st != WHTMIX_SUCCESS || M == 0) return st;
+        if (!xq || !xs || !wgq || !wgs || !wuq || !wus || (y ? yq || ys : !yq || !ys))
+            return WHTMIX_ERROR_INVALID_VALUE;
+        const uint64_t e = elt(dtype);
+        if (!aligned({y}, e) || !aligned({bg, bu}, 4) || !aligned({xq, wgq, wuq, yq}, 16))
+            return WHTMIX_ERROR_MISALIGNED;
+        const uint64_t kw = mx_width(K), nw = mx_width(N), kb = kw / whtmix::kMxBlock,
+                       b = (uint64_t)N * 4;
+        const Range ra{xq, M * kw}, rb{xs, M * kb}, rg{wgq, N * kw}, rgs{wgs, N * kb},
+            ru{wuq, N * kw}, rus{wus, N * kb}, rbg{bg, b}, rbu{bu, b}, ry{y, span(M, N, N, e)},
+            rq{yq, M * nw}, rs{ys, M * (nw / whtmix::kMxBlock)};
+        if (!apart(ry, {ra, rb, rg, rgs, ru, rus, rbg, rbu}) ||
+            !apart(rq, {ra, rb, rg, rgs, ru, rus, rbg, rbu, rs}) ||
+            !apart(rs, {ra, rb, rg, rgs, ru, rus, rbg, rbu}))
+            return WHTMIX_ERROR_INVALID_VALUE;
+        whtmix::GatedMxArgs a{xq, xs, wgq, wuq, wgs, wus, bg, bu, y, yq, ys, M, K, N, activation,
+                              dtype, nullptr, static_cast<hipStream_t>(stream)};
+        return with_workspace(stream, whtmix::gated_mx_bytes(a), "gated in 8 bits", [&](float *p) {
+            a.ws = p;
+            return whtmix::launch_gated_mx(a);
+        });
+    });
+}
+
+int whtmix_embedding_forward(const void *ids, const void *table, void *y, int64_t rows,
+                             int64_t vocab, int64_t C, double scale, int index, int dtype,
+                             void *stream)
+{
+    return guarded([&]() -> int {
+        const int st = check_embedding(rows, vocab, C, scale, index, dtype);
+        if (st != WHTMIX_SUCCESS || rows == 0) return st;
+        if (!ids || !table || !y) return WHTMIX_ERROR_INVALID_VALUE;
+        const uint64_t e = elt(dtype), i = index == WHTMIX_INDEX_I64 ? 8 : 4;
+        if (!aligned({table, y}, e) || !aligned({ids}, i)) return WHTMIX_ERROR_MISALIGNED;
+        if (!apart({y, span(rows, C, C, e)}, {{ids, rows * i}, {table, span(vocab, C, C, e)}}))
+            return WHTMIX_ERROR_INVALID_VALUE;
+        const whtmix::EmbeddingArgs a{ids, table, y, rows, vocab, C, (float)scale,
+                                      index == WHTMIX_INDEX_I64, dtype,
+                                      static_cast<hipStream_t>(stream)};
+        return done(whtmix::launch_embedding(a), "embedding");
+    });
+}
+
+int whtmix_embedding_backward(const void *ids, const void *dy, void *dtable, int64_t rows,
+                              int64_t vocab, int64_t C, double scale, int index, int dtype,
+                              void *stream)
+{
+    return guarded([&]() -> int {
+        const int st = check_embedding(rows, vocab, C, scale, index, dtype);
+        if (st != WHTMIX_SUCCESS) return st;
+        if (!dtable || (rows > 0 && (!ids || !dy))) return WHTMIX_ERROR_INVALID_VALUE;
+        const uint64_t e = elt(dtype), i = index == WHTMIX_INDEX_I64 ? 8 : 4;
+        if (!aligned({dy, dtable}, e) || !aligned({ids}, i)) return WHTMIX_ERROR_MISALIGNED;
+        const Range rt{dtable, span(vocab, C, C, e)};
+        const hipStream_t s = static_cast<hipStream_t>(stream);
+        if (rows == 0) return done(whtmix::launch_zero(dtable, rt.bytes, s), "embedding backward");
+        if (!apart(rt, {{ids, rows * i}, {dy, span(rows, C, C, e)}}))
+            return WHTMIX_ERROR_INVALID_VALUE;
+        whtmix::EmbeddingBackwardArgs a{ids, dy, dtable, rows, vocab, C, (float)scale,
+                                        index == WHTMIX_INDEX_I64, dtype, nullptr, s};
+        return with_workspace(stream, whtmix::embedding_backward_bytes(rows, vocab, C, dtype),
+                              "embedding backward", [&](float *ws) {
+                                  a.ws = ws;
+                                  return whtmix::launch_embedding_backward(a);
                               });
     });
 }

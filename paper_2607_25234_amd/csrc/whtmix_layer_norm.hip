@@ -1,0 +1,500 @@
+// Layer norm with the residual's addition, and its backward pass.
+//
+//   t = x + residual          (float32; h = t rounded to the stream's type)
+//   mu = mean(t),  v = mean((t - mu)^2),  n = (t - mu) / sqrt(v + eps),  y = n w + b
+//   from h:  g = dy w,  dx = dh + (g - mean(g) - n mean(g n)) / sqrt(v + eps)
+//            dw = sum over rows of dy n,   db = sum over rows of dy
+//
+// Bound by memory: a row is read once into the registers of G lanes (R chunks of 16 bytes each)
+// and all that is formed of it leaves from there.  The mean comes first and the squares are of
+// the distances from it, because mean(t^2) - mu^2 cancels where the mean is large beside the
+// spread.  The float32 mean m is itself off by some 2^-24 |m|: the distances' own mean d, summed
+// with their squares, corrects both (v = mean((t - m)^2) - d^2, t - mu = t - m - d).
+// Sums are float32 in a fixed order: a lane's over its own values, then a fixed tree.
+#include "whtmix_row.h"
+
+#include <algorithm>
+
+namespace whtmix {
+namespace {
+
+struct LayerNormKernelArgs {
+    const void *x, *residual;
+    const float *weight, *bias;
+    void *y, *h, *q;
+    uint8_t *scales;
+    int64_t rows, C, ldx;
+    float eps;
+};
+
+// One row on G lanes, R chunks a lane; with R = 0 (rows wider than the registers hold) the row
+// is read three times.
+template <typename T, int G, int R, bool MX>
+__global__ void __launch_bounds__(G > 256 ? G : 256) layer_norm_kernel(LayerNormKernelArgs a)
+{
+    constexpr int N = Chunk<T>::N;
+    constexpr int kRows = G > 256 ? 1 : 256 / G;
+    __shared__ float part[2][48];
+    const int lane = threadIdx.x % G;
+    const int64_t width = MX ? (a.C + kMxBlock - 1) / kMxBlock * kMxBlock : a.C;
+    const float inv = 1.f / (float)a.C;
+    // One chunk a lane: weight and bias are on their way with the first row.
+    float w0[N], b0[N];
+    if constexpr (R == 1) {
+        const int64_t c = (int64_t)lane * N;
+        const int n = (int)min((int64_t)N, max((int64_t)0, a.C - c));
+        load_floats(a.weight + (n ? c : 0), n, w0);
+        load_floats(a.bias ? a.bias + (n ? c : 0) : a.weight, a.bias ? n : 0, b0);
+    }
+    for (int64_t base = (int64_t)blockIdx.x * kRows; base < a.rows;
+         base += (int64_t)gridDim.x * kRows) {
+        const int64_t row = base + threadIdx.x / G;
+        // Rows past the end go through the exchanges with zeros and store nothing.
+        const bool live = row < a.rows;
+        const T *x = (const T *)a.x + (live ? row * a.ldx : 0);
+        const T *r = a.residual ? (const T *)a.residual + (live ? row * a.C : 0) : nullptr;
+        T *y = MX ? nullptr : (T *)a.y + (live ? row * a.C : 0);
+        T *h = a.h ? (T *)a.h + (live ? row * a.C : 0) : nullptr;
+        uint8_t *q = MX ? (uint8_t *)a.q + (live ? row * width : 0) : nullptr;
+        uint8_t *sc = MX ? a.scales + (live ? row * (width / kMxBlock) : 0) : nullptr;
+
+        auto count = [&](int64_t c) { return (int)min((int64_t)N, max((int64_t)0, a.C - c)); };
+        auto load = [&](int64_t c, float (&v)[N]) {
+            const int n = live ? count(c) : 0;
+            Chunk<T>::load(x + (n ? c : 0), n, v);
+            if (r) {
+                float e[N];
+                Chunk<T>::load(r + (n ? c : 0), n, e);
+#pragma unroll
+                for (int i = 0; i < N; ++i) v[i] += e[i];
+            }
+        };
+        // The distances from the mean, of the elements there are, into their sum and squares.
+        auto spread = [&](int64_t c, const float (&v)[N], float mean, float (&s)[2]) {
+            const int n = count(c);
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const float d = i < n ? v[i] - mean : 0.f;
+                s[0] += d;
+                s[1] = fmaf(d, d, s[1]);
+            }
+        };
+        auto emit = [&](int64_t c, float (&v)[N], const float (&w)[N], const float (&b)[N],
+                        float mean, float off, float rstd) {
+            const int n = count(c);
+            if (h && live && n > 0) Chunk<T>::store(h + c, n, v);
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] = fmaf((v[i] - mean - off) * rstd, w[i], b[i]);
+            if constexpr (MX) {
+#pragma unroll
+                for (int i = 0; i < N; ++i) v[i] = i < n ? v[i] : 0.f;
+                if (live) store_mx<T>(v, q, sc, c);
+            } else {
+                if (live && n > 0) Chunk<T>::store(y + c, n, v);
+            }
+        };
+        auto vectors = [&](int64_t c, float (&w)[N], float (&b)[N]) {
+            const int n = count(c);
+            load_floats(a.weight + (n ? c : 0), n, w);
+            load_floats(a.bias ? a.bias + (n ? c : 0) : a.weight, a.bias ? n : 0, b);
+        };
+        float s[1] = {0.f}, t[2] = {0.f, 0.f};
+
+        if constexpr (R > 0) {
+            float v[R][N];
+#pragma unroll
+            for (int j = 0; j < R; ++j) load(((int64_t)j * G + lane) * N, v[j]);
+#pragma unroll
+            for (int j = 0; j < R; ++j)
+#pragma unroll
+                for (int i = 0; i < N; ++i) s[0] += v[j][i];
+            row_sums<G>(s, part[0]);
+            const float mean = s[0] * inv;
+#pragma unroll
+            for (int j = 0; j < R; ++j) spread(((int64_t)j * G + lane) * N, v[j], mean, t);
+            row_sums<G>(t, part[1]);
+            const float off = t[0] * inv;
+            const float rstd = rsqrtf(fmaxf(fmaf(-off, off, t[1] * inv), 0.f) + a.eps);
+#pragma unroll
+            for (int j = 0; j < R; ++j) {
+                const int64_t c = ((int64_t)j * G + lane) * N;
+                if (c >= width) continue;
+                if constexpr (R == 1) {
+                    emit(c, v[j], w0, b0, mean, off, rstd);
+                } else {
+                    float w[N], b[N];
+                    vectors(c, w, b);
+                    emit(c, v[j], w, b, mean, off, rstd);
+                }
+            }
+        } else {
+            for (int64_t c = (int64_t)lane * N; c < a.C; c += (int64_t)G * N) {
+                float v[N];
+                load(c, v);
+#pragma unroll
+                for (int i = 0; i < N; ++i) s[0] += v[i];
+            }
+            row_sums<G>(s, part[0]);
+            const float mean = s[0] * inv;
+            for (int64_t c = (int64_t)lane * N; c < a.C; c += (int64_t)G * N) {
+                float v[N];
+                load(c, v);
+                spread(c, v, mean, t);
+            }
+            row_sums<G>(t, part[1]);
+            const float off = t[0] * inv;
+            const float rstd = rsqrtf(fmaxf(fmaf(-off, off, t[1] * inv), 0.f) + a.eps);
+            // A block's lanes are in the loop together: `width` is a multiple of 32.
+            for (int64_t c = (int64_t)lane * N; c < width; c += (int64_t)G * N) {
+                float v[N], w[N], b[N];
+                load(c, v);
+                vectors(c, w, b);
+                emit(c, v, w, b, mean, off, rstd);
+            }
+        }
+    }
+}
+
+template <typename T, int G, int R, bool MX> hipError_t run_forward(const LayerNormArgs &a)
+{
+    constexpr int kRows = G > 256 ? 1 : 256 / G;
+    const LayerNormKernelArgs k{a.x, a.residual, a.weight, a.bias, a.y, a.h, a.q, a.scales,
+                                a.rows, a.C, a.ldx, a.eps};
+    const int64_t blocks = std::min<int64_t>((a.rows + kRows - 1) / kRows, kMaxBlocks);
+    layer_norm_kernel<T, G, R, MX>
+        <<<dim3((uint32_t)blocks), dim3(G > 256 ? G : 256), 0, a.stream>>>(k);
+    return hipGetLastError();
+}
+
+// Chunks of a row -> lanes and chunks a lane, as the root-mean-square norm's.
+template <typename T, bool MX> hipError_t pick_forward(const LayerNormArgs &a)
+{
+    const int64_t width = MX ? mx_width(a.C) : a.C;
+    const int64_t n = (width + Chunk<T>::N - 1) / Chunk<T>::N;
+    if (n <= 8) return run_forward<T, 8, 1, MX>(a);
+    if (n <= 16) return run_forward<T, 16, 1, MX>(a);
+    if (n <= 32) return run_forward<T, 32, 1, MX>(a);
+    if (n <= 64) return run_forward<T, 64, 1, MX>(a);
+    if (n <= 128) return run_forward<T, 128, 1, MX>(a);
+    if (n <= 256) return run_forward<T, 256, 1, MX>(a);
+    if (n <= 512) return run_forward<T, 512, 1, MX>(a);
+    if (n <= 1024) return run_forward<T, 512, 2, MX>(a);
+    if (n <= 2048) return run_forward<T, 1024, 2, MX>(a);
+    if (n <= 4096) return run_forward<T, 1024, 4, MX>(a);
+    return run_forward<T, 1024, 0, MX>(a);
+}
+
+// ---- backward ----
+struct LayerNormBackwardKernelArgs {
+    const void *h, *dy, *dh;
+    const float *weight;
+    void *dx;
+    float *part;            // [gridDim.x][2][C]: the sums of dy n, then of dy; or null
+    int64_t rows, C;
+    float eps;
+};
+
+// Waves a SIMD that the registers of `values` values a lane leave room for (h, dy, weight, both
+// vectors' sums, and what is computed from them); a workgroup of 1024 takes four.
+constexpr int backward_waves(int lanes, int values)
+{
+    return lanes == 1024 ? 4 : values <= 4 ? 6 : values <= 8 ? 4 : 2;
+}
+
+// Rows go round the grid; a lane keeps its columns' sums of dy n and of dy.  The groups of a
+// workgroup add theirs in order through LDS.
+template <typename T, int G, int R>
+__global__ void __launch_bounds__(G > 256 ? G : 256, backward_waves(G, Chunk<T>::N *R))
+    layer_norm_backward_kernel(LayerNormBackwardKernelArgs a)
+{
+    constexpr int N = Chunk<T>::N;
+    constexpr int kRows = G > 256 ? 1 : 256 / G;
+    __shared__ float parts[2][48];
+    __shared__ float sums[kRows > 1 ? 256 * R * N : 1];
+    const int lane = threadIdx.x % G, grp = threadIdx.x / G;
+    const float inv = 1.f / (float)a.C;
+    float dw[R][N], db[R][N], w0[N];
+#pragma unroll
+    for (int j = 0; j < R; ++j)
+#pragma unroll
+        for (int i = 0; i < N; ++i) dw[j][i] = db[j][i] = 0.f;
+    auto count = [&](int j) {
+        return (int)min((int64_t)N, max((int64_t)0, a.C - ((int64_t)j * G + lane) * N));
+    };
+    auto weights = [&](int j, float (&w)[N]) {
+        const int n = count(j);
+        load_floats(a.weight + (n ? ((int64_t)j * G + lane) * N : 0), n, w);
+    };
+    if constexpr (R == 1) weights(0, w0);
+
+    for (int64_t base = (int64_t)blockIdx.x * kRows; base < a.rows;
+         base += (int64_t)gridDim.x * kRows) {
+        const int64_t row = base + grp;
+        const bool live = row < a.rows;
+        const int64_t at = live ? row * a.C : 0;
+        float h[R][N], dy[R][N];
+        float s[2] = {0.f, 0.f};        // of h, of g
+#pragma unroll
+        for (int j = 0; j < R; ++j) {
+            const int n = live ? count(j) : 0;
+            const int64_t c = at + (n ? ((int64_t)j * G + lane) * N : 0);
+            Chunk<T>::load((const T *)a.h + c, n, h[j]);
+            Chunk<T>::load((const T *)a.dy + c, n, dy[j]);
+        }
+#pragma unroll
+        for (int j = 0; j < R; ++j) {
+            float w[N];
+            if constexpr (R > 1) weights(j, w);
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                s[0] += h[j][i];
+                s[1] = fmaf(dy[j][i], R == 1 ? w0[i] : w[i], s[1]);
+            }
+        }
+        row_sums<G>(s, parts[0]);
+        const float mean = s[0] * inv;
+        float t[3] = {0.f, 0.f, 0.f};   // of the distances d, their squares, g d
+#pragma unroll
+        for (int j = 0; j < R; ++j) {
+            float w[N];
+            if constexpr (R > 1) weights(j, w);
+            const int n = count(j);
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const float d = i < n ? h[j][i] - mean : 0.f;
+                h[j][i] = d;
+                t[0] += d;
+                t[1] = fmaf(d, d, t[1]);
+                t[2] = fmaf(d, dy[j][i] * (R == 1 ? w0[i] : w[i]), t[2]);
+            }
+        }
+        row_sums<G>(t, parts[1]);
+        const float off = t[0] * inv;
+        const float rstd = rsqrtf(fmaxf(fmaf(-off, off, t[1] * inv), 0.f) + a.eps);
+        const float gm = s[1] * inv;                            // mean(g)
+        const float k = fmaf(-off, s[1], t[2]) * rstd * inv;    // mean(g n)
+#pragma unroll
+        for (int j = 0; j < R; ++j) {
+            const int n = live ? count(j) : 0;
+            if (n <= 0) continue;
+            const int64_t c = at + ((int64_t)j * G + lane) * N;
+            float w[N], o[N];
+            if constexpr (R > 1) weights(j, w);
+            if (a.dh) Chunk<T>::load((const T *)a.dh + c, n, o);
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const float nn = (h[j][i] - off) * rstd;
+                const float d = rstd * (fmaf(dy[j][i], R == 1 ? w0[i] : w[i], -gm) - nn * k);
+                o[i] = a.dh ? o[i] + d : d;
+                dw[j][i] = fmaf(dy[j][i], nn, dw[j][i]);
+                db[j][i] += dy[j][i];
+            }
+            Chunk<T>::store((T *)a.dx + c, n, o);
+        }
+    }
+    if (!a.part) return;
+    float *out = a.part + (int64_t)blockIdx.x * 2 * a.C;
+    auto emit = [&](const float (&v)[R][N], float *to) {
+        if constexpr (kRows > 1) {
+            __syncthreads();
+#pragma unroll
+            for (int j = 0; j < R; ++j)
+#pragma unroll
+                for (int i = 0; i < N; ++i)
+                    sums[grp * (G * R * N) + (j * G + lane) * N + i] = v[j][i];
+            __syncthreads();
+            for (int c = threadIdx.x; c < G * R * N && c < a.C; c += 256) {
+                float u = 0.f;
+#pragma unroll
+                for (int g = 0; g < kRows; ++g) u += sums[g * (G * R * N) + c];
+                to[c] = u;
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < R; ++j)
+                store_floats(to + ((int64_t)j * G + lane) * N, count(j), v[j]);
+        }
+    };
+    emit(dw, out);
+    emit(db, out + a.C);
+}
+
+// Rows too wide for registers: what each row's sums give first (stat: [rows][4] of the mean, its
+// correction, 1 / sqrt(v + eps) and mean(g), then [rows] of mean(g n)), then dx and the columns'
+// sums by column chunks.
+template <typename T>
+__global__ void __launch_bounds__(1024) layer_norm_backward_stats(LayerNormBackwardKernelArgs a,
+                                                                  float *stat)
+{
+    constexpr int N = Chunk<T>::N;
+    __shared__ float parts[2][48];
+    const float inv = 1.f / (float)a.C;
+    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        const int64_t at = row * a.C;
+        auto each = [&](auto f) {
+            for (int64_t c = (int64_t)threadIdx.x * N; c < a.C; c += 1024 * N) {
+                const int n = (int)min((int64_t)N, a.C - c);
+                float h[N], dy[N], w[N];
+                Chunk<T>::load((const T *)a.h + at + c, n, h);
+                Chunk<T>::load((const T *)a.dy + at + c, n, dy);
+                load_floats(a.weight + c, n, w);
+#pragma unroll
+                for (int i = 0; i < N; ++i)
+                    if (i < n) f(h[i], dy[i] * w[i]);
+            }
+        };
+        float s[2] = {0.f, 0.f}, t[3] = {0.f, 0.f, 0.f};
+        each([&](float h, float g) {
+            s[0] += h;
+            s[1] += g;
+        });
+        row_sums<1024>(s, parts[0]);
+        const float mean = s[0] * inv;
+        each([&](float h, float g) {
+            const float d = h - mean;
+            t[0] += d;
+            t[1] = fmaf(d, d, t[1]);
+            t[2] = fmaf(d, g, t[2]);
+        });
+        row_sums<1024>(t, parts[1]);
+        const float off = t[0] * inv;
+        const float rstd = rsqrtf(fmaxf(fmaf(-off, off, t[1] * inv), 0.f) + a.eps);
+        if (threadIdx.x == 0) {
+            stat[4 * row] = mean;
+            stat[4 * row + 1] = off;
+            stat[4 * row + 2] = rstd;
+            stat[4 * row + 3] = s[1] * inv;
+            stat[4 * a.rows + row] = fmaf(-off, s[1], t[2]) * rstd * inv;
+        }
+    }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(256)
+    layer_norm_backward_columns(LayerNormBackwardKernelArgs a, const float *stat, int64_t per)
+{
+    constexpr int N = Chunk<T>::N;
+    const int64_t c = ((int64_t)blockIdx.x * 256 + threadIdx.x) * N;
+    const int n = (int)min((int64_t)N, a.C - c);
+    if (n <= 0) return;
+    float dw[N], db[N], w[N];
+    load_floats(a.weight + c, n, w);
+#pragma unroll
+    for (int i = 0; i < N; ++i) dw[i] = db[i] = 0.f;
+    const int64_t end = min(a.rows, ((int64_t)blockIdx.y + 1) * per);
+    for (int64_t row = (int64_t)blockIdx.y * per; row < end; ++row) {
+        const float mean = stat[4 * row], off = stat[4 * row + 1], rstd = stat[4 * row + 2],
+                    gm = stat[4 * row + 3], k = stat[4 * a.rows + row];
+        const int64_t at = row * a.C + c;
+        float h[N], dy[N], o[N];
+        Chunk<T>::load((const T *)a.h + at, n, h);
+        Chunk<T>::load((const T *)a.dy + at, n, dy);
+        if (a.dh) Chunk<T>::load((const T *)a.dh + at, n, o);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const float nn = (h[i] - mean - off) * rstd;
+            const float d = rstd * (fmaf(dy[i], w[i], -gm) - nn * k);
+            o[i] = a.dh ? o[i] + d : d;
+            dw[i] = fmaf(dy[i], nn, dw[i]);
+            db[i] += dy[i];
+        }
+        Chunk<T>::store((T *)a.dx + at, n, o);
+    }
+    if (a.part) {
+        float *out = a.part + (int64_t)blockIdx.y * 2 * a.C + c;
+        store_floats(out, n, dw);
+        store_floats(out + a.C, n, db);
+    }
+}
+
+// Chunks of a row that stay in the backward kernel's registers, at most.
+constexpr int64_t wide_chunks(int per) { return per == 8 ? 2048 : 4096; }
+constexpr int kWideFloats = 5;          // of a row that does not
+
+struct BackwardShape {
+    int lanes, chunks;
+    int threads() const { return lanes > 256 ? lanes : 256; }
+};
+BackwardShape backward_shape(int64_t n)
+{
+    if (n <= 64) return {n <= 8 ? 8 : n <= 16 ? 16 : n <= 32 ? 32 : 64, 1};
+    if (n <= 128) return {128, 1};
+    if (n <= 256) return {256, 1};
+    if (n <= 512) return {512, 1};
+    return {1024, n <= 1024 ? 1 : n <= 2048 ? 2 : 4};
+}
+
+int64_t backward_parts(int64_t rows, int64_t C, int dtype)
+{
+    const int per = dtype == DTYPE_BF16 ? 8 : 4;
+    const int64_t n = (C + per - 1) / per;
+    if (n > wide_chunks(per)) return std::min<int64_t>(rows, 64);
+    // As many workgroups as the 256 compute units hold at a time, each of the same count of rows.
+    const BackwardShape s = backward_shape(n);
+    const int64_t in_block = s.threads() / s.lanes, blocks = (rows + in_block - 1) / in_block;
+    const int at_once = std::max(1, backward_waves(s.lanes, per * s.chunks) * 4 / (s.threads() / 64));
+    return std::min<int64_t>(blocks, 256 * at_once);
+}
+
+template <typename T, int G, int R>
+hipError_t run_backward(const LayerNormBackwardKernelArgs &k, uint32_t blocks, hipStream_t stream)
+{
+    layer_norm_backward_kernel<T, G, R><<<dim3(blocks), dim3(G > 256 ? G : 256), 0, stream>>>(k);
+    return hipGetLastError();
+}
+
+template <typename T> hipError_t backward(const LayerNormBackwardArgs &a)
+{
+    const int64_t n = (a.C + Chunk<T>::N - 1) / Chunk<T>::N;
+    const int64_t parts = backward_parts(a.rows, a.C, a.dtype);
+    const bool sums = a.dweight || a.dbias;
+    const uint32_t b = (uint32_t)parts;
+    const LayerNormBackwardKernelArgs k{a.h, a.dy, a.dh, a.weight, a.dx, sums ? a.ws : nullptr,
+                                        a.rows, a.C, a.eps};
+    hipError_t e;
+    if (n > wide_chunks(Chunk<T>::N)) {
+        float *stat = a.ws + (sums ? parts * 2 * a.C : 0);
+        layer_norm_backward_stats<T><<<dim3((uint32_t)std::min<int64_t>(a.rows, 1 << 16)),
+                                       dim3(1024), 0, a.stream>>>(k, stat);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+        const int64_t per = (a.rows + parts - 1) / parts;
+        layer_norm_backward_columns<T>
+            <<<dim3((uint32_t)((n + 255) / 256), b), dim3(256), 0, a.stream>>>(k, stat, per);
+        e = hipGetLastError();
+    } else if (n <= 8) e = run_backward<T, 8, 1>(k, b, a.stream);
+    else if (n <= 16) e = run_backward<T, 16, 1>(k, b, a.stream);
+    else if (n <= 32) e = run_backward<T, 32, 1>(k, b, a.stream);
+    else if (n <= 64) e = run_backward<T, 64, 1>(k, b, a.stream);
+    else if (n <= 128) e = run_backward<T, 128, 1>(k, b, a.stream);
+    else if (n <= 256) e = run_backward<T, 256, 1>(k, b, a.stream);
+    else if (n <= 512) e = run_backward<T, 512, 1>(k, b, a.stream);
+    else if (n <= 1024) e = run_backward<T, 1024, 1>(k, b, a.stream);
+    else if (n <= 2048) e = run_backward<T, 1024, 2>(k, b, a.stream);
+    else if constexpr (Chunk<T>::N == 4) e = run_backward<T, 1024, 4>(k, b, a.stream);
+    else e = hipErrorInvalidValue;
+    if (e != hipSuccess || !sums) return e;
+    return launch_column_sums(a.ws, parts, a.C, a.dweight, a.dbias, a.stream);
+}
+
+}  // namespace
+
+hipError_t launch_layer_norm(const LayerNormArgs &a)
+{
+    if (a.dtype == DTYPE_BF16)
+        return a.q ? pick_forward<__bf16, true>(a) : pick_forward<__bf16, false>(a);
+    return a.q ? pick_forward<float, true>(a) : pick_forward<float, false>(a);
+}
+
+uint64_t layer_norm_backward_floats(int64_t rows, int64_t C, int dtype, bool sums)
+{
+    const int per = dtype == DTYPE_BF16 ? 8 : 4;
+    return (sums ? (uint64_t)backward_parts(rows, C, dtype) * 2 * C : 0) +
+           ((C + per - 1) / per > wide_chunks(per) ? kWideFloats * (uint64_t)rows : 0);
+}
+
+hipError_t launch_layer_norm_backward(const LayerNormBackwardArgs &a)
+{
+    return a.dtype == DTYPE_BF16 ? backward<__bf16>(a) : backward<float>(a);
+}
+
+}  // namespace whtmix

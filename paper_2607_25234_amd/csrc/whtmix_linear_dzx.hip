@@ -142,7 +142,7 @@ __global__ void __launch_bounds__(256) dzx_kernel(DzxArgs d, GemmArgs g)
     });
     __syncthreads();
     static_assert(4 * kEpilogueFloats * 4 <= sizeof(lds), "the epilogue's rows");
-    finish_wave<__bf16>(g, (float *)lds + wave * kEpilogueFloats, m0 + wm, wn, 0, acc);
+    finish_wave<__bf16, PLAIN>(g, (float *)lds + wave * kEpilogueFloats, m0 + wm, wn, 0, acc);
 }
 
 }  // namespace

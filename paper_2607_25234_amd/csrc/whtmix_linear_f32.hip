@@ -21,6 +21,7 @@ constexpr int kRowBytes = 64;      // of a plane: 32 bf16, of one row or of 32 r
 template <Layout L, int ROWS> __device__ __forceinline__ int place_chunk(int outer, int chunk)
 {
     if constexpr (L == K_CONTIGUOUS) return outer * kRowBytes + (chunk ^ ((outer >> 2) & 3)) * 16;
+    else if constexpr (ROWS == 64) return outer * (2 * ROWS) + (chunk ^ (2 * outer & 4)) * 16;
     else return outer * (2 * ROWS) + (chunk ^ ((4 * (outer & 3)) & (ROWS / 8 - 1))) * 16;
 }
 
@@ -151,13 +152,14 @@ __device__ __forceinline__ bf16x8 fragment(const char *plane, int row0, int k0)
 }
 
 // The tile again with float32 products (v_mfma_f32_32x32x2_f32).
-template <Layout LA, Layout LB, int BM, int BN, int WM>
+template <Layout LA, Layout LB, int BM, int BC, int NB, int WM>
 __device__ __forceinline__ void float32_tile(const GemmArgs &g, Stage<LA, BM> &sa,
-                                             Stage<LB, BN> &sb, float *lds, int64_t m0, int64_t n0,
-                                             int64_t kbeg, int64_t kend, int wm, int wn,
+                                             Stage<LB, BC> (&sb)[NB], float *lds, int64_t m0,
+                                             int64_t n0, int64_t kbeg, int64_t kend, int wm, int wn,
                                              f32x16 (&acc)[WM][2])
 {
-    constexpr int kA = Stage<LA, BM>::kF32Row, kB = Stage<LB, BN>::kF32Row;
+    constexpr int kA = Stage<LA, BM>::kF32Row, kB = Stage<LB, BC>::kF32Row;
+    constexpr int kApart = NB == 1 ? 32 : kStep * kB;       // of a wave's columns, 32 by 32
     const int lane = threadIdx.x & 63;
     float *la = lds, *lb = lds + kStep * kA;
 #pragma unroll
@@ -167,13 +169,16 @@ __device__ __forceinline__ void float32_tile(const GemmArgs &g, Stage<LA, BM> &s
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
     sa.init(g.a, g.lda, g.M, kend, m0, kbeg);
-    sb.init(g.b, g.ldb, g.N, kend, n0, kbeg);
+    sb[0].init(g.b, g.ldb, g.N, kend, n0, kbeg);
+    if constexpr (NB == 2) sb[1].init(g.b2, g.ldb2, g.N, kend, n0, kbeg);
     for (int64_t k = kbeg; k < kend; k += kStep) {
         sa.load();
-        sb.load();
+#pragma unroll
+        for (int b = 0; b < NB; ++b) sb[b].load();
         __syncthreads();
         sa.store_f32(la);
-        sb.store_f32(lb);
+#pragma unroll
+        for (int b = 0; b < NB; ++b) sb[b].store_f32(lb + b * kStep * kB);
         __syncthreads();
         for (int kk = 0; kk < kStep; kk += 2) {
             const float *pa = la + (kk + (lane >> 5)) * kA + wm + (lane & 31);
@@ -182,7 +187,7 @@ __device__ __forceinline__ void float32_tile(const GemmArgs &g, Stage<LA, BM> &s
             for (int i = 0; i < WM; ++i)
 #pragma unroll
                 for (int j = 0; j < 2; ++j)
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(pb[32 * j], pa[32 * i],
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(pb[kApart * j], pa[32 * i],
                                                                      acc[i][j], 0, 0, 0);
         }
     }
@@ -192,19 +197,21 @@ __device__ __forceinline__ void float32_tile(const GemmArgs &g, Stage<LA, BM> &s
 // products of this one; two or three workgroups fill in for each other at the barriers.
 // Bound by the splits' vector instructions: 131072 x 64 x 256 with gelu 57-66 us (168 MB at
 // 2.5-2.9 TB/s, two steps a tile), 3001 x 1000 x 2003's gradients 105 us each, 115 TFLOP/s.
-template <Layout LA, Layout LB, int BM, int BN>
+template <Layout LA, Layout LB, int FORM, int BM, int BN>
 __global__ void __launch_bounds__(256) gemm_kernel(GemmArgs g)
 {
     constexpr int WAVES_N = BN / 64, WAVES_M = 4 / WAVES_N, WM = BM / WAVES_M / 32;
-    constexpr int kPlaneA = Stage<LA, BM>::kPlane, kPlaneB = Stage<LB, BN>::kPlane;
-    constexpr int kPlanes = P * (kPlaneA + kPlaneB), kEpilogue = 4 * kEpilogueFloats * 4;
-    static_assert(kStep * (Stage<LA, BM>::kF32Row + Stage<LB, BN>::kF32Row) * 4 <= kPlanes,
+    // B's tile, or GATED both B's, one after the other, of as many columns each.
+    constexpr int NB = FORM == GATED ? 2 : 1, BC = BN / NB;
+    constexpr int kPlaneA = Stage<LA, BM>::kPlane, kPlaneB = Stage<LB, BC>::kPlane;
+    constexpr int kPlanes = P * (kPlaneA + NB * kPlaneB), kEpilogue = 4 * kEpilogueFloats * 4;
+    static_assert(kStep * (Stage<LA, BM>::kF32Row + NB * Stage<LB, BC>::kF32Row) * 4 <= kPlanes,
                   "float32 staging in the planes' place");
     __shared__ __attribute__((aligned(16))) char lds[kPlanes > kEpilogue ? kPlanes : kEpilogue];
     const int wave = threadIdx.x >> 6;
-    const int64_t m0 = (int64_t)blockIdx.x * BM, n0 = (int64_t)blockIdx.y * BN;
+    const int64_t m0 = (int64_t)blockIdx.x * BM, n0 = (int64_t)blockIdx.y * BC;
     const int64_t kbeg = (int64_t)blockIdx.z * g.k_per, kend = min(g.K, kbeg + g.k_per);
-    const int wm = wave % WAVES_M * (WM * 32), wn = wave / WAVES_M * 64;
+    const int wm = wave % WAVES_M * (WM * 32), wn = wave / WAVES_M * (64 / NB);
     char *la = lds, *lb = lds + P * kPlaneA;
     f32x16 acc[WM][2];
 #pragma unroll
@@ -215,21 +222,26 @@ __global__ void __launch_bounds__(256) gemm_kernel(GemmArgs g)
             for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
 
     Stage<LA, BM> sa;
-    Stage<LB, BN> sb;
-    float top_a[Stage<LA, BM>::kTops] = {}, top_b[Stage<LB, BN>::kTops] = {};   // what the splits hold
+    Stage<LB, BC> sb[NB];
+    float top_a[Stage<LA, BM>::kTops] = {}, top_b[NB][Stage<LB, BC>::kTops] = {};   // what the splits hold
     sa.init(g.a, g.lda, g.M, kend, m0, kbeg);
-    sb.init(g.b, g.ldb, g.N, kend, n0, kbeg);
+    sb[0].init(g.b, g.ldb, g.N, kend, n0, kbeg);
+    if constexpr (NB == 2) sb[1].init(g.b2, g.ldb2, g.N, kend, n0, kbeg);
     sa.load();
-    sb.load();
+#pragma unroll
+    for (int b = 0; b < NB; ++b) sb[b].load();
     for (int64_t k = kbeg; k < kend; k += kStep) {
         __syncthreads();
         sa.largest(top_a);
-        sb.largest(top_b);
+#pragma unroll
+        for (int b = 0; b < NB; ++b) sb[b].largest(top_b[b]);
         sa.store(la);
-        sb.store(lb);
+#pragma unroll
+        for (int b = 0; b < NB; ++b) sb[b].store(lb + b * P * kPlaneB);
         if (k + kStep < kend) {
             sa.load();
-            sb.load();
+#pragma unroll
+            for (int b = 0; b < NB; ++b) sb[b].load();
         }
         __syncthreads();
 #pragma unroll
@@ -247,7 +259,8 @@ __global__ void __launch_bounds__(256) gemm_kernel(GemmArgs g)
                 bf16x8 fb[P];
 #pragma unroll
                 for (int p = 0; p < P; ++p)
-                    fb[p] = fragment<LB, BN>(lb + p * kPlaneB, wn + 32 * j, kk);
+                    fb[p] = fragment<LB, BC>(lb + ((NB - 1) * j * P + p) * kPlaneB,
+                                             wn + (NB == 1 ? 32 * j : 0), kk);
 #pragma unroll
                 for (int s = P - 1; s >= 0; --s)
 #pragma unroll
@@ -266,12 +279,15 @@ __global__ void __launch_bounds__(256) gemm_kernel(GemmArgs g)
 #pragma unroll
     for (int i = 0; i < Stage<LA, BM>::kTops; ++i) any = any || bad(top_a[i]);
 #pragma unroll
-    for (int i = 0; i < Stage<LB, BN>::kTops; ++i) any = any || bad(top_b[i]);
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int i = 0; i < Stage<LB, BC>::kTops; ++i) any = any || bad(top_b[b][i]);
     if (__syncthreads_or(any))
-        float32_tile<LA, LB, BM, BN, WM>(g, sa, sb, (float *)lds, m0, n0, kbeg, kend, wm, wn, acc);
+        float32_tile<LA, LB, BM, BC, NB, WM>(g, sa, sb, (float *)lds, m0, n0, kbeg, kend, wm, wn, acc);
     __syncthreads();
     float *out = (float *)lds + wave * kEpilogueFloats;
-    finish_wave<float>(g, out, m0 + wm, n0 + wn, blockIdx.z, acc);
+    if constexpr (FORM == GATED) finish_gated_wave<float>(g, out, m0 + wm, n0 + wn, blockIdx.z, acc);
+    else finish_wave<float, FORM>(g, out, m0 + wm, n0 + wn, blockIdx.z, acc);
 }
 
 // Rows and columns of a tile: 128 x 128, or fewer rows where there are not more (1 x 2048 x
@@ -297,23 +313,26 @@ uint64_t gemm_bytes(int64_t M, int64_t N, int64_t K)
     return s > 1 ? (uint64_t)s * M * N * 4 : 0;
 }
 
-template <Layout LA, Layout LB>
+// Columns of the tiles' B's together.
+int64_t columns(const GemmArgs &g, Form form) { return form == GATED ? 2 * g.N : g.N; }
+
+template <Layout LA, Layout LB, Form FORM = PLAIN>
 hipError_t run_gemm(GemmArgs g, float *ws, hipStream_t stream)
 {
-    const int64_t s = splits_of(g.M, g.N, g.K);
+    const int64_t n = columns(g, FORM), s = splits_of(g.M, n, g.K);
     const int64_t steps = (g.K + kStep - 1) / kStep;
     g.k_per = (steps + s - 1) / s * kStep;
     const int64_t splits = (g.K + g.k_per - 1) / g.k_per;
     g.part = splits > 1 ? ws : nullptr;
     const int bm = tile_rows(g.M), bn = tile_columns(g.M);
-    const dim3 grid((uint32_t)((g.M + bm - 1) / bm), (uint32_t)((g.N + bn - 1) / bn),
+    const dim3 grid((uint32_t)((g.M + bm - 1) / bm), (uint32_t)((n + bn - 1) / bn),
                     (uint32_t)splits);
-    if (bm == 32) gemm_kernel<LA, LB, 32, 256><<<grid, dim3(256), 0, stream>>>(g);
-    else if (bm == 64) gemm_kernel<LA, LB, 64, 256><<<grid, dim3(256), 0, stream>>>(g);
-    else gemm_kernel<LA, LB, 128, 128><<<grid, dim3(256), 0, stream>>>(g);
+    if (bm == 32) gemm_kernel<LA, LB, FORM, 32, 256><<<grid, dim3(256), 0, stream>>>(g);
+    else if (bm == 64) gemm_kernel<LA, LB, FORM, 64, 256><<<grid, dim3(256), 0, stream>>>(g);
+    else gemm_kernel<LA, LB, FORM, 128, 128><<<grid, dim3(256), 0, stream>>>(g);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || splits == 1) return e;
-    return launch_split_sum<float>(g, (int)splits, stream);
+    return launch_split_sum<float, FORM>(g, (int)splits, stream);
 }
 
 // ---- operands split in a pass of their own ----
@@ -388,7 +407,7 @@ struct SplitOperand {
 };
 
 // Sums of a wave's tile from the float32 operands in memory, for values that do not split.
-template <int WM>
+template <int FORM, int WM>
 __device__ __forceinline__ void float32_wave(const GemmArgs &g, Layout la, Layout lb, int64_t m0,
                                              int64_t n0, int64_t kbeg, int64_t kend,
                                              f32x16 (&acc)[WM][2])
@@ -409,7 +428,10 @@ __device__ __forceinline__ void float32_wave(const GemmArgs &g, Layout la, Layou
 #pragma unroll
         for (int i = 0; i < WM; ++i) a[i] = at(g.a, la, g.lda, m0 + 32 * i + (lane & 31), g.M, k);
 #pragma unroll
-        for (int j = 0; j < 2; ++j) b[j] = at(g.b, lb, g.ldb, n0 + 32 * j + (lane & 31), g.N, k);
+        for (int j = 0; j < 2; ++j)
+            b[j] = FORM == GATED && j == 1
+                       ? at(g.b2, lb, g.ldb2, n0 + (lane & 31), g.N, k)
+                       : at(g.b, lb, g.ldb, n0 + 32 * j + (lane & 31), g.N, k);
 #pragma unroll
         for (int i = 0; i < WM; ++i)
 #pragma unroll
@@ -422,10 +444,12 @@ __device__ __forceinline__ void float32_wave(const GemmArgs &g, Layout la, Layou
 // 16384 x 4096 x 4096 2500 us, 219 TFLOP/s of float32 or 1.3 PFLOP/s of bf16 products; 3001 x 1000
 // x 2003 85 us, 141: 384 tiles of 128 x 128 leave the second of two places on half of the units
 // empty.
-template <int BM, int BN, int WAVES_M, int WAVES_N>
+template <int FORM, int BM, int BN, int WAVES_M, int WAVES_N>
 __global__ void __launch_bounds__(64 * WAVES_M *WAVES_N)
-    gemm_split_kernel(GemmArgs g, SplitOperand a, SplitOperand b, uint32_t tiles_m, uint32_t tiles_n)
+    gemm_split_kernel(GemmArgs g, SplitOperand a, SplitOperand b, SplitOperand b2, uint32_t tiles_m,
+                      uint32_t tiles_n)
 {
+    constexpr int NB = FORM == GATED ? 2 : 1, BC = BN / NB;    // as in gemm_kernel
     constexpr int NW = WAVES_M * WAVES_N, WM = BM / WAVES_M / 32;
     static_assert(BN / WAVES_N == 64, "a wave's epilogue takes 64 columns");
     constexpr int kA = P * BM * kRowTermBytes, kB = P * BN * kRowTermBytes, kBuffer = kA + kB;
@@ -437,10 +461,10 @@ __global__ void __launch_bounds__(64 * WAVES_M *WAVES_N)
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     uint32_t tm, tn, split;
     place_tile(blockIdx.x, gridDim.x, tiles_m, tiles_n, tm, tn, split);
-    const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * BN;
+    const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * BC;
     const int64_t kbeg = (int64_t)split * g.k_per, kend = min(g.K, kbeg + g.k_per);
     const int steps = (int)((kend - kbeg + kBlockK - 1) / kBlockK);
-    const int wm = (wave % WAVES_M) * (WM * 32), wn = (wave / WAVES_M) * 64;
+    const int wm = (wave % WAVES_M) * (WM * 32), wn = (wave / WAVES_M) * (64 / NB);
     const uint32_t lds_wave =
         (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds + wave * 1024;
 
@@ -449,8 +473,11 @@ __global__ void __launch_bounds__(64 * WAVES_M *WAVES_N)
 #pragma unroll
     for (int i = 0; i < kCopies; ++i) {
         const bool ofb = i >= kCopiesA;
-        const int piece = (ofb ? i - kCopiesA : i) * NW + wave, per = (ofb ? BN : BM) / 32;
-        const SplitOperand &o = ofb ? b : a;
+        int piece = (ofb ? i - kCopiesA : i) * NW + wave;
+        const int per = (ofb ? BC : BM) / 32;
+        const bool second = ofb && piece >= P * per;
+        if (second) piece -= P * per;
+        const SplitOperand &o = second ? b2 : ofb ? b : a;
         from[i] = o.terms + ((kbeg / kBlockK * P + piece / per) * o.rows + (ofb ? n0 : m0) +
                              piece % per * 32) * kRowTermBytes;
     }
@@ -488,9 +515,11 @@ __global__ void __launch_bounds__(64 * WAVES_M *WAVES_N)
                 fa[p][i] = *(const bf16x8 *)(here + (p * BM + wm + 32 * i) * kRowTermBytes + row + half);
 #pragma unroll
             for (int j = 0; j < 2; ++j)
-                fb[P - 1 - p][j] = *(const bf16x8 *)(here + kA +
-                                                     ((P - 1 - p) * BN + wn + 32 * j) * kRowTermBytes +
-                                                     row + half);
+                fb[P - 1 - p][j] = *(const bf16x8 *)(
+                    here + kA +
+                    (((NB - 1) * j * P + P - 1 - p) * BC + wn + (NB == 1 ? 32 * j : 0)) *
+                        kRowTermBytes +
+                    row + half);
         }
         // The six largest of the nine products, small ones first: what is left out is below
         // 2^-24 of |x| |w|.
@@ -516,13 +545,17 @@ __global__ void __launch_bounds__(64 * WAVES_M *WAVES_N)
     const int64_t g0 = kbeg / (4 * kBlockK), g1 = (kend + 4 * kBlockK - 1) / (4 * kBlockK);
     for (int64_t i = threadIdx.x; i < (g1 - g0) * (BM / 64 + BN / 64); i += 64 * NW) {
         const int64_t grp = g0 + i / (BM / 64 + BN / 64), r = i % (BM / 64 + BN / 64);
+        const int64_t rb = r - BM / 64;
+        const SplitOperand &o = NB == 2 && rb >= BC / 64 ? b2 : b;
         bad = bad || (r < BM / 64 ? a.flags[grp * (a.rows / 64) + m0 / 64 + r]
-                                  : b.flags[grp * (b.rows / 64) + n0 / 64 + r - BM / 64]) != 0;
+                                  : o.flags[grp * (o.rows / 64) + n0 / 64 + rb % (BC / 64)]) != 0;
     }
     if (__syncthreads_or(bad))
-        float32_wave<WM>(g, a.layout, b.layout, m0 + wm, n0 + wn, kbeg, kend, acc);
+        float32_wave<FORM, WM>(g, a.layout, b.layout, m0 + wm, n0 + wn, kbeg, kend, acc);
     __syncthreads();
-    finish_wave<float>(g, (float *)lds + wave * kEpilogueFloats, m0 + wm, n0 + wn, split, acc);
+    float *out = (float *)lds + wave * kEpilogueFloats;
+    if constexpr (FORM == GATED) finish_gated_wave<float>(g, out, m0 + wm, n0 + wn, split, acc);
+    else finish_wave<float, FORM>(g, out, m0 + wm, n0 + wn, split, acc);
 }
 
 // Whether the passes that split the operands (10 bytes an element at 4.5 TB/s, and two launches
@@ -587,45 +620,64 @@ hipError_t split_operand(const void *p, Layout l, int64_t ld, int64_t rows, int6
     return hipGetLastError();
 }
 
+template <Form FORM>
 hipError_t run_split(GemmArgs g, Layout la, Layout lb, void *ws, hipStream_t stream)
 {
     char *w = (char *)ws;
-    SplitOperand a{}, b{};
+    SplitOperand a{}, b{}, b2{};
     hipError_t e = split_operand(g.a, la, g.lda, g.M, g.K, w, a, stream);
     if (e == hipSuccess) e = split_operand(g.b, lb, g.ldb, g.N, g.K, w, b, stream);
+    if (FORM == GATED && e == hipSuccess) e = split_operand(g.b2, lb, g.ldb2, g.N, g.K, w, b2, stream);
     if (e != hipSuccess) return e;
-    const SplitPlan p = plan_split(g.M, g.N, g.K);
+    const SplitPlan p = plan_split(g.M, columns(g, FORM), g.K);
     g.k_per = p.k_per;
     g.part = p.splits > 1 ? (float *)w : nullptr;
     const dim3 grid(p.tiles_m * p.tiles_n * (uint32_t)p.splits);
     if (p.large)
-        gemm_split_kernel<256, 256, 2, 4><<<grid, dim3(512), 0, stream>>>(g, a, b, p.tiles_m, p.tiles_n);
+        gemm_split_kernel<FORM, 256, 256, 2, 4>
+            <<<grid, dim3(512), 0, stream>>>(g, a, b, b2, p.tiles_m, p.tiles_n);
     else
-        gemm_split_kernel<128, 128, 2, 2><<<grid, dim3(256), 0, stream>>>(g, a, b, p.tiles_m, p.tiles_n);
+        gemm_split_kernel<FORM, 128, 128, 2, 2>
+            <<<grid, dim3(256), 0, stream>>>(g, a, b, b2, p.tiles_m, p.tiles_n);
     e = hipGetLastError();
     if (e != hipSuccess || p.splits == 1) return e;
-    return launch_split_sum<float>(g, p.splits, stream);
+    return launch_split_sum<float, FORM>(g, p.splits, stream);
+}
+
+uint64_t bytes_of(const GemmArgs &g, Form form)
+{
+    const int64_t n = columns(g, form);
+    if (!splits_first(g.M, n, g.K)) return gemm_bytes(g.M, n, g.K);
+    const SplitPlan p = plan_split(g.M, n, g.K);
+    auto up = [](uint64_t v) { return (v + 1023) / 1024 * 1024; };
+    return up(split_bytes(g.M, g.K)) + (form == GATED ? 2 : 1) * up(split_bytes(g.N, g.K)) +
+           (p.splits > 1 ? (uint64_t)p.splits * g.M * n * 4 : 0);
 }
 
 }  // namespace
 
-uint64_t gemm_f32_bytes(const GemmArgs &g)
-{
-    if (!splits_first(g.M, g.N, g.K)) return gemm_bytes(g.M, g.N, g.K);
-    const SplitPlan p = plan_split(g.M, g.N, g.K);
-    auto up = [](uint64_t v) { return (v + 1023) / 1024 * 1024; };
-    return up(split_bytes(g.M, g.K)) + up(split_bytes(g.N, g.K)) +
-           (p.splits > 1 ? (uint64_t)p.splits * g.M * g.N * 4 : 0);
-}
+uint64_t gemm_f32_bytes(const GemmArgs &g) { return bytes_of(g, PLAIN); }
 
 hipError_t gemm_f32(const GemmArgs &g, Layout la, Layout lb, void *ws, hipStream_t stream)
 {
-    if (splits_first(g.M, g.N, g.K)) return run_split(g, la, lb, ws, stream);
+    if (splits_first(g.M, g.N, g.K)) return run_split<PLAIN>(g, la, lb, ws, stream);
     float *w = (float *)ws;
     if (la == K_CONTIGUOUS && lb == K_STRIDED)
         return run_gemm<K_CONTIGUOUS, K_STRIDED>(g, w, stream);
     if (la == K_CONTIGUOUS) return run_gemm<K_CONTIGUOUS, K_CONTIGUOUS>(g, w, stream);
     return run_gemm<K_STRIDED, K_STRIDED>(g, w, stream);
+}
+
+uint64_t gemm_f32_bytes(const GemmArgs &g, Form form) { return bytes_of(g, form); }
+
+hipError_t gemm_f32(const GemmArgs &g, Form form, void *ws, hipStream_t stream)
+{
+    const bool first = splits_first(g.M, columns(g, form), g.K);
+    if (form == GATED)
+        return first ? run_split<GATED>(g, K_CONTIGUOUS, K_STRIDED, ws, stream)
+                     : run_gemm<K_CONTIGUOUS, K_STRIDED, GATED>(g, (float *)ws, stream);
+    return first ? run_split<HALVES>(g, K_STRIDED, K_STRIDED, ws, stream)
+                 : run_gemm<K_STRIDED, K_STRIDED, HALVES>(g, (float *)ws, stream);
 }
 
 }  // namespace whtmix

@@ -10,7 +10,7 @@
 // lanes (R chunks of 16 bytes each), its sum of squares goes over the lanes,
 // and y and h leave from the registers.  Sums are float32: a lane's over its
 // own values, then a fixed tree, so results do not change from run to run.
-#include "whtmix_vec.h"
+#include "whtmix_row.h"
 
 #include <algorithm>
 
@@ -62,32 +62,6 @@ struct NormKernelArgs {
     int64_t rows, C, ldx;
     float eps;
 };
-
-// A chunk in 8 bits with its block's scale.  A block of 32 is 32 / N
-// neighbouring lanes, all of which call this (chunks past C hold zeros).
-template <typename T>
-__device__ __forceinline__ void store_mx(const float (&v)[Chunk<T>::N], uint8_t *q,
-                                         uint8_t *scales, int64_t c)
-{
-    constexpr int N = Chunk<T>::N;
-    uint32_t top = 0;
-#pragma unroll
-    for (int i = 0; i < N; ++i) top = max(top, mx_magnitude(v[i]));
-#pragma unroll
-    for (int d = 1; d < kMxBlock / N; d <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, d));
-    const uint32_t byte = mx_scale_byte(top);
-    const float inv = mx_inverse(byte);
-    uint32_t w[N / 4];
-#pragma unroll
-    for (int i = 0; i < N / 4; ++i)
-        w[i] = mx_pack(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3], inv);
-    __builtin_memcpy(__builtin_assume_aligned(q + c, N), w, N);
-    if (c % kMxBlock == 0) scales[c / kMxBlock] = (uint8_t)byte;
-}
-
-// Workgroups of a launch, at most: rows beyond go round the grid (a launch holds fewer
-// than 2^32 threads).
-constexpr int64_t kMaxBlocks = int64_t(1) << 21;
 
 // One row on G lanes.  R chunks a lane stay in registers; with R = 0 (rows
 // wider than that) the row is read twice.  Bound by memory, and narrow rows share a workgroup.
@@ -502,11 +476,11 @@ template <typename T> hipError_t pick_backward(const NormBackwardArgs &a)
     return launch_column_sum(a.ws, parts, a.C, a.dweight, a.stream);
 }
 
-// Column sums of partial rows: 32 columns a workgroup, 32 rows at a time, each
+// Column sums of partial rows, to `out` and those from `half` on to `out2`: 32 columns a workgroup, 32 rows at a time, each
 // thread's rows in order and then the 32 sums in order.  2048 x 128: 5-7 us, a launch and
 // its loads' latency.
 __global__ void __launch_bounds__(1024) column_sum_kernel(const float *part, int64_t n, int64_t C,
-                                                          float *out)
+                                                          float *out, int64_t half, float *out2)
 {
     __shared__ float s[32][33];
     const int cx = threadIdx.x & 31, ry = threadIdx.x >> 5;
@@ -526,7 +500,8 @@ __global__ void __launch_bounds__(1024) column_sum_kernel(const float *part, int
         float u = 0.f;
 #pragma unroll
         for (int r = 0; r < 32; ++r) u += s[r][cx];
-        out[c] = u;
+        float *to = c < half ? out : out2;
+        if (to) to[c < half ? c : c - half] = u;
     }
 }
 
@@ -590,7 +565,16 @@ hipError_t launch_dequantize(const void *q, const uint8_t *scales, void *y, int6
 hipError_t launch_column_sum(const float *part, int64_t n, int64_t C, float *out,
                              hipStream_t stream)
 {
-    column_sum_kernel<<<dim3((uint32_t)((C + 31) / 32)), dim3(1024), 0, stream>>>(part, n, C, out);
+    column_sum_kernel<<<dim3((uint32_t)((C + 31) / 32)), dim3(1024), 0, stream>>>(part, n, C, out, C,
+                                                                                  nullptr);
+    return hipGetLastError();
+}
+
+hipError_t launch_column_sums(const float *part, int64_t n, int64_t C, float *first, float *second,
+                              hipStream_t stream)
+{
+    column_sum_kernel<<<dim3((uint32_t)((2 * C + 31) / 32)), dim3(1024), 0, stream>>>(
+        part, n, 2 * C, first, C, second);
     return hipGetLastError();
 }
 

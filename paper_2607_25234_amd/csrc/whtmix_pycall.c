@@ -190,14 +190,15 @@ static PyObject *call(PyObject *self, PyObject *const *args, Py_ssize_t nargs)
 
 /* call_rows(function_address, pointers, sizes, codes, stream[, eps]) -> status
  *
- * The feed-forward sublayer's entry points: `pointers`, `sizes` and `codes` are
- * tuples of the device pointers, the 64-bit sizes and the int codes (activation,
- * dtype) in the entry point's order, eps the norms' last argument before dtype.
+ * The row operators' entry points: `pointers`, `sizes` and `codes` are
+ * tuples of the device pointers, the 64-bit sizes and the int codes (activation or
+ * index type, dtype) in the entry point's order, eps the norms' and the embedding's (its
+ * scale) last argument before them.
  * Each signature is a case of its own. */
 static PyObject *call_rows(PyObject *self, PyObject *const *args, Py_ssize_t nargs)
 {
     (void)self;
-    void *f, *p[9], *st;
+    void *f, *p[11], *st;
     int64_t z[4];
     int c[2], status = 0;
     double eps = 0.0;
@@ -210,11 +211,12 @@ static PyObject *call_rows(PyObject *self, PyObject *const *args, Py_ssize_t nar
     const Py_ssize_t np = PyTuple_GET_SIZE(args[1]), nz = PyTuple_GET_SIZE(args[2]),
                      nc = PyTuple_GET_SIZE(args[3]);
     /* pointers, sizes, codes and eps of each signature */
-    const int key = nargs == 6 ? (int)(1000 + np * 100 + nz * 10 + nc)
+    const int key = nargs == 6 ? (int)(2000 + np * 100 + nz * 10 + nc)
                                : (int)(np * 100 + nz * 10 + nc);
-    if (np > 9 || nz > 4 || nc > 2 ||
-        (key != 1531 && key != 1631 && key != 1621 && key != 331 && key != 321 && key != 642 &&
-         key != 742 && key != 932)) {
+    if (np > 11 || nz > 4 || nc > 2 ||
+        (key != 2531 && key != 2631 && key != 2621 && key != 331 && key != 321 && key != 642 &&
+         key != 742 && key != 932 && key != 2731 && key != 2721 && key != 842 && key != 1142 &&
+         key != 1132 && key != 2332)) {
         PyErr_SetString(PyExc_TypeError, "call_rows(): no entry point takes these arguments");
         return NULL;
     }
@@ -244,15 +246,15 @@ static PyObject *call_rows(PyObject *self, PyObject *const *args, Py_ssize_t nar
     typedef int64_t I;
     Py_BEGIN_ALLOW_THREADS
     switch (key) {
-    case 1531: /* whtmix_norm_forward */
+    case 2531: /* whtmix_norm_forward */
         status = ((int (*)(P, P, P, P, P, I, I, I, double, int, P))f)(
             p[0], p[1], p[2], p[3], p[4], z[0], z[1], z[2], eps, c[0], st);
         break;
-    case 1631: /* whtmix_norm_mx_forward */
+    case 2631: /* whtmix_norm_mx_forward, whtmix_layer_norm_forward */
         status = ((int (*)(P, P, P, P, P, P, I, I, I, double, int, P))f)(
             p[0], p[1], p[2], p[3], p[4], p[5], z[0], z[1], z[2], eps, c[0], st);
         break;
-    case 1621: /* whtmix_norm_backward */
+    case 2621: /* whtmix_norm_backward */
         status = ((int (*)(P, P, P, P, P, P, I, I, double, int, P))f)(
             p[0], p[1], p[2], p[3], p[4], p[5], z[0], z[1], eps, c[0], st);
         break;
@@ -270,6 +272,32 @@ static PyObject *call_rows(PyObject *self, PyObject *const *args, Py_ssize_t nar
     case 742: /* whtmix_linear_backward */
         status = ((int (*)(P, P, P, P, P, P, P, I, I, I, I, int, int, P))f)(
             p[0], p[1], p[2], p[3], p[4], p[5], p[6], z[0], z[1], z[2], z[3], c[0], c[1], st);
+        break;
+    case 2731: /* whtmix_layer_norm_mx_forward */
+        status = ((int (*)(P, P, P, P, P, P, P, I, I, I, double, int, P))f)(
+            p[0], p[1], p[2], p[3], p[4], p[5], p[6], z[0], z[1], z[2], eps, c[0], st);
+        break;
+    case 2721: /* whtmix_layer_norm_backward */
+        status = ((int (*)(P, P, P, P, P, P, P, I, I, double, int, P))f)(
+            p[0], p[1], p[2], p[3], p[4], p[5], p[6], z[0], z[1], eps, c[0], st);
+        break;
+    case 842: /* whtmix_gated_forward */
+        status = ((int (*)(P, P, P, P, P, P, P, P, I, I, I, I, int, int, P))f)(
+            p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7], z[0], z[1], z[2], z[3], c[0], c[1], st);
+        break;
+    case 1142: /* whtmix_gated_backward */
+        status = ((int (*)(P, P, P, P, P, P, P, P, P, P, P, I, I, I, I, int, int, P))f)(
+            p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7], p[8], p[9], p[10], z[0], z[1], z[2],
+            z[3], c[0], c[1], st);
+        break;
+    case 1132: /* whtmix_gated_mx_forward */
+        status = ((int (*)(P, P, P, P, P, P, P, P, P, P, P, I, I, I, int, int, P))f)(
+            p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7], p[8], p[9], p[10], z[0], z[1], z[2],
+            c[0], c[1], st);
+        break;
+    case 2332: /* whtmix_embedding_forward, whtmix_embedding_backward */
+        status = ((int (*)(P, P, P, I, I, I, double, int, int, P))f)(
+            p[0], p[1], p[2], z[0], z[1], z[2], eps, c[0], c[1], st);
         break;
     default: /* 932: whtmix_linear_mx_forward */
         status = ((int (*)(P, P, P, P, P, P, P, P, P, I, I, I, int, int, P))f)(

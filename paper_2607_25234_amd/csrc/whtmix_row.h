@@ -1,0 +1,100 @@
+// Device helpers of the kernels that hold a row in the registers of G lanes: sums over them, and
+// the row's chunks in block-scaled 8 bits.
+#pragma once
+
+#include "whtmix_vec.h"
+
+namespace whtmix {
+
+// The value of the lane `CTRL` (a DPP control) names.
+template <int CTRL> __device__ __forceinline__ float lane_move(float v)
+{
+    return bits_f32((uint32_t)__builtin_amdgcn_update_dpp(0, (int)f32_bits(v), CTRL, 0xf, 0xf, true));
+}
+
+// Sum over groups of G neighbouring lanes of a wave (G a power of two), in every lane, by vector
+// instructions alone: neighbours in a quad, then mirrored halves of 8 and of 16 (whose lanes hold
+// equal sums by then), then the rows of 16 and the halves of the wave trade places.
+template <int G> __device__ __forceinline__ float lane_sum(float v)
+{
+    static_assert(G >= 2 && G <= 64 && (G & (G - 1)) == 0, "a power of two of lanes");
+    v += lane_move<0xB1>(v);
+    if constexpr (G >= 4) v += lane_move<0x4E>(v);
+    if constexpr (G >= 8) v += lane_move<0x141>(v);
+    if constexpr (G >= 16) v += lane_move<0x140>(v);
+    if constexpr (G >= 32) {
+        const auto r = __builtin_amdgcn_permlane16_swap(f32_bits(v), f32_bits(v), false, false);
+        v = bits_f32((uint32_t)r[0]) + bits_f32((uint32_t)r[1]);
+    }
+    if constexpr (G >= 64) {
+        const auto r = __builtin_amdgcn_permlane32_swap(f32_bits(v), f32_bits(v), false, false);
+        v = bits_f32((uint32_t)r[0]) + bits_f32((uint32_t)r[1]);
+    }
+    return v;
+}
+
+// K sums over the G lanes that hold a row.  For rows wider than a wave `part` (LDS, K floats for
+// each wave of the workgroup) is another one than in the call before, whose reads may
+// still be under way.
+template <int G, int K>
+__device__ __forceinline__ void row_sums(float (&v)[K], float *part)
+{
+#pragma unroll
+    for (int k = 0; k < K; ++k) v[k] = lane_sum<(G < 64 ? G : 64)>(v[k]);
+    if constexpr (G > 64) {
+        part += threadIdx.x / G * (G / 64) * K;
+        if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+            for (int k = 0; k < K; ++k) part[(threadIdx.x % G >> 6) * K + k] = v[k];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < K; ++k) v[k] = 0.f;
+#pragma unroll
+        for (int i = 0; i < G / 64; ++i)
+#pragma unroll
+            for (int k = 0; k < K; ++k) v[k] += part[i * K + k];
+    }
+}
+
+// A chunk in 8 bits with its block's scale.  A block of 32 is 32 / N
+// neighbouring lanes, all of which call this (chunks past C hold zeros).
+template <typename T>
+__device__ __forceinline__ void store_mx(const float (&v)[Chunk<T>::N], uint8_t *q,
+                                         uint8_t *scales, int64_t c)
+{
+    constexpr int N = Chunk<T>::N;
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) top = max(top, mx_magnitude(v[i]));
+#pragma unroll
+    for (int d = 1; d < kMxBlock / N; d <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, d));
+    const uint32_t byte = mx_scale_byte(top);
+    const float inv = mx_inverse(byte);
+    uint32_t w[N / 4];
+#pragma unroll
+    for (int i = 0; i < N / 4; ++i)
+        w[i] = mx_pack(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3], inv);
+    __builtin_memcpy(__builtin_assume_aligned(q + c, N), w, N);
+    if (c % kMxBlock == 0) scales[c / kMxBlock] = (uint8_t)byte;
+}
+
+// A chunk's floats of a vector of C, those past its end as zeros.
+template <int N> __device__ __forceinline__ void load_floats(const float *p, int n, float (&v)[N])
+{
+#pragma unroll
+    for (int i = 0; i < N; i += 4) Chunk<float>::load(p + i, n - i, *(float(*)[4])(v + i));
+}
+
+template <int N>
+__device__ __forceinline__ void store_floats(float *p, int n, const float (&v)[N])
+{
+#pragma unroll
+    for (int i = 0; i < N; i += 4) Chunk<float>::store(p + i, n - i, *(const float(*)[4])(v + i));
+}
+
+// Workgroups of a launch, at most: rows beyond go round the grid (a launch holds fewer
+// than 2^32 threads).
+constexpr int64_t kMaxBlocks = int64_t(1) << 21;
+
+}  // namespace whtmix

@@ -9,6 +9,9 @@ that need it raises.
     n, h = norm(y, weight, x)     # the residual's addition and a norm
     u = linear(n, w1, b1, activation="gelu")      # the feed-forward products
     o = linear(u, w2, b2, residual=h)
+    e = embedding(ids, table, scale=8.0)          # rows of a table by token ids
+    n, h = layer_norm(e, weight, bias)
+    u = gated(n, w_gate, w_up, activation="silu")         # act(n w_gate) * (n w_up)
 """
 from __future__ import annotations
 
@@ -26,16 +29,25 @@ PLAN_NAMES = {v: k for k, v in PLANS.items()}
 
 ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
 MX_BLOCK = 32
+INDEX_I32, INDEX_I64 = 0, 1
 
 # Every symbol include/whtmix.h declares.
 EXPORTS = (
     "whtmix_backward",
     "whtmix_backward_separable",
     "whtmix_dequantize_mx",
+    "whtmix_embedding_backward",
+    "whtmix_embedding_forward",
     "whtmix_forward",
     "whtmix_forward_ex",
     "whtmix_forward_noalloc",
     "whtmix_forward_separable",
+    "whtmix_gated_backward",
+    "whtmix_gated_forward",
+    "whtmix_gated_mx_forward",
+    "whtmix_layer_norm_backward",
+    "whtmix_layer_norm_forward",
+    "whtmix_layer_norm_mx_forward",
     "whtmix_linear_backward",
     "whtmix_linear_forward",
     "whtmix_linear_mx_forward",
@@ -80,8 +92,8 @@ class PlanInfo(ctypes.Structure):
                 ("module_outer_bits", ctypes.c_int), ("module_backward_fused", ctypes.c_int)]
 
 
-# The feed-forward entry points: counts of pointers, sizes and int codes, and whether
-# eps stands before the codes.
+# The row operators' entry points: counts of pointers, sizes and int codes, and whether
+# eps (the embedding's scale) stands before the codes.
 _ROW_CALLS = {
     "whtmix_norm_forward": (5, 3, 1, True),
     "whtmix_norm_mx_forward": (6, 3, 1, True),
@@ -91,6 +103,14 @@ _ROW_CALLS = {
     "whtmix_linear_forward": (6, 4, 2, False),
     "whtmix_linear_backward": (7, 4, 2, False),
     "whtmix_linear_mx_forward": (9, 3, 2, False),
+    "whtmix_layer_norm_forward": (6, 3, 1, True),
+    "whtmix_layer_norm_mx_forward": (7, 3, 1, True),
+    "whtmix_layer_norm_backward": (7, 2, 1, True),
+    "whtmix_gated_forward": (8, 4, 2, False),
+    "whtmix_gated_backward": (11, 4, 2, False),
+    "whtmix_gated_mx_forward": (11, 3, 2, False),
+    "whtmix_embedding_forward": (3, 3, 2, True),
+    "whtmix_embedding_backward": (3, 3, 2, True),
 }
 
 _lib = None
@@ -644,11 +664,13 @@ def _torch():
         import torch
         # the codes first: another thread takes the module for the sign that they are there
         _CODES.update({torch.float32: DTYPE_F32, torch.bfloat16: DTYPE_BF16})
+        _INDEX.update({torch.int32: INDEX_I32, torch.int64: INDEX_I64})
         _torch_module = torch
     return _torch_module
 
 
 _CODES = {}
+_INDEX = {}
 
 
 def _operand(t, what):
@@ -922,6 +944,235 @@ def linear_mx(xq, xs, wq, ws, bias=None, activation: str = "none", residual=None
     _run_rows("whtmix_linear_mx_forward", dev, stream,
               (pxq, pxs, pwq, pws, pb, pr, _ptr(out), _ptr(q), _ptr(s)), (M, K, N), (act, code))
     return (q, s) if out_mx else out
+
+
+# ---- layer norm, gated products, embedding ----
+
+def layer_norm(x, weight, bias=None, residual=None, eps: float = 1e-6, out=None, stream=None):
+    """Layer norm with the residual's addition: (y, h) with h = x + residual (x itself
+    without one) and y = (h - mean(h)) / sqrt(mean((h - mean(h))^2) + eps) * weight + bias,
+    formed before h is rounded.
+
+    x: [..., C] float32 or bfloat16 (rows may be columns of a wider tensor);
+    weight, bias: float32 [C]; residual: a contiguous tensor of x's shape and type;
+    out: optional contiguous tensor for y (may be x itself; without a residual
+    h is None then, since x holds y)."""
+    T = _torch_module or _torch()
+    dt, rows, C, ld, dev = _operand(x, "x")
+    shape, dtype = x.shape, x.dtype
+    pw = _tensor(weight, (C,), T.float32, dev, "weight")
+    pb = 0 if bias is None else _tensor(bias, (C,), T.float32, dev, "bias")
+    h, pr, ph = x, 0, 0
+    if residual is not None:
+        pr = _tensor(residual, shape, dtype, dev, "residual")
+        h = T.empty_like(residual)
+        ph = h.data_ptr()
+    if out is None:
+        out = T.empty_like(x, memory_format=T.contiguous_format)
+        py = out.data_ptr()
+    else:
+        py = _tensor(out, shape, dtype, dev, "out")
+        if residual is None and py == x.data_ptr():
+            h = None
+    _run_rows("whtmix_layer_norm_forward", dev, stream, (x.data_ptr(), pr, pw, pb, py, ph),
+              (rows, C, ld), (dt,), eps)
+    return out, h
+
+
+def layer_norm_mx(x, weight, bias=None, residual=None, eps: float = 1e-6, stream=None):
+    """layer_norm() with y in block-scaled 8 bits: (q, scales, h), q and scales as norm_mx."""
+    T = _torch_module or _torch()
+    dt, rows, C, ld, dev = _operand(x, "x")
+    shape = x.shape
+    pw = _tensor(weight, (C,), T.float32, dev, "weight")
+    pb = 0 if bias is None else _tensor(bias, (C,), T.float32, dev, "bias")
+    h, pr, ph = x, 0, 0
+    if residual is not None:
+        pr = _tensor(residual, shape, x.dtype, dev, "residual")
+        h = T.empty_like(residual)
+        ph = h.data_ptr()
+    q, scales = _new_mx(x, shape[:-1], C)
+    _run_rows("whtmix_layer_norm_mx_forward", dev, stream,
+              (x.data_ptr(), pr, pw, pb, q.data_ptr(), scales.data_ptr(), ph), (rows, C, ld),
+              (dt,), eps)
+    return q, scales, h
+
+
+def layer_norm_backward(h, weight, dy, dh=None, eps: float = 1e-6, want_dweight: bool = True,
+                        want_dbias: bool = True, dx=None, stream=None):
+    """Gradients through layer_norm() from its kept h: (dx, dweight, dbias), dx the gradient
+    of x and of the residual (dh, the gradient of h, is added), the others float32 (None
+    when not wanted).  dx may be dy or dh."""
+    T = _torch_module or _torch()
+    dt, rows, C, _, dev = _operand(h, "h")
+    shape, dtype = h.shape, h.dtype
+    ptr = (_tensor(h, shape, dtype, dev, "h"), _tensor(weight, (C,), T.float32, dev, "weight"),
+           _tensor(dy, shape, dtype, dev, "dy"),
+           0 if dh is None else _tensor(dh, shape, dtype, dev, "dh"))
+    if dx is None:
+        dx = T.empty_like(h)
+    dweight = T.empty_like(weight) if want_dweight else None
+    dbias = T.empty_like(weight) if want_dbias else None
+    _run_rows("whtmix_layer_norm_backward", dev, stream,
+              (*ptr, _tensor(dx, shape, dtype, dev, "dx"), _ptr(dweight), _ptr(dbias)), (rows, C),
+              (dt,), eps)
+    return dx, dweight, dbias
+
+
+def _gates(x, w_gate, w_up, K, dev):
+    """(N, the weights' addresses) of a gated product's weights."""
+    if w_gate.dim() != 2:
+        raise ValueError("w_gate must be [K, N]")
+    N = w_gate.shape[1]
+    return (N, _tensor(w_gate, (K, N), x.dtype, dev, "w_gate"),
+            _tensor(w_up, (K, N), x.dtype, dev, "w_up"))
+
+
+def gated(x, w_gate, w_up, b_gate=None, b_up=None, activation: str = "silu",
+          want_z: bool = False, out=None, stream=None):
+    """activation(x w_gate + b_gate) * (x w_up + b_up), both products in one kernel; with
+    want_z also both products with their biases, which gated_backward reads: (y, z_gate, z_up).
+
+    x: [..., K] float32 or bfloat16 (rows may be columns of a wider tensor); w_gate, w_up:
+    [K, N] of x's type; b_gate, b_up: float32 [N]; activation as linear's; out: optional
+    contiguous [..., N] tensor for y."""
+    T = _torch_module or _torch()
+    dt, M, K, ld, dev = _operand(x, "x")
+    act, dtype = _activation(activation), x.dtype
+    N, pg, pu = _gates(x, w_gate, w_up, K, dev)
+    shape = (*x.shape[:-1], N)
+    pbg = 0 if b_gate is None else _tensor(b_gate, (N,), T.float32, dev, "b_gate")
+    pbu = 0 if b_up is None else _tensor(b_up, (N,), T.float32, dev, "b_up")
+    if out is None:
+        out = x.new_empty(shape)
+        py = out.data_ptr()
+    else:
+        py = _tensor(out, shape, dtype, dev, "out")
+    zg = T.empty_like(out) if want_z else None
+    zu = T.empty_like(out) if want_z else None
+    _run_rows("whtmix_gated_forward", dev, stream,
+              (x.data_ptr(), pg, pu, pbg, pbu, py, _ptr(zg), _ptr(zu)), (M, K, N, ld), (act, dt))
+    return (out, zg, zu) if want_z else out
+
+
+def gated_backward(x, w_gate, w_up, dy, z_gate, z_up, activation: str = "silu",
+                   want_dx: bool = True, want_dw: bool = True, want_dbias: bool = True,
+                   stream=None):
+    """Gradients through gated() for the upstream gradient dy: (dx, dw_gate, dw_up, db_gate,
+    db_up), the biases' float32 and the others in x's type; what is not wanted is None.
+    z_gate, z_up: what gated kept."""
+    T = _torch_module or _torch()
+    dt, M, K, ld, dev = _operand(x, "x")
+    act, dtype = _activation(activation), x.dtype
+    N, pg, pu = _gates(x, w_gate, w_up, K, dev)
+    shape = (*x.shape[:-1], N)
+    pdy = _tensor(dy, shape, dtype, dev, "dy")
+    pzg = _tensor(z_gate, shape, dtype, dev, "z_gate")
+    pzu = _tensor(z_up, shape, dtype, dev, "z_up")
+    if not (want_dx or want_dw or want_dbias):
+        raise ValueError("nothing to compute")
+    dx = T.empty_like(x, memory_format=T.contiguous_format) if want_dx else None
+    dwg, dwu = (T.empty_like(w_gate), T.empty_like(w_up)) if want_dw else (None, None)
+    dbg = x.new_empty(N, dtype=T.float32) if want_dbias else None
+    dbu = x.new_empty(N, dtype=T.float32) if want_dbias else None
+    _run_rows("whtmix_gated_backward", dev, stream,
+              (x.data_ptr(), pg, pu, pdy, pzg, pzu, _ptr(dx), _ptr(dwg), _ptr(dwu), _ptr(dbg),
+               _ptr(dbu)), (M, K, N, ld), (act, dt))
+    return dx, dwg, dwu, dbg, dbu
+
+
+def gated_mx(xq, xs, wgq, wgs, wuq, wus, b_gate=None, b_up=None, activation: str = "silu",
+             out_mx: bool = False, dtype=None, out=None, stream=None):
+    """gated() on block-scaled 8 bits: xq, xs as norm_mx or quantize_mx give them, [..., K];
+    wgq, wgs and wuq, wus the weights' columns as rows, [N, K].  Returns y [..., N] in dtype
+    (out's, else bfloat16), or with out_mx (q, scales) of the result.  Sums as linear_mx's."""
+    T = _torch_module or _torch()
+    M, K, pxq, pxs, dev = _mx(xq, xs, "xq")
+    act = _activation(activation)
+    if wgq.dim() != 2:
+        raise ValueError("wgq must be [N, K]")
+    N, Kw, pgq, pgs, wdev = _mx(wgq, wgs, "wgq")
+    if Kw != K or wdev != dev:
+        raise ValueError(f"wgq must hold rows of {K} on xq's device")
+    if wuq.shape != wgq.shape:
+        raise ValueError("wuq must have wgq's shape")
+    _, _, puq, pus, udev = _mx(wuq, wus, "wuq")
+    if udev != dev:
+        raise ValueError("wuq must be on xq's device")
+    lead = xq.shape[:-1]
+    pbg = 0 if b_gate is None else _tensor(b_gate, (N,), T.float32, dev, "b_gate")
+    pbu = 0 if b_up is None else _tensor(b_up, (N,), T.float32, dev, "b_up")
+    if dtype is None:
+        dtype = out.dtype if out is not None else T.bfloat16
+    code = _CODES.get(dtype)
+    if code is None:
+        raise TypeError(f"the output must be float32 or bfloat16, not {dtype}")
+    q = s = None
+    if out_mx:
+        if out is not None:
+            raise ValueError("out is for outputs that are not in 8 bits")
+        q, s = _new_mx(xq, lead, N)
+    elif out is None:
+        out = xq.new_empty((*lead, N), dtype=dtype)
+    else:
+        _tensor(out, (*lead, N), dtype, dev, "out")
+    _run_rows("whtmix_gated_mx_forward", dev, stream,
+              (pxq, pxs, pgq, pgs, puq, pus, pbg, pbu, _ptr(out), _ptr(q), _ptr(s)), (M, K, N),
+              (act, code))
+    return (q, s) if out_mx else out
+
+
+def _ids(ids, like, what):
+    """(index code, address) of a contiguous int32 or int64 tensor on the device of `like`."""
+    code = _INDEX.get(ids.dtype)
+    if code is None:
+        raise TypeError(f"ids must be int32 or int64, got {ids.dtype}")
+    if not ids.is_contiguous() or ids.get_device() != like.get_device():
+        raise ValueError(f"ids must be contiguous and on {what}'s device")
+    return code, ids.data_ptr()
+
+
+def embedding(ids, table, scale: float = 1.0, out=None, stream=None):
+    """scale * table[ids], [*ids.shape, C] of the table's type: the rows of table [vocab, C]
+    (float32 or bfloat16, contiguous) that ids (int32 or int64, any shape) name.  A negative id
+    is padding, whose row is zeros; an id of vocab or more gives NaN.  out: optional contiguous
+    tensor for the rows."""
+    _torch_module or _torch()
+    if table.dim() != 2:
+        raise ValueError("table must be [vocab, C]")
+    dt, V, C, _, dev = _operand(table, "table")
+    pt = _tensor(table, (V, C), table.dtype, dev, "table")
+    index, pi = _ids(ids, table, "table")
+    shape = (*ids.shape, C)
+    if out is None:
+        out = table.new_empty(shape)
+        py = out.data_ptr()
+    else:
+        py = _tensor(out, shape, table.dtype, dev, "out")
+    _run_rows("whtmix_embedding_forward", dev, stream, (pi, pt, py), (ids.numel(), V, C),
+              (index, dt), scale)
+    return out
+
+
+def embedding_backward(ids, dy, vocab: int, scale: float = 1.0, stream=None):
+    """The gradient of embedding()'s table [vocab, C] for the upstream gradient dy
+    [*ids.shape, C], in dy's type: every row is written, in an order of sums that does not
+    change from run to run.  Padding and ids of vocab or more have none."""
+    _torch_module or _torch()
+    if not dy.is_cuda:
+        raise ValueError("dy must be on a GPU device")
+    dt = _CODES.get(dy.dtype)
+    if dt is None:
+        raise TypeError(f"dy must be float32 or bfloat16, got {dy.dtype}")
+    if dy.dim() < 1:
+        raise ValueError("dy must be [*ids.shape, C]")
+    C, dev = dy.shape[-1], dy.get_device()
+    pdy = _tensor(dy, (*ids.shape, C), dy.dtype, dev, "dy")
+    index, pi = _ids(ids, dy, "dy")
+    dtable = dy.new_empty((vocab, C))
+    _run_rows("whtmix_embedding_backward", dev, stream, (pi, pdy, dtable.data_ptr()),
+              (ids.numel(), vocab, C), (index, dt), scale)
+    return dtable
 
 
 def release_workspaces() -> None:

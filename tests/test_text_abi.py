@@ -1,0 +1,201 @@
+"""Argument checks of layer norm, gated products and embedding, on the host: every refusal comes
+before any HIP call, through the call module and through ctypes alike."""
+from __future__ import annotations
+
+import re
+
+import pytest
+
+from paper_2607_25234_amd import whtmix
+
+INVALID, DTYPE, MISALIGNED, MEMORY, LARGE = 1, 3, 4, 5, 7
+FAR = [(1 << 45) + (i << 41) for i in range(11)]      # addresses 2 TiB apart
+
+# name: pointers, sizes, codes, eps or scale
+GOOD = {
+    "whtmix_layer_norm_forward": (6, (4, 64, 64), (0,), (1e-6,)),
+    "whtmix_layer_norm_mx_forward": (7, (64, 64, 64), (0,), (1e-6,)),
+    "whtmix_layer_norm_backward": (7, (4, 64), (0,), (1e-6,)),
+    "whtmix_gated_forward": (8, (4, 64, 96, 64), (1, 0), ()),
+    "whtmix_gated_backward": (11, (4, 64, 96, 64), (1, 0), ()),
+    "whtmix_gated_mx_forward": (11, (64, 64, 96), (1, 0), ()),
+    "whtmix_embedding_forward": (3, (4, 50, 64), (1, 0), (2.0,)),
+    "whtmix_embedding_backward": (3, (4, 50, 64), (1, 0), (2.0,)),
+}
+NEEDED = {
+    "whtmix_layer_norm_forward": (0, 2, 4), "whtmix_layer_norm_mx_forward": (0, 2, 4, 5),
+    "whtmix_layer_norm_backward": (0, 1, 2, 4), "whtmix_gated_forward": (0, 1, 2, 5),
+    "whtmix_gated_backward": (0, 1, 2, 3, 4, 5), "whtmix_gated_mx_forward": (0, 1, 2, 3, 4, 5),
+    "whtmix_embedding_forward": (0, 1, 2), "whtmix_embedding_backward": (0, 1, 2),
+}
+OUTPUTS = {
+    "whtmix_layer_norm_forward": (4, 5), "whtmix_layer_norm_mx_forward": (4, 5, 6),
+    "whtmix_layer_norm_backward": (4, 5, 6), "whtmix_gated_forward": (5, 6, 7),
+    "whtmix_gated_backward": (6, 7, 8, 9, 10), "whtmix_gated_mx_forward": (8,),
+    "whtmix_embedding_forward": (2,), "whtmix_embedding_backward": (2,),
+}
+IN_PLACE = {("whtmix_layer_norm_forward", 4, 0), ("whtmix_layer_norm_forward", 5, 0),
+            ("whtmix_layer_norm_forward", 5, 1), ("whtmix_layer_norm_mx_forward", 6, 0),
+            ("whtmix_layer_norm_mx_forward", 6, 1), ("whtmix_layer_norm_backward", 4, 2),
+            ("whtmix_layer_norm_backward", 4, 3)}
+BYTES = {"whtmix_layer_norm_mx_forward": (5,), "whtmix_gated_mx_forward": (1, 3, 5)}   # any address
+
+
+def pointers(name):
+    p = FAR[:GOOD[name][0]]
+    if name == "whtmix_gated_mx_forward":
+        p[9] = p[10] = 0          # y, not 8 bits
+    return p
+
+
+def status(name, p, sizes, codes, eps, refused=True):
+    st = whtmix.call_rows(name, tuple(p), tuple(sizes), tuple(codes), 0, *eps)
+    f = getattr(whtmix.lib(), name)
+    assert st == f(*p, *sizes, *eps, *codes, 0)
+    assert bool(st) is refused, (name, p, sizes, codes, eps)      # what goes through would launch
+    return st
+
+
+@pytest.mark.parametrize("name", GOOD)
+def test_sizes_codes_and_eps(name):
+    _, sizes, codes, eps = GOOD[name]
+    p = pointers(name)
+    for code in (2, -1, 99):
+        assert status(name, p, sizes, (*codes[:-1], code), eps) == DTYPE
+    bad = list(sizes)
+    bad[0] = -1
+    assert status(name, p, bad, codes, eps) == INVALID
+    bad[0] = (1 << 30) + 1
+    assert status(name, p, bad, codes, eps) == LARGE
+    embedding, gated = "embedding" in name, "gated" in name
+    for i in (1, 2) if embedding or gated else (1,):
+        most = 1 << (30 if embedding and i == 1 else 21 if gated and i == 2 else 22)
+        for v, want in ((0, INVALID), (-5, INVALID), (most + 1, LARGE)):
+            bad = list(sizes)
+            bad[i] = v
+            if name.endswith("norm_forward") or "norm_mx" in name or len(sizes) == 4:
+                bad[-1] = max(bad[-1], v)         # ldx follows the width
+            assert status(name, p, bad, codes, eps) == want, (i, v)
+    if len(sizes) == 4 or "norm_forward" in name or "norm_mx" in name:
+        assert status(name, p, (*sizes[:-1], 63), codes, eps) == INVALID      # ldx below the width
+        assert status(name, p, (*sizes[:-1], (1 << 31) + 1), codes, eps) == LARGE
+    for e in (float("nan"), float("inf"), 1e39) + ((-1e-6,) if "norm" in name else ()):
+        if eps:
+            assert status(name, p, sizes, codes, (e,)) == INVALID
+    if gated:
+        for act in (-1, 5, 1 << 20):
+            assert status(name, p, sizes, (act, 0), eps) == INVALID
+    if embedding:
+        for index in (-1, 2, 64):
+            assert status(name, p, sizes, (index, 0), eps) == DTYPE
+
+
+@pytest.mark.parametrize("name", GOOD)
+def test_pointers(name):
+    n, sizes, codes, eps = GOOD[name]
+    for i in NEEDED[name]:
+        p = pointers(name)
+        p[i] = 0
+        assert status(name, p, sizes, codes, eps) == INVALID, i
+    p = pointers(name)
+    for i in [i for i, v in enumerate(p) if v]:
+        q = list(p)
+        q[i] += 1
+        if i not in BYTES.get(name, ()):
+            assert status(name, q, sizes, codes, eps) == MISALIGNED, i
+    for o in OUTPUTS[name]:
+        for i in range(n):
+            if i == o or not p[i]:
+                continue
+            q = list(p)
+            q[o] = q[i]
+            if (name, o, i) not in IN_PLACE:
+                assert status(name, q, sizes, codes, eps) == INVALID, (o, i)
+            q[o] = q[i] + 16                        # a partial overlap is never allowed
+            assert status(name, q, sizes, codes, eps) == INVALID, (o, i)
+
+
+def test_outputs_and_their_combinations():
+    def backward(**off):
+        p = FAR[:11]
+        for i in off["off"]:
+            p[i] = 0
+        return status("whtmix_gated_backward", p, (4, 64, 96, 64), (1, 0), ())
+    assert backward(off=(6, 7, 8, 9, 10)) == INVALID
+    for half in (7, 8, 9, 10):                  # one weight's or one bias's gradient alone
+        assert backward(off=(half,)) == INVALID
+    for y, q, s in ((1, 1, 1), (0, 1, 0), (0, 0, 1), (0, 0, 0), (1, 0, 1), (1, 1, 0)):
+        p = FAR[:11]
+        for i, keep in zip((8, 9, 10), (y, q, s)):
+            p[i] *= keep
+        assert status("whtmix_gated_mx_forward", p, (4, 64, 96), (0, 0), ()) == INVALID
+    for i in (9, 10):                           # 8-bit outputs over an input or one another
+        for j in [j for j in range(11) if j not in (8, i)]:
+            p = FAR[:11]
+            p[8], p[i] = 0, p[j]
+            assert status("whtmix_gated_mx_forward", p, (64, 64, 96), (0, 0), ()) == INVALID
+    # x in a wider array is not overwritten in place
+    assert status("whtmix_layer_norm_forward", [FAR[0], 0, FAR[2], 0, FAR[0], 0], (4, 64, 80),
+                  (0,), (1e-6,)) == INVALID
+
+
+def test_no_rows_is_a_no_op():
+    for name in ("whtmix_layer_norm_forward", "whtmix_layer_norm_mx_forward",
+                 "whtmix_gated_forward", "whtmix_gated_mx_forward", "whtmix_embedding_forward"):
+        n, sizes, codes, eps = GOOD[name]
+        status(name, (0,) * n, (0, *sizes[1:]), codes, eps, refused=False)
+
+
+def workspace(name, p, sizes, codes, eps=()):
+    """Bytes that a call asks for, from the test hook's refusal."""
+    assert status(name, p, sizes, codes, eps) == MEMORY
+    return int(re.search(r"of (\d+) bytes", whtmix.last_error()).group(1))
+
+
+def test_workspaces(monkeypatch):
+    """What the header says of each."""
+    torch = pytest.importorskip("torch")
+    if torch.cuda.device_count() > 0:
+        pytest.skip("fake device addresses are for hosts without a GPU")
+    monkeypatch.setenv("WHTMIX_TEST_FAIL_WORKSPACE", "1")
+    for dtype in (0, 1):
+        for rows, C in ((1, 64), (10 ** 8, 8), (10 ** 6, 128), (5000, 4096), (3000, 16384)):
+            f = workspace("whtmix_layer_norm_backward", FAR[:7], (rows, C), (dtype,), (1e-6,)) // 4
+            assert 2 * C <= f <= 1536 * 2 * C, (rows, C)
+        for rows, C in ((1, 16392), (5000, 20000), (10 ** 6, 70001)):
+            p = [*FAR[:5], 0, 0]
+            assert workspace("whtmix_layer_norm_backward", p, (rows, C), (dtype,), (1e-6,)) \
+                == 20 * rows
+        # 16 bytes a token (each of four arrays to whole 256 bytes), counts, partial sums
+        for rows, V, C in ((1, 1, 1), (4096, 50000, 64), (4097, 50000, 64), (10 ** 6, 300, 1000)):
+            b = workspace("whtmix_embedding_backward", FAR[:3], (rows, V, C), (1, dtype), (1.0,))
+            tiles = -(-rows // 4096)
+            fixed = 16 * rows + 2048 * (tiles + 1)
+            assert fixed + rows * C * 4 // 128 <= b <= fixed + 1024 + (-(-rows // 8)) * 2 * C * 4
+        M, K, N = 300, 136, 344
+        b = workspace("whtmix_gated_backward", FAR[:11], (M, K, N, K), (4, dtype))
+        assert b >= (4 - 2 * dtype) * (2 * M * N + 2 * K * N)
+    assert "WHTMIX_TEST_FAIL_WORKSPACE" in whtmix.last_error()
+
+
+def test_python_refusals():
+    torch = pytest.importorskip("torch")
+    x, w, g = torch.zeros(4, 64), torch.zeros(64, 32), torch.ones(64)
+    q, s = x.to(torch.float8_e4m3fn), torch.zeros(4, 2, dtype=torch.uint8)
+    ids = torch.zeros(4, dtype=torch.int64)
+    for f in (lambda: whtmix.layer_norm(x, g), lambda: whtmix.layer_norm_mx(x, g),
+              lambda: whtmix.layer_norm_backward(x, g, x), lambda: whtmix.gated(x, w, w),
+              lambda: whtmix.gated_backward(x, w, w, x, x, x),
+              lambda: whtmix.gated_mx(q, s, q, s, q, s), lambda: whtmix.embedding(ids, x),
+              lambda: whtmix.embedding(ids, g), lambda: whtmix.embedding_backward(ids, x, 7)):
+        with pytest.raises(ValueError):       # host tensors
+            f()
+
+
+def test_call_module_refuses_what_no_entry_point_takes():
+    m = whtmix._call()
+    for args in ((1, (0,) * 11, (0,) * 4, (0,) * 2, 0, 1.0), (1, (0,) * 3, (0,) * 3, (0,) * 2, 0),
+                 (1, (0,), (0,) * 4, (0,) * 2, 0, 1.0), (1, (0,) * 12, (0,) * 4, (0,) * 2, 0),
+                 (1, (0,) * 8, (0,) * 4, (0,), 0), (1, (0,) * 7, (0,) * 3, (0,), 0)):
+        with pytest.raises(TypeError):
+            m.call_rows(*args)
