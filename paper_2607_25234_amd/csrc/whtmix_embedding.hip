@@ -1,13 +1,14 @@
 // Rows of a table by token ids, and the table's gradient by sorted tokens.
 //
 //   y[n] = scale table[id_n]                       (id < 0: zeros; id >= vocab: NaN)
-//   dtable[v] = scale sum over n with id_n = v of dy[n], in ascending n
+//   dtable[v] = scale sum over n with id_n = v of dy[n]
 //
-// The gradient sorts (id, n) pairs, stable, by radix: equal ids then lie together in ascending n,
-// and each run of them is summed in float32 in that order, without atomics on values, so results do
-// not change from run to run.  Runs may be of one token or of all of them, so the sorted list is cut
-// into ranges of equal length: a range adds what it holds, writes the runs that end in it, and
-// leaves the sums of those that go on to be joined in order by a kernel of its own.
+// The gradient sorts (id, n) pairs, stable, by radix: equal ids then lie together in ascending n.
+// Each run of them is summed in float32 in that order, stretch by stretch, without atomics on
+// values, so results do not change from run to run.  Runs may be of one token or of all of them, so
+// the sorted list is cut into ranges of equal length: a workgroup adds what its range holds,
+// writes the runs that lie in it, and leaves the sums of the others to be joined in order by a
+// kernel of its own.
 #include "whtmix_row.h"
 
 #include <algorithm>
@@ -92,7 +93,7 @@ template <typename T, typename Id> hipError_t forward(const EmbeddingArgs &a)
 // Pairs of (key, n), the key an id of the table or `vocab` for tokens that have no gradient, which
 // come last.  Digits of up to 9 bits: byte tokens and their padding are sorted in one pass.
 constexpr int kBins = 512, kDigitBits = 9;
-constexpr int kSortThreads = 512, kSortWaves = kSortThreads / 64, kItems = 8;
+constexpr int kSortThreads = 512, kSortWaves = kSortThreads / 64, kItems = 4;
 constexpr int kTile = kSortThreads * kItems;
 
 struct SortArgs {
@@ -183,9 +184,10 @@ struct SortLds {
 };
 
 // The items' ranks among those of their digit in the wave, and in lds.count how many there are.
-__device__ __forceinline__ void rank_items(SortLds &lds, const uint32_t (&key)[kItems],
-                                           const bool (&in)[kItems], int shift, int bits,
-                                           uint32_t (&digit)[kItems], uint32_t (&rank)[kItems])
+template <int ITEMS>
+__device__ __forceinline__ void rank_items(SortLds &lds, const uint32_t (&key)[ITEMS],
+                                           const bool (&in)[ITEMS], int shift, int bits,
+                                           uint32_t (&digit)[ITEMS], uint32_t (&rank)[ITEMS])
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     uint32_t *count = lds.count[wave];
@@ -193,7 +195,7 @@ __device__ __forceinline__ void rank_items(SortLds &lds, const uint32_t (&key)[k
     for (int i = 0; i < kBins / 64; ++i) count[i * 64 + lane] = 0;
     wave_fence();
 #pragma unroll
-    for (int j = 0; j < kItems; ++j) {
+    for (int j = 0; j < ITEMS; ++j) {
         digit[j] = (key[j] >> shift) & ((1u << bits) - 1);
         // The lanes with the same digit.
         uint64_t same = __ballot(in[j]);
@@ -263,13 +265,13 @@ __global__ void __launch_bounds__(kSortThreads) scatter_kernel(SortArgs a)
         before = a.counts[(int64_t)blockIdx.x * kBins + threadIdx.x];
         all = a.counts[(int64_t)a.tiles * kBins + threadIdx.x];
     } else {
-        for (uint32_t t = 0; t < a.tiles; t += 16) {
-            uint32_t v[16];
+        for (uint32_t t = 0; t < a.tiles; t += 32) {
+            uint32_t v[32];
 #pragma unroll
-            for (uint32_t u = 0; u < 16; ++u)
+            for (uint32_t u = 0; u < 32; ++u)
                 v[u] = t + u < a.tiles ? a.counts[(int64_t)(t + u) * kBins + threadIdx.x] : 0;
 #pragma unroll
-            for (uint32_t u = 0; u < 16; ++u) {
+            for (uint32_t u = 0; u < 32; ++u) {
                 before += t + u < blockIdx.x ? v[u] : 0;
                 all += v[u];
             }
@@ -341,7 +343,7 @@ struct SumArgs {
     void *dtable;
     float *part;            // [ranges][2][C]: of the run a range goes on with, of the one it leaves
     int64_t rows, vocab, C, ranges;
-    int range;              // tokens of a range
+    int stretch, range;     // tokens of a group of lanes, of a workgroup's groups together
     int lanes_log2;
     uint32_t slices;        // groups of columns
     uint32_t sum_blocks;    // workgroups that sum; the others write the zeros
@@ -375,8 +377,106 @@ template <typename T> __device__ __forceinline__ void zero_rows(const SumArgs &a
     }
 }
 
+// LDS of a workgroup whose groups of lanes take neighbouring stretches of a sorted list.
+template <int N, int THREADS> struct StretchLds {
+    float first[THREADS * N], last[THREADS * N];    // sums of a stretch's first, last run
+    uint8_t state[THREADS];
+};
+
+// Sums the runs of equal keys in the list's entries [begin, end), of `size` in all; entry i has
+// key_of(i) and the row row_of(i), whose chunk of columns load() brings.  A run that lies in the range goes to
+// write(key, s); the sums of one that comes from before it or goes on behind it to left(which,
+// key, s), which = 0 or 1.  Each group of lanes takes `stretch` entries; what goes on from
+// one to the next is joined in order through LDS.
+template <typename T, int THREADS, typename Key, typename Row, typename Load, typename Write,
+          typename Left>
+__device__ __forceinline__ void sum_runs(StretchLds<Chunk<T>::N, THREADS> &lds, int64_t begin,
+                                         int64_t end, int64_t size, int stretch, int lanes_log2,
+                                         Key key_of, Row row_of, Load load, Write write, Left left)
+{
+    constexpr int N = Chunk<T>::N, U = 8;
+    enum { BEFORE = 1, AFTER = 2, WHOLE = 4 };      // of the runs that are left there
+    const int groups = THREADS >> lanes_log2;
+    const int lane = threadIdx.x & ((1 << lanes_log2) - 1), grp = threadIdx.x >> lanes_log2;
+    const int64_t i0 = begin + (int64_t)grp * stretch, i1 = min(end, i0 + stretch);
+    auto keep = [&](float *to, const float (&s)[N]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int k = 0; k < N; ++k) to[threadIdx.x * N + k] = s[k];
+    };
+    int mine = 0;
+    uint32_t key = 0, key0 = 0;
+    float s[N];
+    if (i0 < end) {
+        key = key0 = key_of(i0);
+        bool before = i0 > 0 && key_of(i0 - 1) == key;
+        const bool after = i1 < size && key_of(i1) == key_of(i1 - 1);
+        if (before) mine = BEFORE;
+#pragma unroll
+        for (int k = 0; k < N; ++k) s[k] = 0.f;
+        for (int64_t i = i0; i < i1; i += U) {
+            uint32_t ku[U], row[U];
+            RawChunk<T> v[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                ku[u] = key_of(min(i + u, i1 - 1));
+                row[u] = row_of(min(i + u, i1 - 1));
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) load(row[u], i + u < i1, ku[u], v[u]);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (ku[u] != key) {
+                    if (before) keep(lds.first, s);
+                    else write(key, s);
+                    before = false;
+                    key = ku[u];
+#pragma unroll
+                    for (int k = 0; k < N; ++k) s[k] = 0.f;
+                }
+#pragma unroll
+                for (int k = 0; k < N; ++k) s[k] += v[u][k];
+            }
+        }
+        if (before) {
+            keep(lds.first, s);
+            if (after) mine |= WHOLE;
+        } else if (after) {
+            keep(lds.last, s);
+            mine |= AFTER;
+        } else {
+            write(key, s);
+        }
+    }
+    lds.state[threadIdx.x] = (uint8_t)mine;
+    __syncthreads();
+    // A run from `s` on through the stretches that follow: whether it goes on past the range.
+    auto join = [&](bool on) __attribute__((always_inline)) {
+        for (int q = grp + 1; on && q < groups; ++q) {
+            const int t = (q << lanes_log2) + lane;
+#pragma unroll
+            for (int k = 0; k < N; ++k) s[k] += lds.first[t * N + k];
+            on = lds.state[t] & WHOLE;
+        }
+        return on;
+    };
+    if (grp == 0 && (mine & BEFORE)) {
+#pragma unroll
+        for (int k = 0; k < N; ++k) s[k] = lds.first[threadIdx.x * N + k];
+        join(mine & WHOLE);
+        left(0, key0, s);
+    }
+    if (mine & AFTER) {
+#pragma unroll
+        for (int k = 0; k < N; ++k) s[k] = lds.last[threadIdx.x * N + k];
+        if (join(true)) left(1, key, s);
+        else write(key, s);
+    }
+}
+
 template <typename T> __global__ void __launch_bounds__(256) sum_kernel(SumArgs a)
 {
+    constexpr int N = Chunk<T>::N;
+    __shared__ StretchLds<N, 256> lds;
     if (blockIdx.x >= a.sum_blocks) {
         const int64_t step = (int64_t)(gridDim.x - a.sum_blocks) * 4 * kZeroRows;
         for (int64_t v = ((int64_t)(blockIdx.x - a.sum_blocks) * 4 + (threadIdx.x >> 6)) * kZeroRows;
@@ -384,56 +484,28 @@ template <typename T> __global__ void __launch_bounds__(256) sum_kernel(SumArgs 
             zero_rows<T>(a, v);
         return;
     }
-    constexpr int N = Chunk<T>::N, U = 8;
-    const int groups = 256 >> a.lanes_log2;
-    const int lane = threadIdx.x & ((1 << a.lanes_log2) - 1), grp = threadIdx.x >> a.lanes_log2;
-    const int64_t r = (int64_t)(blockIdx.x / a.slices) * groups + grp;
+    const int lane = threadIdx.x & ((1 << a.lanes_log2) - 1);
+    const int64_t r = blockIdx.x / a.slices;
     const int64_t c = (((int64_t)(blockIdx.x % a.slices) << a.lanes_log2) + lane) * N;
-    const int n = (int)min((int64_t)N, a.C - c);
-    if (r >= a.ranges || n <= 0) return;
-    const int64_t i0 = r * a.range, i1 = min(a.rows, i0 + a.range);
-    uint32_t key = a.keys[i0];
-    bool before = i0 > 0 && a.keys[i0 - 1] == key;
-    float s[N];
-#pragma unroll
-    for (int k = 0; k < N; ++k) s[k] = 0.f;
-    auto flush = [&](bool after) __attribute__((always_inline)) {
-        if (key >= (uint64_t)a.vocab) return;
-        if (before || after) {
-            store_floats(a.part + (r * 2 + (before ? 0 : 1)) * a.C + c, n, s);
-        } else {
+    const int n = (int)max((int64_t)0, min((int64_t)N, a.C - c));
+    const T *dy = (const T *)a.dy + (n ? c : 0);
+    float *part = a.part + 2 * r * a.C + c;
+    sum_runs<T, 256>(
+        lds, r * a.range, min(a.rows, (r + 1) * a.range), a.rows, a.stretch, a.lanes_log2,
+        [&](int64_t i) __attribute__((always_inline)) { return a.keys[i]; },
+        [&](int64_t i) __attribute__((always_inline)) { return a.at[i]; },
+        [&](uint32_t row, bool in, uint32_t key, RawChunk<T> &v) __attribute__((always_inline)) {
+            v.load(dy + (int64_t)row * a.C, in && key < (uint64_t)a.vocab ? n : 0);
+        },
+        [&](uint32_t key, float (&s)[N]) __attribute__((always_inline)) {
+            if (key >= (uint64_t)a.vocab || n == 0) return;
 #pragma unroll
             for (int k = 0; k < N; ++k) s[k] *= a.scale;
             Chunk<T>::store((T *)a.dtable + (int64_t)key * a.C + c, n, s);
-        }
-    };
-    for (int64_t i = i0; i < i1; i += U) {
-        uint32_t ku[U], at[U];
-        float v[U][N];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int64_t j = min(i + u, i1 - 1);
-            ku[u] = a.keys[j];
-            at[u] = a.at[j];
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            Chunk<T>::load((const T *)a.dy + (int64_t)at[u] * a.C + c,
-                           i + u < i1 && ku[u] < (uint64_t)a.vocab ? n : 0, v[u]);
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (ku[u] != key) {
-                flush(false);
-                before = false;
-                key = ku[u];
-#pragma unroll
-                for (int k = 0; k < N; ++k) s[k] = 0.f;
-            }
-#pragma unroll
-            for (int k = 0; k < N; ++k) s[k] += v[u][k];
-        }
-    }
-    flush(i1 < a.rows && a.keys[i1] == key);
+        },
+        [&](int which, uint32_t key, float (&s)[N]) __attribute__((always_inline)) {
+            if (key < (uint64_t)a.vocab) store_floats(part + which * a.C, n, s);
+        });
 }
 
 // The runs that go over several ranges: the workgroup of the range in which one starts adds its
@@ -490,10 +562,120 @@ template <typename T> __global__ void __launch_bounds__(256) join_kernel(SumArgs
     Chunk<T>::store((T *)a.dtable + (int64_t)key * a.C + c, n, s);
 }
 
+// ---- few ids ----
+// A vocabulary of a digit's size (byte tokens): a workgroup sorts its own tokens in LDS and writes
+// the sums of each id's to memory, one row of C floats an id; a second kernel adds those of an
+// id in order.  Two launches in place of four.
+struct FewArgs {
+    const void *ids, *dy;
+    void *dtable;
+    float *part;            // [tiles][vocab][C]
+    uint32_t *counts;       // [tiles][vocab]: how many tokens of the tile have the id
+    int64_t rows, C;
+    int vocab, bits, stretch, lanes_log2;
+    uint32_t tiles;
+    float scale;
+};
+
+constexpr int kFewItems = 2, kFewTile = kSortThreads * kFewItems;
+
+template <typename T, typename Id>
+__global__ void __launch_bounds__(kSortThreads) few_ids_kernel(FewArgs a)
+{
+    constexpr int N = Chunk<T>::N;
+    __shared__ SortLds lds;
+    __shared__ StretchLds<N, kSortThreads> runs;
+    __shared__ uint16_t keys[kFewTile], ats[kFewTile];
+    const int64_t base = (int64_t)blockIdx.x * kFewTile;
+    const int size = (int)min((int64_t)kFewTile, a.rows - base);
+    uint32_t key[kFewItems], digit[kFewItems], rank[kFewItems];
+    int at[kFewItems];
+    bool in[kFewItems];
+#pragma unroll
+    for (int j = 0; j < kFewItems; ++j) {
+        at[j] = (int)(threadIdx.x >> 6) * (64 * kFewItems) + j * 64 + (int)(threadIdx.x & 63);
+        in[j] = at[j] < size;
+        const uint64_t id = in[j] ? (uint64_t)(int64_t)((const Id *)a.ids)[base + at[j]] : 0;
+        key[j] = id < (uint64_t)a.vocab ? (uint32_t)id : (uint32_t)a.vocab;
+    }
+    rank_items(lds, key, in, 0, a.bits, digit, rank);
+    __syncthreads();
+    uint32_t all = 0;
+#pragma unroll
+    for (int w = 0; w < kSortWaves; ++w) all += lds.count[w][threadIdx.x];
+    if ((int)threadIdx.x < a.vocab) a.counts[(int64_t)blockIdx.x * a.vocab + threadIdx.x] = all;
+    wave_starts(lds, sum_before(lds, all));
+#pragma unroll
+    for (int j = 0; j < kFewItems; ++j) {
+        if (!in[j]) continue;
+        const uint32_t to = lds.count[threadIdx.x >> 6][digit[j]] + rank[j];
+        keys[to] = (uint16_t)key[j];
+        ats[to] = (uint16_t)at[j];
+    }
+    __syncthreads();
+    const int64_t c = (threadIdx.x & ((1 << a.lanes_log2) - 1)) * N;
+    const int n = (int)max((int64_t)0, min((int64_t)N, a.C - c));
+    const T *dy = (const T *)a.dy + base * a.C + (n ? c : 0);
+    float *part = a.part + (int64_t)blockIdx.x * a.vocab * a.C + c;
+    sum_runs<T, kSortThreads>(
+        runs, 0, size, size, a.stretch, a.lanes_log2,
+        [&](int64_t i) __attribute__((always_inline)) { return (uint32_t)keys[i]; },
+        [&](int64_t i) __attribute__((always_inline)) { return (uint32_t)ats[i]; },
+        [&](uint32_t row, bool in, uint32_t key, RawChunk<T> &v) __attribute__((always_inline)) {
+            v.load(dy + (int64_t)row * a.C, in && (int)key < a.vocab ? n : 0);
+        },
+        [&](uint32_t key, float (&s)[N]) __attribute__((always_inline)) {
+            if ((int)key < a.vocab) store_floats(part + (int64_t)key * a.C, n, s);
+        },
+        [](int, uint32_t, float (&)[N]) __attribute__((always_inline)) {});    // no run leaves a tile
+}
+
+// A chunk's sums over the tiles: the workgroup's groups of lanes take stretches of them.
+template <typename T> __global__ void __launch_bounds__(256) few_ids_join_kernel(FewArgs a)
+{
+    constexpr int N = Chunk<T>::N, U = 8;
+    __shared__ float sums[256 * N];
+    const int groups = 256 >> a.lanes_log2;
+    const int lane = threadIdx.x & ((1 << a.lanes_log2) - 1), grp = threadIdx.x >> a.lanes_log2;
+    const int64_t v = blockIdx.x, c = (int64_t)lane * N;
+    const int n = (int)max((int64_t)0, min((int64_t)N, a.C - c));
+    const uint32_t per = (a.tiles + groups - 1) / groups;
+    const uint32_t from = min(a.tiles, grp * per), to = min(a.tiles, from + per);
+    float s[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) s[k] = 0.f;
+    for (uint32_t t = from; t < to; t += U) {
+        uint32_t some[U];
+        float p[U][N];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const uint32_t q = min(t + u, to - 1);
+            some[u] = a.counts[(int64_t)q * a.vocab + v];
+            load_floats(a.part + ((int64_t)q * a.vocab + v) * a.C + (n ? c : 0),
+                        t + u < to ? n : 0, p[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int k = 0; k < N; ++k) s[k] += some[u] ? p[u][k] : 0.f;    // else never written
+    }
+#pragma unroll
+    for (int k = 0; k < N; ++k) sums[threadIdx.x * N + k] = s[k];
+    __syncthreads();
+    if (grp > 0 || n == 0) return;
+    for (int g = 1; g < groups; ++g)
+#pragma unroll
+        for (int k = 0; k < N; ++k) s[k] += sums[((g << a.lanes_log2) + lane) * N + k];
+#pragma unroll
+    for (int k = 0; k < N; ++k) s[k] *= a.scale;
+    Chunk<T>::store((T *)a.dtable + v * a.C + c, n, s);
+}
+
 struct Plan {
+    bool few;
     int bits, passes;       // of a digit; of the sort
     int64_t tiles;
-    int range, lanes_log2;
+    int stretch, range, lanes_log2;
     int64_t ranges, slices;
     uint64_t pairs, counts, part;   // bytes: one of four arrays; counts; partial sums
     bool scan;
@@ -512,9 +694,21 @@ Plan make_plan(int64_t rows, int64_t vocab, int64_t C, int dtype)
     const int per = dtype == DTYPE_BF16 ? 8 : 4;
     const int64_t chunks = (C + per - 1) / per;
     p.lanes_log2 = log2_up(chunks, 6);
+    // Ids of one digit and rows of a wave, where the tiles' sums are cheap to move.
+    const int64_t few_tiles = (rows + kFewTile - 1) / kFewTile;
+    const uint64_t few_part = (uint64_t)few_tiles * vocab * C * 4;
+    if (vocab < kBins && chunks <= 64 && few_part <= uint64_t(24) << 20) {
+        p.few = true;
+        p.tiles = few_tiles;
+        p.stretch = kFewTile >> (9 - p.lanes_log2);
+        p.counts = up256((uint64_t)few_tiles * vocab * 4);
+        p.part = few_part;
+        return p;
+    }
     p.slices = (chunks + (1 << p.lanes_log2) - 1) >> p.lanes_log2;
-    // Ranges for 2^17 lanes, of 8 to 256 tokens.
-    p.range = 1 << (3 + log2_up(rows * chunks >> 20, 5));
+    // Stretches for 2^17 lanes, of 8 to 256 tokens.
+    p.stretch = 1 << (3 + log2_up(rows * chunks >> 20, 5));
+    p.range = p.stretch * (256 >> p.lanes_log2);
     p.ranges = (rows + p.range - 1) / p.range;
     p.pairs = up256((uint64_t)rows * 4);
     p.counts = up256((uint64_t)(p.tiles + 1) * kBins * 4);
@@ -556,19 +750,36 @@ hipError_t sort(const EmbeddingBackwardArgs &a, const Plan &p, char *ws, const u
     return hipSuccess;
 }
 
+template <typename T> hipError_t backward_few(const EmbeddingBackwardArgs &a, const Plan &p)
+{
+    FewArgs f{};
+    f.ids = a.ids, f.dy = a.dy, f.dtable = a.dtable;
+    f.counts = (uint32_t *)a.ws, f.part = (float *)((char *)a.ws + p.counts);
+    f.rows = a.rows, f.C = a.C, f.vocab = (int)a.vocab, f.bits = p.bits, f.stretch = p.stretch;
+    f.lanes_log2 = p.lanes_log2, f.tiles = (uint32_t)p.tiles, f.scale = a.scale;
+    const dim3 grid((uint32_t)p.tiles), block(kSortThreads);
+    if (a.wide_ids) few_ids_kernel<T, int64_t><<<grid, block, 0, a.stream>>>(f);
+    else few_ids_kernel<T, int32_t><<<grid, block, 0, a.stream>>>(f);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    few_ids_join_kernel<T><<<dim3((uint32_t)a.vocab), dim3(256), 0, a.stream>>>(f);
+    return hipGetLastError();
+}
+
 template <typename T> hipError_t backward(const EmbeddingBackwardArgs &a)
 {
     const Plan p = make_plan(a.rows, a.vocab, a.C, a.dtype);
+    if (p.few) return backward_few<T>(a, p);
     char *ws = (char *)a.ws;
     SumArgs s{};
     hipError_t e = a.wide_ids ? sort<int64_t>(a, p, ws, s.keys, s.at)
                               : sort<int32_t>(a, p, ws, s.keys, s.at);
     if (e != hipSuccess) return e;
     s.dy = a.dy, s.dtable = a.dtable, s.part = (float *)(ws + 4 * p.pairs + p.counts);
-    s.rows = a.rows, s.vocab = a.vocab, s.C = a.C, s.ranges = p.ranges, s.range = p.range;
+    s.rows = a.rows, s.vocab = a.vocab, s.C = a.C;
+    s.ranges = p.ranges, s.range = p.range, s.stretch = p.stretch;
     s.lanes_log2 = p.lanes_log2, s.slices = (uint32_t)p.slices, s.scale = a.scale;
-    const int64_t groups = 256 >> p.lanes_log2;
-    s.sum_blocks = (uint32_t)((p.ranges + groups - 1) / groups * p.slices);
+    s.sum_blocks = (uint32_t)(p.ranges * p.slices);
     const int64_t zeros = std::min<int64_t>((a.vocab + 4 * kZeroRows - 1) / (4 * kZeroRows), 1 << 20);
     sum_kernel<T><<<dim3(s.sum_blocks + (uint32_t)zeros), dim3(256), 0, a.stream>>>(s);
     if ((e = hipGetLastError()) != hipSuccess || p.ranges < 2) return e;

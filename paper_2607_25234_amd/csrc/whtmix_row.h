@@ -79,6 +79,36 @@ __device__ __forceinline__ void store_mx(const float (&v)[Chunk<T>::N], uint8_t 
     if (c % kMxBlock == 0) scales[c / kMxBlock] = (uint8_t)byte;
 }
 
+// A chunk as it lies in memory, for loads whose values are needed later: half the registers of
+// bf16's floats.
+template <typename T> struct RawChunk {
+    uint32_t u[4];
+    __device__ __forceinline__ void load(const T *p, int n)
+    {
+        if (n >= Chunk<T>::N) {
+            __builtin_memcpy(u, p, 16);
+            return;
+        }
+        if constexpr (Chunk<T>::N == 4) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) u[i] = i < n ? f32_bits(p[i]) : 0u;
+        } else {
+            const uint16_t *h = (const uint16_t *)p;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                u[i] = (2 * i < n ? (uint32_t)h[2 * i] : 0u) |
+                       (2 * i + 1 < n ? (uint32_t)h[2 * i + 1] << 16 : 0u);
+        }
+    }
+    __device__ __forceinline__ void zero() { u[0] = u[1] = u[2] = u[3] = 0; }
+    // Element i (a constant after unrolling).
+    __device__ __forceinline__ float operator[](int i) const
+    {
+        if constexpr (Chunk<T>::N == 4) return bits_f32(u[i]);
+        else return bits_f32(i & 1 ? u[i >> 1] & 0xffff0000u : u[i >> 1] << 16);
+    }
+};
+
 // A chunk's floats of a vector of C, those past its end as zeros.
 template <int N> __device__ __forceinline__ void load_floats(const float *p, int n, float (&v)[N])
 {

@@ -166,12 +166,17 @@ def test_workspaces(monkeypatch):
             p = [*FAR[:5], 0, 0]
             assert workspace("whtmix_layer_norm_backward", p, (rows, C), (dtype,), (1e-6,)) \
                 == 20 * rows
-        # 16 bytes a token (each of four arrays to whole 256 bytes), counts, partial sums
-        for rows, V, C in ((1, 1, 1), (4096, 50000, 64), (4097, 50000, 64), (10 ** 6, 300, 1000)):
+        # 16 bytes a token (each of four arrays to whole 256 bytes), counts, partial sums; or a
+        # small vocabulary's partial sums and counts
+        for rows, V, C in ((1, 600, 1), (4096, 50000, 64), (4097, 50000, 64), (10 ** 6, 512, 1000),
+                           (10 ** 6, 300, 1000), (10 ** 6, 300, 64)):
             b = workspace("whtmix_embedding_backward", FAR[:3], (rows, V, C), (1, dtype), (1.0,))
-            tiles = -(-rows // 4096)
-            fixed = 16 * rows + 2048 * (tiles + 1)
-            assert fixed + rows * C * 4 // 128 <= b <= fixed + 1024 + (-(-rows // 8)) * 2 * C * 4
+            fixed = 16 * rows + 2048 * (-(-rows // 2048) + 1)
+            assert fixed <= b <= fixed + 1024 + (-(-rows // 32)) * 2 * C * 4, (rows, V, C)
+        for rows, V, C in ((1, 1, 1), (131072, 256, 64), (4000, 511, 256)):
+            b = workspace("whtmix_embedding_backward", FAR[:3], (rows, V, C), (1, dtype), (1.0,))
+            counts = 4 * V * -(-rows // 1024)
+            assert counts * (C + 1) <= b <= counts + 256 + (24 << 20)
         M, K, N = 300, 136, 344
         b = workspace("whtmix_gated_backward", FAR[:11], (M, K, N, K), (4, dtype))
         assert b >= (4 - 2 * dtype) * (2 * M * N + 2 * K * N)
