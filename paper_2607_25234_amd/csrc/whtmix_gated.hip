@@ -7,7 +7,8 @@
 // Forward both products run in one tile kernel (FORM GATED of the products), so that x is read
 // once and neither sum leaves the registers.  Backward dzg and dzu are the halves of one matrix
 // [M][2 Np]: dx is one product over its 2 Np columns, the weights' gradients one product with its
-// 2 Np columns (forms TWO_K and HALVES), one launch each in place of two.
+// 2 Np columns (forms TWO_K and HALVES), one launch each in place of two.  Narrow inputs form dx
+// in the pass that forms dzg and dzu (whtmix_gated_dzx.hip).
 #include "whtmix_gemm.h"
 
 #include <algorithm>
@@ -15,33 +16,33 @@
 namespace whtmix {
 namespace {
 
-// dzg and dzu with the columns' sums of the unrounded values: 32 threads across 256 columns, 8
-// rows at a time; the workgroup's 8 sums of a column are added in order.  They are rounded to the
-// type of dy, what the matrix cores read; columns N .. width - 1 of each half are zeros.
-constexpr int kDzRows = 8, kDzCols = 256;
-
+// dzg and dzu with the columns' sums of the unrounded values.  `across` threads take a row's
+// chunks of 8 columns, the workgroup's other threads the rows below: with whole rows the memory
+// it touches is contiguous whatever their width.  The threads' sums of a column are added in
+// order.  The values are rounded to the type of dy, what the matrix cores read; columns N .. width -
+// 1 of each half are zeros.
 template <typename T>
 __global__ void __launch_bounds__(256)
     gated_dz_kernel(const T *dy, const T *zg, const T *zu, T *dz, float *part, int64_t M, int64_t N,
-                    int64_t width, int64_t per, int act)
+                    int64_t width, int64_t per, int across, int act)
 {
-    __shared__ float sums[kDzRows][kDzCols + 8];
-    const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
-    const int64_t n = (int64_t)blockIdx.x * kDzCols + tx * 8;
+    __shared__ float sums[256 * 9];
+    const int down = 256 / across, tx = threadIdx.x % across, ty = threadIdx.x / across;
+    const int64_t n = ((int64_t)blockIdx.x * across + tx) * 8;
     const int cnt = (int)max((int64_t)0, min((int64_t)8, N - n));
     float sg[8], su[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) sg[i] = su[i] = 0.f;
     const int64_t end = min(M, ((int64_t)blockIdx.y + 1) * per);
-    if (n < width)
+    if (n < width && ty < down)
         with_act(act, [&](auto tag) {
             constexpr int ACT = decltype(tag)::value;
             constexpr int U = 2;
-            for (int64_t m = (int64_t)blockIdx.y * per + ty; m < end; m += U * kDzRows) {
+            for (int64_t m = (int64_t)blockIdx.y * per + ty; m < end; m += U * down) {
                 float d[U][8], g[U][8], u[U][8];
 #pragma unroll
                 for (int k = 0; k < U; ++k) {
-                    const int64_t r = m + k * kDzRows;
+                    const int64_t r = m + k * down;
                     const int c = r < end ? cnt : 0;
                     const int64_t at = c ? r * N + n : 0;
                     load8(dy + at, c, d[k]);
@@ -50,12 +51,13 @@ __global__ void __launch_bounds__(256)
                 }
 #pragma unroll
                 for (int k = 0; k < U; ++k) {
-                    const int64_t r = m + k * kDzRows;
+                    const int64_t r = m + k * down;
                     if (r >= end) break;
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
-                        const float a = act_of<ACT>(g[k][i]);
-                        g[k][i] = d[k][i] * u[k][i] * act_grad<ACT>(g[k][i]);
+                        float a, da;
+                        act_both<ACT>(g[k][i], a, da);
+                        g[k][i] = d[k][i] * u[k][i] * da;
                         u[k][i] = d[k][i] * a;
                         if (i >= cnt) g[k][i] = u[k][i] = 0.f;
                         sg[i] += g[k][i];
@@ -69,25 +71,51 @@ __global__ void __launch_bounds__(256)
             }
         });
     if (!part) return;
-    const int64_t c = (int64_t)blockIdx.x * kDzCols + threadIdx.x;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sums[ty][tx * 8 + i] = h ? su[i] : sg[i];
+        for (int i = 0; i < 8; ++i) sums[threadIdx.x * 9 + i] = h ? su[i] : sg[i];
         __syncthreads();
-        float t = 0.f;
-#pragma unroll
-        for (int r = 0; r < kDzRows; ++r) t += sums[r][threadIdx.x];
-        if (c < N) part[((int64_t)blockIdx.y * 2 + h) * N + c] = t;
+        for (int c = threadIdx.x; c < 8 * across; c += 256) {
+            const int64_t col = (int64_t)blockIdx.x * 8 * across + c;
+            if (col >= N) continue;
+            float t = 0.f;
+            for (int r = 0; r < down; ++r) t += sums[(r * across + c / 8) * 9 + c % 8];
+            part[((int64_t)blockIdx.y * 2 + h) * N + col] = t;
+        }
     }
 }
 
-// Workgroups down the rows: about 1024 in all, 32 rows or more each.
-int64_t dz_parts(int64_t M, int64_t N)
+// Threads across the columns of `width`: whole rows where that leaves less than a quarter of the
+// workgroup idle, else the most of 32, 16 and 8 that cover the width to an eighth.
+int dz_across(int64_t width)
 {
-    const int64_t cols = (N + kDzCols - 1) / kDzCols;
+    const int64_t chunks = width / 8;
+    if (chunks <= 256 && 256 / chunks * chunks >= 192) return (int)chunks;
+    for (int t = 32; t > 8; t /= 2)
+        if ((chunks + t - 1) / t * t * 8 <= chunks * 9) return t;
+    return 8;
+}
+
+// Workgroups down the rows: about 1024 in all, 32 rows or more each.
+int64_t dz_parts(int64_t M, int64_t width)
+{
+    const int64_t across = 8 * dz_across(width), cols = (width + across - 1) / across;
     return std::max<int64_t>(1, std::min<int64_t>((M + 31) / 32, 1024 / cols));
+}
+
+template <typename T>
+hipError_t launch_dz(const GatedBackwardArgs &a, int64_t width, T *dz, float *sums, int64_t &rows)
+{
+    const int across = dz_across(width);
+    const int64_t parts = dz_parts(a.M, width), per = (a.M + parts - 1) / parts;
+    rows = (a.M + per - 1) / per;
+    const dim3 grid((uint32_t)((width + 8 * across - 1) / (8 * across)), (uint32_t)rows);
+    gated_dz_kernel<T><<<grid, dim3(256), 0, a.stream>>>((const T *)a.dy, (const T *)a.zg,
+                                                         (const T *)a.zu, dz, sums, a.M, a.N, width,
+                                                         per, across, a.act);
+    return hipGetLastError();
 }
 
 // Both weights' rows side by side, [K][2 width], with zeros past N: B of one product over both.
@@ -111,6 +139,7 @@ uint64_t align256(uint64_t v) { return (v + 255) / 256 * 256; }
 // What a backward call is made of.
 struct Parts {
     int64_t width;          // Np: of each half of dz
+    bool together;          // dz, its sums and dx in one pass
     bool two_k;             // dx reads both weights where they lie
     uint64_t dz, sums, weights, product;    // bytes
 };
@@ -140,13 +169,18 @@ Parts parts_of(const GatedBackwardArgs &a)
     const bool bf16 = a.dtype == DTYPE_BF16;
     const int e = bf16 ? 2 : 4;
     auto aligned = [](const void *q) { return reinterpret_cast<uintptr_t>(q) % 16 == 0; };
-    p.width = (a.N + 7) / 8 * 8;
+    // bf16: whole cache lines, float32: whole chunks of the stores
+    p.width = bf16 ? (a.N + 63) / 64 * 64 : (a.N + 7) / 8 * 8;
+    p.together = gated_dzx_takes(a);
     p.two_k = bf16 && a.N % 64 == 0 && aligned(a.wg) && aligned(a.wu);
     if (a.dx || a.dwg) p.dz = align256((uint64_t)a.M * 2 * p.width * e);
-    if (a.dbg) p.sums = align256((uint64_t)dz_parts(a.M, a.N) * 2 * a.N * 4);
+    if (a.dbg)
+        p.sums = align256((uint64_t)(p.together ? gated_dzx_parts(a.M) : dz_parts(a.M, p.width)) * 2 *
+                          a.N * 4);
     // a workspace's address is aligned: null stands for it
-    if (a.dx && !p.two_k) p.weights = align256((uint64_t)a.K * 2 * p.width * e);
-    if (a.dx) {
+    const bool product = a.dx && !p.together;
+    if (product && !p.two_k) p.weights = align256((uint64_t)a.K * 2 * p.width * e);
+    if (product) {
         const GemmArgs g = dx_args(a, p, nullptr, nullptr);
         p.product = !bf16     ? gemm_f32_bytes(g)
                     : p.two_k ? gemm_bf16_bytes(g, TWO_K)
@@ -167,17 +201,14 @@ template <typename T> hipError_t backward(const GatedBackwardArgs &a)
     float *sums = p.sums ? (float *)(ws + p.dz) : nullptr;
     T *joined = (T *)(ws + p.dz + p.sums);
     void *rest = ws + p.dz + p.sums + p.weights;
-    const int64_t parts = dz_parts(a.M, a.N), per = (a.M + parts - 1) / parts;
-    const dim3 grid((uint32_t)((p.width + kDzCols - 1) / kDzCols), (uint32_t)((a.M + per - 1) / per));
-    gated_dz_kernel<T><<<grid, dim3(256), 0, a.stream>>>((const T *)a.dy, (const T *)a.zg,
-                                                         (const T *)a.zu, dz, sums, a.M, a.N,
-                                                         p.width, per, a.act);
-    hipError_t e = hipGetLastError();
+    int64_t parts = gated_dzx_parts(a.M);
+    hipError_t e = p.together ? launch_gated_dzx(a, p.width, dz, sums)
+                              : launch_dz<T>(a, p.width, dz, sums, parts);
     if (e != hipSuccess) return e;
-    if (sums && (e = launch_column_sums(sums, grid.y, a.N, a.dbg, a.dbu, a.stream)) != hipSuccess)
+    if (sums && (e = launch_column_sums(sums, parts, a.N, a.dbg, a.dbu, a.stream)) != hipSuccess)
         return e;
     constexpr bool kBf16 = std::is_same_v<T, __bf16>;
-    if (a.dx) {
+    if (a.dx && !p.together) {
         if (!p.two_k) {
             const int64_t blocks = std::min<int64_t>((a.K * 2 * (p.width / 8) + 255) / 256, 1 << 16);
             join_weights_kernel<T><<<dim3((uint32_t)blocks), dim3(256), 0, a.stream>>>(

@@ -415,7 +415,7 @@ struct TilePlan {
     int splits;
 };
 
-inline TilePlan plan_tiles(int64_t M, int64_t N, int64_t K, int step_k)
+inline TilePlan plan_tiles(int64_t M, int64_t N, int64_t K, int step_k, bool gated = false)
 {
     TilePlan p{};
     auto tiles = [&](int bm, int bn) __attribute__((always_inline)) { return ((M + bm - 1) / bm) * ((N + bn - 1) / bn); };
@@ -438,6 +438,10 @@ inline TilePlan plan_tiles(int64_t M, int64_t N, int64_t K, int step_k)
     // hide), or two where their parts stay long (128 x 262144 x 512: 76 us, 84 us with one).
     int64_t s = t >= 256 ? 1 : 256 / t;
     if (t < 256 && p.bm < 256 && steps / (2 * s) >= 32) s *= 2;
+    // Both weights of a gated product of few rows: two workgroups a unit where one leaves more
+    // units empty (1 x 4096 x 2 x 12288, 96 tiles: 38 us in five parts, 45 in two; 17 x 4096 x 2 x
+    // 16384 8 bits, 128 tiles: 31 in four, 27 in two).
+    if (gated && M <= 64 && t < 256 && 20 * (256 / t) < 9 * (512 / t)) s = 512 / t;
     s = s < steps / 4 ? s : steps / 4;
     if (s < 1) s = 1;
     p.k_per = (steps + s - 1) / s * step_k;
@@ -445,16 +449,17 @@ inline TilePlan plan_tiles(int64_t M, int64_t N, int64_t K, int step_k)
     return p;
 }
 
-inline uint64_t tile_part_bytes(int64_t M, int64_t N, int64_t K, int step_k)
+inline uint64_t tile_part_bytes(int64_t M, int64_t N, int64_t K, int step_k, bool gated = false)
 {
-    const TilePlan p = plan_tiles(M, N, K, step_k);
+    const TilePlan p = plan_tiles(M, N, K, step_k, gated);
     return p.splits > 1 ? (uint64_t)p.splits * M * N * 4 : 0;
 }
 
 template <int EB, bool EXACT, typename T, Layout LA, Layout LB, int FORM = PLAIN>
 hipError_t run_tiles(GemmArgs g, float *part, hipStream_t stream)
 {
-    const TilePlan p = plan_tiles(g.M, FORM == GATED ? 2 * g.N : g.N, g.K, kStepBytes / EB);
+    const TilePlan p = plan_tiles(g.M, FORM == GATED ? 2 * g.N : g.N, g.K, kStepBytes / EB,
+                                  FORM == GATED);
     g.k_per = p.k_per;
     g.part = p.splits > 1 ? part : nullptr;
     const dim3 grid(p.tiles_m * p.tiles_n * (uint32_t)p.splits);

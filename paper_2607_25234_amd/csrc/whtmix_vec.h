@@ -185,6 +185,29 @@ template <int ACT> __device__ __forceinline__ float act_grad(float z)
     return 1.f;
 }
 
+// Both at once, by the same operations: the exponential and the reciprocal are shared.
+template <int ACT> __device__ __forceinline__ void act_both(float z, float &a, float &da)
+{
+    if constexpr (ACT == ACT_GELU) {
+        const float e = gauss(z), q = gauss_tail(z, e);
+        a = fmaf(-fminf(fabsf(z), 64.f), q, fmaxf(z, 0.f));
+        da = fmaf(fminf(fmaxf(z, -64.f), 64.f) * 0.39894228040143268f, e, z < 0.f ? q : 1.f - q);
+    } else if constexpr (ACT == ACT_GELU_TANH) {
+        const float s = __builtin_amdgcn_rcpf(
+            1.f + fast_exp(-kGeluC * z * fmaf(0.044715f * z, z, 1.f)));
+        const float c = fminf(fmaxf(z, -64.f), 64.f);
+        a = z * s;
+        da = fmaf(c * s * (1.f - s), kGeluC * fmaf(0.134145f * c, c, 1.f), s);
+    } else if constexpr (ACT == ACT_SILU) {
+        const float s = __builtin_amdgcn_rcpf(1.f + fast_exp(-z));
+        a = z * s;
+        da = fmaf(a, 1.f - s, s);
+    } else {
+        a = act_of<ACT>(z);
+        da = act_grad<ACT>(z);
+    }
+}
+
 // f<ACT>() for the run-time activation (uniform over the grid).
 template <typename F> __device__ __forceinline__ void with_act(int act, F f)
 {
