@@ -9,7 +9,7 @@
 // and all that is formed of it leaves from there.  The mean comes first and the squares are of
 // the distances from it, because mean(t^2) - mu^2 cancels where the mean is large beside the
 // spread.  The float32 mean m is itself off by some 2^-24 |m|: the distances' own mean d, summed
-// with their squares, corrects both (v = mean((t - m)^2) - d^2, t - mu = t - m - d).
+// with their squares, corrects both (v = mean((t - m)^2) - d^2, mu = m + d, kept as two floats).
 // Sums are float32 in a fixed order: a lane's over its own values, then a fixed tree.
 #include "whtmix_row.h"
 
@@ -27,129 +27,174 @@ struct LayerNormKernelArgs {
     float eps;
 };
 
+// What a row's sums give: of its elements their sum s, and about m = s / C the sums t0 of the
+// distances and t1 of their squares.  m + d is kept as hi + lo: t - hi - lo rounds once where
+// the mean is moderate, and still holds where it is far larger than the spread.
+struct RowStats {
+    float hi, lo, rstd;
+};
+__device__ __forceinline__ RowStats row_stats(float m, float t0, float t1, float C, float eps)
+{
+    const float d = t0 / C, v = fmaxf(fmaf(-d, d, t1 / C), 0.f) + eps;
+    RowStats r;
+    r.hi = m + d;
+    r.lo = (m - r.hi) + d;
+    // The hardware's reciprocal root to its last bit, by a step of Newton's.
+    const float e = rsqrtf(v);
+    const float c = fmaf(0.5f * e, fmaf(-v * e, e, 1.f), e);
+    r.rstd = c == c ? c : e;        // (v = 0, or Inf)
+    return r;
+}
+
+// Workgroups that a unit holds at a time, by the waves a SIMD that their registers leave room for.
+constexpr int forward_waves(int chunks) { return chunks == 1 ? 6 : 4; }
+constexpr int threads_of(int G) { return G > 256 ? G : 256; }
+
 // One row on G lanes, R chunks a lane; with R = 0 (rows wider than the registers hold) the row
-// is read three times.
+// is read three times.  With one chunk a lane rows go round the grid and the next one is on its
+// way while this one is formed.  Values for the 8-bit form keep the parts that roundings on the
+// way would leave out: off by a few 2^-24, one value in 10^5 moves to the next of the 8-bit ones.
 template <typename T, int G, int R, bool MX>
-__global__ void __launch_bounds__(G > 256 ? G : 256) layer_norm_kernel(LayerNormKernelArgs a)
+__global__ void __launch_bounds__(threads_of(G), forward_waves(R))
+    layer_norm_kernel(LayerNormKernelArgs a)
 {
     constexpr int N = Chunk<T>::N;
-    constexpr int kRows = G > 256 ? 1 : 256 / G;
+    constexpr int kRows = threads_of(G) / G;
     __shared__ float part[2][48];
     const int lane = threadIdx.x % G;
     const int64_t width = MX ? (a.C + kMxBlock - 1) / kMxBlock * kMxBlock : a.C;
-    const float inv = 1.f / (float)a.C;
-    // One chunk a lane: weight and bias are on their way with the first row.
-    float w0[N], b0[N];
-    if constexpr (R == 1) {
-        const int64_t c = (int64_t)lane * N;
-        const int n = (int)min((int64_t)N, max((int64_t)0, a.C - c));
-        load_floats(a.weight + (n ? c : 0), n, w0);
-        load_floats(a.bias ? a.bias + (n ? c : 0) : a.weight, a.bias ? n : 0, b0);
-    }
-    for (int64_t base = (int64_t)blockIdx.x * kRows; base < a.rows;
-         base += (int64_t)gridDim.x * kRows) {
-        const int64_t row = base + threadIdx.x / G;
-        // Rows past the end go through the exchanges with zeros and store nothing.
-        const bool live = row < a.rows;
-        const T *x = (const T *)a.x + (live ? row * a.ldx : 0);
-        const T *r = a.residual ? (const T *)a.residual + (live ? row * a.C : 0) : nullptr;
-        T *y = MX ? nullptr : (T *)a.y + (live ? row * a.C : 0);
-        T *h = a.h ? (T *)a.h + (live ? row * a.C : 0) : nullptr;
-        uint8_t *q = MX ? (uint8_t *)a.q + (live ? row * width : 0) : nullptr;
-        uint8_t *sc = MX ? a.scales + (live ? row * (width / kMxBlock) : 0) : nullptr;
-
-        auto count = [&](int64_t c) { return (int)min((int64_t)N, max((int64_t)0, a.C - c)); };
-        auto load = [&](int64_t c, float (&v)[N]) {
-            const int n = live ? count(c) : 0;
-            Chunk<T>::load(x + (n ? c : 0), n, v);
-            if (r) {
-                float e[N];
-                Chunk<T>::load(r + (n ? c : 0), n, e);
+    const float C = (float)a.C;
+    auto count = [&](int64_t c) { return (int)min((int64_t)N, max((int64_t)0, a.C - c)); };
+    auto vectors = [&](int64_t c, float (&w)[N], float (&b)[N]) {
+        const int n = count(c);
+        load_floats(a.weight + (n ? c : 0), n, w);
+        load_floats(a.bias ? a.bias + (n ? c : 0) : a.weight, a.bias ? n : 0, b);
+    };
+    // The distances from the mean, of the elements there are, into their sum and squares.
+    auto spread = [&](int n, const float (&v)[N], float m, float (&t)[2]) {
 #pragma unroll
-                for (int i = 0; i < N; ++i) v[i] += e[i];
-            }
-        };
-        // The distances from the mean, of the elements there are, into their sum and squares.
-        auto spread = [&](int64_t c, const float (&v)[N], float mean, float (&s)[2]) {
-            const int n = count(c);
+        for (int i = 0; i < N; ++i) {
+            const float d = i < n ? v[i] - m : 0.f;
+            t[0] += d;
+            t[1] = fmaf(d, d, t[1]);
+        }
+    };
+    auto emit = [&](int64_t row, int64_t c, float (&v)[N], const float (&w)[N],
+                    const float (&b)[N], const RowStats &r) {
+        const int n = count(c);
+        if (a.h && n > 0) Chunk<T>::store((T *)a.h + row * a.C + c, n, v);
+        if constexpr (MX) {
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                const float d = i < n ? v[i] - mean : 0.f;
-                s[0] += d;
-                s[1] = fmaf(d, d, s[1]);
+                // the distance and its product with rstd, each with what its rounding left out
+                const float d = v[i] - r.hi, z = d - v[i], p = d * r.rstd;
+                const float dl = ((v[i] - (d - z)) - (r.hi + z)) - r.lo;
+                const float pl = fmaf(dl, r.rstd, fmaf(d, r.rstd, -p));
+                v[i] = i < n ? fmaf(p, w[i], fmaf(pl, w[i], b[i])) : 0.f;
             }
-        };
-        auto emit = [&](int64_t c, float (&v)[N], const float (&w)[N], const float (&b)[N],
-                        float mean, float off, float rstd) {
-            const int n = count(c);
-            if (h && live && n > 0) Chunk<T>::store(h + c, n, v);
+            store_mx<T>(v, (uint8_t *)a.q + row * width, a.scales + row * (width / kMxBlock), c);
+        } else {
 #pragma unroll
-            for (int i = 0; i < N; ++i) v[i] = fmaf((v[i] - mean - off) * rstd, w[i], b[i]);
-            if constexpr (MX) {
-#pragma unroll
-                for (int i = 0; i < N; ++i) v[i] = i < n ? v[i] : 0.f;
-                if (live) store_mx<T>(v, q, sc, c);
-            } else {
-                if (live && n > 0) Chunk<T>::store(y + c, n, v);
-            }
-        };
-        auto vectors = [&](int64_t c, float (&w)[N], float (&b)[N]) {
-            const int n = count(c);
-            load_floats(a.weight + (n ? c : 0), n, w);
-            load_floats(a.bias ? a.bias + (n ? c : 0) : a.weight, a.bias ? n : 0, b);
-        };
-        float s[1] = {0.f}, t[2] = {0.f, 0.f};
+            for (int i = 0; i < N; ++i) v[i] = fmaf((v[i] - r.hi - r.lo) * r.rstd, w[i], b[i]);
+            if (n > 0) Chunk<T>::store((T *)a.y + row * a.C + c, n, v);
+        }
+    };
 
-        if constexpr (R > 0) {
-            float v[R][N];
+    if constexpr (R == 1) {
+        const int64_t c = (int64_t)lane * N;
+        const int n = count(c);
+        RawChunk<T> x, r;
+        auto load = [&](int64_t row) {
+            const bool live = row < a.rows && n > 0;
+            x.load((const T *)a.x + (live ? row * a.ldx + c : 0), live ? n : 0);
+            if (a.residual)
+                r.load((const T *)a.residual + (live ? row * a.C + c : 0), live ? n : 0);
+        };
+        int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / G;
+        const int64_t step = (int64_t)gridDim.x * kRows;
+        load(row);
+        float w[N], b[N];
+        vectors(c, w, b);
+        // Rows past the end go through the exchanges with zeros and store nothing.
+        for (int64_t base = (int64_t)blockIdx.x * kRows; base < a.rows; base += step, row += step) {
+            float v[N], s[1] = {0.f}, t[2] = {0.f, 0.f};
 #pragma unroll
-            for (int j = 0; j < R; ++j) load(((int64_t)j * G + lane) * N, v[j]);
+            for (int i = 0; i < N; ++i) {
+                v[i] = x[i];
+                if (a.residual) v[i] += r[i];
+            }
+            if (base + step < a.rows) load(row + step);
 #pragma unroll
-            for (int j = 0; j < R; ++j)
-#pragma unroll
-                for (int i = 0; i < N; ++i) s[0] += v[j][i];
+            for (int i = 0; i < N; ++i) s[0] += v[i];
             row_sums<G>(s, part[0]);
-            const float mean = s[0] * inv;
-#pragma unroll
-            for (int j = 0; j < R; ++j) spread(((int64_t)j * G + lane) * N, v[j], mean, t);
+            const float m = s[0] / C;
+            spread(n, v, m, t);
             row_sums<G>(t, part[1]);
-            const float off = t[0] * inv;
-            const float rstd = rsqrtf(fmaxf(fmaf(-off, off, t[1] * inv), 0.f) + a.eps);
+            const RowStats st = row_stats(m, t[0], t[1], C, a.eps);
+            if (row < a.rows && c < width) emit(row, c, v, w, b, st);
+        }
+    } else {
+        // A workgroup a row.
+        for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+            const T *x = (const T *)a.x + row * a.ldx;
+            const T *r = a.residual ? (const T *)a.residual + row * a.C : nullptr;
+            auto load = [&](int64_t c, float (&v)[N]) {
+                const int n = count(c);
+                Chunk<T>::load(x + (n ? c : 0), n, v);
+                if (r) {
+                    float e[N];
+                    Chunk<T>::load(r + (n ? c : 0), n, e);
 #pragma unroll
-            for (int j = 0; j < R; ++j) {
-                const int64_t c = ((int64_t)j * G + lane) * N;
-                if (c >= width) continue;
-                if constexpr (R == 1) {
-                    emit(c, v[j], w0, b0, mean, off, rstd);
-                } else {
+                    for (int i = 0; i < N; ++i) v[i] += e[i];
+                }
+            };
+            float s[1] = {0.f}, t[2] = {0.f, 0.f};
+            if constexpr (R > 0) {
+                float v[R][N];
+#pragma unroll
+                for (int j = 0; j < R; ++j) load(((int64_t)j * G + lane) * N, v[j]);
+#pragma unroll
+                for (int j = 0; j < R; ++j)
+#pragma unroll
+                    for (int i = 0; i < N; ++i) s[0] += v[j][i];
+                row_sums<G>(s, part[0]);
+                const float m = s[0] / C;
+#pragma unroll
+                for (int j = 0; j < R; ++j)
+                    spread(count(((int64_t)j * G + lane) * N), v[j], m, t);
+                row_sums<G>(t, part[1]);
+                const RowStats st = row_stats(m, t[0], t[1], C, a.eps);
+#pragma unroll
+                for (int j = 0; j < R; ++j) {
+                    const int64_t c = ((int64_t)j * G + lane) * N;
+                    if (c >= width) continue;
                     float w[N], b[N];
                     vectors(c, w, b);
-                    emit(c, v[j], w, b, mean, off, rstd);
+                    emit(row, c, v[j], w, b, st);
                 }
-            }
-        } else {
-            for (int64_t c = (int64_t)lane * N; c < a.C; c += (int64_t)G * N) {
-                float v[N];
-                load(c, v);
+            } else {
+                for (int64_t c = (int64_t)lane * N; c < a.C; c += (int64_t)G * N) {
+                    float v[N];
+                    load(c, v);
 #pragma unroll
-                for (int i = 0; i < N; ++i) s[0] += v[i];
-            }
-            row_sums<G>(s, part[0]);
-            const float mean = s[0] * inv;
-            for (int64_t c = (int64_t)lane * N; c < a.C; c += (int64_t)G * N) {
-                float v[N];
-                load(c, v);
-                spread(c, v, mean, t);
-            }
-            row_sums<G>(t, part[1]);
-            const float off = t[0] * inv;
-            const float rstd = rsqrtf(fmaxf(fmaf(-off, off, t[1] * inv), 0.f) + a.eps);
-            // A block's lanes are in the loop together: `width` is a multiple of 32.
-            for (int64_t c = (int64_t)lane * N; c < width; c += (int64_t)G * N) {
-                float v[N], w[N], b[N];
-                load(c, v);
-                vectors(c, w, b);
-                emit(c, v, w, b, mean, off, rstd);
+                    for (int i = 0; i < N; ++i) s[0] += v[i];
+                }
+                row_sums<G>(s, part[0]);
+                const float m = s[0] / C;
+                for (int64_t c = (int64_t)lane * N; c < a.C; c += (int64_t)G * N) {
+                    float v[N];
+                    load(c, v);
+                    spread(count(c), v, m, t);
+                }
+                row_sums<G>(t, part[1]);
+                const RowStats st = row_stats(m, t[0], t[1], C, a.eps);
+                // A block's lanes are in the loop together: `width` is a multiple of 32.
+                for (int64_t c = (int64_t)lane * N; c < width; c += (int64_t)G * N) {
+                    float v[N], w[N], b[N];
+                    load(c, v);
+                    vectors(c, w, b);
+                    emit(row, c, v, w, b, st);
+                }
             }
         }
     }
@@ -157,16 +202,18 @@ __global__ void __launch_bounds__(G > 256 ? G : 256) layer_norm_kernel(LayerNorm
 
 template <typename T, int G, int R, bool MX> hipError_t run_forward(const LayerNormArgs &a)
 {
-    constexpr int kRows = G > 256 ? 1 : 256 / G;
+    constexpr int kRows = threads_of(G) / G;
     const LayerNormKernelArgs k{a.x, a.residual, a.weight, a.bias, a.y, a.h, a.q, a.scales,
                                 a.rows, a.C, a.ldx, a.eps};
-    const int64_t blocks = std::min<int64_t>((a.rows + kRows - 1) / kRows, kMaxBlocks);
+    const int64_t at_once = 256 * (forward_waves(R) * 4 / (threads_of(G) / 64));
+    const int64_t blocks =
+        std::min<int64_t>((a.rows + kRows - 1) / kRows, R == 1 ? at_once : kMaxBlocks);
     layer_norm_kernel<T, G, R, MX>
-        <<<dim3((uint32_t)blocks), dim3(G > 256 ? G : 256), 0, a.stream>>>(k);
+        <<<dim3((uint32_t)blocks), dim3(threads_of(G)), 0, a.stream>>>(k);
     return hipGetLastError();
 }
 
-// Chunks of a row -> lanes and chunks a lane, as the root-mean-square norm's.
+// Chunks of a row -> lanes and chunks a lane.
 template <typename T, bool MX> hipError_t pick_forward(const LayerNormArgs &a)
 {
     const int64_t width = MX ? mx_width(a.C) : a.C;
@@ -177,6 +224,7 @@ template <typename T, bool MX> hipError_t pick_forward(const LayerNormArgs &a)
     if (n <= 64) return run_forward<T, 64, 1, MX>(a);
     if (n <= 128) return run_forward<T, 128, 1, MX>(a);
     if (n <= 256) return run_forward<T, 256, 1, MX>(a);
+    if (n <= 384) return run_forward<T, 384, 1, MX>(a);
     if (n <= 512) return run_forward<T, 512, 1, MX>(a);
     if (n <= 1024) return run_forward<T, 512, 2, MX>(a);
     if (n <= 2048) return run_forward<T, 1024, 2, MX>(a);
