@@ -7,7 +7,7 @@ namespace whtmix {
 uint64_t gated_mx_gemm_bytes(const GemmArgs &g)
 {
     return packed_bytes(g.as, g.M, g.K / kMxBlock) + packed_bytes(g.bs, g.N, g.K / kMxBlock) +
-           packed_bytes(g.bs2, g.N, g.K / kMxBlock) + tile_part_bytes(g.M, 2 * g.N, g.K, kStepBytes, true);
+           packed_bytes(g.bs2, g.N, g.K / kMxBlock) + tile_part_bytes(g.M, 2 * g.N, g.K, kStepBytes);
 }
 
 template <bool EXACT, typename T> static hipError_t run(const GemmArgs &g, void *ws, hipStream_t s)

@@ -415,7 +415,7 @@ struct TilePlan {
     int splits;
 };
 
-inline TilePlan plan_tiles(int64_t M, int64_t N, int64_t K, int step_k, bool gated = false)
+inline TilePlan plan_tiles(int64_t M, int64_t N, int64_t K, int step_k, bool two_a_unit = false)
 {
     TilePlan p{};
     auto tiles = [&](int bm, int bn) __attribute__((always_inline)) { return ((M + bm - 1) / bm) * ((N + bn - 1) / bn); };
@@ -438,10 +438,10 @@ inline TilePlan plan_tiles(int64_t M, int64_t N, int64_t K, int step_k, bool gat
     // hide), or two where their parts stay long (128 x 262144 x 512: 76 us, 84 us with one).
     int64_t s = t >= 256 ? 1 : 256 / t;
     if (t < 256 && p.bm < 256 && steps / (2 * s) >= 32) s *= 2;
-    // Both weights of a gated product of few rows: two workgroups a unit where one leaves more
-    // units empty (1 x 4096 x 2 x 12288, 96 tiles: 38 us in five parts, 45 in two; 17 x 4096 x 2 x
-    // 16384 8 bits, 128 tiles: 31 in four, 27 in two).
-    if (gated && M <= 64 && t < 256 && 20 * (256 / t) < 9 * (512 / t)) s = 512 / t;
+    // Both weights of a bf16 gated product of few rows: two workgroups a unit where one leaves more
+    // units empty (1 x 4096 x 2 x 12288, 96 tiles: 44 us in five parts, 51 in two; 16 x 4096 x 2 x
+    // 11264 45 and 51).  Not of 8 bits: 64 x 4096 x 2 x 11264 33 us in two parts, 40 in five.
+    if (two_a_unit && M <= 64 && t < 256 && 20 * (256 / t) < 9 * (512 / t)) s = 512 / t;
     s = s < steps / 4 ? s : steps / 4;
     if (s < 1) s = 1;
     p.k_per = (steps + s - 1) / s * step_k;
@@ -449,9 +449,9 @@ inline TilePlan plan_tiles(int64_t M, int64_t N, int64_t K, int step_k, bool gat
     return p;
 }
 
-inline uint64_t tile_part_bytes(int64_t M, int64_t N, int64_t K, int step_k, bool gated = false)
+inline uint64_t tile_part_bytes(int64_t M, int64_t N, int64_t K, int step_k, bool two_a_unit = false)
 {
-    const TilePlan p = plan_tiles(M, N, K, step_k, gated);
+    const TilePlan p = plan_tiles(M, N, K, step_k, two_a_unit);
     return p.splits > 1 ? (uint64_t)p.splits * M * N * 4 : 0;
 }
 
@@ -459,7 +459,7 @@ template <int EB, bool EXACT, typename T, Layout LA, Layout LB, int FORM = PLAIN
 hipError_t run_tiles(GemmArgs g, float *part, hipStream_t stream)
 {
     const TilePlan p = plan_tiles(g.M, FORM == GATED ? 2 * g.N : g.N, g.K, kStepBytes / EB,
-                                  FORM == GATED);
+                                  FORM == GATED && EB == 2);
     g.k_per = p.k_per;
     g.part = p.splits > 1 ? part : nullptr;
     const dim3 grid(p.tiles_m * p.tiles_n * (uint32_t)p.splits);

@@ -440,6 +440,8 @@ __device__ __forceinline__ void float32_wave(const GemmArgs &g, Layout la, Layou
     }
 }
 
+__device__ __forceinline__ int piece_of(int i, int pieces) { return i < pieces ? i : i - pieces; }
+
 // Three buffers: a step's copies (16 k of three terms of both operands) have two steps to land.
 // 16384 x 4096 x 4096 2500 us, 219 TFLOP/s of float32 or 1.3 PFLOP/s of bf16 products; 3001 x 1000
 // x 2003 85 us, 141: 384 tiles of 128 x 128 leave the second of two places on half of the units
@@ -453,8 +455,8 @@ __global__ void __launch_bounds__(64 * WAVES_M *WAVES_N)
     constexpr int NW = WAVES_M * WAVES_N, WM = BM / WAVES_M / 32;
     static_assert(BN / WAVES_N == 64, "a wave's epilogue takes 64 columns");
     constexpr int kA = P * BM * kRowTermBytes, kB = P * BN * kRowTermBytes, kBuffer = kA + kB;
-    constexpr int kCopies = kBuffer / 1024 / NW, kCopiesA = kA / 1024 / NW;
-    static_assert(kBuffer % (1024 * NW) == 0 && kA % (1024 * NW) == 0, "whole copies");
+    constexpr int kPieces = kBuffer / 1024, kPiecesA = kA / 1024, kCopies = (kPieces + NW - 1) / NW;
+    static_assert(kBuffer % 1024 == 0 && kA % 1024 == 0, "whole pieces");
     constexpr int kEpilogue = NW * kEpilogueFloats * 4;
     __shared__ __attribute__((aligned(1024))) char lds[3 * kBuffer > kEpilogue ? 3 * kBuffer
                                                                                : kEpilogue];
@@ -465,29 +467,31 @@ __global__ void __launch_bounds__(64 * WAVES_M *WAVES_N)
     const int64_t kbeg = (int64_t)split * g.k_per, kend = min(g.K, kbeg + g.k_per);
     const int steps = (int)((kend - kbeg + kBlockK - 1) / kBlockK);
     const int wm = (wave % WAVES_M) * (WM * 32), wn = (wave / WAVES_M) * (64 / NB);
-    const uint32_t lds_wave =
-        (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds + wave * 1024;
+    const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
 
-    // 1024 bytes a copy: 32 rows of a term.
+    // 1024 bytes a piece: 32 rows of a term, A's and then B's (those behind an operand's padding
+    // repeat its last).  Where they do not come out even some are copied twice.
     const char *from[kCopies];
+    int64_t ahead[kCopies];
 #pragma unroll
     for (int i = 0; i < kCopies; ++i) {
-        const bool ofb = i >= kCopiesA;
-        int piece = (ofb ? i - kCopiesA : i) * NW + wave;
+        const int nth = piece_of(i * NW + wave, kPieces);
+        const bool ofb = nth >= kPiecesA;
+        int piece = ofb ? nth - kPiecesA : nth;
         const int per = (ofb ? BC : BM) / 32;
         const bool second = ofb && piece >= P * per;
         if (second) piece -= P * per;
         const SplitOperand &o = second ? b2 : ofb ? b : a;
-        from[i] = o.terms + ((kbeg / kBlockK * P + piece / per) * o.rows + (ofb ? n0 : m0) +
-                             piece % per * 32) * kRowTermBytes;
+        const int64_t row = min((ofb ? n0 : m0) + piece % per * 32, o.rows - 32);
+        from[i] = o.terms + ((kbeg / kBlockK * P + piece / per) * o.rows + row) * kRowTermBytes;
+        ahead[i] = P * o.rows * kRowTermBytes;
     }
-    const int64_t ahead_a = P * a.rows * kRowTermBytes, ahead_b = P * b.rows * kRowTermBytes;
     auto copy = [&](int t) __attribute__((always_inline)) {
-        const uint32_t to = lds_wave + (uint32_t)(t % 3) * kBuffer;
+        const uint32_t to = lds_base + (uint32_t)(t % 3) * kBuffer;
 #pragma unroll
         for (int i = 0; i < kCopies; ++i) {
-            copy16(from[i], lane * 16, to + i * NW * 1024);
-            from[i] += i < kCopiesA ? ahead_a : ahead_b;
+            copy16(from[i], lane * 16, to + piece_of(i * NW + wave, kPieces) * 1024);
+            from[i] += ahead[i];
         }
     };
 
@@ -547,7 +551,7 @@ __global__ void __launch_bounds__(64 * WAVES_M *WAVES_N)
         const int64_t grp = g0 + i / (BM / 64 + BN / 64), r = i % (BM / 64 + BN / 64);
         const int64_t rb = r - BM / 64;
         const SplitOperand &o = NB == 2 && rb >= BC / 64 ? b2 : b;
-        bad = bad || (r < BM / 64 ? a.flags[grp * (a.rows / 64) + m0 / 64 + r]
+        bad = bad || (r < BM / 64 ? a.flags[grp * (a.rows / 64) + min(m0 / 64 + r, a.rows / 64 - 1)]
                                   : o.flags[grp * (o.rows / 64) + n0 / 64 + rb % (BC / 64)]) != 0;
     }
     if (__syncthreads_or(bad))
@@ -572,7 +576,7 @@ bool splits_first(int64_t M, int64_t N, int64_t K)
 }
 
 struct SplitPlan {
-    bool large;
+    int rows;               // of a tile: 128 (128 columns), 192 or 256 (256 columns)
     uint32_t tiles_m, tiles_n;
     int64_t k_per;
     int splits;
@@ -582,8 +586,9 @@ SplitPlan plan_split(int64_t M, int64_t N, int64_t K)
 {
     SplitPlan p{};
     auto tiles = [&](int b) { return ((M + b - 1) / b) * ((N + b - 1) / b); };
-    p.large = tiles(256) >= 192 && 16 * tiles(256) <= 5 * tiles(128);
-    const int b = p.large ? 256 : 128, at_once = p.large ? 256 : 512;
+    const bool large = tiles(256) >= 192 && 16 * tiles(256) <= 5 * tiles(128);
+    const int b = large ? 256 : 128, at_once = large ? 256 : 512;
+    p.rows = b;
     p.tiles_m = (uint32_t)((M + b - 1) / b);
     p.tiles_n = (uint32_t)((N + b - 1) / b);
     // Parts of k where that fills the device's last round better: each part costs a pass over
@@ -598,6 +603,11 @@ SplitPlan plan_split(int64_t M, int64_t N, int64_t K)
     }
     p.k_per = (steps + best - 1) / best * 4 * kBlockK;
     p.splits = (int)((K + p.k_per - 1) / p.k_per);
+    // Tiles of 192 rows where those leave fewer units idle in the last round.
+    if (large && p.splits == 1) {
+        const int64_t m = (M + 191) / 192, t192 = m * p.tiles_n;
+        if ((t192 + 255) / 256 * 192 < (t + 255) / 256 * 256) p.rows = 192, p.tiles_m = (uint32_t)m;
+    }
     return p;
 }
 
@@ -633,8 +643,11 @@ hipError_t run_split(GemmArgs g, Layout la, Layout lb, void *ws, hipStream_t str
     g.k_per = p.k_per;
     g.part = p.splits > 1 ? (float *)w : nullptr;
     const dim3 grid(p.tiles_m * p.tiles_n * (uint32_t)p.splits);
-    if (p.large)
+    if (p.rows == 256)
         gemm_split_kernel<FORM, 256, 256, 2, 4>
+            <<<grid, dim3(512), 0, stream>>>(g, a, b, b2, p.tiles_m, p.tiles_n);
+    else if (p.rows == 192)
+        gemm_split_kernel<FORM, 192, 256, 2, 4>
             <<<grid, dim3(512), 0, stream>>>(g, a, b, b2, p.tiles_m, p.tiles_n);
     else
         gemm_split_kernel<FORM, 128, 128, 2, 2>

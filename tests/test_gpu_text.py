@@ -201,7 +201,8 @@ def test_gated_backward(M, K, N, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("M,K,N", [(4096, 264, 1600), (2100, 520, 1601), (4100, 128, 344)])
+@pytest.mark.parametrize("M,K,N", [(4096, 264, 1600), (2100, 520, 1601), (4100, 128, 344),
+                                   (3001, 400, 2003)])
 def test_gated_on_large_tiles(M, K, N, dtype):
     """Tiles of 256 x 256 forward and backward, and float32 operands split in a pass of their own;
     N at and beside the columns of a tile and of a step."""
@@ -220,6 +221,23 @@ def test_gated_on_large_tiles(M, K, N, dtype):
     want = text_ref.gated_backward(x, wg, wu, dy, zg.cpu(), zu.cpu(), "silu", bf)
     for i, (name, g, (r, b)) in enumerate(zip(("dx", "dwg", "dwu", "dbg", "dbu"), got, want)):
         ref.check(name, g, r, b + (ref.rounded(r, bf) if i < 3 else 0))
+
+
+@pytest.mark.parametrize("M,K,N", [(3001, 400, 4006), (2880, 130, 4090)])
+def test_float32_products_in_tiles_of_192_rows(M, K, N):
+    """Rows that 256 leave units idle with; the last tile goes past the operands' padding."""
+    from paper_2607_25234_amd import whtmix
+    dev = device()
+    say("192_rows", M, K, N)
+    x, w = draw(1, M, K), draw(2, K, N, std=K ** -0.5)
+    z = x.double() @ w.double()
+    bound = ref.sum_bound(K, x.double().abs() @ w.double().abs())
+    ref.check("z", whtmix.linear(x.to(dev), w.to(dev)), z, bound)
+    x[M - 1], x[7] = x[M - 1] * 2.0 ** -110, x[7] * 2.0 ** -110      # rows that do not split
+    w = w * 2.0 ** 40
+    z = x.double() @ w.double()
+    bound = ref.sum_bound(K, x.double().abs() @ w.double().abs())
+    ref.check("tiny", whtmix.linear(x.to(dev), w.to(dev)), z, bound)
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
