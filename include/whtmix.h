@@ -567,8 +567,8 @@ WHTMIX_API int whtmix_layer_norm_mx_forward(const void *x, const void *residual,
  *   dx        [rows][C] of `dtype`: the gradient of x and of the residual;
  *             may be dy or dh.
  *   dweight, dbias  [C] float32, or NULL to skip.
- * Both are summed in a fixed order.  Workspace: for them, up to 1536 rows of 2 C
- * floats; for rows of more than 16384 elements, five floats a row besides.
+ * Both are summed in a fixed order.  Workspace: for them, none for a few rows and
+ * up to 1536 rows of 2 C floats; for rows of more than 16384 elements, five floats a row besides.
  */
 WHTMIX_API int whtmix_layer_norm_backward(const void *h, const float *weight,
                                const void *dy, const void *dh, void *dx,

@@ -5,8 +5,8 @@
 Compiles every HIP / C++ source under csrc/ with hipcc, one process per
 source in parallel, and links them into one shared library beside this file.
 Packed FP32 instructions are disabled for all device code.  Then builds the
-binding's CPython call module (csrc/whtmix_pycall.c, host code only) with the
-host C compiler.
+binding's CPython call module (csrc/whtmix_pycall.c) and its calls on torch
+tensors (csrc/whtmix_torch.cc), both host code only, with the host compilers.
 """
 from __future__ import annotations
 
@@ -24,6 +24,7 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(HERE, "libwhtmix.so")
 PYCALL = os.path.join(HERE, "_whtmix_call" + sysconfig.get_config_var("EXT_SUFFIX"))
+TORCH_CALLS = os.path.join(HERE, "_whtmix_torch" + sysconfig.get_config_var("EXT_SUFFIX"))
 ARCH = "gfx950"
 
 COMPILE_FLAGS = [
@@ -70,6 +71,24 @@ def build_pycall(out: str = PYCALL, verbose: bool = False) -> str:
     return out
 
 
+def build_torch_calls(out: str = TORCH_CALLS, verbose: bool = False) -> str:
+    """The binding's calls on torch tensors (host code, against the installed torch)."""
+    import torch
+
+    cxx = os.environ.get("CXX", "g++")
+    rocm = os.environ.get("ROCM_PATH", "/opt/rocm")
+    at = os.path.dirname(torch.__file__)
+    src = os.path.join(CSRC, "whtmix_torch.cc")
+    _run([cxx, "-O2", "-std=c++17", "-shared", "-fPIC", "-Wall", "-D__HIP_PLATFORM_AMD__=1",
+          "-DUSE_ROCM=1", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+          "-isystem", os.path.join(at, "include"), "-isystem", os.path.join(rocm, "include"),
+          f"-I{sysconfig.get_paths()['include']}", src, "-o", out + ".tmp",
+          "-L" + os.path.join(at, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_hip"],
+         verbose, src)
+    os.replace(out + ".tmp", out)
+    return out
+
+
 def build(out: str = LIB, extra: tuple = (), verbose: bool = False, jobs: int = 0) -> str:
     """Compile each source to an object (in parallel), then link."""
     srcs = sources()
@@ -83,6 +102,7 @@ def build(out: str = LIB, extra: tuple = (), verbose: bool = False, jobs: int = 
     os.replace(out + ".tmp", out)
     if out == LIB:
         build_pycall(verbose=verbose)
+        build_torch_calls(verbose=verbose)
     return out
 
 

@@ -238,6 +238,7 @@ struct LayerNormBackwardKernelArgs {
     const float *weight;
     void *dx;
     float *part;            // [gridDim.x][2][C]: the sums of dy n, then of dy; or null
+    float *dweight, *dbias; // with part null: [C] or null
     int64_t rows, C;
     float eps;
 };
@@ -340,9 +341,9 @@ __global__ void __launch_bounds__(G > 256 ? G : 256, backward_waves(G, Chunk<T>:
             Chunk<T>::store((T *)a.dx + c, n, o);
         }
     }
-    if (!a.part) return;
-    float *out = a.part + (int64_t)blockIdx.x * 2 * a.C;
+    // To this workgroup's partial sums, or where it is the only one to the gradients.
     auto emit = [&](const float (&v)[R][N], float *to) {
+        if (!to) return;
         if constexpr (kRows > 1) {
             __syncthreads();
 #pragma unroll
@@ -363,8 +364,9 @@ __global__ void __launch_bounds__(G > 256 ? G : 256, backward_waves(G, Chunk<T>:
                 store_floats(to + ((int64_t)j * G + lane) * N, count(j), v[j]);
         }
     };
-    emit(dw, out);
-    emit(db, out + a.C);
+    float *out = a.part ? a.part + (int64_t)blockIdx.x * 2 * a.C : nullptr;
+    emit(dw, out ? out : a.dweight);
+    emit(db, out ? out + a.C : a.dbias);
 }
 
 // Rows too wide for registers: what each row's sums give first (stat: [rows][4] of the mean, its
@@ -480,6 +482,7 @@ int64_t backward_parts(int64_t rows, int64_t C, int dtype)
     // As many workgroups as the 256 compute units hold at a time, each of the same count of rows.
     const BackwardShape s = backward_shape(n);
     const int64_t in_block = s.threads() / s.lanes, blocks = (rows + in_block - 1) / in_block;
+    if (blocks <= 4) return 1;          // one workgroup and no launch more
     const int at_once = std::max(1, backward_waves(s.lanes, per * s.chunks) * 4 / (s.threads() / 64));
     return std::min<int64_t>(blocks, 256 * at_once);
 }
@@ -497,10 +500,11 @@ template <typename T> hipError_t backward(const LayerNormBackwardArgs &a)
     const int64_t parts = backward_parts(a.rows, a.C, a.dtype);
     const bool sums = a.dweight || a.dbias;
     const uint32_t b = (uint32_t)parts;
-    const LayerNormBackwardKernelArgs k{a.h, a.dy, a.dh, a.weight, a.dx, sums ? a.ws : nullptr,
-                                        a.rows, a.C, a.eps};
+    const bool wide = n > wide_chunks(Chunk<T>::N), joined = sums && (wide || parts > 1);
+    const LayerNormBackwardKernelArgs k{a.h, a.dy, a.dh, a.weight, a.dx, joined ? a.ws : nullptr,
+                                        a.dweight, a.dbias, a.rows, a.C, a.eps};
     hipError_t e;
-    if (n > wide_chunks(Chunk<T>::N)) {
+    if (wide) {
         float *stat = a.ws + (sums ? parts * 2 * a.C : 0);
         layer_norm_backward_stats<T><<<dim3((uint32_t)std::min<int64_t>(a.rows, 1 << 16)),
                                        dim3(1024), 0, a.stream>>>(k, stat);
@@ -520,7 +524,7 @@ template <typename T> hipError_t backward(const LayerNormBackwardArgs &a)
     else if (n <= 2048) e = run_backward<T, 1024, 2>(k, b, a.stream);
     else if constexpr (Chunk<T>::N == 4) e = run_backward<T, 1024, 4>(k, b, a.stream);
     else e = hipErrorInvalidValue;
-    if (e != hipSuccess || !sums) return e;
+    if (e != hipSuccess || !joined) return e;
     return launch_column_sums(a.ws, parts, a.C, a.dweight, a.dbias, a.stream);
 }
 
@@ -536,8 +540,10 @@ hipError_t launch_layer_norm(const LayerNormArgs &a)
 uint64_t layer_norm_backward_floats(int64_t rows, int64_t C, int dtype, bool sums)
 {
     const int per = dtype == DTYPE_BF16 ? 8 : 4;
-    return (sums ? (uint64_t)backward_parts(rows, C, dtype) * 2 * C : 0) +
-           ((C + per - 1) / per > wide_chunks(per) ? kWideFloats * (uint64_t)rows : 0);
+    const bool wide = (C + per - 1) / per > wide_chunks(per);
+    const int64_t parts = backward_parts(rows, C, dtype);
+    return (sums && (wide || parts > 1) ? (uint64_t)parts * 2 * C : 0) +
+           (wide ? kWideFloats * (uint64_t)rows : 0);
 }
 
 hipError_t launch_layer_norm_backward(const LayerNormBackwardArgs &a)

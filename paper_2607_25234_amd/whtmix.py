@@ -836,12 +836,16 @@ def dequantize_mx(q, scales, C: int | None = None, dtype=None, stream=None):
     """The values q and scales stand for, [..., C] (default: the stored width)
     in dtype (bfloat16, the default, or float32)."""
     T = _torch_module or _torch()
+    dtype = dtype or T.bfloat16
+    code = _CODES.get(dtype)
+    if stream is None and C is not None and code is not None:
+        r = (_ordinary_module or _ordinary()).dequantize_mx(q, scales, C, code)
+        if r is not None:
+            return _taken(r, "dequantize_mx")[0]
     rows, w, pq, ps, dev = _mx(q, scales, "q")
     C = w if C is None else C
     if mx_width(C) != w:
         raise ValueError(f"{C} columns are not stored in {w}")
-    dtype = dtype or T.bfloat16
-    code = _CODES.get(dtype)
     if code is None:
         raise TypeError(f"the output must be float32 or bfloat16, not {dtype}")
     y = q.new_empty((*q.shape[:-1], C), dtype=dtype)
@@ -948,6 +952,45 @@ def linear_mx(xq, xs, wq, ws, bias=None, activation: str = "none", residual=None
 
 # ---- layer norm, gated products, embedding ----
 
+_ORDINARY = ("layer_norm_forward", "layer_norm_mx_forward", "layer_norm_backward", "gated_forward",
+             "gated_backward", "gated_mx_forward", "embedding_forward", "embedding_backward",
+             "dequantize_mx")
+_ordinary_module = None
+
+
+class _NotBuilt:
+    """In the place of the module below where it is not built: no call is taken."""
+
+    def __getattr__(self, name):
+        return lambda *args: None
+
+
+def _ordinary():
+    """The module (csrc/whtmix_torch.cc) that makes ordinary calls of these functions in C++:
+    checks, allocations and the entry point, 2 to 4 us a call less than here.  Its functions
+    return None for calls that they leave to the code here, and a status that is not
+    success as an int."""
+    global _ordinary_module
+    if _ordinary_module is None:
+        T, L = _torch(), lib()
+        try:
+            from paper_2607_25234_amd import _whtmix_torch as m
+        except ImportError:
+            m = _NotBuilt()
+        else:
+            m.bind(tuple(ctypes.cast(getattr(L, "whtmix_" + name), ctypes.c_void_p).value
+                         for name in _ORDINARY), T.nn.Parameter)
+        _ordinary_module = m
+    return _ordinary_module
+
+
+def _taken(result, name):
+    """An ordinary call's tensors."""
+    if type(result) is int:
+        raise WhtmixError(result, "whtmix_" + name)
+    return result
+
+
 def layer_norm(x, weight, bias=None, residual=None, eps: float = 1e-6, out=None, stream=None):
     """Layer norm with the residual's addition: (y, h) with h = x + residual (x itself
     without one) and y = (h - mean(h)) / sqrt(mean((h - mean(h))^2) + eps) * weight + bias,
@@ -957,6 +1000,10 @@ def layer_norm(x, weight, bias=None, residual=None, eps: float = 1e-6, out=None,
     weight, bias: float32 [C]; residual: a contiguous tensor of x's shape and type;
     out: optional contiguous tensor for y (may be x itself; without a residual
     h is None then, since x holds y)."""
+    if out is None and stream is None:
+        r = (_ordinary_module or _ordinary()).layer_norm(x, weight, bias, residual, eps)
+        if r is not None:
+            return _taken(r, "layer_norm_forward")
     T = _torch_module or _torch()
     dt, rows, C, ld, dev = _operand(x, "x")
     shape, dtype = x.shape, x.dtype
@@ -981,6 +1028,10 @@ def layer_norm(x, weight, bias=None, residual=None, eps: float = 1e-6, out=None,
 
 def layer_norm_mx(x, weight, bias=None, residual=None, eps: float = 1e-6, stream=None):
     """layer_norm() with y in block-scaled 8 bits: (q, scales, h), q and scales as norm_mx."""
+    if stream is None:
+        r = (_ordinary_module or _ordinary()).layer_norm_mx(x, weight, bias, residual, eps)
+        if r is not None:
+            return _taken(r, "layer_norm_mx_forward")
     T = _torch_module or _torch()
     dt, rows, C, ld, dev = _operand(x, "x")
     shape = x.shape
@@ -1003,6 +1054,11 @@ def layer_norm_backward(h, weight, dy, dh=None, eps: float = 1e-6, want_dweight:
     """Gradients through layer_norm() from its kept h: (dx, dweight, dbias), dx the gradient
     of x and of the residual (dh, the gradient of h, is added), the others float32 (None
     when not wanted).  dx may be dy or dh."""
+    if dx is None and stream is None:
+        r = (_ordinary_module or _ordinary()).layer_norm_backward(h, weight, dy, dh, eps,
+                                                                 want_dweight, want_dbias)
+        if r is not None:
+            return _taken(r, "layer_norm_backward")
     T = _torch_module or _torch()
     dt, rows, C, _, dev = _operand(h, "h")
     shape, dtype = h.shape, h.dtype
@@ -1036,6 +1092,11 @@ def gated(x, w_gate, w_up, b_gate=None, b_up=None, activation: str = "silu",
     x: [..., K] float32 or bfloat16 (rows may be columns of a wider tensor); w_gate, w_up:
     [K, N] of x's type; b_gate, b_up: float32 [N]; activation as linear's; out: optional
     contiguous [..., N] tensor for y."""
+    if out is None and stream is None:
+        r = (_ordinary_module or _ordinary()).gated(x, w_gate, w_up, b_gate, b_up,
+                                                   _activation(activation), want_z)
+        if r is not None:
+            return _taken(r, "gated_forward") if want_z else _taken(r, "gated_forward")[0]
     T = _torch_module or _torch()
     dt, M, K, ld, dev = _operand(x, "x")
     act, dtype = _activation(activation), x.dtype
@@ -1061,6 +1122,11 @@ def gated_backward(x, w_gate, w_up, dy, z_gate, z_up, activation: str = "silu",
     """Gradients through gated() for the upstream gradient dy: (dx, dw_gate, dw_up, db_gate,
     db_up), the biases' float32 and the others in x's type; what is not wanted is None.
     z_gate, z_up: what gated kept."""
+    if stream is None:
+        r = (_ordinary_module or _ordinary()).gated_backward(
+            x, w_gate, w_up, dy, z_gate, z_up, _activation(activation), want_dx, want_dw, want_dbias)
+        if r is not None:
+            return _taken(r, "gated_backward")
     T = _torch_module or _torch()
     dt, M, K, ld, dev = _operand(x, "x")
     act, dtype = _activation(activation), x.dtype
@@ -1086,6 +1152,11 @@ def gated_mx(xq, xs, wgq, wgs, wuq, wus, b_gate=None, b_up=None, activation: str
     """gated() on block-scaled 8 bits: xq, xs as norm_mx or quantize_mx give them, [..., K];
     wgq, wgs and wuq, wus the weights' columns as rows, [N, K].  Returns y [..., N] in dtype
     (out's, else bfloat16), or with out_mx (q, scales) of the result.  Sums as linear_mx's."""
+    if dtype is None and out is None and stream is None:
+        r = (_ordinary_module or _ordinary()).gated_mx(
+            xq, xs, wgq, wgs, wuq, wus, b_gate, b_up, _activation(activation), out_mx)
+        if r is not None:
+            return _taken(r, "gated_mx_forward") if out_mx else _taken(r, "gated_mx_forward")[0]
     T = _torch_module or _torch()
     M, K, pxq, pxs, dev = _mx(xq, xs, "xq")
     act = _activation(activation)
@@ -1137,6 +1208,10 @@ def embedding(ids, table, scale: float = 1.0, out=None, stream=None):
     (float32 or bfloat16, contiguous) that ids (int32 or int64, any shape) name.  A negative id
     is padding, whose row is zeros; an id of vocab or more gives NaN.  out: optional contiguous
     tensor for the rows."""
+    if out is None and stream is None:
+        r = (_ordinary_module or _ordinary()).embedding(ids, table, scale)
+        if r is not None:
+            return _taken(r, "embedding_forward")[0]
     _torch_module or _torch()
     if table.dim() != 2:
         raise ValueError("table must be [vocab, C]")
@@ -1158,6 +1233,10 @@ def embedding_backward(ids, dy, vocab: int, scale: float = 1.0, stream=None):
     """The gradient of embedding()'s table [vocab, C] for the upstream gradient dy
     [*ids.shape, C], in dy's type: every row is written, in an order of sums that does not
     change from run to run.  Padding and ids of vocab or more have none."""
+    if stream is None:
+        r = (_ordinary_module or _ordinary()).embedding_backward(ids, dy, vocab, scale)
+        if r is not None:
+            return _taken(r, "embedding_backward")[0]
     _torch_module or _torch()
     if not dy.is_cuda:
         raise ValueError("dy must be on a GPU device")

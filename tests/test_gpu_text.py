@@ -589,6 +589,77 @@ def program(dev, dt, M, V, C, N, seed=0):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_ordinary_calls_and_the_others(dtype, monkeypatch):
+    """Calls that the module on torch tensors takes give what the Python way does, and it takes
+    them; those that are not ordinary go the Python way, which raises or takes them."""
+    from paper_2607_25234_amd import whtmix
+    dev, dt = device(), DTYPES[dtype]
+    say("ordinary", dtype)
+    m = whtmix._ordinary()
+    assert not isinstance(m, whtmix._NotBuilt)
+    args = program(dev, dt, 300, 50, 264, 344)
+    ids, table, dy, w, b, wg, wu, g8, u8 = args
+    dy3 = dy.reshape(3, 100, 264)
+    bg = torch.randn(344, device=dev)
+    fast = all_calls(*args)
+    more = [whtmix.layer_norm(dy3, w, None)[0], whtmix.layer_norm_mx(dy3, w)[0].view(torch.uint8),
+            *whtmix.gated(dy3, wg, wu, bg, None, "gelu", want_z=True),
+            whtmix.embedding(ids.reshape(3, 100).to(torch.int32), table),
+            whtmix.embedding(ids[7], table)]
+    kept = whtmix.layer_norm(torch.nn.Parameter(dy), w)
+    assert whtmix.layer_norm(dy, w)[1] is dy and whtmix.layer_norm_mx(dy, w)[2] is dy
+    taken = []
+    monkeypatch.setattr(whtmix, "_ordinary_module", whtmix._NotBuilt())
+    for x, y in zip(fast, all_calls(*args)):
+        assert torch.equal(x, y) and x.dtype == y.dtype
+    slow = [whtmix.layer_norm(dy3, w, None)[0], whtmix.layer_norm_mx(dy3, w)[0].view(torch.uint8),
+            *whtmix.gated(dy3, wg, wu, bg, None, "gelu", want_z=True),
+            whtmix.embedding(ids.reshape(3, 100).to(torch.int32), table),
+            whtmix.embedding(ids[7], table)]
+    for x, y in zip(more, slow):
+        assert torch.equal(x, y) and x.shape == y.shape
+    assert torch.equal(kept[0], whtmix.layer_norm(dy, w)[0])
+    for name in ("layer_norm", "layer_norm_mx"):
+        f = getattr(m, name)
+        assert f(dy, w, b, dy, 1e-6) is not None
+        for bad in ((dy[:, :8], w[:8], None, None, 1e-6), (dy, w[:8], b, None, 1e-6),
+                    (dy, w.to(torch.bfloat16), b, None, 1e-6), (dy.double(), w, b, None, 1e-6),
+                    (dy, w, b, dy3, 1e-6), (dy[0], w, b, None, 1e-6), (dy.cpu(), w, b, None, 1e-6),
+                    (dy, w.cpu(), b, None, 1e-6), (dy[:0], w, b, dy[:0], 1e-6),
+                    (dy, None, b, None, 1e-6), (None, w, b, None, 1e-6),
+                    (dy.t(), w, b, None, 1e-6)):
+            assert f(*bad) is None, (name, len(taken))
+            taken.append(bad)
+        assert f(dy, w, b, dy, -1.0) == 1 and f(dy, w, b, dy, math.nan) == 1     # a status
+        with pytest.raises(TypeError):
+            f(dy, w, b, dy)
+        with pytest.raises(TypeError):
+            f(dy, w, b, dy, "eps")
+    assert m.gated(dy, wg, wu[:, :8], None, None, 4, False) is None
+    assert m.gated(dy, wg[0], wu, None, None, 4, False) is None
+    assert m.gated(dy, wg, wu, None, None, 9, False) == 1
+    assert m.gated_backward(dy, wg, wu, dy, dy, dy, 4, True, True, True) is None
+    assert m.gated_mx(dy, w, *g8, *u8, None, None, 4, False) is None
+    assert m.embedding(ids.float(), table, 1.0) is None and m.embedding(ids, w, 1.0) is None
+    assert m.embedding(ids, table, math.inf) == 1
+    assert m.embedding_backward(ids, dy, 0, 1.0) is None
+    assert m.embedding_backward(ids[:7], dy, 50, 1.0) is None
+    monkeypatch.setattr(whtmix, "_ordinary_module", m)
+    for f in (lambda: whtmix.layer_norm(dy, w, eps=-1.0), lambda: whtmix.embedding(ids, table, math.nan),
+              lambda: whtmix.embedding_backward(ids, dy, 0)):
+        with pytest.raises(whtmix.WhtmixError):
+            f()
+    with pytest.raises(ValueError):
+        whtmix.gated(dy, wg, wu, activation="tanh")
+    with pytest.raises(ValueError):
+        whtmix.gated(dy, wg, wu[:, :8])
+    with pytest.raises(ValueError):
+        whtmix.embedding_backward(ids[:7], dy, 50)
+    with pytest.raises(TypeError):
+        whtmix.embedding(ids.float(), table)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("M,V,C,N", [(300, 50, 264, 344), (9000, 700, 64, 172)])
 def test_streams_repeats_and_graph_replays(M, V, C, N, dtype):
     """The same bits every time, on another stream, and from a graph captured on a stream whose

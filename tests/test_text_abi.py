@@ -159,7 +159,7 @@ def test_workspaces(monkeypatch):
         pytest.skip("fake device addresses are for hosts without a GPU")
     monkeypatch.setenv("WHTMIX_TEST_FAIL_WORKSPACE", "1")
     for dtype in (0, 1):
-        for rows, C in ((1, 64), (10 ** 8, 8), (10 ** 6, 128), (5000, 4096), (3000, 16384)):
+        for rows, C in ((200, 640), (10 ** 8, 8), (10 ** 6, 128), (5000, 4096), (3000, 16384)):
             f = workspace("whtmix_layer_norm_backward", FAR[:7], (rows, C), (dtype,), (1e-6,)) // 4
             assert 2 * C <= f <= 1536 * 2 * C, (rows, C)
         for rows, C in ((1, 16392), (5000, 20000), (10 ** 6, 70001)):
@@ -204,3 +204,30 @@ def test_call_module_refuses_what_no_entry_point_takes():
                  (1, (0,) * 8, (0,) * 4, (0,), 0), (1, (0,) * 7, (0,) * 3, (0,), 0)):
         with pytest.raises(TypeError):
             m.call_rows(*args)
+
+
+def test_torch_calls_leave_what_is_not_ordinary():
+    """The module on torch tensors takes no host tensor and nothing that is none."""
+    torch = pytest.importorskip("torch")
+    m = whtmix._ordinary()
+    assert not isinstance(m, whtmix._NotBuilt)
+    x, w = torch.zeros(4, 64), torch.ones(64)
+    ids = torch.zeros(4, dtype=torch.int64)
+    for o in (x, None, 3, [1.0]):
+        assert m.layer_norm(o, w, None, None, 1e-6) is None
+        assert m.layer_norm_mx(o, w, None, None, 1e-6) is None
+        assert m.layer_norm_backward(o, w, x, None, 1e-6, True, True) is None
+        assert m.gated(o, x, x, None, None, 4, False) is None
+        assert m.gated_backward(o, x, x, x, x, x, 4, True, True, True) is None
+        assert m.gated_mx(o, x, x, x, x, x, None, None, 4, False) is None
+        assert m.dequantize_mx(o, x, 64, 1) is None
+        assert m.embedding(ids, o, 1.0) is None and m.embedding_backward(ids, o, 7, 1.0) is None
+    for f, n in ((m.layer_norm, 5), (m.gated, 7), (m.gated_mx, 10), (m.embedding, 3)):
+        with pytest.raises(TypeError):
+            f(*[x] * (n - 1))
+    for bad in ((), ((1, 2), int), ([0] * 9, int)):
+        with pytest.raises(TypeError):
+            m.bind(*bad)
+    assert whtmix._NotBuilt().layer_norm(x) is None
+    with pytest.raises(whtmix.WhtmixError):
+        whtmix._taken(1, "layer_norm_forward")
