@@ -48,7 +48,7 @@ __global__ void __launch_bounds__(256) embedding_kernel(EmbeddingKernelArgs a)
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const bool real = (uint64_t)id[u] < (uint64_t)a.vocab;
-            Chunk<T>::load((const T *)a.table + (real ? id[u] * a.C + c : 0), real ? n : 0, v[u]);
+            load_row<T>((const T *)a.table + (real ? id[u] * a.C + c : 0), real ? n : 0, v[u]);
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -61,7 +61,7 @@ __global__ void __launch_bounds__(256) embedding_kernel(EmbeddingKernelArgs a)
 #pragma unroll
                 for (int i = 0; i < N; ++i) v[u][i] = 0.f;
             }
-            Chunk<T>::store((T *)a.y + row * a.C + c, n, v[u]);
+            store_row<T>((T *)a.y + row * a.C + c, n, v[u]);
         }
     }
 }
@@ -373,7 +373,7 @@ template <typename T> __device__ __forceinline__ void zero_rows(const SumArgs &a
     for (int r = 0; r < kZeroRows; ++r) {
         if (!(rows >> r & 1)) continue;
         for (int64_t k = lane; k < chunks; k += 64)
-            Chunk<T>::store(to + r * a.C + k * N, (int)min((int64_t)N, a.C - k * N), zero);
+            store_row<T>(to + r * a.C + k * N, (int)min((int64_t)N, a.C - k * N), zero);
     }
 }
 
@@ -501,7 +501,7 @@ template <typename T> __global__ void __launch_bounds__(256) sum_kernel(SumArgs 
             if (key >= (uint64_t)a.vocab || n == 0) return;
 #pragma unroll
             for (int k = 0; k < N; ++k) s[k] *= a.scale;
-            Chunk<T>::store((T *)a.dtable + (int64_t)key * a.C + c, n, s);
+            store_row<T>((T *)a.dtable + (int64_t)key * a.C + c, n, s);
         },
         [&](int which, uint32_t key, float (&s)[N]) __attribute__((always_inline)) {
             if (key < (uint64_t)a.vocab) store_floats(part + which * a.C, n, s);
@@ -559,7 +559,7 @@ template <typename T> __global__ void __launch_bounds__(256) join_kernel(SumArgs
         for (int k = 0; k < N; ++k) s[k] += sums[((g << a.lanes_log2) + lane) * N + k];
 #pragma unroll
     for (int k = 0; k < N; ++k) s[k] *= a.scale;
-    Chunk<T>::store((T *)a.dtable + (int64_t)key * a.C + c, n, s);
+    store_row<T>((T *)a.dtable + (int64_t)key * a.C + c, n, s);
 }
 
 // ---- few ids ----
@@ -668,7 +668,7 @@ template <typename T> __global__ void __launch_bounds__(256) few_ids_join_kernel
         for (int k = 0; k < N; ++k) s[k] += sums[((g << a.lanes_log2) + lane) * N + k];
 #pragma unroll
     for (int k = 0; k < N; ++k) s[k] *= a.scale;
-    Chunk<T>::store((T *)a.dtable + v * a.C + c, n, s);
+    store_row<T>((T *)a.dtable + v * a.C + c, n, s);
 }
 
 struct Plan {
@@ -700,14 +700,16 @@ Plan make_plan(int64_t rows, int64_t vocab, int64_t C, int dtype)
     if (vocab < kBins && chunks <= 64 && few_part <= uint64_t(24) << 20) {
         p.few = true;
         p.tiles = few_tiles;
-        p.stretch = kFewTile >> (9 - p.lanes_log2);
+        const int64_t groups = kSortThreads >> p.lanes_log2;
+        p.stretch = (int)((std::min<int64_t>(rows, kFewTile) + groups - 1) / groups);
         p.counts = up256((uint64_t)few_tiles * vocab * 4);
         p.part = few_part;
         return p;
     }
     p.slices = (chunks + (1 << p.lanes_log2) - 1) >> p.lanes_log2;
-    // Stretches for 2^17 lanes, of 8 to 256 tokens.
-    p.stretch = 1 << (3 + log2_up(rows * chunks >> 20, 5));
+    // Stretches for 2^18 lanes, of 8 to 256 tokens (194910 x 240 bf16: 64 us, 74 for half as many lanes
+    // and 70 for twice as many; 65536 x 1024: 62, 66 and 65).
+    p.stretch = 1 << (3 + log2_up(rows * chunks >> 21, 5));
     p.range = p.stretch * (256 >> p.lanes_log2);
     p.ranges = (rows + p.range - 1) / p.range;
     p.pairs = up256((uint64_t)rows * 4);

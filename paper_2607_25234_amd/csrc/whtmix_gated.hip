@@ -10,11 +10,20 @@
 // 2 Np columns (forms TWO_K and HALVES), one launch each in place of two.  Narrow inputs form dx
 // in the pass that forms dzg and dzu (whtmix_gated_dzx.hip).
 #include "whtmix_gemm.h"
+#include "whtmix_row.h"
 
 #include <algorithm>
 
 namespace whtmix {
 namespace {
+
+template <typename T> __device__ __forceinline__ void load_eight(const T *p, int n, float (&v)[8])
+{
+    constexpr int N = Chunk<T>::N;
+#pragma unroll
+    for (int i = 0; i < 8; i += N)
+        load_row<T>(p + i, max(0, n - i), *(float(*)[N])(v + i));
+}
 
 // dzg and dzu with the columns' sums of the unrounded values.  `across` threads take a row's
 // chunks of 8 columns, the workgroup's other threads the rows below: with whole rows the memory
@@ -45,9 +54,9 @@ __global__ void __launch_bounds__(256)
                     const int64_t r = m + k * down;
                     const int c = r < end ? cnt : 0;
                     const int64_t at = c ? r * N + n : 0;
-                    load8(dy + at, c, d[k]);
-                    load8(zg + at, c, g[k]);
-                    load8(zu + at, c, u[k]);
+                    load_eight(dy + at, c, d[k]);
+                    load_eight(zg + at, c, g[k]);
+                    load_eight(zu + at, c, u[k]);
                 }
 #pragma unroll
                 for (int k = 0; k < U; ++k) {
@@ -87,9 +96,9 @@ __global__ void __launch_bounds__(256)
     }
 }
 
-// Threads across the columns of `width`: whole rows of up to 64 chunks where that leaves at most a
-// quarter of the workgroup idle (262144 x 344: 237 us, 298 by 16 threads), else the most of 32, 16 and
-// 8 that cover the width to an eighth (3001 x 2003 float32: 29 us, 56 by whole rows).
+// Threads across the columns of `width`: whole rows of up to 64 chunks where that leaves at
+// most a quarter of the workgroup idle (262144 x 344: 237 us, 298 by 16 threads), else the most of 32,
+// 16 and 8 that cover the width to an eighth (3001 x 2003 float32: 29 us, 56 by whole rows).
 int dz_across(int64_t width)
 {
     const int64_t chunks = width / 8;

@@ -7,7 +7,7 @@ namespace whtmix {
 uint64_t gemm_bf16_bytes(const GemmArgs &g, Form form)
 {
     const int64_t columns = form == GATED ? 2 * g.N : g.N;
-    const uint64_t parts = tile_part_bytes(g.M, columns, g.K, kStepBytes / 2, form == GATED);
+    const uint64_t parts = tile_part_bytes(g.M, columns, g.K, kStepBytes / 2, form != PLAIN);
     if (form == TWO_K) return parts;
     if (form == HALVES)
         return parts + side(g.a, K_STRIDED, g.M, g.K, g.lda).bytes() +

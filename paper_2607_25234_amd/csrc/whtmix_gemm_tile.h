@@ -438,10 +438,13 @@ inline TilePlan plan_tiles(int64_t M, int64_t N, int64_t K, int step_k, bool two
     // hide), or two where their parts stay long (128 x 262144 x 512: 76 us, 84 us with one).
     int64_t s = t >= 256 ? 1 : 256 / t;
     if (t < 256 && p.bm < 256 && steps / (2 * s) >= 32) s *= 2;
-    // Both weights of a bf16 gated product of few rows: two workgroups a unit where one leaves more
-    // units empty (1 x 4096 x 2 x 12288, 96 tiles: 44 us in five parts, 51 in two; 16 x 4096 x 2 x
-    // 11264 45 and 51).  Not of 8 bits: 64 x 4096 x 2 x 11264 33 us in two parts, 40 in five.
-    if (two_a_unit && M <= 64 && t < 256 && 20 * (256 / t) < 9 * (512 / t)) s = 512 / t;
+    // The gated forms of bf16: two workgroups a unit where that leaves a tenth fewer places empty (1 x
+    // 4096 x 2 x 12288, 96 tiles: 44 us in five parts, 51 in two; 16 x 4096 x 2 x 11264 45 and 51), and
+    // of more rows where their parts stay long.  Not of 8 bits: 64 x 4096 x 2 x 11264 33 us in two
+    // parts, 40 in five.
+    if (two_a_unit && t < 256 && (M <= 64 || steps / (512 / t) >= 16) &&
+        20 * (s * t <= 256 ? 2 * s : s) < 18 * (512 / t))
+        s = 512 / t;
     s = s < steps / 4 ? s : steps / 4;
     if (s < 1) s = 1;
     p.k_per = (steps + s - 1) / s * step_k;
@@ -459,7 +462,7 @@ template <int EB, bool EXACT, typename T, Layout LA, Layout LB, int FORM = PLAIN
 hipError_t run_tiles(GemmArgs g, float *part, hipStream_t stream)
 {
     const TilePlan p = plan_tiles(g.M, FORM == GATED ? 2 * g.N : g.N, g.K, kStepBytes / EB,
-                                  FORM == GATED && EB == 2);
+                                  FORM != PLAIN && EB == 2);
     g.k_per = p.k_per;
     g.part = p.splits > 1 ? part : nullptr;
     const dim3 grid(p.tiles_m * p.tiles_n * (uint32_t)p.splits);

@@ -82,7 +82,7 @@ __global__ void __launch_bounds__(threads_of(G), forward_waves(R))
     auto emit = [&](int64_t row, int64_t c, float (&v)[N], const float (&w)[N],
                     const float (&b)[N], const RowStats &r) {
         const int n = count(c);
-        if (a.h && n > 0) Chunk<T>::store((T *)a.h + row * a.C + c, n, v);
+        if (a.h && n > 0) store_row<T>((T *)a.h + row * a.C + c, n, v);
         if constexpr (MX) {
 #pragma unroll
             for (int i = 0; i < N; ++i) {
@@ -96,7 +96,7 @@ __global__ void __launch_bounds__(threads_of(G), forward_waves(R))
         } else {
 #pragma unroll
             for (int i = 0; i < N; ++i) v[i] = fmaf((v[i] - r.hi - r.lo) * r.rstd, w[i], b[i]);
-            if (n > 0) Chunk<T>::store((T *)a.y + row * a.C + c, n, v);
+            if (n > 0) store_row<T>((T *)a.y + row * a.C + c, n, v);
         }
     };
 
@@ -140,10 +140,10 @@ __global__ void __launch_bounds__(threads_of(G), forward_waves(R))
             const T *r = a.residual ? (const T *)a.residual + row * a.C : nullptr;
             auto load = [&](int64_t c, float (&v)[N]) {
                 const int n = count(c);
-                Chunk<T>::load(x + (n ? c : 0), n, v);
+                load_row<T>(x + (n ? c : 0), n, v);
                 if (r) {
                     float e[N];
-                    Chunk<T>::load(r + (n ? c : 0), n, e);
+                    load_row<T>(r + (n ? c : 0), n, e);
 #pragma unroll
                     for (int i = 0; i < N; ++i) v[i] += e[i];
                 }
@@ -287,8 +287,8 @@ __global__ void __launch_bounds__(G > 256 ? G : 256, backward_waves(G, Chunk<T>:
         for (int j = 0; j < R; ++j) {
             const int n = live ? count(j) : 0;
             const int64_t c = at + (n ? ((int64_t)j * G + lane) * N : 0);
-            Chunk<T>::load((const T *)a.h + c, n, h[j]);
-            Chunk<T>::load((const T *)a.dy + c, n, dy[j]);
+            load_row<T>((const T *)a.h + c, n, h[j]);
+            load_row<T>((const T *)a.dy + c, n, dy[j]);
         }
 #pragma unroll
         for (int j = 0; j < R; ++j) {
@@ -329,7 +329,7 @@ __global__ void __launch_bounds__(G > 256 ? G : 256, backward_waves(G, Chunk<T>:
             const int64_t c = at + ((int64_t)j * G + lane) * N;
             float w[N], o[N];
             if constexpr (R > 1) weights(j, w);
-            if (a.dh) Chunk<T>::load((const T *)a.dh + c, n, o);
+            if (a.dh) load_row<T>((const T *)a.dh + c, n, o);
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 const float nn = (h[j][i] - off) * rstd;
@@ -338,7 +338,7 @@ __global__ void __launch_bounds__(G > 256 ? G : 256, backward_waves(G, Chunk<T>:
                 dw[j][i] = fmaf(dy[j][i], nn, dw[j][i]);
                 db[j][i] += dy[j][i];
             }
-            Chunk<T>::store((T *)a.dx + c, n, o);
+            store_row<T>((T *)a.dx + c, n, o);
         }
     }
     // To this workgroup's partial sums, or where it is the only one to the gradients.
@@ -385,8 +385,8 @@ __global__ void __launch_bounds__(1024) layer_norm_backward_stats(LayerNormBackw
             for (int64_t c = (int64_t)threadIdx.x * N; c < a.C; c += 1024 * N) {
                 const int n = (int)min((int64_t)N, a.C - c);
                 float h[N], dy[N], w[N];
-                Chunk<T>::load((const T *)a.h + at + c, n, h);
-                Chunk<T>::load((const T *)a.dy + at + c, n, dy);
+                load_row<T>((const T *)a.h + at + c, n, h);
+                load_row<T>((const T *)a.dy + at + c, n, dy);
                 load_floats(a.weight + c, n, w);
 #pragma unroll
                 for (int i = 0; i < N; ++i)
@@ -437,9 +437,9 @@ __global__ void __launch_bounds__(256)
                     gm = stat[4 * row + 3], k = stat[4 * a.rows + row];
         const int64_t at = row * a.C + c;
         float h[N], dy[N], o[N];
-        Chunk<T>::load((const T *)a.h + at, n, h);
-        Chunk<T>::load((const T *)a.dy + at, n, dy);
-        if (a.dh) Chunk<T>::load((const T *)a.dh + at, n, o);
+        load_row<T>((const T *)a.h + at, n, h);
+        load_row<T>((const T *)a.dy + at, n, dy);
+        if (a.dh) load_row<T>((const T *)a.dh + at, n, o);
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const float nn = (h[i] - mean - off) * rstd;
@@ -448,7 +448,7 @@ __global__ void __launch_bounds__(256)
             dw[i] = fmaf(dy[i], nn, dw[i]);
             db[i] += dy[i];
         }
-        Chunk<T>::store((T *)a.dx + at, n, o);
+        store_row<T>((T *)a.dx + at, n, o);
     }
     if (a.part) {
         float *out = a.part + (int64_t)blockIdx.y * 2 * a.C + c;
