@@ -476,26 +476,37 @@ template <typename T> hipError_t pick_backward(const NormBackwardArgs &a)
     return launch_column_sum(a.ws, parts, a.C, a.dweight, a.stream);
 }
 
-// Column sums of partial rows, to `out` and those from `half` on to `out2`: 32 columns a workgroup, 32 rows at a time, each
-// thread's rows in order and then the 32 sums in order.  2048 x 128: 5-7 us, a launch and
-// its loads' latency.
+// Column sums of partial rows, to `out` and those from `half` on to `out2`: COLS columns a workgroup,
+// 1024 / COLS rows at a time, each thread's rows in order and then their sums in order.  2048 x
+// 128: 5-7 us, a launch and its loads' latency; 2048 x 688 11 us, 8 with 8 columns.
+template <int COLS>
 __global__ void __launch_bounds__(1024) column_sum_kernel(const float *part, int64_t n, int64_t C,
                                                           float *out, int64_t half, float *out2)
 {
-    __shared__ float s[32][33];
-    const int cx = threadIdx.x & 31, ry = threadIdx.x >> 5;
-    const int64_t c = (int64_t)blockIdx.x * 32 + cx;
+    constexpr int kDown = 1024 / COLS;
+    __shared__ float s[kDown][COLS + 1];
+    const int cx = threadIdx.x % COLS, ry = threadIdx.x / COLS;
+    const int64_t c = (int64_t)blockIdx.x * COLS + cx;
     float t = 0.f;
-    for (int64_t r = ry; r < n; r += 8 * 32) {      // eight loads in flight
+    for (int64_t r = ry; r < n; r += 8 * kDown) {      // eight loads in flight
         float v[8];
 #pragma unroll
         for (int u = 0; u < 8; ++u)
-            v[u] = c < C && r + u * 32 < n ? part[(r + u * 32) * C + c] : 0.f;
+            v[u] = c < C && r + u * kDown < n ? part[(r + u * kDown) * C + c] : 0.f;
 #pragma unroll
         for (int u = 0; u < 8; ++u) t += v[u];
     }
     s[ry][cx] = t;
     __syncthreads();
+    if constexpr (kDown > 32) {         // 32 sums of a column again
+        constexpr int kFold = kDown / 32;
+        float u = 0.f;
+#pragma unroll
+        for (int r = 0; r < kFold; ++r) u += ry < 32 ? s[ry * kFold + r][cx] : 0.f;
+        __syncthreads();
+        if (ry < 32) s[ry][cx] = u;
+        __syncthreads();
+    }
     if (ry == 0 && c < C) {
         float u = 0.f;
 #pragma unroll
@@ -565,16 +576,21 @@ hipError_t launch_dequantize(const void *q, const uint8_t *scales, void *y, int6
 hipError_t launch_column_sum(const float *part, int64_t n, int64_t C, float *out,
                              hipStream_t stream)
 {
-    column_sum_kernel<<<dim3((uint32_t)((C + 31) / 32)), dim3(1024), 0, stream>>>(part, n, C, out, C,
-                                                                                  nullptr);
+    column_sum_kernel<32><<<dim3((uint32_t)((C + 31) / 32)), dim3(1024), 0, stream>>>(
+        part, n, C, out, C, nullptr);
     return hipGetLastError();
 }
 
 hipError_t launch_column_sums(const float *part, int64_t n, int64_t C, float *first, float *second,
                               hipStream_t stream)
 {
-    column_sum_kernel<<<dim3((uint32_t)((2 * C + 31) / 32)), dim3(1024), 0, stream>>>(
-        part, n, 2 * C, first, C, second);
+    // Many rows of few columns: narrower workgroups, more of them.
+    if (n >= 512 && C <= 1024)
+        column_sum_kernel<8><<<dim3((uint32_t)((2 * C + 7) / 8)), dim3(1024), 0, stream>>>(
+            part, n, 2 * C, first, C, second);
+    else
+        column_sum_kernel<32><<<dim3((uint32_t)((2 * C + 31) / 32)), dim3(1024), 0, stream>>>(
+            part, n, 2 * C, first, C, second);
     return hipGetLastError();
 }
 
