@@ -200,6 +200,37 @@ def test_gated_backward(M, K, N, dtype):
             assert torch.equal(a, b) if (i + 1) // 2 == which else a is None
 
 
+@pytest.mark.parametrize("M,K,N,act", [
+    (49152, 128, 520, "silu"), (49151, 128, 520, "silu"), (49200, 60, 1024, "none"),
+    (49153, 16, 1032, "gelu"), (49155, 7, 272, "relu"), (32769, 128, 256, "gelu_tanh"),
+    (32767, 128, 256, "gelu"), (32768, 1, 64, "gelu"), (49300, 129, 344, "silu"),
+    (49163, 90, 343, "relu")])
+def test_gated_backward_of_many_rows(M, K, N, act):
+    """dz, its sums and dx in one pass over the rows or apart: sizes at and beside the rule's, with
+    rows and columns of dx that end inside a tile and N that ends inside a step."""
+    from paper_2607_25234_amd import whtmix
+    dev, dt = device(), torch.bfloat16
+    say("gated_backward_many", M, K, N, act)
+    x, wg, wu, _, _ = gated_case(M, K, N, "bf16")
+    dy, zg, zu = (draw(s, M, N, std=std, dtype=dt) for s, std in ((11, 1.0), (12, 2.0), (13, 2.0)))
+    args = *to(dev, x, wg, wu, dy, zg, zu), act
+    got = whtmix.gated_backward(*args)
+    want = text_ref.gated_backward(x, wg, wu, dy, zg, zu, act, True)
+    names = "dx", "dwg", "dwu", "dbg", "dbu"
+    for i, (name, g, (r, b)) in enumerate(zip(names, got, want)):
+        ref.check(name, g, r, b + (ref.rounded(r, True) if i < 3 else 0))
+    again = whtmix.gated_backward(*args)
+    assert all(torch.equal(a, b) for a, b in zip(again, got))
+    for which in range(3):      # each alone: the sums' order may be another
+        one = whtmix.gated_backward(*args, want_dx=which == 0, want_dw=which == 1,
+                                    want_dbias=which == 2)
+        for i, (name, g, (r, b)) in enumerate(zip(names, one, want)):
+            if (i + 1) // 2 != which:
+                assert g is None
+            else:
+                ref.check(name, g, r, b + (ref.rounded(r, True) if i < 3 else 0))
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("M,K,N", [(4096, 264, 1600), (2100, 520, 1601), (4100, 128, 344),
                                    (3001, 400, 2003)])
