@@ -80,7 +80,8 @@ template <typename T, typename Id> hipError_t forward(const EmbeddingArgs &a)
     const EmbeddingKernelArgs k{a.ids, a.table, a.y, a.rows, a.vocab, a.C, a.scale, l};
     const uint32_t across = (uint32_t)((chunks + (1 << l) - 1) >> l);
     auto blocks = [&](int U) {
-        return (uint32_t)std::min<int64_t>((a.rows + groups * U - 1) / (groups * U), 1 << 20);
+        return (uint32_t)std::min<int64_t>((a.rows + groups * U - 1) / (groups * U),
+                                           kMaxBlocks / across);
     };
     if (blocks(4) * across >= 1024)
         embedding_kernel<T, Id, 4><<<dim3(blocks(4), across), dim3(256), 0, a.stream>>>(k);
@@ -384,10 +385,10 @@ template <int N, int THREADS> struct StretchLds {
 };
 
 // Sums the runs of equal keys in the list's entries [begin, end), of `size` in all; entry i has
-// key_of(i) and the row row_of(i), whose chunk of columns load() brings.  A run that lies in the range goes to
-// write(key, s); the sums of one that comes from before it or goes on behind it to left(which,
-// key, s), which = 0 or 1.  Each group of lanes takes `stretch` entries; what goes on from
-// one to the next is joined in order through LDS.
+// key_of(i) and the row row_of(i), whose chunk of columns load() brings.  A run that lies in the
+// range goes to write(key, s); the sums of one that comes from before it or goes on behind it to
+// left(which, key, s), which = 0 or 1.  Each group of lanes takes `stretch` entries; what goes on
+// from one to the next is joined in order through LDS.
 template <typename T, int THREADS, typename Key, typename Row, typename Load, typename Write,
           typename Left>
 __device__ __forceinline__ void sum_runs(StretchLds<Chunk<T>::N, THREADS> &lds, int64_t begin,
