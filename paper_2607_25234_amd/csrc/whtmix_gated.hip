@@ -149,6 +149,7 @@ uint64_t align256(uint64_t v) { return (v + 255) / 256 * 256; }
 // What a backward call is made of.
 struct Parts {
     int64_t width;          // Np: of each half of dz
+    int64_t pitch;          // between dz's rows
     bool together;          // dz, its sums and dx in one pass
     bool two_k;             // dx reads both weights where they lie
     uint64_t dz, sums, weights, product;    // bytes
@@ -167,7 +168,7 @@ GemmArgs dx_args(const GatedBackwardArgs &a, const Parts &p, const void *dz, con
 GemmArgs dw_args(const GatedBackwardArgs &a, const Parts &p, const void *dz)
 {
     GemmArgs g{};
-    g.a = a.x, g.lda = a.ldx, g.b = dz, g.ldb = 2 * p.width;
+    g.a = a.x, g.lda = a.ldx, g.b = dz, g.ldb = p.pitch;
     g.M = a.K, g.N = 2 * p.width, g.K = a.M;
     g.y = a.dwg, g.y2 = a.dwu, g.half = p.width, g.half_n = a.N;
     return g;
@@ -182,10 +183,11 @@ Parts parts_of(const GatedBackwardArgs &a)
     // bf16: whole cache lines, float32: whole chunks of the stores
     p.width = bf16 ? (a.N + 63) / 64 * 64 : (a.N + 7) / 8 * 8;
     p.together = gated_dzx_takes(a);
+    p.pitch = p.together ? gated_dzx_pitch(a.N, p.width) : 2 * p.width;
     p.two_k = bf16 && a.N % 64 == 0 && aligned(a.wg) && aligned(a.wu);
-    if (a.dx || a.dwg) p.dz = align256((uint64_t)a.M * 2 * p.width * e);
+    if (a.dx || a.dwg) p.dz = align256((uint64_t)a.M * p.pitch * e);
     if (a.dbg)
-        p.sums = align256((uint64_t)(p.together ? gated_dzx_parts(a.M) : dz_parts(a.M, p.width)) * 2 *
+        p.sums = align256((uint64_t)(p.together ? gated_dzx_parts(a) : dz_parts(a.M, p.width)) * 2 *
                           a.N * 4);
     // a workspace's address is aligned: null stands for it
     const bool product = a.dx && !p.together;
@@ -211,7 +213,7 @@ template <typename T> hipError_t backward(const GatedBackwardArgs &a)
     float *sums = p.sums ? (float *)(ws + p.dz) : nullptr;
     T *joined = (T *)(ws + p.dz + p.sums);
     void *rest = ws + p.dz + p.sums + p.weights;
-    int64_t parts = gated_dzx_parts(a.M);
+    int64_t parts = p.together ? gated_dzx_parts(a) : 0;
     hipError_t e = p.together ? launch_gated_dzx(a, p.width, dz, sums)
                               : launch_dz<T>(a, p.width, dz, sums, parts);
     if (e != hipSuccess) return e;

@@ -482,9 +482,11 @@ hipError_t gated_mx_gemm(GemmArgs g, int dtype, void *ws, hipStream_t stream);
 bool dzx_takes(const LinearBackwardArgs &a);
 int64_t dzx_parts(int64_t M);
 hipError_t launch_dzx(const LinearBackwardArgs &a, void *dz, float *part);
-// The same of a gated product (whtmix_gated_dzx.hip): dz [M][2 width], part [parts][2][N].
+// The same of a gated product (whtmix_gated_dzx.hip): dz [M] rows a pitch apart, its second half
+// `width` columns on; part [parts][2][N].
 bool gated_dzx_takes(const GatedBackwardArgs &a);
-int64_t gated_dzx_parts(int64_t M);
+int64_t gated_dzx_parts(const GatedBackwardArgs &a);
+int64_t gated_dzx_pitch(int64_t N, int64_t width);
 hipError_t launch_gated_dzx(const GatedBackwardArgs &a, int64_t width, void *dz, float *part);
 uint64_t gemm_mx_bytes(const GemmArgs &g);
 hipError_t gemm_mx(GemmArgs g, int dtype, void *ws, hipStream_t stream);
