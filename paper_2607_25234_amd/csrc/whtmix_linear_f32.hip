@@ -352,14 +352,26 @@ uint64_t split_bytes(int64_t rows, int64_t k)
            (uint64_t)split_groups(k) * (split_rows(rows) / 64) * 4;
 }
 
+struct SplitJob {
+    const float *src;
+    int64_t ld, rows;
+    char *out;
+    uint32_t *flags;
+    uint32_t across, blocks;        // workgroups along the rows, and in all
+    Layout layout;
+};
+
+// Workgroup `at` of an operand's.
 template <Layout L>
-__global__ void __launch_bounds__(256) split_kernel(const float *src, int64_t ld, int64_t rows,
-                                                    int64_t K, char *out, uint32_t *flags)
+__device__ __forceinline__ void split_block(const SplitJob &job, int64_t K, uint32_t at)
 {
+    const float *src = job.src;
+    const int64_t ld = job.ld, rows = job.rows;
     const int t = threadIdx.x;
     // Sixteen k of a row a thread; neighbouring lanes take neighbouring rows.
-    const int64_t row = (int64_t)blockIdx.x * 64 + (L == K_CONTIGUOUS ? t % 16 + t / 64 * 16 : t % 64);
-    const int64_t block = (int64_t)blockIdx.y * 4 + (L == K_CONTIGUOUS ? t / 16 % 4 : t / 64);
+    const int64_t row = (int64_t)(at % job.across) * 64 +
+                        (L == K_CONTIGUOUS ? t % 16 + t / 64 * 16 : t % 64);
+    const int64_t block = (int64_t)(at / job.across) * 4 + (L == K_CONTIGUOUS ? t / 16 % 4 : t / 64);
     const int64_t k0 = block * kBlockK;
     const int n = row < rows ? (int)max((int64_t)0, min((int64_t)kBlockK, K - k0)) : 0;
     float v[16];
@@ -375,9 +387,9 @@ __global__ void __launch_bounds__(256) split_kernel(const float *src, int64_t ld
     float top = 0.f;
 #pragma unroll
     for (int i = 0; i < 16; ++i) top = fmaxf(top, fabsf(v[i]));
-    const int64_t padded = (int64_t)gridDim.x * 64;
+    const int64_t padded = (int64_t)job.across * 64;
     if (block < split_blocks(K)) {
-        char *to = out + (block * P * padded + row) * kRowTermBytes;
+        char *to = job.out + (block * P * padded + row) * kRowTermBytes;
         const int swap = (int)(row >> 3 & 1) * 16;
 #pragma unroll
         for (int s = 0; s < P; ++s) {
@@ -396,7 +408,21 @@ __global__ void __launch_bounds__(256) split_kernel(const float *src, int64_t ld
         }
     }
     const int bad = __syncthreads_or(top >= kSplitMax || (top != 0.f && top < kSplitMin));
-    if (t == 0) flags[(int64_t)blockIdx.y * gridDim.x + blockIdx.x] = bad ? 1u : 0u;
+    if (t == 0) job.flags[at] = bad ? 1u : 0u;
+}
+
+// All operands of a product in one launch, the smaller under the larger's end: 3001 x 1000 x 2 x 2003
+// gated 145 us, 152 in three launches, its gradients 390 and 398; 3001 x 1000 x 2003 86 and 91.
+__global__ void __launch_bounds__(256) split_kernel(SplitJob a, SplitJob b, SplitJob b2, int64_t K)
+{
+    uint32_t at = blockIdx.x;
+    SplitJob job = a;
+    if (at >= a.blocks) {
+        at -= a.blocks, job = b;
+        if (at >= b.blocks) at -= b.blocks, job = b2;
+    }
+    if (job.layout == K_CONTIGUOUS) split_block<K_CONTIGUOUS>(job, K, at);
+    else split_block<K_STRIDED>(job, K, at);
 }
 
 struct SplitOperand {
@@ -562,10 +588,10 @@ __global__ void __launch_bounds__(64 * WAVES_M *WAVES_N)
     else finish_wave<float, FORM>(g, out, m0 + wm, n0 + wn, split, acc);
 }
 
-// Whether the passes that split the operands (10 bytes an element at 4.5 TB/s, and two launches
+// Whether the passes that split the operands (10 bytes an element at 4.5 TB/s, and a launch
 // more) cost less than what the tile kernel saves: it reaches about 210 TFLOP/s of float32, the
 // kernel that splits on the way about 150.  Measured, first against second: 16384 x 4096 x
-// 4096 2567 and 3219 us, 3001 x 1000 x 2003 91 and 107 us, 512 x 2048 x 2048 56 and 43 us, 65536 x
+// 4096 2567 and 3219 us, 3001 x 1000 x 2003 86 and 107 us, 512 x 2048 x 2048 56 and 43 us, 65536 x
 // 128 x 512 90 and 76 us.
 bool splits_first(int64_t M, int64_t N, int64_t K)
 {
@@ -611,23 +637,19 @@ SplitPlan plan_split(int64_t M, int64_t N, int64_t K)
     return p;
 }
 
-hipError_t split_operand(const void *p, Layout l, int64_t ld, int64_t rows, int64_t K, char *&ws,
-                         SplitOperand &o, hipStream_t stream)
+SplitJob split_operand(const void *p, Layout l, int64_t ld, int64_t rows, int64_t K, char *&ws,
+                       SplitOperand &o)
 {
     o.rows = split_rows(rows);
     o.terms = ws;
     o.layout = l;
     char *flags = ws + (uint64_t)split_blocks(K) * P * o.rows * kRowTermBytes;
     o.flags = (const uint32_t *)flags;
-    const dim3 grid((uint32_t)(o.rows / 64), (uint32_t)split_groups(K));
-    if (l == K_CONTIGUOUS)
-        split_kernel<K_CONTIGUOUS><<<grid, dim3(256), 0, stream>>>((const float *)p, ld, rows, K, ws,
-                                                                   (uint32_t *)flags);
-    else
-        split_kernel<K_STRIDED><<<grid, dim3(256), 0, stream>>>((const float *)p, ld, rows, K, ws,
-                                                                (uint32_t *)flags);
+    const uint32_t across = (uint32_t)(o.rows / 64);
+    const SplitJob job{(const float *)p, ld, rows, ws, (uint32_t *)flags, across,
+                       across * (uint32_t)split_groups(K), l};
     ws += (split_bytes(rows, K) + 1023) / 1024 * 1024;
-    return hipGetLastError();
+    return job;
 }
 
 template <Form FORM>
@@ -635,9 +657,12 @@ hipError_t run_split(GemmArgs g, Layout la, Layout lb, void *ws, hipStream_t str
 {
     char *w = (char *)ws;
     SplitOperand a{}, b{}, b2{};
-    hipError_t e = split_operand(g.a, la, g.lda, g.M, g.K, w, a, stream);
-    if (e == hipSuccess) e = split_operand(g.b, lb, g.ldb, g.N, g.K, w, b, stream);
-    if (FORM == GATED && e == hipSuccess) e = split_operand(g.b2, lb, g.ldb2, g.N, g.K, w, b2, stream);
+    const SplitJob ja = split_operand(g.a, la, g.lda, g.M, g.K, w, a);
+    const SplitJob jb = split_operand(g.b, lb, g.ldb, g.N, g.K, w, b);
+    SplitJob jb2{};
+    if (FORM == GATED) jb2 = split_operand(g.b2, lb, g.ldb2, g.N, g.K, w, b2);
+    split_kernel<<<dim3(ja.blocks + jb.blocks + jb2.blocks), dim3(256), 0, stream>>>(ja, jb, jb2, g.K);
+    hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     const SplitPlan p = plan_split(g.M, columns(g, FORM), g.K);
     g.k_per = p.k_per;
