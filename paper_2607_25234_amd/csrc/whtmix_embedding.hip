@@ -9,6 +9,10 @@
 // the sorted list is cut into ranges of equal length: a workgroup adds what its range holds,
 // writes the runs that lie in it, and leaves the sums of the others to be joined in order by a
 // kernel of its own.
+//
+// Bound by memory where tokens are many: 65536 x 1024 bf16 of a table of 50000 rows 37 us forward (268 MB,
+// table rows that come often out of the caches), and backward 61 us of sums, 25 of sorting in
+// two passes and 6 of joining.  17 rows 2.6 us: the latency of an id and then a row.
 #include "whtmix_row.h"
 
 #include <algorithm>
@@ -566,7 +570,7 @@ template <typename T> __global__ void __launch_bounds__(256) join_kernel(SumArgs
 // ---- few ids ----
 // A vocabulary of a digit's size (byte tokens): a workgroup sorts its own tokens in LDS and writes
 // the sums of each id's to memory, one row of C floats an id; a second kernel adds those of an
-// id in order.  Two launches in place of four.
+// id in order.  Two launches in place of four (131072 x 64 float32 of 256 ids: 15 + 4 us).
 struct FewArgs {
     const void *ids, *dy;
     void *dtable;
@@ -695,10 +699,15 @@ Plan make_plan(int64_t rows, int64_t vocab, int64_t C, int dtype)
     const int per = dtype == DTYPE_BF16 ? 8 : 4;
     const int64_t chunks = (C + per - 1) / per;
     p.lanes_log2 = log2_up(chunks, 6);
-    // Ids of one digit and rows of a wave, where the tiles' sums are cheap to move.
+    // Ids of one digit, where the tiles' sums are few: a tile's time goes by C and by the ids (us so and
+    // by the whole sort, 16384 tokens: C = 64, 256 ids, float32 15.5 and 19.7; C = 128, 256 ids, bf16 20.0 and
+    // 21.2; C = 128, 500 ids 24.0 and 20.6; C = 256, 256 ids 26.6 and 20.6; 262144 tokens, C = 128, 256 ids,
+    // 32 MiB of sums, 32 and 40), and lists that one workgroup sorts are quick (1000 tokens: C = 128, 256
+    // ids 20.3 and 15.4, C = 8 21.0 and 9.9, C = 32 14.2 and 17.1; 300, C = 64, bf16 12.5 and 15.4).
     const int64_t few_tiles = (rows + kFewTile - 1) / kFewTile;
     const uint64_t few_part = (uint64_t)few_tiles * vocab * C * 4;
-    if (vocab < kBins && chunks <= 64 && few_part <= uint64_t(24) << 20) {
+    if (vocab < kBins && C <= 128 && vocab * C <= 1 << 15 && few_part <= uint64_t(32) << 20 &&
+        (rows > kTile || (C >= 32 && C <= 64))) {
         p.few = true;
         p.tiles = few_tiles;
         const int64_t groups = kSortThreads >> p.lanes_log2;

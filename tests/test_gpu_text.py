@@ -526,6 +526,26 @@ def test_embedding_backward(rows, V, C, dtype):
             assert torch.equal(got.cpu()[ids[at].long()], dy[at])
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,V,C", [(2048, 100, 16), (2049, 100, 16), (2048, 256, 64), (1025, 256, 32),
+                                      (2500, 256, 128), (2500, 257, 128), (2500, 200, 129),
+                                      (2500, 511, 64), (2500, 512, 64), (262144, 256, 128),
+                                      (262145, 256, 128), (70000, 3, 1)])
+def test_embedding_backward_of_few_ids(rows, V, C, dtype):
+    """At and beside the sizes that choose between the tiles' sums and the whole sort."""
+    from paper_2607_25234_amd import whtmix
+    dev, bf = device(), dtype == "bf16"
+    say("embedding_few", rows, V, C, dtype)
+    gen = torch.Generator().manual_seed(rows + V + C)
+    ids = torch.randint(-1, V + 1, (rows,), generator=gen)      # padding and one past the table
+    ids[rows // 3: rows // 2] = V // 2                          # a long run
+    dy = draw(3, rows, C, dtype=DTYPES[dtype])
+    got = whtmix.embedding_backward(ids.to(dev), dy.to(dev), V, 0.5)
+    want, bound = text_ref.embedding_backward(ids, dy, V, 0.5, bf)
+    ref.check("dtable", got, want, bound)
+    assert torch.equal(got, whtmix.embedding_backward(ids.to(dev), dy.to(dev), V, 0.5))
+
+
 def test_embedding_order_of_sums():
     """Equal tokens are added in ascending order: 2^24 and then ones, which do not add to it, and
     as many rows of its negative, leave exactly the ones after it."""
