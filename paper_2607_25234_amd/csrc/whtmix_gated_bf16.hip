@@ -1,5 +1,7 @@
 // The other forms of bf16 products on the tile kernel: two products of the same rows whose sums
 // meet in the epilogue, one whose columns are of two outputs, one whose k is of two operands.
+// One row, 1 x 4096 x 2 x 12288: 38 us for the weights' 201 MB (5.3 TB/s) and 5 for the sum of the
+// parts of k; a kernel of multiply-adds on the weights as they stream took 48 in all.
 #include "whtmix_pack.h"
 
 namespace whtmix {

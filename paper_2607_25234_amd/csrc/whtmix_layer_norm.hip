@@ -11,6 +11,10 @@
 // spread.  The float32 mean m is itself off by some 2^-24 |m|: the distances' own mean d, summed
 // with their squares, corrects both (v = mean((t - m)^2) - d^2, mu = m + d, kept as two floats).
 // Sums are float32 in a fixed order: a lane's over its own values, then a fixed tree.
+//
+// 8192 x 4096 bf16 to 8 bits 51 us (4.6 TB/s of 235 MB), 262144 x 128 bf16 45 us forward and 47
+// backward (5.9 and 5.7 TB/s, in part out of the caches), 5003 x 1111 float32 15 and 18 us; one row of
+// 4096 3.1 us, the latency of its loads and of two sums.
 #include "whtmix_row.h"
 
 #include <algorithm>
@@ -52,7 +56,8 @@ constexpr int threads_of(int G) { return G > 256 ? G : 256; }
 
 // One row on G lanes, R chunks a lane; with R = 0 (rows wider than the registers hold) the row
 // is read three times.  With one chunk a lane rows go round the grid and the next one is on its
-// way while this one is formed.  Values for the 8-bit form keep the parts that roundings on the
+// way while this one is formed (8192 x 4096 to 8 bits 51 us, 62 with a workgroup a row).  Values for
+// the 8-bit form keep the parts that roundings on the
 // way would leave out: off by a few 2^-24, one value in 10^5 moves to the next of the 8-bit ones.
 template <typename T, int G, int R, bool MX>
 __global__ void __launch_bounds__(threads_of(G), forward_waves(R))
