@@ -657,8 +657,8 @@ WHTMIX_API int whtmix_embedding_forward(const void *ids, const void *table, void
  *             names it.  Padding and ids of vocab or more have no gradient.
  * Sums are float32, in an order that ids, rows, vocab and C fix.  Workspace: 16
  * bytes a token, 2048 bytes for every 2048 tokens, and C floats for every 16
- * tokens at most; or, for vocabularies below 512, up to 24 MiB of partial sums
- * and 4 vocab bytes for every 1024 tokens.
+ * tokens at most; or, for vocabularies below 512 of rows of up to 128, up to 24
+ * MiB of partial sums and 4 vocab bytes for every 1024 tokens.
  */
 WHTMIX_API int whtmix_embedding_backward(const void *ids, const void *dy, void *dtable,
                               int64_t rows, int64_t vocab, int64_t C,

@@ -529,7 +529,8 @@ def test_embedding_backward(rows, V, C, dtype):
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("rows,V,C", [(2048, 100, 16), (2049, 100, 16), (2048, 256, 64), (1025, 256, 32),
                                       (2500, 256, 128), (2500, 257, 128), (2500, 200, 129),
-                                      (2500, 511, 64), (2500, 512, 64), (262144, 256, 128),
+                                      (2500, 511, 64), (2500, 512, 64), (196608, 256, 128),
+                                      (196609, 256, 128), (262144, 256, 128),
                                       (262145, 256, 128), (70000, 3, 1)])
 def test_embedding_backward_of_few_ids(rows, V, C, dtype):
     """At and beside the sizes that choose between the tiles' sums and the whole sort."""

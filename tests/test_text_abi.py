@@ -169,11 +169,11 @@ def test_workspaces(monkeypatch):
         # 16 bytes a token (each of four arrays to whole 256 bytes), counts, partial sums; or a
         # small vocabulary's partial sums and counts
         for rows, V, C in ((1, 600, 1), (4096, 50000, 64), (4097, 50000, 64), (10 ** 6, 512, 1000),
-                           (10 ** 6, 300, 1000), (10 ** 6, 300, 64)):
+                           (10 ** 6, 300, 1000), (10 ** 6, 300, 64), (1, 1, 1), (4000, 511, 256)):
             b = workspace("whtmix_embedding_backward", FAR[:3], (rows, V, C), (1, dtype), (1.0,))
             fixed = 16 * rows + 2048 * (-(-rows // 2048) + 1)
             assert fixed <= b <= fixed + 1024 + (-(-rows // 32)) * 2 * C * 4, (rows, V, C)
-        for rows, V, C in ((1, 1, 1), (131072, 256, 64), (4000, 511, 256)):
+        for rows, V, C in ((300, 1, 32), (131072, 256, 64), (4000, 511, 64), (196608, 256, 128)):
             b = workspace("whtmix_embedding_backward", FAR[:3], (rows, V, C), (1, dtype), (1.0,))
             counts = 4 * V * -(-rows // 1024)
             assert counts * (C + 1) <= b <= counts + 256 + (24 << 20)
