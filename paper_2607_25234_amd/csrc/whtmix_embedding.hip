@@ -699,11 +699,12 @@ Plan make_plan(int64_t rows, int64_t vocab, int64_t C, int dtype)
     const int per = dtype == DTYPE_BF16 ? 8 : 4;
     const int64_t chunks = (C + per - 1) / per;
     p.lanes_log2 = log2_up(chunks, 6);
-    // Ids of one digit, where the tiles' sums are few: a tile's time goes by C and by the ids (us so and
-    // by the whole sort, 16384 tokens: C = 64, 256 ids, float32 15.5 and 19.7; C = 128, 256 ids, bf16 20.0 and
-    // 21.2; C = 128, 500 ids 24.0 and 20.6; C = 256, 256 ids 26.6 and 20.6; 262144 tokens, C = 64, 256 ids,
-    // 16 MiB of sums, 24 and 38: 24 MiB are the most a caller is told of), and lists that one workgroup sorts are quick (1000 tokens: C = 128, 256
-    // ids 20.3 and 15.4, C = 8 21.0 and 9.9, C = 32 14.2 and 17.1; 300, C = 64, bf16 12.5 and 15.4).
+    // Ids of one digit, where the tiles' sums are few: a tile's time goes by C and by the ids (us so
+    // and by the whole sort, 16384 tokens: C = 64, 256 ids, float32 15.5 and 19.7; C = 128, 256 ids,
+    // bf16 20.0 and 21.2; C = 128, 500 ids 24.0 and 20.6; C = 256, 256 ids 26.6 and 20.6; 262144
+    // tokens, C = 64, 256 ids, float32 24 and 38).  24 MiB of sums are the most a caller is told of.
+    // Lists that one workgroup sorts are quick (1000 tokens, bf16: C = 128, 256 ids 20.3 and 15.4, C =
+    // 8 21.0 and 9.9, C = 32 14.2 and 17.1; 300 tokens, C = 64 12.5 and 15.4).
     const int64_t few_tiles = (rows + kFewTile - 1) / kFewTile;
     const uint64_t few_part = (uint64_t)few_tiles * vocab * C * 4;
     if (vocab < kBins && C <= 128 && vocab * C <= 1 << 15 && few_part <= uint64_t(24) << 20 &&

@@ -282,7 +282,8 @@ hipError_t launch_gated_dzx(const GatedBackwardArgs &a, int64_t width, void *dz,
     const int apart = rows_apart(a.N);
     const uint32_t groups = groups_of(a.M, a.N);
     const GatedDzxArgs d{(const __bf16 *)a.dy, (const __bf16 *)a.zg, (const __bf16 *)a.zu, a.wg, a.wu,
-                         (__bf16 *)dz, part, (__bf16 *)a.dx, a.M, a.N, a.K, width, gated_dzx_pitch(a.N, width), groups, apart};
+                         (__bf16 *)dz, part, (__bf16 *)a.dx, a.M, a.N, a.K, width,
+                         gated_dzx_pitch(a.N, width), groups, apart};
     const auto kernel = a.act == ACT_RELU        ? gated_dzx_kernel<ACT_RELU>
                         : a.act == ACT_GELU      ? gated_dzx_kernel<ACT_GELU>
                         : a.act == ACT_GELU_TANH ? gated_dzx_kernel<ACT_GELU_TANH>

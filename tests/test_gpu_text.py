@@ -712,7 +712,7 @@ def test_ordinary_calls_and_the_others(dtype, monkeypatch):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("M,V,C,N", [(300, 50, 264, 344), (9000, 700, 64, 172)])
+@pytest.mark.parametrize("M,V,C,N", [(300, 50, 264, 344), (9000, 700, 64, 172), (49300, 200, 64, 344)])
 def test_streams_repeats_and_graph_replays(M, V, C, N, dtype):
     """The same bits every time, on another stream, and from a graph captured on a stream whose
     workspace earlier calls sized, replayed on new inputs with eager work between."""
@@ -739,6 +739,22 @@ def test_streams_repeats_and_graph_replays(M, V, C, N, dtype):
         got = [t.clone() for t in outs]
         for i, (a, b) in enumerate(zip(got, all_calls(*args))):
             assert torch.equal(a, b), (k, i)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("M,V,C,N", [(300, 50, 264, 343), (9000, 700, 64, 172), (49300, 200, 64, 344),
+                                     (3001, 130, 400, 1003)])
+def test_after_a_call_full_of_nan(M, V, C, N, dtype):
+    """What a call leaves in the workspace reaches no other call: the same bits after one whose
+    intermediate values are all NaN."""
+    dev, dt = device(), DTYPES[dtype]
+    say("after_nan", M, V, C, N, dtype)
+    args = program(dev, dt, M, V, C, N)
+    first = all_calls(*args)
+    bad = [args[0].clamp(min=0), *(torch.full_like(t, float("nan")) for t in args[1:7]), *args[7:]]
+    assert all(t.isnan().all() for t in all_calls(*bad)[:14])
+    for i, (a, b) in enumerate(zip(all_calls(*args), first)):
+        assert torch.equal(a, b), i
 
 
 def test_two_threads():
