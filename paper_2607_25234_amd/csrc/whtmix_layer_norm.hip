@@ -8,12 +8,17 @@
 // Bound by memory: a row is read once into the registers of G lanes (R chunks of 16 bytes each)
 // and all that is formed of it leaves from there.  The mean comes first and the squares are of
 // the distances from it, because mean(t^2) - mu^2 cancels where the mean is large beside the
-// spread.  The float32 mean m is itself off by some 2^-24 |m|: the distances' own mean d, summed
-// with their squares, corrects both (v = mean((t - m)^2) - d^2, mu = m + d, kept as two floats).
+// spread.  The float32 mean is itself off by some 2^-24 |mu|, so distances are taken from a pivot p
+// near it, and their own mean d, summed with their squares, gives both (v = mean((t - p)^2) - d^2,
+// mu = p + d, kept as two floats).  Rows of bf16 lie on a coarse grid, of which every t - p would
+// drop the same low bits of a p that has all 24: a bias that d would take for its own.  p is
+// therefore rounded to 2^-12 of the spread, which makes such distances and their sums exact
+// (error of mu in units of 2^-24 of the spread, root mean square, 512 rows of 4096 values in bf16 of mean 0
+// and deviation 1: 0.006, 0.28 about the mean with all its bits; of mean 1: 0.005 and 0.31).
 // Sums are float32 in a fixed order: a lane's over its own values, then a fixed tree.
 //
-// 8192 x 4096 bf16 to 8 bits 51 us (4.6 TB/s of 235 MB), 262144 x 128 bf16 45 us forward and 47
-// backward (5.9 and 5.7 TB/s, in part out of the caches), 5003 x 1111 float32 15 and 18 us; one row of
+// 8192 x 4096 bf16 to 8 bits 50 us (4.7 TB/s of 235 MB), 262144 x 128 bf16 45 us forward and 48
+// backward (5.9 and 5.6 TB/s, in part out of the caches), 5003 x 1111 float32 14 and 17 us; one row of
 // 4096 3.1 us, the latency of its loads and of two sums.
 #include "whtmix_row.h"
 
@@ -31,18 +36,30 @@ struct LayerNormKernelArgs {
     float eps;
 };
 
-// What a row's sums give: of its elements their sum s, and about m = s / C the sums t0 of the
-// distances and t1 of their squares.  m + d is kept as hi + lo: t - hi - lo rounds once where
-// the mean is moderate, and still holds where it is far larger than the spread.
+// What distances are taken from, by a row's mean m and the mean of its squares: m to 2^-12 of the
+// spread or down to half of that (the next power of two).  Of a mean beyond 16 spreads all bits are
+// kept: values are near it there, and their distances exact; and where squares overflow or
+// cancel to nothing.
+__device__ __forceinline__ float row_pivot(float m, float squares)
+{
+    const float q = fmaxf(fmaf(-m, m, squares), 0.f);
+    const uint32_t spread = ((f32_bits(q) >> 23) + 127) >> 1;       // its exponent
+    const float on = bits_f32((spread + 11) << 23 | 0x400000u);     // 1.5 * 2^11 of it
+    return m * m <= 256.f * q && q < bits_f32(0x7f800000u) ? (m + on) - on : m;
+}
+
+// What a row's sums give: of the distances from its pivot p their sum t0 and their squares' t1.
+// The mean p + d is kept as hi + lo: t - hi - lo rounds once where the mean is moderate, and
+// still holds where it is far larger than the spread.
 struct RowStats {
     float hi, lo, rstd;
 };
-__device__ __forceinline__ RowStats row_stats(float m, float t0, float t1, float C, float eps)
+__device__ __forceinline__ RowStats row_stats(float p, float t0, float t1, float C, float eps)
 {
     const float d = t0 / C, v = fmaxf(fmaf(-d, d, t1 / C), 0.f) + eps;
     RowStats r;
-    r.hi = m + d;
-    r.lo = (m - r.hi) + d;
+    r.hi = p + d;
+    r.lo = (p - r.hi) + d;
     // The hardware's reciprocal root to its last bit, by a step of Newton's.
     const float e = rsqrtf(v);
     const float c = fmaf(0.5f * e, fmaf(-v * e, e, 1.f), e);
@@ -56,7 +73,7 @@ constexpr int threads_of(int G) { return G > 256 ? G : 256; }
 
 // One row on G lanes, R chunks a lane; with R = 0 (rows wider than the registers hold) the row
 // is read three times.  With one chunk a lane rows go round the grid and the next one is on its
-// way while this one is formed (8192 x 4096 to 8 bits 51 us, 62 with a workgroup a row).  Values for
+// way while this one is formed (8192 x 4096 to 8 bits 50 us; 62 with a workgroup a row).  Values for
 // the 8-bit form keep the parts that roundings on the
 // way would leave out: off by a few 2^-24, one value in 10^5 moves to the next of the 8-bit ones.
 template <typename T, int G, int R, bool MX>
@@ -68,18 +85,26 @@ __global__ void __launch_bounds__(threads_of(G), forward_waves(R))
     __shared__ float part[2][48];
     const int lane = threadIdx.x % G;
     const int64_t width = MX ? (a.C + kMxBlock - 1) / kMxBlock * kMxBlock : a.C;
-    const float C = (float)a.C;
+    const float C = (float)a.C, inv = 1.f / C;
     auto count = [&](int64_t c) { return (int)min((int64_t)N, max((int64_t)0, a.C - c)); };
     auto vectors = [&](int64_t c, float (&w)[N], float (&b)[N]) {
         const int n = count(c);
         load_floats(a.weight + (n ? c : 0), n, w);
         load_floats(a.bias ? a.bias + (n ? c : 0) : a.weight, a.bias ? n : 0, b);
     };
-    // The distances from the mean, of the elements there are, into their sum and squares.
-    auto spread = [&](int n, const float (&v)[N], float m, float (&t)[2]) {
+    // The values (zeros past the row's end) into their sum and squares.
+    auto total = [&](const float (&v)[N], float (&s)[2]) {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const float d = i < n ? v[i] - m : 0.f;
+            s[0] += v[i];
+            s[1] = fmaf(v[i], v[i], s[1]);
+        }
+    };
+    // The distances from the pivot, of the elements there are, likewise.
+    auto spread = [&](int n, const float (&v)[N], float p, float (&t)[2]) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const float d = i < n ? v[i] - p : 0.f;
             t[0] += d;
             t[1] = fmaf(d, d, t[1]);
         }
@@ -122,20 +147,19 @@ __global__ void __launch_bounds__(threads_of(G), forward_waves(R))
         vectors(c, w, b);
         // Rows past the end go through the exchanges with zeros and store nothing.
         for (int64_t base = (int64_t)blockIdx.x * kRows; base < a.rows; base += step, row += step) {
-            float v[N], s[1] = {0.f}, t[2] = {0.f, 0.f};
+            float v[N], s[2] = {0.f, 0.f}, t[2] = {0.f, 0.f};
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 v[i] = x[i];
                 if (a.residual) v[i] += r[i];
             }
             if (base + step < a.rows) load(row + step);
-#pragma unroll
-            for (int i = 0; i < N; ++i) s[0] += v[i];
+            total(v, s);
             row_sums<G>(s, part[0]);
-            const float m = s[0] / C;
-            spread(n, v, m, t);
+            const float p = row_pivot(s[0] * inv, s[1] * inv);
+            spread(n, v, p, t);
             row_sums<G>(t, part[1]);
-            const RowStats st = row_stats(m, t[0], t[1], C, a.eps);
+            const RowStats st = row_stats(p, t[0], t[1], C, a.eps);
             if (row < a.rows && c < width) emit(row, c, v, w, b, st);
         }
     } else {
@@ -153,22 +177,20 @@ __global__ void __launch_bounds__(threads_of(G), forward_waves(R))
                     for (int i = 0; i < N; ++i) v[i] += e[i];
                 }
             };
-            float s[1] = {0.f}, t[2] = {0.f, 0.f};
+            float s[2] = {0.f, 0.f}, t[2] = {0.f, 0.f};
             if constexpr (R > 0) {
                 float v[R][N];
 #pragma unroll
                 for (int j = 0; j < R; ++j) load(((int64_t)j * G + lane) * N, v[j]);
 #pragma unroll
-                for (int j = 0; j < R; ++j)
-#pragma unroll
-                    for (int i = 0; i < N; ++i) s[0] += v[j][i];
+                for (int j = 0; j < R; ++j) total(v[j], s);
                 row_sums<G>(s, part[0]);
-                const float m = s[0] / C;
+                const float p = row_pivot(s[0] * inv, s[1] * inv);
 #pragma unroll
                 for (int j = 0; j < R; ++j)
-                    spread(count(((int64_t)j * G + lane) * N), v[j], m, t);
+                    spread(count(((int64_t)j * G + lane) * N), v[j], p, t);
                 row_sums<G>(t, part[1]);
-                const RowStats st = row_stats(m, t[0], t[1], C, a.eps);
+                const RowStats st = row_stats(p, t[0], t[1], C, a.eps);
 #pragma unroll
                 for (int j = 0; j < R; ++j) {
                     const int64_t c = ((int64_t)j * G + lane) * N;
@@ -181,18 +203,17 @@ __global__ void __launch_bounds__(threads_of(G), forward_waves(R))
                 for (int64_t c = (int64_t)lane * N; c < a.C; c += (int64_t)G * N) {
                     float v[N];
                     load(c, v);
-#pragma unroll
-                    for (int i = 0; i < N; ++i) s[0] += v[i];
+                    total(v, s);
                 }
                 row_sums<G>(s, part[0]);
-                const float m = s[0] / C;
+                const float p = row_pivot(s[0] * inv, s[1] * inv);
                 for (int64_t c = (int64_t)lane * N; c < a.C; c += (int64_t)G * N) {
                     float v[N];
                     load(c, v);
-                    spread(count(c), v, m, t);
+                    spread(count(c), v, p, t);
                 }
                 row_sums<G>(t, part[1]);
-                const RowStats st = row_stats(m, t[0], t[1], C, a.eps);
+                const RowStats st = row_stats(p, t[0], t[1], C, a.eps);
                 // A block's lanes are in the loop together: `width` is a multiple of 32.
                 for (int64_t c = (int64_t)lane * N; c < width; c += (int64_t)G * N) {
                     float v[N], w[N], b[N];
@@ -287,7 +308,7 @@ __global__ void __launch_bounds__(G > 256 ? G : 256, backward_waves(G, Chunk<T>:
         const bool live = row < a.rows;
         const int64_t at = live ? row * a.C : 0;
         float h[R][N], dy[R][N];
-        float s[2] = {0.f, 0.f};        // of h, of g
+        float s[3] = {0.f, 0.f, 0.f};   // of h, of g, of h's squares
 #pragma unroll
         for (int j = 0; j < R; ++j) {
             const int n = live ? count(j) : 0;
@@ -303,10 +324,11 @@ __global__ void __launch_bounds__(G > 256 ? G : 256, backward_waves(G, Chunk<T>:
             for (int i = 0; i < N; ++i) {
                 s[0] += h[j][i];
                 s[1] = fmaf(dy[j][i], R == 1 ? w0[i] : w[i], s[1]);
+                s[2] = fmaf(h[j][i], h[j][i], s[2]);
             }
         }
         row_sums<G>(s, parts[0]);
-        const float mean = s[0] * inv;
+        const float pivot = row_pivot(s[0] * inv, s[2] * inv);
         float t[3] = {0.f, 0.f, 0.f};   // of the distances d, their squares, g d
 #pragma unroll
         for (int j = 0; j < R; ++j) {
@@ -315,7 +337,7 @@ __global__ void __launch_bounds__(G > 256 ? G : 256, backward_waves(G, Chunk<T>:
             const int n = count(j);
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                const float d = i < n ? h[j][i] - mean : 0.f;
+                const float d = i < n ? h[j][i] - pivot : 0.f;
                 h[j][i] = d;
                 t[0] += d;
                 t[1] = fmaf(d, d, t[1]);
@@ -374,8 +396,8 @@ __global__ void __launch_bounds__(G > 256 ? G : 256, backward_waves(G, Chunk<T>:
     emit(db, out ? out + a.C : a.dbias);
 }
 
-// Rows too wide for registers: what each row's sums give first (stat: [rows][4] of the mean, its
-// correction, 1 / sqrt(v + eps) and mean(g), then [rows] of mean(g n)), then dx and the columns'
+// Rows too wide for registers: what each row's sums give first (stat: [rows][4] of the pivot, the
+// mean's distance from it, 1 / sqrt(v + eps) and mean(g), then [rows] of mean(g n)), then dx and the columns'
 // sums by column chunks.
 template <typename T>
 __global__ void __launch_bounds__(1024) layer_norm_backward_stats(LayerNormBackwardKernelArgs a,
@@ -398,15 +420,16 @@ __global__ void __launch_bounds__(1024) layer_norm_backward_stats(LayerNormBackw
                     if (i < n) f(h[i], dy[i] * w[i]);
             }
         };
-        float s[2] = {0.f, 0.f}, t[3] = {0.f, 0.f, 0.f};
+        float s[3] = {0.f, 0.f, 0.f}, t[3] = {0.f, 0.f, 0.f};
         each([&](float h, float g) {
             s[0] += h;
             s[1] += g;
+            s[2] = fmaf(h, h, s[2]);
         });
         row_sums<1024>(s, parts[0]);
-        const float mean = s[0] * inv;
+        const float pivot = row_pivot(s[0] * inv, s[2] * inv);
         each([&](float h, float g) {
-            const float d = h - mean;
+            const float d = h - pivot;
             t[0] += d;
             t[1] = fmaf(d, d, t[1]);
             t[2] = fmaf(d, g, t[2]);
@@ -415,7 +438,7 @@ __global__ void __launch_bounds__(1024) layer_norm_backward_stats(LayerNormBackw
         const float off = t[0] * inv;
         const float rstd = rsqrtf(fmaxf(fmaf(-off, off, t[1] * inv), 0.f) + a.eps);
         if (threadIdx.x == 0) {
-            stat[4 * row] = mean;
+            stat[4 * row] = pivot;
             stat[4 * row + 1] = off;
             stat[4 * row + 2] = rstd;
             stat[4 * row + 3] = s[1] * inv;
@@ -438,7 +461,7 @@ __global__ void __launch_bounds__(256)
     for (int i = 0; i < N; ++i) dw[i] = db[i] = 0.f;
     const int64_t end = min(a.rows, ((int64_t)blockIdx.y + 1) * per);
     for (int64_t row = (int64_t)blockIdx.y * per; row < end; ++row) {
-        const float mean = stat[4 * row], off = stat[4 * row + 1], rstd = stat[4 * row + 2],
+        const float pivot = stat[4 * row], off = stat[4 * row + 1], rstd = stat[4 * row + 2],
                     gm = stat[4 * row + 3], k = stat[4 * a.rows + row];
         const int64_t at = row * a.C + c;
         float h[N], dy[N], o[N];
@@ -447,7 +470,7 @@ __global__ void __launch_bounds__(256)
         if (a.dh) load_row<T>((const T *)a.dh + at, n, o);
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const float nn = (h[i] - mean - off) * rstd;
+            const float nn = (h[i] - pivot - off) * rstd;
             const float d = rstd * (fmaf(dy[i], w[i], -gm) - nn * k);
             o[i] = a.dh ? o[i] + d : d;
             dw[i] = fmaf(dy[i], nn, dw[i]);

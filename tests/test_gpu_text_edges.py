@@ -1,0 +1,89 @@
+"""GPU tests of layer norm, gated products and embedding where a small error would not show beside
+the bounds of random rows: exact sums, calls that go round the grid, joined stretches."""
+from __future__ import annotations
+
+import pytest
+import torch
+
+from tests import layer_ref as ref
+from tests.gpu_util import device, say
+from tests.test_gpu_layer import DTYPES, draw
+
+pytestmark = pytest.mark.gpu
+
+
+# ---- layer norm: the mean ----
+
+def exact_rows(C, rows=6):
+    """(large, small), both [rows, C] and their sum exact in bf16, with a known mean far below the
+    last bit of the large values: up to 16 pairs v, -v of multiples of 1/2 in [64, 128), and 8
+    multiples of 2^-13 that come to an odd one below 2^-6; zeros elsewhere, the columns from C / 2
+    on among them.  Every partial sum is a multiple of 2^-13 below 2^11, which float32 holds: the
+    row's sum is exact in any order."""
+    g = torch.Generator().manual_seed(C)
+    pairs = min(16, max(1, C // 64))
+    large, small = torch.zeros(rows, C), torch.zeros(rows, C)
+    for r in range(rows):
+        at = torch.randperm(C // 2, generator=g)
+        v = torch.randint(128, 256, (pairs,), generator=g) / 2
+        large[r, at[:pairs]], large[r, at[pairs:2 * pairs]] = v, -v
+        k = torch.randint(-60, 61, (8,), generator=g)
+        k[7] = 2 * r + 71 - k[:7].sum()
+        while k[7].abs() > 250:
+            k[:7] = torch.randint(-20, 21, (7,), generator=g)
+            k[7] = 2 * r + 71 - k[:7].sum()
+        small[r, at[2 * pairs:2 * pairs + 8]] = k * 2.0 ** -13
+    assert torch.equal(large + small, (large + small).bfloat16().float())
+    return large, small
+
+
+EXACT = [64, 1111, 2048, 4096, 8192, 40000]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("C", EXACT)
+@pytest.mark.parametrize("res", [False, True])
+def test_layer_norm_mean_of_exact_sums(C, dtype, res):
+    """Where t is 0 the output is -mean * rstd * w, which nothing but the mean's own error can move: with
+    an exact sum the mean is off by its division, 1 U of it, rstd by 4 U (the squares' sum, the
+    division by C, the root) and the products by 2 U."""
+    from paper_2607_25234_amd import whtmix
+    dev, dt, bf = device(), DTYPES[dtype], dtype == "bf16"
+    say("exact_mean", C, dtype, res)
+    large, small = exact_rows(C)
+    t = large + small
+    x, r = (large, small) if res else (t, None)
+    w = 1 + draw(2, C, std=0.1)
+    T = t.double()
+    mu = T.mean(-1, keepdim=True)
+    want = -mu * ((T - mu).square().mean(-1, keepdim=True) + 1e-6).rsqrt() * w.double()
+    zero = t == 0
+    args = (x.to(dt).to(dev), w.to(dev), None, None if r is None else r.to(dt).to(dev))
+    y, _ = whtmix.layer_norm(*args)
+    off = (y.cpu().double() - want).abs()
+    assert bool((off <= want.abs() * 8 * ref.U + ref.rounded(want, bf))[zero].all()), \
+        float((off / want.abs())[zero].max())
+    q, s, _ = whtmix.layer_norm_mx(*args)
+    got = whtmix.dequantize_mx(q, s, C, torch.float32).cpu().double()
+    first = (C // 2 + 31) // 32 * 32        # whole blocks of such values: e4m3's normal numbers
+    off = ((got - want).abs() / want.abs())[:, first:]
+    assert float(off.max()) <= 2.0 ** -4 + 8 * ref.U
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("C", EXACT)
+def test_layer_norm_backward_mean_of_exact_sums(C, dtype):
+    """The weight's gradient of the columns from C / 2 on is the sum over rows of -dy mean rstd: each
+    term off by 8 U as above and the sum by 1 U of the terms' magnitudes a row."""
+    from paper_2607_25234_amd import whtmix
+    dev, dt = device(), DTYPES[dtype]
+    say("exact_mean_backward", C, dtype)
+    large, small = exact_rows(C)
+    h, dy, w = (large + small).to(dt), draw(3, *large.shape, dtype=dt), 1 + draw(2, C, std=0.1)
+    _, dw, _ = whtmix.layer_norm_backward(h.to(dev), w.to(dev), dy.to(dev))
+    T = h.double()
+    mu = T.mean(-1, keepdim=True)
+    terms = -dy.double() * mu * ((T - mu).square().mean(-1, keepdim=True) + 1e-6).rsqrt()
+    off = (dw.cpu().double() - terms.sum(0)).abs()
+    ok = off <= (8 + h.shape[0]) * ref.U * terms.abs().sum(0)
+    assert bool(ok[C // 2:].all()), float((off / terms.abs().sum(0))[C // 2:].max())
