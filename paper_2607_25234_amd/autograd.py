@@ -121,6 +121,10 @@ class WHTMixBlockSeparableFunction(torch.autograd.Function):
         return dx, dwi.to(w_in.dtype), dgt, dgc, dwo.to(w_out.dtype)
 
 
+# The Functions below that keep something for their backward pass alone take the grad mode of
+# the call as `grad`: inside forward it is always off, and needs_input_grad follows the tensors
+# whatever the mode.
+
 def _strided_rows(x):
     """x, or a copy where its rows are not contiguous or not a constant distance apart."""
     try:
@@ -132,12 +136,12 @@ def _strided_rows(x):
 
 class WHTMixNormFunction(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, weight, residual, eps):
+    def forward(ctx, x, weight, residual, eps, grad):
         x, weight = _strided_rows(x), weight.contiguous()
         y, h = whtmix.norm(x, weight, None if residual is None else residual.contiguous(), eps)
-        if residual is None:      # the stream is x itself
-            h = x.contiguous()
-        ctx.save_for_backward(h, weight)
+        if grad and any(ctx.needs_input_grad):
+            # without a residual the stream is x itself
+            ctx.save_for_backward(x.contiguous() if residual is None else h, weight)
         ctx.eps, ctx.residual = eps, residual is not None
         return (y, h) if residual is not None else y
 
@@ -148,16 +152,16 @@ class WHTMixNormFunction(torch.autograd.Function):
         dx, dw = whtmix.norm_backward(h, weight, dy.contiguous(),
                                       None if dh is None else dh.contiguous(), ctx.eps,
                                       want_dweight=ctx.needs_input_grad[1])
-        return dx, dw, dx if ctx.residual else None, None
+        return dx, dw, dx if ctx.residual else None, None, None
 
 
 class WHTMixLinearFunction(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, w, bias, activation, residual):
+    def forward(ctx, x, w, bias, activation, residual, grad):
         x, w = _strided_rows(x), w.contiguous()
         z = None
         # z is kept only where the activation's derivative needs it
-        keep = activation != "none" and any(ctx.needs_input_grad[:3])
+        keep = grad and activation != "none" and any(ctx.needs_input_grad[:3])
         y = whtmix.linear(x, w, None if bias is None else bias.contiguous(), activation,
                           None if residual is None else residual.contiguous(), want_z=keep)
         if keep:
@@ -176,18 +180,18 @@ class WHTMixLinearFunction(torch.autograd.Function):
             dx, dw, db = whtmix.linear_backward(x, w, dy.contiguous(), z, ctx.activation,
                                                 want_dx=want[0], want_dw=want[1],
                                                 want_dbias=want[2])
-        return dx, dw, db, None, dy if want[4] else None
+        return dx, dw, db, None, dy if want[4] else None, None
 
 
 class WHTMixLayerNormFunction(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, weight, bias, residual, eps):
+    def forward(ctx, x, weight, bias, residual, eps, grad):
         x, weight = _strided_rows(x), weight.contiguous()
         y, h = whtmix.layer_norm(x, weight, None if bias is None else bias.contiguous(),
                                  None if residual is None else residual.contiguous(), eps)
-        if residual is None:      # the stream is x itself
-            h = x.contiguous()
-        ctx.save_for_backward(h, weight)
+        if grad and any(ctx.needs_input_grad):
+            # without a residual the stream is x itself
+            ctx.save_for_backward(x.contiguous() if residual is None else h, weight)
         ctx.eps, ctx.residual = eps, residual is not None
         return (y, h) if residual is not None else y
 
@@ -199,15 +203,15 @@ class WHTMixLayerNormFunction(torch.autograd.Function):
                                                 None if dh is None else dh.contiguous(), ctx.eps,
                                                 want_dweight=ctx.needs_input_grad[1],
                                                 want_dbias=ctx.needs_input_grad[2])
-        return dx, dw, db, dx if ctx.residual else None, None
+        return dx, dw, db, dx if ctx.residual else None, None, None
 
 
 class WHTMixGatedFunction(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, w_gate, w_up, b_gate, b_up, activation):
+    def forward(ctx, x, w_gate, w_up, b_gate, b_up, activation, grad):
         x, w_gate, w_up = _strided_rows(x), w_gate.contiguous(), w_up.contiguous()
         zg = zu = None
-        keep = any(ctx.needs_input_grad)
+        keep = grad and any(ctx.needs_input_grad)
         y = whtmix.gated(x, w_gate, w_up, None if b_gate is None else b_gate.contiguous(),
                          None if b_up is None else b_up.contiguous(), activation, want_z=keep)
         if keep:
@@ -225,7 +229,7 @@ class WHTMixGatedFunction(torch.autograd.Function):
             x, w_gate, w_up, dy.contiguous(), zg, zu, ctx.activation, want_dx=want[0],
             want_dw=want[1] or want[2], want_dbias=want[3] or want[4])
         return (dx, dwg if want[1] else None, dwu if want[2] else None,
-                dbg if want[3] else None, dbu if want[4] else None, None)
+                dbg if want[3] else None, dbu if want[4] else None, None, None)
 
 
 class WHTMixEmbeddingFunction(torch.autograd.Function):
@@ -246,29 +250,28 @@ class WHTMixEmbeddingFunction(torch.autograd.Function):
 def whtmix_norm(x, weight, residual=None, eps: float = 1e-6):
     """Differentiable norm with the residual's addition: (y, h), h = x + residual (x itself
     without one).  weight float32, and its gradient."""
-    if residual is None:
-        return WHTMixNormFunction.apply(x, weight, None, eps), x
-    return WHTMixNormFunction.apply(x, weight, residual, eps)
+    out = WHTMixNormFunction.apply(x, weight, residual, eps, torch.is_grad_enabled())
+    return (out, x) if residual is None else out
 
 
 def whtmix_linear(x, w, bias=None, activation: str = "none", residual=None):
     """Differentiable activation(x w + bias) + residual; dw in w's type, the
     bias and its gradient float32."""
-    return WHTMixLinearFunction.apply(x, w, bias, activation, residual)
+    return WHTMixLinearFunction.apply(x, w, bias, activation, residual, torch.is_grad_enabled())
 
 
 def whtmix_layer_norm(x, weight, bias=None, residual=None, eps: float = 1e-6):
     """Differentiable layer norm with the residual's addition: (y, h), h = x + residual (x
     itself without one).  weight and bias float32, and their gradients."""
-    if residual is None:
-        return WHTMixLayerNormFunction.apply(x, weight, bias, None, eps), x
-    return WHTMixLayerNormFunction.apply(x, weight, bias, residual, eps)
+    out = WHTMixLayerNormFunction.apply(x, weight, bias, residual, eps, torch.is_grad_enabled())
+    return (out, x) if residual is None else out
 
 
 def whtmix_gated(x, w_gate, w_up, b_gate=None, b_up=None, activation: str = "silu"):
     """Differentiable activation(x w_gate + b_gate) * (x w_up + b_up); the weights' gradients
     in their type, the biases and theirs float32."""
-    return WHTMixGatedFunction.apply(x, w_gate, w_up, b_gate, b_up, activation)
+    return WHTMixGatedFunction.apply(x, w_gate, w_up, b_gate, b_up, activation,
+                                     torch.is_grad_enabled())
 
 
 def whtmix_embedding(ids, table, scale: float = 1.0):
