@@ -604,8 +604,9 @@ WHTMIX_API int whtmix_gated_forward(const void *x, const void *wg, const void *w
  *   dbg, dbu  [N] float32, or both NULL to skip.
  * dzg and dzu enter the products rounded to `dtype` (as whtmix_linear_backward's
  * dz) and the biases' sums unrounded.  Sums over rows are made in a fixed
- * order.  Workspace: dzg and dzu, partial sums, the weights side by side where
- * N is not a multiple of 64 (or `dtype` float32), and what the products take.
+ * order.  Workspace: dzg and dzu where a product reads them from memory, partial
+ * sums, the weights side by side where N is not a multiple of 64 (or `dtype`
+ * float32), and what the products take.
  */
 WHTMIX_API int whtmix_gated_backward(const void *x, const void *wg, const void *wu,
                           const void *dy, const void *zg, const void *zu,

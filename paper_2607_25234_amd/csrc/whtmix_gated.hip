@@ -190,7 +190,7 @@ Parts parts_of(const GatedBackwardArgs &a)
     p.together = gated_dzx_takes(a);
     p.pitch = p.together ? gated_dzx_pitch(a.N, p.width) : 2 * p.width;
     p.two_k = bf16 && a.N % 64 == 0 && aligned(a.wg) && aligned(a.wu);
-    if (a.dx || a.dwg) p.dz = align256((uint64_t)a.M * p.pitch * e);
+    if (a.dwg || (a.dx && !p.together)) p.dz = align256((uint64_t)a.M * p.pitch * e);
     if (a.dbg)
         p.sums = align256((uint64_t)(p.together ? gated_dzx_parts(a) : dz_parts(a.M, p.width)) * 2 *
                           a.N * 4);

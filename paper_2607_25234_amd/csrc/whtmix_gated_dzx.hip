@@ -3,8 +3,8 @@
 // and everything is bound by memory.
 //
 // A workgroup takes 128 rows through all N in steps of 64: it forms dzg and dzu in registers,
-// writes them (rounded to bf16, what the matrix cores read) to memory for the weights' gradients and
-// to LDS for its own product, and multiplies with both weights' step, which copies bring to LDS
+// writes them (rounded to bf16, what the matrix cores read) to memory for the weights' gradients, where
+// those are asked for, and to LDS for its own product, and multiplies with both weights' step, which copies bring to LDS
 // meanwhile.  The next step's dy, zg and zu are on their way during the products.  One set of
 // buffers, 66 KiB, so that two workgroups share a compute unit: one's products and barriers pass
 // under the other's loads.
@@ -28,7 +28,7 @@ constexpr int kRows = 128, kCols = 128, kN = 64;   // rows, columns of dx, n of 
 struct GatedDzxArgs {
     const __bf16 *dy, *zg, *zu;
     const void *wg, *wu;
-    __bf16 *dz;             // [M] rows `pitch` apart, dzu `width` behind dzg
+    __bf16 *dz;             // [M] rows `pitch` apart, dzu `width` behind dzg; or null
     float *part;            // [groups * apart][2][N] sums of the unrounded values, or null
     __bf16 *dx;             // [M][K]
     int64_t M, N, K, width, pitch;
@@ -175,7 +175,7 @@ __global__ void __launch_bounds__(256, 2) gated_dzx_kernel(GatedDzxArgs d)
         const bool in = column(t, chunk * 8);
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            if (in && row0 + 32 * i < rows) {
+            if (d.dz && in && row0 + 32 * i < rows) {
                 __bf16 *to = d.dz + to0 + (int64_t)(32 * i * d.apart) * d.pitch + t * kN;
                 *(u32x4 *)to = *(const u32x4 *)place(i);
                 *(u32x4 *)(to + d.width) = *(const u32x4 *)(place(i) + kTileBytes);

@@ -483,7 +483,7 @@ bool dzx_takes(const LinearBackwardArgs &a);
 int64_t dzx_parts(int64_t M);
 hipError_t launch_dzx(const LinearBackwardArgs &a, void *dz, float *part);
 // The same of a gated product (whtmix_gated_dzx.hip): dz [M] rows a pitch apart, its second half
-// `width` columns on; part [parts][2][N].
+// `width` columns on, or null; part [parts][2][N].
 bool gated_dzx_takes(const GatedBackwardArgs &a);
 int64_t gated_dzx_parts(const GatedBackwardArgs &a);
 int64_t gated_dzx_pitch(int64_t N, int64_t width);

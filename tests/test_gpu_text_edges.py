@@ -87,3 +87,25 @@ def test_layer_norm_backward_mean_of_exact_sums(C, dtype):
     off = (dw.cpu().double() - terms.sum(0)).abs()
     ok = off <= (8 + h.shape[0]) * ref.U * terms.abs().sum(0)
     assert bool(ok[C // 2:].all()), float((off / terms.abs().sum(0))[C // 2:].max())
+
+
+# ---- gated products ----
+
+@pytest.mark.parametrize("M,K,N,act", [(32768, 128, 64, "silu"), (49161, 97, 344, "gelu"),
+                                       (49300, 128, 520, "relu")])
+def test_gated_backward_of_frozen_weights(M, K, N, act):
+    """Without the weights' gradients the pass of dzg, dzu and dx leaves those two out; dx and the
+    biases' gradients are those of the whole call."""
+    from paper_2607_25234_amd import whtmix
+    dev, dt = device(), torch.bfloat16
+    say("gated_backward_frozen", M, K, N, act)
+    x, wg, wu = (draw(s, *shape, dtype=dt).to(dev) for s, shape in
+                 ((1, (M, K)), (2, (K, N)), (3, (K, N))))
+    dy, zg, zu = (draw(s, M, N, dtype=dt).to(dev) for s in (11, 12, 13))
+    whole = whtmix.gated_backward(x, wg, wu, dy, zg, zu, act)
+    for bias in (True, False):
+        got = whtmix.gated_backward(x, wg, wu, dy, zg, zu, act, want_dw=False, want_dbias=bias)
+        assert got[1] is None and got[2] is None
+        assert torch.equal(got[0], whole[0])
+        if bias:
+            assert torch.equal(got[3], whole[3]) and torch.equal(got[4], whole[4])

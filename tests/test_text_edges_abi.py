@@ -1,0 +1,27 @@
+"""What layer norm, gated products and embedding do with calls that ask for little, on the host."""
+from __future__ import annotations
+
+import pytest
+
+from paper_2607_25234_amd import whtmix
+from tests.test_text_abi import FAR, workspace
+
+
+@pytest.fixture
+def no_device(monkeypatch):
+    torch = pytest.importorskip("torch")
+    if torch.cuda.device_count() > 0:
+        pytest.skip("fake device addresses are for hosts without a GPU")
+    monkeypatch.setenv("WHTMIX_TEST_FAIL_WORKSPACE", "1")
+
+
+@pytest.mark.parametrize("M,N", [(262144, 344), (32768, 64), (49152, 1024)])
+def test_gated_backward_without_weights_keeps_no_dz(no_device, M, N):
+    """Where dx is formed in the pass of dzg and dzu, nothing but the weights' gradients reads them
+    from memory: without those the workspace is the biases' partial sums, two rows of N for each
+    64 rows at most."""
+    p = FAR[:11]
+    whole = workspace("whtmix_gated_backward", p, (M, 128, N, 128), (4, 1))
+    assert whole >= 4 * M * N
+    p[7] = p[8] = 0
+    assert workspace("whtmix_gated_backward", p, (M, 128, N, 128), (4, 1)) <= M // 64 * 2 * N * 4
