@@ -490,7 +490,8 @@ WHTMIX_API int whtmix_linear_forward(const void *x, const void *w,
  *   dbias     [N] float32, or NULL to skip.
  * The residual's gradient is dy itself.  dz enters the products rounded to
  * `dtype` (bf16: what the matrix cores read; for a float32 dz pass float32
- * copies) and dbias unrounded.  Sums over rows are made in a fixed order.  Workspace: dz, partial sums, and what the
+ * copies) and dbias unrounded.  Sums over rows are made in a fixed order.  Workspace:
+ * dz where a product reads it from memory, partial sums, and what the
  * forward product takes.
  */
 WHTMIX_API int whtmix_linear_backward(const void *x, const void *w,

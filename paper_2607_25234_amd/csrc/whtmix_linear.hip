@@ -126,7 +126,9 @@ BackwardLayoutBytes backward_bytes(const LinearBackwardArgs &a)
 {
     BackwardLayoutBytes l;
     const int e = a.dtype == DTYPE_BF16 ? 2 : 4;
-    if (a.act != ACT_NONE) l.dz = align256((uint64_t)a.M * a.N * e);
+    // what a product reads: dz, where it is not dy itself
+    if (a.act != ACT_NONE && (a.dw || (a.dx && !dzx_takes(a))))
+        l.dz = align256((uint64_t)a.M * a.N * e);
     if (a.dbias)
         l.part = align256((uint64_t)(dzx_takes(a) ? dzx_parts(a.M) : dz_parts(a.M, a.N)) * a.N * 4);
     const void *dz = a.act != ACT_NONE ? nullptr : a.dy;    // a workspace's address is aligned
@@ -141,7 +143,7 @@ template <typename T> hipError_t linear_backward(const LinearBackwardArgs &a)
 {
     const BackwardLayoutBytes l = backward_bytes(a);
     char *ws = (char *)a.ws;
-    T *dz = (T *)ws;
+    T *dz = l.dz ? (T *)ws : nullptr;
     float *part = (float *)(ws + l.dz);
     void *rest = ws + l.dz + l.part;
     hipError_t e;
@@ -157,8 +159,7 @@ template <typename T> hipError_t linear_backward(const LinearBackwardArgs &a)
         const dim3 grid((uint32_t)((a.N + kDzCols - 1) / kDzCols),
                         (uint32_t)((a.M + per - 1) / per));
         dz_kernel<T><<<grid, dim3(256), 0, a.stream>>>(
-            (const T *)a.dy, (const T *)a.z, a.dx || a.dw ? dz : nullptr,
-            a.dbias ? part : nullptr, a.M, a.N, per, a.act);
+            (const T *)a.dy, (const T *)a.z, dz, a.dbias ? part : nullptr, a.M, a.N, per, a.act);
         if ((e = hipGetLastError()) != hipSuccess) return e;
         if (a.dbias && (e = launch_column_sum(part, grid.y, a.N, a.dbias, a.stream)) != hipSuccess)
             return e;

@@ -3,8 +3,8 @@
 //
 // Apart, dz is written by one kernel and read again by dx's: 262144 x 128 x 512 took 192 and 81 us.
 // Here a workgroup takes 128 rows through all N in steps of 64: it forms dz in registers, writes
-// it (rounded to bf16, what the matrix cores read) to memory for dw's product and to LDS for its own, and multiplies with w's step, which copies
-// bring to LDS meanwhile.  The next step's dy and z are on their way during the products.
+// it (rounded to bf16, what the matrix cores read) to memory for dw's product, where that is asked for, and to LDS for
+// its own, and multiplies with w's step, which copies bring to LDS meanwhile.  The next step's dy and z are on their way during the products.
 // Together 197-232 us: 872 MB at 3.8-4.4 TB/s, about what dz alone took.
 #include "whtmix_gemm_tile.h"
 
@@ -15,7 +15,7 @@ constexpr int kRows = 128, kCols = 128, kN = 64;   // rows, columns of dx, n of 
 
 struct DzxArgs {
     const __bf16 *dy, *z;
-    __bf16 *dz;
+    __bf16 *dz;             // [M][N] or null
     float *part;            // [workgroups][N] sums of the unrounded dz, or null
     int64_t M, N;
     int act;
@@ -111,7 +111,7 @@ __global__ void __launch_bounds__(256) dzx_kernel(DzxArgs d, GemmArgs g)
             const bool in = t * kN + chunk * 8 < d.N;
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                if (in && m0 + row0 + 32 * i < d.M)
+                if (d.dz && in && m0 + row0 + 32 * i < d.M)
                     *(u32x4 *)(d.dz + at0 + (int64_t)(32 * i) * d.N + t * kN) = out[i];
             if (t + 1 < steps) {
                 load(t + 1);

@@ -109,3 +109,31 @@ def test_gated_backward_of_frozen_weights(M, K, N, act):
         assert torch.equal(got[0], whole[0])
         if bias:
             assert torch.equal(got[3], whole[3]) and torch.equal(got[4], whole[4])
+
+
+@pytest.mark.parametrize("M,K,N,act", [(32768, 128, 64, "silu"), (49161, 97, 344, "gelu"),
+                                       (3000, 40, 77, "gelu_tanh")])
+def test_linear_backward_of_frozen_weights(M, K, N, act):
+    """The same of the single product."""
+    from paper_2607_25234_amd import whtmix
+    dev, dt = device(), torch.bfloat16
+    say("linear_backward_frozen", M, K, N, act)
+    x, w, dy, z = (draw(s, *shape, dtype=dt).to(dev) for s, shape in
+                   ((1, (M, K)), (2, (K, N)), (11, (M, N)), (12, (M, N))))
+    whole = whtmix.linear_backward(x, w, dy, z, act)
+    for dx in (True, False):
+        for bias in (True, False):
+            if dx or bias:
+                got = whtmix.linear_backward(x, w, dy, z, act, want_dx=dx, want_dw=False,
+                                             want_dbias=bias)
+                assert got[1] is None
+                if dx:
+                    assert torch.equal(got[0], whole[0])
+                if dx and bias:
+                    assert torch.equal(got[2], whole[2])
+                elif bias:      # the sums' order may be another
+                    want = (dy.double() * ref.act_grad(act, z.double())).sum(0)
+                    mag = (dy.double() * ref.act_grad(act, z.double())).abs().sum(0)
+                    bound = ref.sum_bound(M, mag) + (dy.double().abs()
+                                                     * ref.grad_bound(act, z.double())).sum(0)
+                    ref.check("dbias", got[2], want.cpu(), bound.cpu())

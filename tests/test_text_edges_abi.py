@@ -25,3 +25,17 @@ def test_gated_backward_without_weights_keeps_no_dz(no_device, M, N):
     assert whole >= 4 * M * N
     p[7] = p[8] = 0
     assert workspace("whtmix_gated_backward", p, (M, 128, N, 128), (4, 1)) <= M // 64 * 2 * N * 4
+
+
+@pytest.mark.parametrize("M,N", [(262144, 344), (32768, 64), (49152, 1024)])
+def test_linear_backward_without_weights_keeps_no_dz(no_device, M, N):
+    """As the gated product's: one row of N for each 64 rows at most, and no more than that
+    for the bias's gradient alone."""
+    p = FAR[:7]
+    assert workspace("whtmix_linear_backward", p, (M, 128, N, 128), (4, 1)) >= 2 * M * N
+    p[5] = 0
+    assert workspace("whtmix_linear_backward", p, (M, 128, N, 128), (4, 1)) <= M // 64 * N * 4
+    p[4] = 0
+    for dtype in (0, 1):
+        assert workspace("whtmix_linear_backward", p, (M, 128, N, 128), (4, dtype)) \
+            <= M // 32 * N * 4
