@@ -290,7 +290,8 @@ int whtmix_linear_backward(const void *x, const void *w, const void *dy, const v
         if (st == WHTMIX_SUCCESS) st = check_sizes(M, {K, N}, ldx, K);
         if (st == WHTMIX_SUCCESS) st = check_act(activation);
         if (st != WHTMIX_SUCCESS) return st;
-        if (!dx && !dw && !dbias) return WHTMIX_ERROR_INVALID_VALUE;
+        if (M > 0 && !dx && !dw && !dbias)      // (a dx without rows has no address)
+            return WHTMIX_ERROR_INVALID_VALUE;
         const uint64_t e = elt(dtype);
         if (!aligned({x, w, dy, z, dx, dw}, e) || !aligned({dbias}, 4))
             return WHTMIX_ERROR_MISALIGNED;
@@ -449,7 +450,7 @@ int whtmix_gated_backward(const void *x, const void *wg, const void *wu, const v
         if (st == WHTMIX_SUCCESS) st = check_act(activation);
         if (st == WHTMIX_SUCCESS && N > kMaxGated) st = WHTMIX_ERROR_TOO_LARGE;
         if (st != WHTMIX_SUCCESS) return st;
-        if ((!dx && !dwg && !dbg) || !dwg != !dwu || !dbg != !dbu)
+        if ((M > 0 && !dx && !dwg && !dbg) || !dwg != !dwu || !dbg != !dbu)
             return WHTMIX_ERROR_INVALID_VALUE;
         const uint64_t e = elt(dtype);
         if (!aligned({x, wg, wu, dy, zg, zu, dx, dwg, dwu}, e) || !aligned({dbg, dbu}, 4))

@@ -137,3 +137,22 @@ def test_linear_backward_of_frozen_weights(M, K, N, act):
                     bound = ref.sum_bound(M, mag) + (dy.double().abs()
                                                      * ref.grad_bound(act, z.double())).sum(0)
                     ref.check("dbias", got[2], want.cpu(), bound.cpu())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("want", ["dx", "dw", "dbias"])
+def test_products_backward_without_rows(dtype, want):
+    """Each gradient alone of no rows: one of no rows, or zeros."""
+    from paper_2607_25234_amd import whtmix
+    dev, dt = device(), DTYPES[dtype]
+    x, dy = torch.empty(0, 24, dtype=dt, device=dev), torch.empty(0, 40, dtype=dt, device=dev)
+    w = draw(1, 24, 40, dtype=dt).to(dev)
+    wants = {"want_" + k: k == want for k in ("dx", "dw", "dbias")}
+    got = (*whtmix.linear_backward(x, w, dy, **wants),
+           *whtmix.gated_backward(x, w, w, dy, dy, dy, **wants))
+    shapes = [{"dx": (0, 24), "dw": (24, 40), "dbias": (40,)}[k]
+              for k in ("dx", "dw", "dbias", "dx", "dw", "dw", "dbias", "dbias")]
+    kinds = ["dx", "dw", "dbias", "dx", "dw", "dw", "dbias", "dbias"]
+    for g, shape, kind in zip(got, shapes, kinds):
+        assert (g is None) is (kind != want)
+        assert g is None or (g.shape == shape and not g.any())

@@ -4,7 +4,7 @@ from __future__ import annotations
 import pytest
 
 from paper_2607_25234_amd import whtmix
-from tests.test_text_abi import FAR, workspace
+from tests.test_text_abi import FAR, INVALID, status, workspace
 
 
 @pytest.fixture
@@ -39,3 +39,15 @@ def test_linear_backward_without_weights_keeps_no_dz(no_device, M, N):
     for dtype in (0, 1):
         assert workspace("whtmix_linear_backward", p, (M, 128, N, 128), (4, dtype)) \
             <= M // 32 * N * 4
+
+
+@pytest.mark.parametrize("name,inputs,outputs", [("whtmix_gated_backward", 6, 5),
+                                                 ("whtmix_linear_backward", 4, 3)])
+def test_backward_for_x_alone_without_rows(name, inputs, outputs):
+    """The gradient of no rows has no address: as with the forward products, nothing to do."""
+    none = [0] * outputs
+    for act in (0, 1):
+        for given in (FAR[:inputs], [0] * inputs):
+            status(name, given + none, (0, 64, 96, 64), (act, 0), (), refused=False)
+    for rows in (-1, 1):
+        assert status(name, FAR[:inputs] + none, (rows, 64, 96, 64), (0, 0), ()) == INVALID
