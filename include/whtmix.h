@@ -539,8 +539,9 @@ WHTMIX_API int whtmix_linear_mx_forward(const void *xq, const uint8_t *xs,
  *   y         [rows][C] of `dtype`; may be x (with ldx = C).
  *   h         [rows][C] of `dtype`, t rounded, or NULL; may be x (with ldx =
  *             C) or the residual, but not y.
- * y is formed from t before its rounding.  eps >= 0 and finite.  Squares are of
- * distances from the mean, in float32 (below 2^64 in magnitude).
+ * y is formed from t before its rounding.  eps >= 0 and finite.  A row's sums, of
+ * its values and of their squared distances from the mean, are float32, in the
+ * backward pass too: both below 2^128, which distances up to 2^64 / sqrt(C) keep.
  */
 WHTMIX_API int whtmix_layer_norm_forward(const void *x, const void *residual,
                               const float *weight, const float *bias, void *y,

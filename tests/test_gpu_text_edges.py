@@ -6,6 +6,7 @@ import pytest
 import torch
 
 from tests import layer_ref as ref
+from tests import text_ref
 from tests.gpu_util import device, say
 from tests.test_gpu_layer import DTYPES, draw
 
@@ -87,6 +88,34 @@ def test_layer_norm_backward_mean_of_exact_sums(C, dtype):
     off = (dw.cpu().double() - terms.sum(0)).abs()
     ok = off <= (8 + h.shape[0]) * ref.U * terms.abs().sum(0)
     assert bool(ok[C // 2:].all()), float((off / terms.abs().sum(0))[C // 2:].max())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("C", [64, 1111, 4096, 40000])
+def test_layer_norm_of_the_largest_spread(C, dtype):
+    """Distances all over a row at 0.97 of the bound 2^64 / sqrt(C), about 0 and about a mean
+    of 64 times as much, whose own squares overflow."""
+    from paper_2607_25234_amd import whtmix
+    dev, dt, bf = device(), DTYPES[dtype], dtype == "bf16"
+    say("largest", C, dtype)
+    sign = torch.where(torch.arange(C) % 2 == 0, 1.0, -1.0)
+    sign = sign.repeat(4, 1)[:, torch.randperm(C, generator=torch.Generator().manual_seed(C))]
+    a = 2.0 ** 64 / C ** 0.5 * 0.97
+    if bf:      # whole steps of the mean's type too
+        step = 2.0 ** (int(torch.tensor(a).log2().floor()) - 1)
+        a = a // step * step
+    mean = torch.tensor([0.0, 0.0, 64.0, -64.0])[:, None] * 2.0 ** int(torch.tensor(a).log2().floor())
+    x = (mean + a * sign).to(dt)
+    w, b = 1 + draw(2, C, std=0.1), draw(5, C, std=0.3)
+    y, _ = whtmix.layer_norm(x.to(dev), w.to(dev), b.to(dev))
+    want, bound, _ = text_ref.layer_norm(x, None, w, b, 1e-6)
+    ref.check("y", y, want, bound + ref.rounded(want, bf))
+    dy = draw(3, 4, C, dtype=dt)
+    dx, dw, db = whtmix.layer_norm_backward(x.to(dev), w.to(dev), dy.to(dev))
+    rx, bx, rw, bw, rb, bb = text_ref.layer_norm_backward(x, w, dy, None, 1e-6)
+    ref.check("dx", dx, rx, bx + ref.rounded(rx, bf))
+    ref.check("dweight", dw, rw, bw)
+    ref.check("dbias", db, rb, bb)
 
 
 # ---- gated products ----
