@@ -118,6 +118,50 @@ def test_layer_norm_of_the_largest_spread(C, dtype):
     ref.check("dbias", db, rb, bb)
 
 
+# More rows than twice as many as the device holds at a time, the last round of them partial: each
+# workgroup goes on from row to row with the next one on its way.
+ROUNDS = [(2000, 4096, "bf16"), (2500, 1111, "f32"), (3200, 2048, "bf16"), (7000, 1024, "bf16"),
+          (14001, 512, "bf16"), (27001, 250, "bf16"), (52003, 40, "f32"), (101003, 61, "bf16")]
+
+
+@pytest.mark.parametrize("rows,C,dtype", ROUNDS)
+@pytest.mark.parametrize("res", [False, True])
+def test_layer_norm_round_the_grid(rows, C, dtype, res):
+    from paper_2607_25234_amd import whtmix
+    dev, dt, bf = device(), DTYPES[dtype], dtype == "bf16"
+    say("round_the_grid", rows, C, dtype, res)
+    x, w, b = draw(1, rows, C, dtype=dt) + 0.5, 1 + draw(2, C, std=0.1), draw(5, C, std=0.3)
+    r = draw(3, rows, C, std=2.0, dtype=dt) if res else None
+    want, bound, t = text_ref.layer_norm(x, r, w, b, 1e-6)
+    own = ref.rounded(t, bf) + (x.double().abs() + t.abs()) * 2 * ref.U
+
+    def given():
+        return x.to(dev), w.to(dev), b.to(dev), None if r is None else r.to(dev)
+
+    y, h = whtmix.layer_norm(*given())
+    ref.check("y", y, want, bound + ref.rounded(want, bf))
+    ref.check("h", h, t, own)
+    # y in x's place, and h in x's or the residual's, while later rows are on their way
+    args = given()
+    z, _ = whtmix.layer_norm(*args, out=args[0])
+    assert z is args[0] and torch.equal(z, y)
+    for at in (0, 3) if res else (0,):
+        args = given()
+        z = torch.empty_like(y)
+        p = [0 if a is None else a.data_ptr() for a in args]
+        assert whtmix.call_rows("whtmix_layer_norm_forward",
+                                (p[0], p[3], p[1], p[2], z.data_ptr(), p[at]), (rows, C, C),
+                                (whtmix.DTYPE_BF16 if bf else whtmix.DTYPE_F32,),
+                                torch.cuda.current_stream().cuda_stream, 1e-6) == 0
+        assert torch.equal(z, y) and torch.equal(args[at], h)
+    # in 8 bits: the rounding's half step besides, of the block's scale below its normal numbers
+    q, s, h8 = whtmix.layer_norm_mx(*given())
+    assert torch.equal(h8, h)
+    got = whtmix.dequantize_mx(q, s, C, torch.float32)
+    last = s.cpu().double().sub(127).exp2().repeat_interleave(32, -1)[:, :C] * 2.0 ** -9
+    ref.check("8 bits", got, want, bound + torch.maximum((want.abs() + bound) * 2.0 ** -4, last / 2))
+
+
 # ---- gated products ----
 
 @pytest.mark.parametrize("M,K,N,act", [(32768, 128, 64, "silu"), (49161, 97, 344, "gelu"),
