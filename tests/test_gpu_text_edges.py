@@ -229,3 +229,26 @@ def test_products_backward_without_rows(dtype, want):
     for g, shape, kind in zip(got, shapes, kinds):
         assert (g is None) is (kind != want)
         assert g is None or (g.shape == shape and not g.any())
+
+
+# ---- embedding ----
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,V,C", [(20000, 600, 64), (70001, 5000, 8), (30000, 3, 1000),
+                                      (9000, 256, 64), (50000, 200, 33)])
+def test_embedding_gradient_of_long_runs(rows, V, C, dtype):
+    """Runs over many stretches, workgroups and ranges: an id of half of the tokens, one of an eighth,
+    and the rest.  Small whole numbers: float32 holds every partial sum, so the result is the
+    sum in any order, rounded once."""
+    from paper_2607_25234_amd import whtmix
+    dev, dt = device(), DTYPES[dtype]
+    say("long_runs", rows, V, C, dtype)
+    g = torch.Generator().manual_seed(rows)
+    ids, u = torch.randint(-1, V, (rows,), generator=g), torch.rand(rows, generator=g)
+    ids[u < 0.5] = V // 2
+    ids[u > 0.875] = V - 1
+    dy = torch.randint(-8, 9, (rows, C), generator=g)
+    want = torch.zeros(V + 1, C, dtype=torch.int64).index_add_(0, ids % (V + 1), dy)[:V]
+    assert int(dy.abs().sum(0).max()) < 1 << 24
+    got = whtmix.embedding_backward(ids.to(dev), dy.to(dt).to(dev), V)
+    assert torch.equal(got.cpu(), want.to(dt))
