@@ -438,11 +438,17 @@ inline TilePlan plan_tiles(int64_t M, int64_t N, int64_t K, int step_k, bool two
     // hide), or two where their parts stay long (128 x 262144 x 512: 76 us, 84 us with one).
     int64_t s = t >= 256 ? 1 : 256 / t;
     if (t < 256 && p.bm < 256 && steps / (2 * s) >= 32) s *= 2;
-    // The gated forms of bf16: two workgroups a unit where that leaves a tenth fewer places empty (1 x
-    // 4096 x 2 x 12288, 96 tiles: 44 us in five parts, 51 in two; 16 x 4096 x 2 x 11264 45 and 51), and
-    // of more rows where their parts stay long.  Not of 8 bits: 64 x 4096 x 2 x 11264 33 us in two
-    // parts, 40 in five.
-    if (two_a_unit && t < 256 && (M <= 64 || steps / (512 / t) >= 16) &&
+    // The gated forms of bf16: two workgroups a unit where that leaves a tenth fewer places empty and
+    // k is long beside the rows, whose partial sums it multiplies (us in the parts above and in more;
+    // tiles of 256 columns, K = 64 M at least: 1 x 4096 x 2 x 12288 50 and 44, 32 x 4096 x 2 x 11264
+    // 52 and 47, 64 x 4096 x 2 x 11264 54 and 52, 32 x 2048 30 and 30, 64 x 3584 x 2 x 12288 50 and
+    // 52, 64 x 2048 x 2 x 11264 32 and 36; of 128, 40 M: 33 x 2048 x 2 x 5632 25 and 22, 64 x 2560 29
+    // and 26, 64 x 1536 20 and 20, 64 x 1024 15 and 17), and of more rows where their parts stay long:
+    // 128 x 8192 x 2 x 5632 68 and 62, 200 x 8192 x 2 x 2816 52 and 48, the weights' gradients of 16384
+    // x 256 x 2 x 2730 197 and 188 and of 65536 x 1024 x 2 x 683 383 and 330, dx of 512 x 2816 x 2 x
+    // 5632 72 and 67.  Not of 8 bits: 64 x 4096 x 2 x 11264 33 us in two parts, 40 in five.
+    if (two_a_unit && t < 256 &&
+        (M <= 64 ? K >= (p.bn == 256 ? 64 : 40) * M : steps / (512 / t) >= 16) &&
         20 * (s * t <= 256 ? 2 * s : s) < 18 * (512 / t))
         s = 512 / t;
     s = s < steps / 4 ? s : steps / 4;
