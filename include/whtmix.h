@@ -490,8 +490,9 @@ WHTMIX_API int whtmix_linear_forward(const void *x, const void *w,
  *   dbias     [N] float32, or NULL to skip.
  * The residual's gradient is dy itself.  dz enters the products rounded to
  * `dtype` (bf16: what the matrix cores read; for a float32 dz pass float32
- * copies) and dbias unrounded.  Sums over rows are made in a fixed order.  Workspace:
- * dz where a product reads it from memory, partial sums, and what the
+ * copies) and dbias unrounded.  Sums over rows are made in a fixed order, which
+ * sizes and the outputs asked for choose: dbias may differ in its last bits with
+ * and without dx.  Workspace: dz where a product reads it from memory, partial sums, and what the
  * forward product takes.
  */
 WHTMIX_API int whtmix_linear_backward(const void *x, const void *w,
@@ -606,7 +607,8 @@ WHTMIX_API int whtmix_gated_forward(const void *x, const void *wg, const void *w
  *   dbg, dbu  [N] float32, or both NULL to skip.
  * dzg and dzu enter the products rounded to `dtype` (as whtmix_linear_backward's
  * dz) and the biases' sums unrounded.  Sums over rows are made in a fixed
- * order.  Workspace: dzg and dzu where a product reads them from memory, partial
+ * order, which sizes and the outputs asked for choose: dbg and dbu may differ in
+ * their last bits with and without dx.  Workspace: dzg and dzu where a product reads them from memory, partial
  * sums, the weights side by side where N is not a multiple of 64 (or `dtype`
  * float32), and what the products take.
  */

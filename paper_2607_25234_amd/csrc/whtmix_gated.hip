@@ -13,7 +13,8 @@
 // 8192 x 4096 x 2 x 12288 bf16: forward 1315 us (1.25 PFLOP/s, the matrix cores 70%
 // busy), dz 211 (4.8 TB/s), dx 1256, the weights' gradients 1245 (1.31 and 1.32 PFLOP/s).  262144 x
 // 128 x 2 x 344: forward 184 us (608 MB), the weights' gradients 127 + 8.  3001 x 1000 x 2 x 2003
-// float32: forward 145 us, dz 29, dx 152 + 12, the weights' gradients 128 + 14, splits 3 x 30.
+// float32, kernel by kernel: forward 137-145 us, dz 29, dx 145-152 + 12, the weights' gradients 122-128
+// + 13, splits 3 x 30.
 #include "whtmix_gemm.h"
 #include "whtmix_row.h"
 

@@ -51,7 +51,8 @@ template <int EB, Layout L, int R, int NW> struct Operand {
         // A cycle of an LDS read serves 16 lanes: 16 rows of 128 bytes fall on all 64 banks
         // when every second row's chunks are permuted alike.
         if constexpr (L == K_CONTIGUOUS) return chunk ^ ((outer >> 1) & 7);
-        else if constexpr (kRowChunks == 8) return chunk ^ (2 * outer & 4);   // two k on all banks
+        // two k on all banks (a single product's dw of 131072 x 64 x 16384 674 us before and since)
+        else if constexpr (kRowChunks == 8) return chunk ^ (2 * outer & 4);
         else return chunk ^ ((4 * (outer & 3)) & (kRowChunks - 1));
     }
     // The (row or k, chunk) that copy i of this lane fetches.

@@ -21,6 +21,7 @@ constexpr int kRowBytes = 64;      // of a plane: 32 bf16, of one row or of 32 r
 template <Layout L, int ROWS> __device__ __forceinline__ int place_chunk(int outer, int chunk)
 {
     if constexpr (L == K_CONTIGUOUS) return outer * kRowBytes + (chunk ^ ((outer >> 2) & 3)) * 16;
+    // (the gated form's halves; a single product's dw of 131072 x 64 x 256 63 us before and since)
     else if constexpr (ROWS == 64) return outer * (2 * ROWS) + (chunk ^ (2 * outer & 4)) * 16;
     else return outer * (2 * ROWS) + (chunk ^ ((4 * (outer & 3)) & (ROWS / 8 - 1))) * 16;
 }
@@ -411,8 +412,9 @@ __device__ __forceinline__ void split_block(const SplitJob &job, int64_t K, uint
     if (t == 0) job.flags[at] = bad ? 1u : 0u;
 }
 
-// All operands of a product in one launch, the smaller under the larger's end: 3001 x 1000 x 2 x 2003
-// gated 145 us, 152 in three launches, its gradients 390 and 398; 3001 x 1000 x 2003 86 and 91.
+// All operands of a product in one launch, the smaller under the larger's end (whole calls: 3001 x
+// 1000 x 2 x 2003 gated 145 us, 152 in three launches, its gradients 390 and 398; 3001 x 1000 x
+// 2003 86 and 91).
 __global__ void __launch_bounds__(256) split_kernel(SplitJob a, SplitJob b, SplitJob b2, int64_t K)
 {
     uint32_t at = blockIdx.x;
