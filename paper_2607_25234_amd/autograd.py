@@ -121,10 +121,6 @@ class WHTMixBlockSeparableFunction(torch.autograd.Function):
         return dx, dwi.to(w_in.dtype), dgt, dgc, dwo.to(w_out.dtype)
 
 
-# The Functions below that keep something for their backward pass alone take the grad mode of
-# the call as `grad`: inside forward it is always off, and needs_input_grad follows the tensors
-# whatever the mode.
-
 def _strided_rows(x):
     """x, or a copy where its rows are not contiguous or not a constant distance apart."""
     try:
@@ -134,9 +130,14 @@ def _strided_rows(x):
     return x if rows <= 1 or ld >= width else x.contiguous()
 
 
+# The Functions that keep something for their backward pass alone take the grad mode of the call as
+# `grad`: inside forward it is always off, and needs_input_grad follows the tensors whatever
+# the mode.
+
+
 class WHTMixNormFunction(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, weight, residual, eps, grad):
+    def forward(ctx, x, weight, residual, eps, grad=True):
         x, weight = _strided_rows(x), weight.contiguous()
         y, h = whtmix.norm(x, weight, None if residual is None else residual.contiguous(), eps)
         if grad and any(ctx.needs_input_grad):
@@ -157,7 +158,7 @@ class WHTMixNormFunction(torch.autograd.Function):
 
 class WHTMixLinearFunction(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, w, bias, activation, residual, grad):
+    def forward(ctx, x, w, bias, activation, residual, grad=True):
         x, w = _strided_rows(x), w.contiguous()
         z = None
         # z is kept only where the activation's derivative needs it
@@ -185,7 +186,7 @@ class WHTMixLinearFunction(torch.autograd.Function):
 
 class WHTMixLayerNormFunction(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, weight, bias, residual, eps, grad):
+    def forward(ctx, x, weight, bias, residual, eps, grad=True):
         x, weight = _strided_rows(x), weight.contiguous()
         y, h = whtmix.layer_norm(x, weight, None if bias is None else bias.contiguous(),
                                  None if residual is None else residual.contiguous(), eps)
@@ -208,7 +209,7 @@ class WHTMixLayerNormFunction(torch.autograd.Function):
 
 class WHTMixGatedFunction(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, w_gate, w_up, b_gate, b_up, activation, grad):
+    def forward(ctx, x, w_gate, w_up, b_gate, b_up, activation, grad=True):
         x, w_gate, w_up = _strided_rows(x), w_gate.contiguous(), w_up.contiguous()
         zg = zu = None
         keep = grad and any(ctx.needs_input_grad)

@@ -86,3 +86,20 @@ def test_gradients_of_calls_among_ones_without(kept):
     assert torch.allclose(alone, want)
     for a, c in zip(got, torch.autograd.grad(want, (w, g, b))):
         assert torch.allclose(a, c, rtol=1e-10, atol=1e-12)
+
+
+def test_the_functions_by_themselves(kept):
+    """Applied without the mode they keep what they kept before."""
+    p = torch.nn.Parameter
+    x = torch.randn(6, 8, dtype=torch.float64)
+    w, g, b = (p(torch.randn(s, dtype=torch.float64)) for s in ((8, 8), (8,), (8,)))
+    y = autograd.WHTMixLayerNormFunction.apply(x, g, b, None, 1e-6)
+    y = autograd.WHTMixGatedFunction.apply(y, w, w, b, b, "silu")
+    y = autograd.WHTMixNormFunction.apply(y, g, None, 1e-6)
+    y = autograd.WHTMixLinearFunction.apply(y, w, b, "silu", None)
+    assert kept == [True, True]
+    want = plain_linear(plain_norm(plain_gated(plain_layer_norm(x, g, b)[0], w, w, b, b), g)[0], w,
+                        b, "silu")
+    for a, c in zip(torch.autograd.grad(y.sum(), (w, g, b)),
+                    torch.autograd.grad(want.sum(), (w, g, b))):
+        assert torch.allclose(a, c, rtol=1e-10, atol=1e-12)
