@@ -14,9 +14,10 @@
 // many columns before the rows, and dz's rows lie so far apart that they start alike: every access is
 // to a whole line.  262144 x 128 x 344 297 us (309 from each row's start on, 351 with dz's rows at
 // whole lines), x 336 270 (291, 320), x 352 256 (273, 271); the weights' gradients read such rows
-// no slower (127 and 129 us); without dz (no weights' gradients) 160 us for dx, 188 with the sums.  Of 516 MiB of operands the counters have 982 MiB read from each row's
-// start on and 603 so (scaled by what they give for a copy), and 422 written: 3.6 TB/s.  The waves wait
-// for 58% of their time, vector instructions take 27%, products 8%.
+// no slower (127 and 129 us); without dz (no weights' gradients) 160 us for dx, 188 with the sums.
+// Of 516 MiB of operands the counters have 982 MiB read from each row's start on and 603 so (scaled
+// by what they give for a copy), and 422 written: 3.6 TB/s.  The waves wait for 58% of their time,
+// vector instructions take 27%, products 8%.
 #include "whtmix_gemm_tile.h"
 #include "whtmix_row.h"
 
